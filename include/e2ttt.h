@@ -258,6 +258,52 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
                                 const float* d_gamma, void* dq_raw, void* dk_raw, float* da_eta, float* da_beta,
                                 float* da_alpha, void* stream);
 
+/* Gated delta rule: the fast-weight layer's linear relative (the paper's comparison systems, Table "ttt_comparison": one gradient step per
+ * token on a linear map), with the same tokens and gates.  Per sequence and head a state S [dv, dk], moved token by token:
+ *   S'_t = exp(log_gamma_t) S_{t-1},   e_t = v_t - S'_t k_t,   S_t = S'_t + eta_t e_t k_t^T,   o_t = scale S_t q_t.
+ * H value heads share Hk query / key heads: value head h reads head h / (H / Hk).
+ *   q, k         [B,Hk,L,dk] io_dtype       v, o  [B,H,L,dv] io_dtype
+ *   eta          [B,H,L] fp32               the learning rate (any finite value; 0 writes nothing)
+ *   log_gamma    [B,H,L] fp32               logarithm of the decay, <= 0 (e2ttt_prepare_fwd's gamma: its logarithm); -inf (and anything below
+ *                                           -1000) forgets the state before the token, as at the start of another document
+ *   S            [B,H,dv,dk] fp32           rows are outputs, as in the fast-weight matrices
+ * e2ttt_delta_fwd runs whole sequences in chunks of 32 tokens on the tensor cores; e2ttt_delta_step is the recurrent form for a few
+ * tokens (decoding), without a workspace; both move the same state and may follow each other.
+ * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly; outputs are rounded once.  A NaN or an
+ * infinity at one token reaches all outputs and gradients of its chunk of 32 tokens (of its block of 64 in the reverse pass) and what follows it.
+ * Arguments are refused as everywhere: E2TTT_ERR_NULL / _SHAPE / _DTYPE / _WORKSPACE / _ALIGN / _ARCH / _CUDA.  Tensors need the
+ * alignment of their elements only; 16 bytes, and widths that are a multiple of 8, load faster. */
+typedef struct {
+    int32_t B, H, Hk; /* batch, value heads, query / key heads (H a multiple of Hk) */
+    int32_t L;        /* tokens per sequence, any number */
+    int32_t dk, dv;   /* widths of a query / key and of a value, 1..128 */
+    int32_t io_dtype; /* e2ttt_dtype of q, k, v, o and their gradients */
+    float scale;      /* of the outputs; 1 / sqrt(dk) is usual, 1 for the library's normalised queries */
+} e2ttt_delta_params;
+
+/* Bytes of workspace of e2ttt_delta_fwd with this save_states (and of e2ttt_delta_bwd: save_states = 1).  `bytes` is a host pointer. */
+E2TTT_API int e2ttt_delta_workspace_bytes(const e2ttt_delta_params* p, int save_states, size_t* bytes);
+
+/* S_init may be NULL (zeros); S_final may alias S_init.  workspace: 256-byte aligned; with save_states != 0 it holds, after the call, what
+ * e2ttt_delta_bwd reads. */
+E2TTT_API int e2ttt_delta_fwd(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
+                              const float* log_gamma, const float* S_init, void* o, float* S_final, void* workspace,
+                              size_t workspace_bytes, int save_states, void* stream);
+
+/* Reverse pass: gradients of q, k, v (io_dtype; those of shared query / key heads are summed over the value heads, in a fixed order), eta,
+ * log_gamma and S_init from d_o and dS_final (NULL: zeros).  dS_init may alias dS_final.  states_saved != 0: the workspace still
+ * holds what e2ttt_delta_fwd(save_states = 1) left for the same inputs; 0: it is computed again first.  Where log_gamma is
+ * below -104 (the decay is 0 in 32 bits) its gradient is 0. */
+E2TTT_API int e2ttt_delta_bwd(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
+                              const float* log_gamma, const float* S_init, const void* d_o, const float* dS_final, void* dq, void* dk,
+                              void* dv, float* d_eta, float* d_log_gamma, float* dS_init, void* workspace, size_t workspace_bytes,
+                              int states_saved, void* stream);
+
+/* Recurrent form over the L tokens of the call (meant for one or a few); S_out may alias S.  No workspace: HBM-bound, the state is
+ * read and written once. */
+E2TTT_API int e2ttt_delta_step(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
+                               const float* log_gamma, const float* S, void* o, float* S_out, void* stream);
+
 /* Reads back the device status word of the last launch that used `workspace` (the first word of every
  * workspace).  workspace == NULL reads the word of the scratch array e2ttt_chunk_fwd_noalloc uses on the
  * current device (0 if that entry point has not run there yet).  This is the one entry point that

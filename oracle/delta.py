@@ -1,0 +1,52 @@
+"""Gated delta rule in fp64, token by token, and its adjoint: test infrastructure, no code shared with the GPU path."""
+from __future__ import annotations
+
+import numpy as np
+
+
+def forward(q, k, v, eta, log_gamma, S, scale):
+    """q, k [B,Hk,L,dk], v [B,H,L,dv], eta, log_gamma [B,H,L], S [B,H,dv,dk] or None -> o, S_final (all fp64)."""
+    q, k, v, eta, log_gamma = (np.asarray(x, np.float64) for x in (q, k, v, eta, log_gamma))
+    B, H, L, dv = v.shape
+    r = H // q.shape[1]
+    q, k = np.repeat(q, r, 1), np.repeat(k, r, 1)
+    S = np.zeros((B, H, dv, q.shape[-1])) if S is None else np.array(S, np.float64)
+    o = np.zeros_like(v)
+    for t in range(L):
+        S = np.exp(log_gamma[:, :, t])[..., None, None] * S
+        e = v[:, :, t] - np.einsum("bhij,bhj->bhi", S, k[:, :, t])
+        S = S + (eta[:, :, t, None] * e)[..., :, None] * k[:, :, t, None, :]
+        o[:, :, t] = scale * np.einsum("bhij,bhj->bhi", S, q[:, :, t])
+    return o, S
+
+
+def backward(q, k, v, eta, log_gamma, S, scale, d_o, dS_final):
+    """Adjoints of q, k, v, eta, log_gamma and the start state, from those of o and the final state (None: zeros)."""
+    q0, k0, v, eta, log_gamma, d_o = (np.asarray(x, np.float64) for x in (q, k, v, eta, log_gamma, d_o))
+    B, H, L, dv = v.shape
+    Hk, dk = q0.shape[1], q0.shape[-1]
+    r = H // Hk
+    q, k = np.repeat(q0, r, 1), np.repeat(k0, r, 1)
+    S = np.zeros((B, H, dv, dk)) if S is None else np.array(S, np.float64)
+    decayed, after, es = [], [], []
+    for t in range(L):
+        Sp = np.exp(log_gamma[:, :, t])[..., None, None] * S
+        e = v[:, :, t] - np.einsum("bhij,bhj->bhi", Sp, k[:, :, t])
+        S = Sp + (eta[:, :, t, None] * e)[..., :, None] * k[:, :, t, None, :]
+        decayed.append(Sp), after.append(S), es.append(e)
+    X = np.zeros((B, H, dv, dk)) if dS_final is None else np.array(dS_final, np.float64)
+    dq, d_k, d_v = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)
+    d_eta, d_lg = np.zeros_like(eta), np.zeros_like(eta)
+    for t in range(L - 1, -1, -1):
+        dq[:, :, t] = scale * np.einsum("bhi,bhij->bhj", d_o[:, :, t], after[t])
+        X = X + scale * d_o[:, :, t, :, None] * q[:, :, t, None, :]
+        Xk = np.einsum("bhij,bhj->bhi", X, k[:, :, t])
+        d_eta[:, :, t] = (es[t] * Xk).sum(-1)
+        de = eta[:, :, t, None] * Xk
+        d_k[:, :, t] = np.einsum("bhi,bhij->bhj", eta[:, :, t, None] * es[t], X) - np.einsum("bhi,bhij->bhj", de, decayed[t])
+        d_v[:, :, t] = de
+        X = X - de[..., :, None] * k[:, :, t, None, :]
+        d_lg[:, :, t] = (X * decayed[t]).sum((-1, -2))
+        X = np.exp(log_gamma[:, :, t])[..., None, None] * X
+    group = lambda x: x.reshape(B, Hk, r, L, dk).sum(2)  # noqa: E731
+    return {"dq": group(dq), "dk": group(d_k), "dv": d_v, "d_eta": d_eta, "d_log_gamma": d_lg, "dS": X}

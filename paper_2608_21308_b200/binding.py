@@ -33,6 +33,11 @@ class e2ttt_params(ctypes.Structure):
                 ("ckpt_every", ctypes.c_int32)]
 
 
+class e2ttt_delta_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("L", ctypes.c_int32),
+                ("dk", ctypes.c_int32), ("dv", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class E2TTTError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -75,6 +80,15 @@ def lib() -> ctypes.CDLL:
         L.e2ttt_prepare_bwd.restype = cp
         L.e2ttt_apply.argtypes = [pp, vp, tab, vp, vp]
         L.e2ttt_apply.restype = cp
+        dp = ctypes.POINTER(e2ttt_delta_params)
+        L.e2ttt_delta_workspace_bytes.argtypes = [dp, cp, ctypes.POINTER(ctypes.c_size_t)]
+        L.e2ttt_delta_workspace_bytes.restype = cp
+        L.e2ttt_delta_fwd.argtypes = [dp] + [vp] * 9 + [ctypes.c_size_t, cp, vp]
+        L.e2ttt_delta_fwd.restype = cp
+        L.e2ttt_delta_bwd.argtypes = [dp] + [vp] * 15 + [ctypes.c_size_t, cp, vp]
+        L.e2ttt_delta_bwd.restype = cp
+        L.e2ttt_delta_step.argtypes = [dp] + [vp] * 9
+        L.e2ttt_delta_step.restype = cp
         L.e2ttt_device_status.argtypes = [vp, vp, ctypes.POINTER(cp)]
         L.e2ttt_device_status.restype = cp
         L.e2ttt_selftest_wait_timeout.argtypes = [vp, ctypes.c_size_t, ctypes.c_longlong, vp]
@@ -314,6 +328,73 @@ def e2ttt_chunk_bwd(p, q, k, v, eta, beta, gamma, W_init, M_init, d_o, dW_final,
         int(states_saved), _stream_ptr(stream))
     if st != E2TTT_OK:
         raise E2TTTError(st, "e2ttt_chunk_bwd")
+    return st
+
+
+def make_delta_params(B, H, Hk, L, dk, dv, io_dtype=E2TTT_F32, scale=1.0):
+    return e2ttt_delta_params(B, H, Hk, L, dk, dv, io_dtype, scale)
+
+
+def e2ttt_delta_workspace_bytes(p: e2ttt_delta_params, save_states: int) -> int:
+    n = ctypes.c_size_t()
+    st = (_lib or lib()).e2ttt_delta_workspace_bytes(ctypes.byref(p), int(save_states), ctypes.byref(n))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_delta_workspace_bytes")
+    return int(n.value)
+
+
+def _here(*tensors):
+    """A call runs on the current device: tensors of another one are refused."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"a tensor is on {t.device}, but the current device is cuda:{dev}")
+
+
+def e2ttt_delta_fwd(p, q, k, v, eta, log_gamma, S_init, o, S_final, workspace, save_states=0, stream=None):
+    """int e2ttt_delta_fwd(...) of include/e2ttt.h: the gated delta rule over whole sequences.  Raises on error."""
+    io = _io_torch_dtype(p)
+    sk, sv, s3, ss = (p.B, p.Hk, p.L, p.dk), (p.B, p.H, p.L, p.dv), (p.B, p.H, p.L), (p.B, p.H, p.dv, p.dk)
+    args = (_ptr(q, io, sk, "q"), _ptr(k, io, sk, "k"), _ptr(v, io, sv, "v"), _ptr(eta, _F32, s3, "eta"),
+            _ptr(log_gamma, _F32, s3, "log_gamma"), _ptr(S_init, _F32, ss, "S_init"), _ptr(o, io, sv, "o"),
+            _ptr(S_final, _F32, ss, "S_final"), _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(q, k, v, eta, log_gamma, S_init, o, S_final, workspace)
+    st = (_lib or lib()).e2ttt_delta_fwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, int(save_states),
+                                         _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_delta_fwd")
+    return st
+
+
+def e2ttt_delta_bwd(p, q, k, v, eta, log_gamma, S_init, d_o, dS_final, dq, dk, dv, d_eta, d_log_gamma, dS_init, workspace,
+                    states_saved=0, stream=None):
+    """int e2ttt_delta_bwd(...) of include/e2ttt.h: its reverse pass.  Raises on error."""
+    io = _io_torch_dtype(p)
+    sk, sv, s3, ss = (p.B, p.Hk, p.L, p.dk), (p.B, p.H, p.L, p.dv), (p.B, p.H, p.L), (p.B, p.H, p.dv, p.dk)
+    args = (_ptr(q, io, sk, "q"), _ptr(k, io, sk, "k"), _ptr(v, io, sv, "v"), _ptr(eta, _F32, s3, "eta"),
+            _ptr(log_gamma, _F32, s3, "log_gamma"), _ptr(S_init, _F32, ss, "S_init"), _ptr(d_o, io, sv, "d_o"),
+            _ptr(dS_final, _F32, ss, "dS_final"), _ptr(dq, io, sk, "dq"), _ptr(dk, io, sk, "dk"), _ptr(dv, io, sv, "dv"),
+            _ptr(d_eta, _F32, s3, "d_eta"), _ptr(d_log_gamma, _F32, s3, "d_log_gamma"), _ptr(dS_init, _F32, ss, "dS_init"),
+            _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(q, k, v, eta, log_gamma, S_init, d_o, dS_final, dq, dk, dv, d_eta, d_log_gamma, dS_init, workspace)
+    st = (_lib or lib()).e2ttt_delta_bwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, int(states_saved),
+                                         _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_delta_bwd")
+    return st
+
+
+def e2ttt_delta_step(p, q, k, v, eta, log_gamma, S, o, S_out, stream=None):
+    """int e2ttt_delta_step(...) of include/e2ttt.h: p.L tokens per sequence in the recurrent form.  Raises on error."""
+    io = _io_torch_dtype(p)
+    B, H, L, dv = p.B, p.H, p.L, p.dv
+    sk, sv, s3, ss = (B, p.Hk, L, p.dk), (B, H, L, dv), (B, H, L), (B, H, dv, p.dk)
+    args = (_ptr(q, io, sk, "q"), _ptr(k, io, sk, "k"), _ptr(v, io, sv, "v"), _ptr(eta, _F32, s3, "eta"),
+            _ptr(log_gamma, _F32, s3, "log_gamma"), _ptr(S, _F32, ss, "S"), _ptr(o, io, sv, "o"), _ptr(S_out, _F32, ss, "S_out"))
+    _here(q, k, v, eta, log_gamma, S, o, S_out)
+    st = (_lib or lib()).e2ttt_delta_step(ctypes.byref(p), *args, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_delta_step")
     return st
 
 

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/e2ttt.h"
+#include "api_checks.h"
 #include "apply.h"
 #include "prepare.h"
 #include "simt_layout.h"
@@ -40,9 +41,6 @@ int check_params(const e2ttt_params* p) {
 
 // chunks per recomputed segment of the backward; 0 = every chunk's state is kept
 int segment_chunks(const e2ttt_params* p) { return p->ckpt_every >= 2 ? p->ckpt_every : 0; }
-
-// Every workspace starts with a status block: word 0 is the device status of the last launch that used it.
-constexpr size_t kStatusBytes = 256;
 
 // 1 = a tensor-core specialisation exists for these parameters (the forward; with save_states it also writes the
 // chunk-start states in the layout the SIMT backward reads)
@@ -120,9 +118,9 @@ size_t simt_bytes(const e2ttt_params* p, bool save_states, bool backward, bool n
     return kStatusBytes + l.per_seq * elem * (size_t)p->B * p->H;
 }
 
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+}  // namespace
 
-int check_device() {
+int e2ttt::check_device() {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return E2TTT_ERR_ARCH; }
     static int cached_major[64];
@@ -139,8 +137,6 @@ int check_device() {
     }
     return major == 10 ? E2TTT_OK : E2TTT_ERR_ARCH;
 }
-
-}  // namespace
 
 extern "C" {
 

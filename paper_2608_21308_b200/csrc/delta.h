@@ -1,0 +1,113 @@
+// Gated delta rule: arguments of the launchers and the layout of the workspace (no CUDA types: the host tests read it too).
+//
+// Per sequence and value head a state S [dv, dk] moves token by token:
+//   S'_t = g_t S_{t-1},  e_t = v_t - S'_t k_t,  S_t = S'_t + eta_t e_t k_t^T,  o_t = scale S_t q_t,   g_t = exp(log_gamma_t).
+// A chunk of 32 tokens from its start state S_0 in matrix form, b_t the product of g up to token t, D_ti = b_t / b_i:
+//   P = V - b S_0 K,   e = T P,  T = (I + strict(D (K K^T)) eta)^-1,   u = eta e,
+//   O = scale (b S_0 Q + A u),  A = lower(D (Q K^T)),   S = b_end S_0 + (D_end u)^T K.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+namespace e2ttt {
+
+constexpr int kDeltaChunk = 32;  // tokens per chunk: a warp's row for its gates, two k-steps of the MMAs
+constexpr int kDeltaBlock = 64;  // tokens per saved state (two chunks)
+constexpr int kDeltaMaxD = 128;  // a slice of 16 state rows of 128 columns is a quarter of a warp's registers
+// A chunk's record: T and A (two fp16 terms each, 2 KB a term), eight rows of 32 floats; with saved states also the T of the reverse
+// pass, (I + eta strict(D (K K^T)))^-1.  The forward fetches the first 9 KB, the reverse pass the last 9.
+constexpr int kDeltaRecBytes = 9216;
+constexpr int kDeltaRecSkip = 4096;
+// rows of a record's scalars
+enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecHead = 7 };
+
+struct DeltaShape {
+    int B, H, Hk, L, dk, dv;
+    int f32;  // 1: fp32 I/O
+    float scale;
+};
+
+struct DeltaLayout {
+    int DK;            // columns of a padded state row: 64 or 128
+    int terms;         // fp16 terms of a query or key: 1 (bf16 I/O, exact) or 2
+    int dvp;           // value rows padded to 16
+    int slices;        // dvp / 16: warps that a sequence's state is cut into
+    int nch, nblk;     // chunks of 32 tokens, blocks of 64
+    int64_t N, Nk;     // sequences (value heads), query / key heads
+    size_t qk_bytes;   // query and key tiles of a chunk
+    size_t rec_bytes;  // record of a chunk
+    // offsets in bytes
+    size_t qk, rec, e, o, S, dp, X, part_eta, part_gate, hx, max_u, max_s, max_dp, max_x, max_do, total;
+};
+
+inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
+    DeltaLayout l{};
+    l.DK = s.dk <= 64 ? 64 : 128;
+    l.terms = s.f32 ? 2 : 1;
+    l.dvp = (s.dv + 15) / 16 * 16;
+    l.slices = l.dvp / 16;
+    l.nch = (int)(((int64_t)s.L + kDeltaChunk - 1) / kDeltaChunk);
+    l.nblk = (int)(((int64_t)s.L + kDeltaBlock - 1) / kDeltaBlock);
+    l.N = (int64_t)s.B * s.H;
+    l.Nk = (int64_t)s.B * s.Hk;
+    l.qk_bytes = (size_t)2 * l.terms * 64 * l.DK;
+    l.rec_bytes = kDeltaRecBytes + (save ? 4096 : 0);
+    size_t at = 256;  // the status block
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    l.qk = take((size_t)l.Nk * l.nch * l.qk_bytes);
+    l.rec = take((size_t)l.N * l.nch * l.rec_bytes);
+    if (save) {
+        const size_t tok = (size_t)l.N * l.nch * l.dvp * kDeltaChunk * 4, part = (size_t)l.N * l.nch * l.slices * kDeltaChunk * 4;
+        l.e = take(tok);
+        l.o = take(tok);
+        l.S = take((size_t)l.N * (l.nblk + 1) * l.dvp * l.DK * 4);
+        l.dp = take(tok);
+        l.X = take((size_t)l.N * l.nblk * l.dvp * l.DK * 4);
+        l.part_eta = take(part);
+        l.part_gate = take(part);
+        l.hx = take((size_t)l.N * l.nblk * l.slices * 4);
+        // largest magnitudes per slice: the scales of dq's and dk's operands
+        l.max_u = take((size_t)l.N * l.nch * l.slices * 4);
+        l.max_dp = take((size_t)l.N * l.nch * l.slices * 4);
+        l.max_do = take((size_t)l.N * l.nch * l.slices * 4);
+        l.max_s = take((size_t)l.N * (l.nblk + 1) * l.slices * 4);
+        l.max_x = take((size_t)l.N * l.nblk * l.slices * 4);
+    }
+    l.total = at;
+    return l;
+}
+
+struct DeltaArgs {
+    DeltaShape s;
+    DeltaLayout l;
+    const void *q, *k, *v;
+    const float *eta, *log_gamma, *S_init;  // S_init may be null
+    void* o;                                // may be null (recomputation)
+    float* S_final;                         // may be null (recomputation)
+    char* ws;
+    int save;
+};
+
+struct DeltaBwdArgs {
+    DeltaArgs f;
+    const void* d_o;
+    const float* dS_final;  // may be null
+    void *dq, *dk, *dv;
+    float *d_eta, *d_log_gamma, *dS_init;
+};
+
+struct DeltaStepArgs {
+    DeltaShape s;
+    const void *q, *k, *v;
+    const float *eta, *log_gamma, *S;
+    void* o;
+    float* S_out;
+};
+
+// return a cudaError_t value as int
+int delta_prep_launch(const DeltaArgs& a, void* stream);
+int delta_fwd_launch(const DeltaArgs& a, void* stream);
+int delta_bwd_launch(const DeltaBwdArgs& a, void* stream);
+int delta_step_launch(const DeltaStepArgs& a, void* stream);
+
+}  // namespace e2ttt

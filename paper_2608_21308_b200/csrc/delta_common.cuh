@@ -1,0 +1,111 @@
+// Gated delta rule: fragments, the two-term fp16 form of an operand, tile addressing.
+//
+// Products run as mma.m16n8k16 with fp16 operands and fp32 sums.  A state is cut into slices of 16 value rows, one warp each: the slice
+// stays in a warp's accumulators for the whole sequence, an accumulator tile is the next product's A operand as it is, and no value
+// crosses a warp.  A 128-lane tensor-memory tile would hold one sequence per SM and send the state through tensor memory and back
+// between any two of the four dependent products of a chunk.
+// Operands in 32 bits are used as two fp16 terms, x = 2^-s (hi + lo): 22 bits, and s (a power of two per row or tile, from its largest
+// value) keeps both terms inside fp16's exponents.  What is bf16 on input is one term, exactly.  (Two bf16 terms, 16 bits, leave 3e-6
+// in every product: the fp32 outputs would be ten times less exact.)
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "delta.h"
+#include "sm100.cuh"
+
+namespace e2ttt {
+namespace delta {
+
+constexpr unsigned kAll = 0xffffffffu;
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename IO> __device__ __forceinline__ IO from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// power of two that brings a largest magnitude m into [2^12, 2^13) (2^100 at most: m = 0), and its inverse
+__device__ __forceinline__ void pow2_scale(float m, float& s, float& inv) {
+    int e = 139 - (int)(__float_as_uint(m) >> 23);
+    e = max(-100, min(100, e));
+    s = __uint_as_float((uint32_t)(127 + e) << 23);
+    inv = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+__device__ __forceinline__ float quad_max(float m) {  // over the four lanes that share a fragment row
+    m = fmaxf(m, __shfl_xor_sync(kAll, m, 1));
+    return fmaxf(m, __shfl_xor_sync(kAll, m, 2));
+}
+__device__ __forceinline__ float warp_max(float m) {
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, i));
+    return m;
+}
+
+__device__ __forceinline__ uint32_t pack_half(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& lo) {
+    const __half2 h = __floats2half2_rn(x, y);
+    const float2 f = __half22float2(h);
+    hi = *reinterpret_cast<const uint32_t*>(&h);
+    lo = pack_half(x - f.x, y - f.y);
+}
+
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+// Tiles of fp16 in shared memory and in the workspace: rows of COLS values, the 16-byte piece p of row r at place p ^ swz(r), so that
+// eight rows' pieces of one column (an 8 x 8 matrix of ldmatrix) lie in different banks.
+template <int COLS> __device__ __forceinline__ uint32_t tile_at(int row, int piece) {
+    const int sw = COLS >= 64 ? (row & 7) : ((row >> 1) & 3);
+    return (uint32_t)(row * COLS * 2 + ((piece ^ sw) << 4));
+}
+// B fragments of n-tiles n0, n0 + 1 (8 columns each) at k-step kk from a tile [n][k]: r[0], r[1] the first tile's, r[2], r[3] the second's
+template <int COLS> __device__ __forceinline__ uint32_t addr_nk(uint32_t base, int n0, int kk, int lane) {
+    const int m = lane >> 3, r = lane & 7;
+    return base + tile_at<COLS>(n0 * 8 + (m >> 1) * 8 + r, kk * 2 + (m & 1));
+}
+// the same from a tile [k][n] (with ldsm4_t)
+template <int COLS> __device__ __forceinline__ uint32_t addr_kn(uint32_t base, int n0, int kk, int lane) {
+    const int m = lane >> 3, r = lane & 7;
+    return base + tile_at<COLS>(kk * 16 + (m & 1) * 8 + r, n0 + (m >> 1));
+}
+// A fragments of rows m0.. (16) at k-step kk from a tile [m][k]
+template <int COLS> __device__ __forceinline__ uint32_t addr_mk(uint32_t base, int m0, int kk, int lane) {
+    const int m = lane >> 3, r = lane & 7;
+    return base + tile_at<COLS>(m0 + (m & 1) * 8 + r, kk * 2 + (m >> 1));
+}
+// A fragments from a tile [k][m] (with ldsm4_t)
+template <int COLS> __device__ __forceinline__ uint32_t addr_km(uint32_t base, int m0, int kk, int lane) {
+    const int m = lane >> 3, r = lane & 7;
+    return base + tile_at<COLS>(kk * 16 + (m >> 1) * 8 + r, (m0 >> 3) + (m & 1));
+}
+
+// two adjacent 16 x 8 accumulator tiles as the A operand of one k-step, rows scaled by s0 (rows 0-7) and s1 (rows 8-15), in two terms
+__device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], float s0, float s1, uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+    split(x[0] * s0, x[1] * s0, hi[0], lo[0]);
+    split(x[2] * s1, x[3] * s1, hi[1], lo[1]);
+    split(y[0] * s0, y[1] * s0, hi[2], lo[2]);
+    split(y[2] * s1, y[3] * s1, hi[3], lo[3]);
+}
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(sm100::smem_u32(bar)) : "memory");
+}
+
+}  // namespace delta
+}  // namespace e2ttt

@@ -1,0 +1,263 @@
+// Gated delta rule, what does not depend on the state: one warp per chunk of 32 tokens and query / key head.
+// It writes the chunk's queries and keys as fp16 tiles (scaled by powers of two, zero-padded, swizzled: the kernels that walk the chunks fetch
+// them with bulk copies whatever the caller's width and alignment), and for every value head of the group the record of delta.h:
+// T, A and the products of the decays.  All chunks run side by side.
+#include "delta_common.cuh"
+
+namespace e2ttt {
+namespace {
+using namespace delta;
+
+constexpr int kWarps = 4;
+
+template <int DK, int KT> constexpr int prep_warp_bytes() { return 2 * KT * 64 * DK + 4608 + 256 + 128; }
+
+// largest magnitude of a row tile, then its scaled terms to shared memory and to the workspace
+template <typename IO, int DK, int KT>
+__device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool vec, char* sm, char* out, int lane) {
+    constexpr int P = DK / 8;  // 16-byte pieces of a tile row
+    float m = 0.0f;
+    auto load = [&](int i, float (&x)[8]) {
+        const int r = i / P, c = (i % P) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+        if (r >= rows || c >= d) return;
+        const IO* p = src + (size_t)r * d + c;
+        if (vec) {
+            if (sizeof(IO) == 2) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(p);
+                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] = __uint_as_float(w[j] << 16);
+                    x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                }
+            } else {
+                const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+                x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < d) x[j] = to_f32(p[j]);
+        }
+    };
+#pragma unroll 4
+    for (int i = lane; i < 32 * P; i += 32) {
+        float x[8];
+        load(i, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[j]));
+    }
+    m = warp_max(m);
+    float s, inv;
+    pow2_scale(m, s, inv);
+#pragma unroll 4
+    for (int i = lane; i < 32 * P; i += 32) {
+        float x[8];
+        load(i, x);  // from L1
+        uint4 hi, lo;
+        split(x[0] * s, x[1] * s, hi.x, lo.x);
+        split(x[2] * s, x[3] * s, hi.y, lo.y);
+        split(x[4] * s, x[5] * s, hi.z, lo.z);
+        split(x[6] * s, x[7] * s, hi.w, lo.w);
+        const uint32_t at = tile_at<DK>(i / P, i % P);
+        *reinterpret_cast<uint4*>(sm + at) = hi;
+        *reinterpret_cast<uint4*>(out + at) = hi;
+        if (KT == 2) {
+            *reinterpret_cast<uint4*>(sm + 64 * DK + at) = lo;
+            *reinterpret_cast<uint4*>(out + 64 * DK + at) = lo;
+        }
+    }
+    return inv;
+}
+
+// rows x keys on and below the diagonal blocks: tiles (m, n) with n <= 2 m + 1
+template <int DK, int KT> __device__ __forceinline__ void gram(uint32_t rows, uint32_t keys, float (&c)[6][4], int lane) {
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c[i][j] = 0.0f;
+#pragma unroll 2
+    for (int kk = 0; kk < DK / 16; ++kk) {
+        uint32_t a0[KT][4], a1[KT][4], b0[KT][4], b1[KT][4];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+            ldsm4(a0[t], addr_mk<DK>(rows + t * 64 * DK, 0, kk, lane));
+            ldsm4(a1[t], addr_mk<DK>(rows + t * 64 * DK, 16, kk, lane));
+            ldsm4(b0[t], addr_nk<DK>(keys + t * 64 * DK, 0, kk, lane));
+            ldsm4(b1[t], addr_nk<DK>(keys + t * 64 * DK, 2, kk, lane));
+        }
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int u = 0; u + t < KT; ++u) {
+                mma(c[0], a0[t], b0[u][0], b0[u][1]);
+                mma(c[1], a0[t], b0[u][2], b0[u][3]);
+                mma(c[2], a1[t], b0[u][0], b0[u][1]);
+                mma(c[3], a1[t], b0[u][2], b0[u][3]);
+                mma(c[4], a1[t], b1[u][0], b1[u][1]);
+                mma(c[5], a1[t], b1[u][2], b1[u][3]);
+            }
+    }
+}
+
+// (I + N)^-1 of a strictly lower N column by column, lane = column: x_t = [t == lane] - sum_{i < t} N_ti x_i; two terms to `out`
+__device__ __forceinline__ float invert(const float* Nm, char* out, int lane) {
+    float x[32], most = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 32; ++t) {
+        float y[4] = {t == lane ? 1.0f : 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < t; i += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(Nm + t * 36 + i);
+            y[0] = fmaf(-w.x, x[i], y[0]);
+            if (i + 1 < t) y[1] = fmaf(-w.y, x[i + 1], y[1]);
+            if (i + 2 < t) y[2] = fmaf(-w.z, x[i + 2], y[2]);
+            if (i + 3 < t) y[3] = fmaf(-w.w, x[i + 3], y[3]);
+        }
+        x[t] = (y[0] + y[1]) + (y[2] + y[3]);
+        most = fmaxf(most, fabsf(x[t]));
+    }
+    float s, inv;
+    pow2_scale(warp_max(most), s, inv);
+#pragma unroll
+    for (int t = 0; t < 32; ++t) {
+        const float y = x[t] * s;
+        const __half hi = __float2half_rn(y), lo = __float2half_rn(y - __half2float(hi));
+        const uint32_t at = tile_at<32>(t, lane >> 3) + (lane & 7) * 2;
+        *reinterpret_cast<__half*>(out + at) = hi;
+        *reinterpret_cast<__half*>(out + 2048 + at) = lo;
+    }
+    return inv;
+}
+
+template <typename IO, int DK, int KT>
+__global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaArgs a, const bool vec) {
+    extern __shared__ __align__(1024) char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const DeltaShape& s = a.s;
+    const int64_t item = (int64_t)blockIdx.x * kWarps + warp;
+    if (item >= a.l.Nk * a.l.nch) return;
+    if (item == 0 && lane == 0) *reinterpret_cast<int*>(a.ws) = 0;  // the status word
+    const int64_t nk = item / a.l.nch;
+    const int c = (int)(item % a.l.nch);
+    const int t0 = c * kDeltaChunk, rows = min(kDeltaChunk, s.L - t0);
+    char* sm = smem + warp * prep_warp_bytes<DK, KT>();
+    float* Nm = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK);  // 32 x 32, rows of 36
+    double* run = reinterpret_cast<double*>(sm + 2 * KT * 64 * DK + 4608);
+    float* eta_s = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK + 4608 + 256);
+    char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
+    const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
+    const float ik = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(a.k) + row0, rows, s.dk, vec, sm, out, lane);
+    const float iq = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(a.q) + row0, rows, s.dk, vec, sm + KT * 64 * DK, out + KT * 64 * DK, lane);
+    __syncwarp();
+    const uint32_t ks = sm100::smem_u32(sm), qs = ks + KT * 64 * DK;
+    float kk[6][4], qk[6][4];
+    gram<DK, KT>(ks, ks, kk, lane);
+    gram<DK, KT>(qs, ks, qk, lane);
+    const int g = lane >> 2, c4 = lane & 3, r = s.H / s.Hk;
+    const int64_t b = nk / s.Hk, hk = nk % s.Hk;
+    for (int j = 0; j < r; ++j) {
+        const int64_t n = b * s.H + hk * r + j;
+        const size_t gate = (size_t)n * s.L + t0;
+        // gates: lane = token.  The decays' logarithms are summed in 64 bits (the differences of long sums are what counts); below -1000
+        // a decay is 0 in 32 bits all the same, and infinities leave the differences.
+        float lg = lane < rows ? a.log_gamma[gate + lane] : 0.0f;
+        const float eta = lane < rows ? a.eta[gate + lane] : 0.0f;
+        if (lg < -1000.0f) lg = -1000.0f;
+        double sum = (double)lg;
+#pragma unroll
+        for (int i = 1; i < 32; i <<= 1) {
+            const double y = __shfl_up_sync(kAll, sum, i);
+            if (lane >= i) sum += y;
+        }
+        const double end = __shfl_sync(kAll, sum, 31);
+        __syncwarp();
+        run[lane] = sum;
+        eta_s[lane] = eta;
+        __syncwarp();
+        char* rec = a.ws + a.l.rec + ((size_t)n * a.l.nch + c) * a.l.rec_bytes;
+        float* sc = reinterpret_cast<float*>(rec + 8192);
+        const float bt = expf((float)sum), dend = expf((float)(end - sum));
+        sc[kRecBk * 32 + lane] = bt * ik;
+        sc[kRecBq * 32 + lane] = bt * iq * s.scale;
+        sc[kRecEta * 32 + lane] = eta;
+        sc[kRecDend * 32 + lane] = dend * ik;
+        // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
+        float amax = 0.0f, av[6][4];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+            const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
+                const float D = u <= t ? expf((float)(run[t] - run[u])) : 0.0f;
+                Nm[t * 36 + u] = u < t ? D * kk[i][x] * (ik * ik) * eta_s[u] : 0.0f;
+                av[i][x] = u <= t ? D * qk[i][x] * (iq * ik * s.scale) : 0.0f;
+                amax = fmaxf(amax, fabsf(av[i][x]));
+            }
+        }
+        float as, ai;
+        pow2_scale(warp_max(amax), as, ai);
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {  // the block above the diagonal is read by no product
+            const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i : i - 2;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                uint32_t hi, lo;
+                split(av[i][2 * x] * as, av[i][2 * x + 1] * as, hi, lo);
+                const uint32_t at = tile_at<32>(m0 + g + x * 8, n0) + c4 * 4;
+                *reinterpret_cast<uint32_t*>(rec + 4096 + at) = hi;
+                *reinterpret_cast<uint32_t*>(rec + 6144 + at) = lo;
+            }
+        }
+        __syncwarp();
+        const float ti = invert(Nm, rec, lane);
+        float ri = 0.0f;
+        if (a.save) {  // the same with eta on the rows: what the reverse pass multiplies with
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
+                    Nm[t * 36 + u] = u < t ? expf((float)(run[t] - run[u])) * kk[i][x] * (ik * ik) * eta_s[t] : 0.0f;
+                }
+            }
+            __syncwarp();
+            ri = invert(Nm, rec + kDeltaRecBytes, lane);
+        }
+        if (lane == 0) {
+            sc[kRecHead * 32 + 0] = expf((float)end);
+            sc[kRecHead * 32 + 1] = ti;
+            sc[kRecHead * 32 + 2] = ai;
+            sc[kRecHead * 32 + 3] = ik;
+            sc[kRecHead * 32 + 4] = iq;
+            sc[kRecHead * 32 + 5] = ri;
+        }
+        __syncwarp();
+    }
+}
+
+template <typename IO, int DK, int KT> int launch(const DeltaArgs& a, cudaStream_t st) {
+    constexpr int bytes = kWarps * prep_warp_bytes<DK, KT>();
+    auto kernel = delta_prep_kernel<IO, DK, KT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return (int)e;
+    const bool vec = a.s.dk % 8 == 0 && (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k)) % 16 == 0;
+    const unsigned grid = (unsigned)((a.l.Nk * a.l.nch + kWarps - 1) / kWarps);
+    kernel<<<grid, kWarps * 32, bytes, st>>>(a, vec);
+    return (int)cudaGetLastError();
+}
+
+}  // namespace
+
+int delta_prep_launch(const DeltaArgs& a, void* stream) {
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (a.s.f32) return a.l.DK == 64 ? launch<float, 64, 2>(a, st) : launch<float, 128, 2>(a, st);
+    return a.l.DK == 64 ? launch<__nv_bfloat16, 64, 1>(a, st) : launch<__nv_bfloat16, 128, 1>(a, st);
+}
+
+}  // namespace e2ttt
