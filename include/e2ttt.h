@@ -304,6 +304,35 @@ E2TTT_API int e2ttt_delta_bwd(const e2ttt_delta_params* p, const void* q, const 
 E2TTT_API int e2ttt_delta_step(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
                                const float* log_gamma, const float* S, void* o, float* S_out, void* stream);
 
+/* Block join: what stands between a token-mixing block's heads and the next block (the paper's block ends in a gate and a norm, Fig.
+ * "attention_block"): norm after the block, gate, scaled residual sum, norm before the next block, in one pass.  Per token
+ *   y = o / sqrt(mean_d(o^2) + post_eps) * w_post   (per head),   x_out = x + res_scale * gate(a) * y,
+ *   n = x_out / sqrt(mean(x_out^2) + pre_eps) * w_pre   (over all H d values).
+ *   o                        [B,H,L,d] io_dtype: the block's outputs by heads, as e2ttt_chunk_fwd, e2ttt_apply and e2ttt_delta_* write them
+ *                            (H = 1 with d the model's width: the output of a projection)
+ *   a, x, x_out, n           [B,L,H d] io_dtype, head h at columns h d .. (h + 1) d
+ *   w_post, res_scale, w_pre [H d] fp32
+ * a is NULL with E2TTT_GATE_NONE and required otherwise; w_pre and n_out (d_n, d_w_pre) are given together or not at all (no second norm).
+ * x_out may alias x, n_out may alias a.  H d <= 8192.  fp32 arithmetic, each output rounded once; n is of the unrounded x_out.
+ * Returns E2TTT_OK or E2TTT_ERR_NULL / _SHAPE / _DTYPE / _ALIGN / _WORKSPACE / _ARCH / _CUDA; alignment as for e2ttt_delta_fwd. */
+typedef enum { E2TTT_GATE_NONE = 0, E2TTT_GATE_SIGMOID = 1, E2TTT_GATE_SILU = 2 } e2ttt_gate;
+typedef struct {
+    int32_t B, H, L, d;
+    int32_t io_dtype; /* e2ttt_dtype */
+    int32_t gate;     /* e2ttt_gate */
+    float post_eps, pre_eps; /* >= 0 */
+} e2ttt_join_params;
+E2TTT_API int e2ttt_join_fwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post,
+                             const float* res_scale, const float* w_pre, void* x_out, void* n_out, void* stream);
+
+/* Reverse pass from the forward's inputs: gradients of o, a, x (io_dtype) and of the three vectors (fp32, sums over all tokens in a fixed
+ * order).  d_x may alias d_x_out.  workspace: e2ttt_join_workspace_bytes, 256-byte aligned; partial sums only, no device status. */
+E2TTT_API int e2ttt_join_workspace_bytes(const e2ttt_join_params* p, size_t* bytes);
+E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post,
+                             const float* res_scale, const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a,
+                             void* d_x, float* d_w_post, float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
 /* Reads back the device status word of the last launch that used `workspace` (the first word of every
  * workspace).  workspace == NULL reads the word of the scratch array e2ttt_chunk_fwd_noalloc uses on the
  * current device (0 if that entry point has not run there yet).  This is the one entry point that

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "lib", "libe2ttt.so")
 E2TTT_MLP_GELU, E2TTT_SWIGLU = 0, 1
 E2TTT_F32, E2TTT_BF16 = 0, 1
 E2TTT_IMPL_AUTO, E2TTT_IMPL_SIMT, E2TTT_IMPL_TCGEN05, E2TTT_IMPL_TILED = 0, 1, 2, 3
+E2TTT_GATE_NONE, E2TTT_GATE_SIGMOID, E2TTT_GATE_SILU = 0, 1, 2
 E2TTT_OK = 0
 
 
@@ -36,6 +37,11 @@ class e2ttt_params(ctypes.Structure):
 class e2ttt_delta_params(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("L", ctypes.c_int32),
                 ("dk", ctypes.c_int32), ("dv", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class e2ttt_join_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float)]
 
 
 class E2TTTError(RuntimeError):
@@ -89,6 +95,13 @@ def lib() -> ctypes.CDLL:
         L.e2ttt_delta_bwd.restype = cp
         L.e2ttt_delta_step.argtypes = [dp] + [vp] * 9
         L.e2ttt_delta_step.restype = cp
+        jp = ctypes.POINTER(e2ttt_join_params)
+        L.e2ttt_join_workspace_bytes.argtypes = [jp, ctypes.POINTER(ctypes.c_size_t)]
+        L.e2ttt_join_workspace_bytes.restype = cp
+        L.e2ttt_join_fwd.argtypes = [jp] + [vp] * 9
+        L.e2ttt_join_fwd.restype = cp
+        L.e2ttt_join_bwd.argtypes = [jp] + [vp] * 15 + [ctypes.c_size_t, vp]
+        L.e2ttt_join_bwd.restype = cp
         L.e2ttt_device_status.argtypes = [vp, vp, ctypes.POINTER(cp)]
         L.e2ttt_device_status.restype = cp
         L.e2ttt_selftest_wait_timeout.argtypes = [vp, ctypes.c_size_t, ctypes.c_longlong, vp]
@@ -395,6 +408,49 @@ def e2ttt_delta_step(p, q, k, v, eta, log_gamma, S, o, S_out, stream=None):
     st = (_lib or lib()).e2ttt_delta_step(ctypes.byref(p), *args, _stream_ptr(stream))
     if st != E2TTT_OK:
         raise E2TTTError(st, "e2ttt_delta_step")
+    return st
+
+
+def make_join_params(B, H, L, d, io_dtype=E2TTT_F32, gate=E2TTT_GATE_SILU, post_eps=1e-6, pre_eps=1e-6):
+    return e2ttt_join_params(B, H, L, d, io_dtype, gate, post_eps, pre_eps)
+
+
+def e2ttt_join_workspace_bytes(p: e2ttt_join_params) -> int:
+    n = ctypes.c_size_t()
+    st = (_lib or lib()).e2ttt_join_workspace_bytes(ctypes.byref(p), ctypes.byref(n))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_workspace_bytes")
+    return int(n.value)
+
+
+def e2ttt_join_fwd(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out, stream=None):
+    """int e2ttt_join_fwd(...) of include/e2ttt.h: norm after a block, gate, residual, norm before the next.  Raises on error."""
+    io = _io_torch_dtype(p)
+    so, sx, sw = (p.B, p.H, p.L, p.d), (p.B, p.L, p.H * p.d), (p.H * p.d,)
+    args = (_ptr(o, io, so, "o"), _ptr(a, io, sx, "a"), _ptr(x, io, sx, "x"), _ptr(w_post, _F32, sw, "w_post"),
+            _ptr(res_scale, _F32, sw, "res_scale"), _ptr(w_pre, _F32, sw, "w_pre"), _ptr(x_out, io, sx, "x_out"),
+            _ptr(n_out, io, sx, "n_out"))
+    _here(o, a, x, w_post, res_scale, w_pre, x_out, n_out)
+    st = (_lib or lib()).e2ttt_join_fwd(ctypes.byref(p), *args, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_fwd")
+    return st
+
+
+def e2ttt_join_bwd(p, o, a, x, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre, workspace,
+                   stream=None):
+    """int e2ttt_join_bwd(...) of include/e2ttt.h: its reverse pass.  Raises on error."""
+    io = _io_torch_dtype(p)
+    so, sx, sw = (p.B, p.H, p.L, p.d), (p.B, p.L, p.H * p.d), (p.H * p.d,)
+    args = (_ptr(o, io, so, "o"), _ptr(a, io, sx, "a"), _ptr(x, io, sx, "x"), _ptr(w_post, _F32, sw, "w_post"),
+            _ptr(res_scale, _F32, sw, "res_scale"), _ptr(w_pre, _F32, sw, "w_pre"), _ptr(d_x_out, io, sx, "d_x_out"),
+            _ptr(d_n, io, sx, "d_n"), _ptr(d_o, io, so, "d_o"), _ptr(d_a, io, sx, "d_a"), _ptr(d_x, io, sx, "d_x"),
+            _ptr(d_w_post, _F32, sw, "d_w_post"), _ptr(d_res_scale, _F32, sw, "d_res_scale"), _ptr(d_w_pre, _F32, sw, "d_w_pre"),
+            _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(o, a, x, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre, workspace)
+    st = (_lib or lib()).e2ttt_join_bwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_bwd")
     return st
 
 

@@ -1,0 +1,462 @@
+// Block join, forward and reverse pass.  Per token, o [B,H,L,d] by heads, everything else [B,L,H d]:
+//   y = o / rms(o per head) w_post,   z = gate(a) y,   x_out = x + res_scale z,   n = x_out / rms(x_out) w_pre.
+// Every tensor is read once and written once: HBM bounds both passes.  A CTA takes a token at a time, a thread V neighbouring values of
+// it (16 bytes where widths and addresses allow); a head's sum is a few shuffles where a head's pieces fill an aligned part of a
+// warp, else it goes through shared memory.  The loads of the next token are issued before the sums of this one.
+// Reverse pass, with r = gate(a) y0, y0 = o / rms(o):  d x = d x_out + (adjoint of the second norm),  d w_post = res_scale sum_tokens(dx r),
+// d res_scale = w_post sum_tokens(dx r): one column sum serves both, a second one is d w_pre.  A CTA keeps its tokens' column sums in
+// registers; the CTAs' sums are added by a second launch in a fixed order, so that results repeat bit for bit.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <initializer_list>
+
+#include "../../include/e2ttt.h"
+#include "api_checks.h"
+#include "join.h"
+
+namespace e2ttt {
+namespace {
+
+constexpr unsigned kAll = 0xffffffffu;
+
+__device__ __forceinline__ float ldf(float x) { return x; }
+__device__ __forceinline__ float ldf(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void stf(float& y, float x) { y = x; }
+__device__ __forceinline__ void stf(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
+
+template <typename IO, int V> struct alignas(sizeof(IO) * V) Piece {
+    IO x[V];
+};
+
+// gate and its derivative.  With bf16 I/O both are rounded to 2^-9 right after, the hardware's exponential and division (2^-21) serve.
+template <typename IO> __device__ __forceinline__ float gate_of(float a, int kind, float& deriv) {
+    if (kind == E2TTT_GATE_NONE) { deriv = 0.0f; return 1.0f; }
+    const float e = sizeof(IO) == 2 ? __expf(-a) : expf(-a);  // a -> -inf: e = inf, sig = 0
+    const float sig = sizeof(IO) == 2 ? __fdividef(1.0f, 1.0f + e) : 1.0f / (1.0f + e);
+    if (kind == E2TTT_GATE_SIGMOID) { deriv = sig * (1.0f - sig); return sig; }
+    deriv = sig * fmaf(a, 1.0f - sig, 1.0f);
+    return a * sig;
+}
+
+// Sums over a token's heads and over the token.  `cols` pieces of V values; a head has G of them.
+struct Sums {
+    float *part, *head, *row;  // shared memory: [cols], [H], [2][2][32]
+    int cols, G, H, T, flip;
+    bool lanes;                // a head is an aligned group of G lanes
+};
+
+// v[i]: sum over piece i of the thread -> sum over the piece's head
+template <int NC> __device__ __forceinline__ void head_sums(Sums& s, float (&v)[NC]) {
+    const int tid = threadIdx.x;
+    if (s.lanes) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            for (int x = 1; x < s.G; x <<= 1) v[i] += __shfl_xor_sync(kAll, v[i], x);
+        return;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        if (tid + i * s.T < s.cols) s.part[tid + i * s.T] = v[i];
+    __syncthreads();
+    for (int h = tid >> 5; h < s.H; h += s.T >> 5) {
+        float y = 0.0f;
+        for (int j = tid & 31; j < s.G; j += 32) y += s.part[h * s.G + j];
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) y += __shfl_xor_sync(kAll, y, x);
+        if ((tid & 31) == 0) s.head[h] = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+        if (tid + i * s.T < s.cols) v[i] = s.head[(tid + i * s.T) / s.G];
+}
+
+// sums of u and v over the CTA's threads, in a fixed order; two buffers in turn, so that one barrier is enough
+__device__ __forceinline__ void row_sums(Sums& s, float& u, float& v) {
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+        u += __shfl_xor_sync(kAll, u, x);
+        v += __shfl_xor_sync(kAll, v, x);
+    }
+    const int warps = s.T >> 5;
+    if (warps == 1) return;
+    float* b = s.row + s.flip * 64;
+    s.flip ^= 1;
+    if ((threadIdx.x & 31) == 0) { b[threadIdx.x >> 5] = u; b[32 + (threadIdx.x >> 5)] = v; }
+    __syncthreads();
+    u = v = 0.0f;
+    for (int i = 0; i < warps; ++i) { u += b[i]; v += b[32 + i]; }
+}
+
+__device__ __forceinline__ Sums make_sums(char* smem, int cols, int G, int H) {
+    Sums s;
+    s.row = reinterpret_cast<float*>(smem);
+    s.part = s.row + 128;
+    s.head = s.part + cols;
+    s.cols = cols; s.G = G; s.H = H; s.T = blockDim.x; s.flip = 0;
+    s.lanes = G <= 32 && (G & (G - 1)) == 0;
+    return s;
+}
+
+template <typename IO, int V, int NC>
+__global__ void __launch_bounds__(512) join_fwd_kernel(const JoinArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    using P = Piece<IO, V>;
+    const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
+    Sums sums = make_sums(smem, cols, a.d / V, a.H);
+    const int64_t tokens = (int64_t)a.B * a.L;
+    P po[NC], pa[NC], px[NC];
+    auto load = [&](int64_t tok) {
+        const int64_t b = tok / a.L, l = tok % a.L;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            const int h = c / sums.G, in = c - h * sums.G;
+            po[i] = reinterpret_cast<const P*>(a.o)[((b * a.H + h) * a.L + l) * sums.G + in];
+            px[i] = reinterpret_cast<const P*>(a.x)[tok * cols + c];
+            if (a.a) pa[i] = reinterpret_cast<const P*>(a.a)[tok * cols + c];
+        }
+    };
+    int64_t tok = blockIdx.x;
+    if (tok < tokens) load(tok);
+    for (; tok < tokens; tok += gridDim.x) {
+        float y[NC][V], hs[NC];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            hs[i] = 0.0f;
+            if (tid + i * T >= cols) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                y[i][j] = ldf(po[i].x[j]);
+                hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
+            }
+        }
+        head_sums<NC>(sums, hs);
+        float s2 = 0.0f, none = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            const float inv = rsqrtf(hs[i] / a.d + a.post_eps);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float dg, g = 1.0f;
+                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
+                y[i][j] = fmaf(a.res_scale[c * V + j] * g, y[i][j] * inv * a.w_post[c * V + j], ldf(px[i].x[j]));
+                s2 = fmaf(y[i][j], y[i][j], s2);
+            }
+        }
+        if (tok + gridDim.x < tokens) load(tok + gridDim.x);
+        if (a.w_pre) row_sums(sums, s2, none);
+        const float m = rsqrtf(s2 / D + a.pre_eps);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            P xo, nn;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                stf(xo.x[j], y[i][j]);
+                if (a.w_pre) stf(nn.x[j], y[i][j] * m * a.w_pre[c * V + j]);
+            }
+            reinterpret_cast<P*>(a.x_out)[tok * cols + c] = xo;
+            if (a.w_pre) reinterpret_cast<P*>(a.n_out)[tok * cols + c] = nn;
+        }
+    }
+}
+
+template <typename IO, int V, int NC>
+__global__ void __launch_bounds__(512) join_bwd_kernel(const JoinBwdArgs ba) {
+    extern __shared__ __align__(16) char smem[];
+    using P = Piece<IO, V>;
+    const JoinArgs& a = ba.f;
+    const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
+    Sums sums = make_sums(smem, cols, a.d / V, a.H);
+    const int64_t tokens = (int64_t)a.B * a.L;
+    P po[NC], pa[NC], px[NC], pd[NC], pn[NC];
+    auto at_o = [&](int64_t tok, int c) {
+        const int64_t b = tok / a.L, l = tok % a.L;
+        const int h = c / sums.G;
+        return ((b * a.H + h) * a.L + l) * sums.G + (c - h * sums.G);
+    };
+    auto load = [&](int64_t tok) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            po[i] = reinterpret_cast<const P*>(a.o)[at_o(tok, c)];
+            px[i] = reinterpret_cast<const P*>(a.x)[tok * cols + c];
+            pd[i] = reinterpret_cast<const P*>(ba.d_x_out)[tok * cols + c];
+            if (a.a) pa[i] = reinterpret_cast<const P*>(a.a)[tok * cols + c];
+            if (a.w_pre) pn[i] = reinterpret_cast<const P*>(ba.d_n)[tok * cols + c];
+        }
+    };
+    float R[NC][V], W[NC][V];  // column sums: dx gate y0, and dn x_out / rms
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) R[i][j] = W[i][j] = 0.0f;
+    for (int64_t tok = blockIdx.x; tok < tokens; tok += gridDim.x) {
+        load(tok);
+        float y[NC][V], xo[NC][V], hs[NC], inv[NC];
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            hs[i] = 0.0f;
+            if (tid + i * T >= cols) continue;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                y[i][j] = ldf(po[i].x[j]);
+                hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
+            }
+        }
+        head_sums<NC>(sums, hs);
+        float s2 = 0.0f, sd = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            inv[i] = rsqrtf(hs[i] / a.d + a.post_eps);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float dg, g = 1.0f;
+                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
+                y[i][j] *= inv[i];
+                xo[i][j] = fmaf(a.res_scale[c * V + j] * g, y[i][j] * a.w_post[c * V + j], ldf(px[i].x[j]));
+                s2 = fmaf(xo[i][j], xo[i][j], s2);
+                if (a.w_pre) sd = fmaf(ldf(pn[i].x[j]) * a.w_pre[c * V + j], xo[i][j], sd);
+            }
+        }
+        float m = 0.0f, mean = 0.0f;
+        if (a.w_pre) {
+            row_sums(sums, s2, sd);
+            m = rsqrtf(s2 / D + a.pre_eps);
+            mean = sd * m / D;
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            hs[i] = 0.0f;
+            if (c >= cols) continue;
+            P dx_p, da_p;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float dx = ldf(pd[i].x[j]);
+                if (a.w_pre) {
+                    const float dn = ldf(pn[i].x[j]), h = xo[i][j] * m;
+                    W[i][j] = fmaf(dn, h, W[i][j]);
+                    dx = fmaf(m, fmaf(-h, mean, dn * a.w_pre[c * V + j]), dx);
+                }
+                stf(dx_p.x[j], dx);
+                float dg = 0.0f, g = 1.0f;
+                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
+                const float cw = a.res_scale[c * V + j] * a.w_post[c * V + j];
+                R[i][j] = fmaf(dx * g, y[i][j], R[i][j]);
+                stf(da_p.x[j], dx * cw * y[i][j] * dg);
+                xo[i][j] = dx * cw * g;  // adjoint of y0
+                hs[i] = fmaf(xo[i][j], y[i][j], hs[i]);
+            }
+            reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
+            if (a.a) reinterpret_cast<P*>(ba.d_a)[tok * cols + c] = da_p;
+        }
+        head_sums<NC>(sums, hs);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int c = tid + i * T;
+            if (c >= cols) continue;
+            const float mh = hs[i] / a.d;
+            P do_p;
+#pragma unroll
+            for (int j = 0; j < V; ++j) stf(do_p.x[j], inv[i] * fmaf(-y[i][j], mh, xo[i][j]));
+            reinterpret_cast<P*>(ba.d_o)[at_o(tok, c)] = do_p;
+        }
+    }
+    float* part = ba.part + (size_t)blockIdx.x * 2 * D;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = tid + i * T;
+        if (c >= cols) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            part[c * V + j] = R[i][j];
+            if (a.w_pre) part[D + c * V + j] = W[i][j];
+        }
+    }
+}
+
+// column sums over the CTAs: 32 columns by 8 row groups a CTA
+__global__ void __launch_bounds__(256) join_sum_kernel(const JoinBwdArgs ba, const int rows) {
+    __shared__ float red[2][8][32];
+    const JoinArgs& a = ba.f;
+    const int D = a.H * a.d, lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float r = 0.0f, w = 0.0f;
+    if (c < D) {
+#pragma unroll 4
+        for (int i = group; i < rows; i += 8) {
+            r += ba.part[(size_t)i * 2 * D + c];
+            if (a.w_pre) w += ba.part[(size_t)i * 2 * D + D + c];
+        }
+    }
+    red[0][group][lane] = r;
+    red[1][group][lane] = w;
+    __syncthreads();
+    if (group != 0 || c >= D) return;
+    r = w = 0.0f;
+    for (int i = 0; i < 8; ++i) { r += red[0][i][lane]; w += red[1][i][lane]; }
+    ba.d_w_post[c] = r * a.res_scale[c];
+    ba.d_res_scale[c] = r * a.w_post[c];
+    if (a.w_pre) ba.d_w_pre[c] = w;
+}
+
+// values per piece: the widest that divides a head and that all addresses allow
+int piece_of(const JoinArgs& a, std::initializer_list<const void*> ptrs) {
+    const int size = a.f32 ? 4 : 2;
+    int v = 16 / size;
+    uintptr_t all = 0;
+    for (const void* p : ptrs) all |= reinterpret_cast<uintptr_t>(p);
+    while (v > 1 && (a.d % v || all % (size * v))) v >>= 1;
+    return v;
+}
+
+struct Shape {
+    int threads, smem;
+};
+Shape shape_of(const JoinArgs& a, int V, int NC) {
+    const int cols = a.H * a.d / V, t = (cols + NC - 1) / NC;
+    return {(t + 31) / 32 * 32, (128 + cols + a.H) * 4};
+}
+
+template <typename IO, int V, int NC> int launch_fwd(const JoinArgs& a, cudaStream_t st) {
+    const Shape s = shape_of(a, V, NC);
+    auto kernel = join_fwd_kernel<IO, V, NC>;
+    if (s.smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+        if (e != cudaSuccess) return (int)e;
+    }
+    const int64_t tokens = join_tokens(a), most = 148 * (2048 / s.threads > 32 ? 32 : 2048 / s.threads);
+    kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a);
+    return (int)cudaGetLastError();
+}
+template <typename IO, int V, int NC> int launch_bwd(const JoinBwdArgs& b, cudaStream_t st) {
+    const Shape s = shape_of(b.f, V, NC);
+    auto kernel = join_bwd_kernel<IO, V, NC>;
+    if (s.smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+        if (e != cudaSuccess) return (int)e;
+    }
+    const int grid = join_bwd_grid(join_tokens(b.f));
+    kernel<<<grid, s.threads, s.smem, st>>>(b);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return (int)e;
+    join_sum_kernel<<<(b.f.H * b.f.d + 31) / 32, 256, 0, st>>>(b, grid);
+    return (int)cudaGetLastError();
+}
+
+// 8 values a thread up to 4096 columns (512 threads), 16 above
+#define JOIN_DISPATCH(launch, IO, v, wide, args)                                                           \
+    switch (v) {                                                                                           \
+        case 8: if constexpr (sizeof(IO) == 2) return wide ? launch<IO, 8, 2>(args, st) : launch<IO, 8, 1>(args, st); else return -1; \
+        case 4: return wide ? launch<IO, 4, 4>(args, st) : launch<IO, 4, 2>(args, st);                     \
+        case 2: return wide ? launch<IO, 2, 8>(args, st) : launch<IO, 2, 4>(args, st);                     \
+        default: return wide ? launch<IO, 1, 16>(args, st) : launch<IO, 1, 8>(args, st);                   \
+    }
+
+}  // namespace
+
+int join_fwd_launch(const JoinArgs& a, void* stream) {
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int v = piece_of(a, {a.o, a.a, a.x, a.x_out, a.n_out});
+    const bool wide = a.H * a.d > 4096;
+    if (a.f32) { JOIN_DISPATCH(launch_fwd, float, v, wide, a) }
+    JOIN_DISPATCH(launch_fwd, __nv_bfloat16, v, wide, a)
+}
+
+int join_bwd_launch(const JoinBwdArgs& b, void* stream) {
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int v = piece_of(b.f, {b.f.o, b.f.a, b.f.x, b.d_x_out, b.d_n, b.d_o, b.d_a, b.d_x});
+    const bool wide = b.f.H * b.f.d > 4096;
+    if (b.f.f32) { JOIN_DISPATCH(launch_bwd, float, v, wide, b) }
+    JOIN_DISPATCH(launch_bwd, __nv_bfloat16, v, wide, b)
+}
+
+}  // namespace e2ttt
+
+using namespace e2ttt;
+
+namespace {
+
+int check(const e2ttt_join_params* p) {
+    if (!p) return E2TTT_ERR_NULL;
+    if (p->io_dtype != E2TTT_F32 && p->io_dtype != E2TTT_BF16) return E2TTT_ERR_DTYPE;
+    if (p->B <= 0 || p->H <= 0 || p->L <= 0 || p->d <= 0) return E2TTT_ERR_SHAPE;
+    if ((int64_t)p->H * p->d > kJoinMaxWidth || (int64_t)p->B * p->L > (int64_t)1 << 40) return E2TTT_ERR_SHAPE;
+    if (p->gate != E2TTT_GATE_NONE && p->gate != E2TTT_GATE_SIGMOID && p->gate != E2TTT_GATE_SILU) return E2TTT_ERR_SHAPE;
+    if (!(p->post_eps >= 0.0f) || !(p->pre_eps >= 0.0f)) return E2TTT_ERR_SHAPE;
+    return E2TTT_OK;
+}
+
+bool io_aligned(const e2ttt_join_params* p, std::initializer_list<const void*> ptrs) {
+    for (const void* x : ptrs)
+        if (!aligned(x, p->io_dtype == E2TTT_F32 ? 4 : 2)) return false;
+    return true;
+}
+bool f32_aligned(std::initializer_list<const void*> ptrs) {
+    for (const void* x : ptrs)
+        if (!aligned(x, 4)) return false;
+    return true;
+}
+
+JoinArgs args_of(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
+                 const float* w_pre, void* x_out, void* n_out) {
+    return {p->B, p->H, p->L, p->d, p->io_dtype == E2TTT_F32, p->gate, p->post_eps, p->pre_eps, o, a, x, w_post, res_scale, w_pre, x_out, n_out};
+}
+
+size_t bytes_of(const e2ttt_join_params* p) {
+    return kStatusBytes + (size_t)join_bwd_grid((int64_t)p->B * p->L) * 2 * p->H * p->d * 4;
+}
+
+}  // namespace
+
+extern "C" {
+
+int e2ttt_join_workspace_bytes(const e2ttt_join_params* p, size_t* bytes) {
+    if (!bytes) return E2TTT_ERR_NULL;
+    const int rc = check(p);
+    if (rc) return rc;
+    *bytes = bytes_of(p);
+    return E2TTT_OK;
+}
+
+int e2ttt_join_fwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
+                   const float* w_pre, void* x_out, void* n_out, void* stream) {
+    int rc = check(p);
+    if (rc) return rc;
+    if (!o || !x || !w_post || !res_scale || !x_out || !a != (p->gate == E2TTT_GATE_NONE) || !w_pre != !n_out) return E2TTT_ERR_NULL;
+    if (!io_aligned(p, {o, a, x, x_out, n_out}) || !f32_aligned({w_post, res_scale, w_pre})) return E2TTT_ERR_ALIGN;
+    rc = check_device();
+    if (rc) return rc;
+    return join_fwd_launch(args_of(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out), stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+}
+
+int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
+                   const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a, void* d_x, float* d_w_post,
+                   float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check(p);
+    if (rc) return rc;
+    if (!o || !x || !w_post || !res_scale || !d_x_out || !d_o || !d_x || !d_w_post || !d_res_scale) return E2TTT_ERR_NULL;
+    const bool gated = p->gate != E2TTT_GATE_NONE;
+    if (!a == gated || !d_a == gated || !w_pre != !d_n || !w_pre != !d_w_pre) return E2TTT_ERR_NULL;
+    if (!io_aligned(p, {o, a, x, d_x_out, d_n, d_o, d_a, d_x}) || !f32_aligned({w_post, res_scale, w_pre, d_w_post, d_res_scale, d_w_pre}))
+        return E2TTT_ERR_ALIGN;
+    if (!workspace || workspace_bytes < bytes_of(p)) return E2TTT_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return E2TTT_ERR_ALIGN;
+    rc = check_device();
+    if (rc) return rc;
+    JoinBwdArgs b{args_of(p, o, a, x, w_post, res_scale, w_pre, nullptr, nullptr), d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre,
+                  reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes)};
+    return join_bwd_launch(b, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+}
+
+}  // extern "C"
