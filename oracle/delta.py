@@ -4,6 +4,24 @@ from __future__ import annotations
 import numpy as np
 
 
+def magnitudes(q, k, v, eta, log_gamma, S, scale):
+    """Sums of the magnitudes of an output's terms: what the start state, and every token's update, put into it."""
+    q, k, v, eta, log_gamma = (np.asarray(x, np.float64) for x in (q, k, v, eta, log_gamma))
+    B, H, L, dv = v.shape
+    r = H // q.shape[1]
+    q, k = np.repeat(q, r, 1), np.repeat(k, r, 1)
+    S = np.zeros((B, H, dv, q.shape[-1])) if S is None else np.array(S, np.float64)
+    A, o = np.abs(S), np.zeros_like(v)
+    for t in range(L):
+        g = np.exp(log_gamma[:, :, t])[..., None, None]
+        S, A = g * S, g * A
+        e = v[:, :, t] - np.einsum("bhij,bhj->bhi", S, k[:, :, t])
+        step = (eta[:, :, t, None] * e)[..., :, None] * k[:, :, t, None, :]
+        S, A = S + step, A + np.abs(step)
+        o[:, :, t] = abs(scale) * np.einsum("bhij,bhj->bhi", A, np.abs(q[:, :, t]))
+    return o
+
+
 def forward(q, k, v, eta, log_gamma, S, scale):
     """q, k [B,Hk,L,dk], v [B,H,L,dv], eta, log_gamma [B,H,L], S [B,H,dv,dk] or None -> o, S_final (all fp64)."""
     q, k, v, eta, log_gamma = (np.asarray(x, np.float64) for x in (q, k, v, eta, log_gamma))

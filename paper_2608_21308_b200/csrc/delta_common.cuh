@@ -34,6 +34,23 @@ __device__ __forceinline__ void pow2_scale(float m, float& s, float& inv) {
     s = __uint_as_float((uint32_t)(127 + e) << 23);
     inv = __uint_as_float((uint32_t)(127 - e) << 23);
 }
+// the same from a bound on the magnitudes: [2^13, 2^14), a factor of four below fp16's largest value.  A bound may be 2^10 above what it bounds:
+// the second term's smallest step, 2^-24, is then still 2^-27 of the largest value.
+__device__ __forceinline__ void pow2_bound(float m, float& s, float& inv) {
+    int e = 140 - (int)(__float_as_uint(m) >> 23);
+    e = max(-100, min(100, e));
+    s = __uint_as_float((uint32_t)(127 + e) << 23);
+    inv = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+__device__ __forceinline__ float quad_sum(float m) {
+    m += __shfl_xor_sync(kAll, m, 1);
+    return m + __shfl_xor_sync(kAll, m, 2);
+}
+__device__ __forceinline__ float warp_sum(float m) {
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) m += __shfl_xor_sync(kAll, m, i);
+    return m;
+}
 __device__ __forceinline__ float quad_max(float m) {  // over the four lanes that share a fragment row
     m = fmaxf(m, __shfl_xor_sync(kAll, m, 1));
     return fmaxf(m, __shfl_xor_sync(kAll, m, 2));
@@ -56,7 +73,7 @@ __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& 
 }
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }

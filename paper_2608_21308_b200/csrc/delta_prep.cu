@@ -10,7 +10,7 @@ using namespace delta;
 
 constexpr int kWarps = 4;
 
-template <int DK, int KT> constexpr int prep_warp_bytes() { return 2 * KT * 64 * DK + 4608 + 256 + 128; }
+template <int DK, int KT> constexpr int prep_warp_bytes() { return 2 * KT * 64 * DK + 4608 + 256 + 256; }
 
 // largest magnitude of a row tile, then its scaled terms to shared memory and to the workspace
 template <typename IO, int DK, int KT>
@@ -42,20 +42,7 @@ __device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool
                 if (c + j < d) x[j] = to_f32(p[j]);
         }
     };
-#pragma unroll 4
-    for (int i = lane; i < 32 * P; i += 32) {
-        float x[8];
-        load(i, x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[j]));
-    }
-    m = warp_max(m);
-    float s, inv;
-    pow2_scale(m, s, inv);
-#pragma unroll 4
-    for (int i = lane; i < 32 * P; i += 32) {
-        float x[8];
-        load(i, x);  // from L1
+    auto put = [&](int i, const float (&x)[8], float s) {
         uint4 hi, lo;
         split(x[0] * s, x[1] * s, hi.x, lo.x);
         split(x[2] * s, x[3] * s, hi.y, lo.y);
@@ -68,6 +55,50 @@ __device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool
             *reinterpret_cast<uint4*>(sm + 64 * DK + at) = lo;
             *reinterpret_cast<uint4*>(out + 64 * DK + at) = lo;
         }
+    };
+    float s, inv;
+    if (sizeof(IO) == 2 && vec) {  // the whole tile in flight: 16 bytes a lane and load, one round trip
+        uint4 raw[P];
+        const bool full = rows == kDeltaChunk && d == DK;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int r = (i * 32 + lane) / P, c = (i * 32 + lane) % P * 8;
+            raw[i] = full || (r < rows && c < d) ? *reinterpret_cast<const uint4*>(src + (size_t)r * d + c) : make_uint4(0, 0, 0, 0);
+        }
+        uint32_t top = 0;  // largest magnitude on the bits: both halves of a word at a time
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            top = __vmaxu2(top, raw[i].x & 0x7fff7fffu);
+            top = __vmaxu2(top, raw[i].y & 0x7fff7fffu);
+            top = __vmaxu2(top, raw[i].z & 0x7fff7fffu);
+            top = __vmaxu2(top, raw[i].w & 0x7fff7fffu);
+        }
+        m = __uint_as_float(max(top << 16, top & 0xffff0000u));
+        if (!(m <= 3.4e38f)) m = __uint_as_float(0x7f000000u);  // infinities and NaNs: any scale
+        pow2_scale(warp_max(m), s, inv);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+            put(i * 32 + lane, x, s);
+        }
+        return inv;
+    }
+#pragma unroll 4
+    for (int i = lane; i < 32 * P; i += 32) {
+        float x[8];
+        load(i, x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(x[j]));
+    }
+    pow2_scale(warp_max(m), s, inv);
+#pragma unroll 4
+    for (int i = lane; i < 32 * P; i += 32) {
+        float x[8];
+        load(i, x);  // from L1
+        put(i, x, s);
     }
     return inv;
 }
@@ -103,7 +134,7 @@ template <int DK, int KT> __device__ __forceinline__ void gram(uint32_t rows, ui
 }
 
 // (I + N)^-1 of a strictly lower N column by column, lane = column: x_t = [t == lane] - sum_{i < t} N_ti x_i; two terms to `out`
-__device__ __forceinline__ float invert(const float* Nm, char* out, int lane) {
+__device__ __forceinline__ float invert(const float* Nm, char* out, int lane, float& rows) {
     float x[32], most = 0.0f;
 #pragma unroll
     for (int t = 0; t < 32; ++t) {
@@ -120,6 +151,7 @@ __device__ __forceinline__ float invert(const float* Nm, char* out, int lane) {
         most = fmaxf(most, fabsf(x[t]));
     }
     float s, inv;
+    rows = warp_sum(most);  // no row's sum of magnitudes is larger
     pow2_scale(warp_max(most), s, inv);
 #pragma unroll
     for (int t = 0; t < 32; ++t) {
@@ -147,6 +179,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     float* Nm = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK);  // 32 x 32, rows of 36
     double* run = reinterpret_cast<double*>(sm + 2 * KT * 64 * DK + 4608);
     float* eta_s = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK + 4608 + 256);
+    float* norm_s = eta_s + 32;  // |k|^2
     char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
     const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
     const float ik = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(a.k) + row0, rows, s.dk, vec, sm, out, lane);
@@ -193,6 +226,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             for (int x = 0; x < 4; ++x) {
                 const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
                 const float D = u <= t ? expf((float)(run[t] - run[u])) : 0.0f;
+                if (u == t) norm_s[t] = kk[i][x] * (ik * ik);
                 Nm[t * 36 + u] = u < t ? D * kk[i][x] * (ik * ik) * eta_s[u] : 0.0f;
                 av[i][x] = u <= t ? D * qk[i][x] * (iq * ik * s.scale) : 0.0f;
                 amax = fmaxf(amax, fabsf(av[i][x]));
@@ -213,7 +247,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             }
         }
         __syncwarp();
-        const float ti = invert(Nm, rec, lane);
+        float tsum, rsum;
+        const float ti = invert(Nm, rec, lane, tsum);
         float ri = 0.0f;
         if (a.save) {  // the same with eta on the rows: what the reverse pass multiplies with
             __syncwarp();
@@ -227,15 +262,23 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
                 }
             }
             __syncwarp();
-            ri = invert(Nm, rec + kDeltaRecBytes, lane);
+            ri = invert(Nm, rec + kDeltaRecBytes, lane, rsum);
         }
+        const float kn = sqrtf(norm_s[lane]);
+        const float b_kn = warp_max(bt * kn), umax = warp_max(fabsf(eta)), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
         if (lane == 0) {
-            sc[kRecHead * 32 + 0] = expf((float)end);
-            sc[kRecHead * 32 + 1] = ti;
-            sc[kRecHead * 32 + 2] = ai;
-            sc[kRecHead * 32 + 3] = ik;
-            sc[kRecHead * 32 + 4] = iq;
-            sc[kRecHead * 32 + 5] = ri;
+            float* head = sc + kRecHead * 32;
+            head[kHeadEnd] = expf((float)end);
+            head[kHeadT] = ti;
+            head[kHeadA] = ai;
+            head[kHeadK] = ik;
+            head[kHeadQ] = iq;
+            head[kHeadR] = ri;
+            head[kHeadKn] = b_kn;
+            head[kHeadTsum] = tsum;
+            head[kHeadUmax] = umax;
+            head[kHeadWmax] = wmax;
+            head[kHeadWsum] = wsum;
         }
         __syncwarp();
     }

@@ -5,6 +5,8 @@ magnitude.  TOL: an operand of 32 bits is two fp16 terms (2^-22), a product of t
 3 x 8 + 3 x 2 partial results that are truncated (2^-23 each, partial sums at most about the sum of the magnitudes); four dependent products
 per chunk: 4 (2 x 2^-22 + 30 x 2^-23) = 1.6e-5 of the sum of the magnitudes if all errors had one sign.  They do not, and no sum here exceeds its
 largest magnitude's row by more than sqrt(128): 2e-5 of the largest magnitude holds for the worst value.
+bf16 outputs of a forward without saved states come from products with one fp16 term (half a step: 2^-11) of the start state, of u and of A: an output
+is off by at most 2^-11 of the magnitudes of what the state puts into it and 2 x 2^-11 of what the chunk's tokens do: 2^-10 of the sum of magnitudes.
 """
 import numpy as np
 import pytest
@@ -78,12 +80,14 @@ class Run:
         return {"o": self.o, "S": self.S_out}
 
 
-def check(got, ref):
+def check(got, ref, single=None):
+    """single: the inputs, where the outputs are of products with one term."""
+    terms = None if single is None or got["o"].dtype != torch.bfloat16 else O.magnitudes(**single)
     for n, t in got.items():
         y, r = t.double().cpu().numpy(), ref[n]
         half = torch.finfo(t.dtype).eps / 2
         assert np.isfinite(y).all(), n
-        over = np.abs(y - r) - half * np.abs(r) - TOL * np.abs(r).max()
+        over = np.abs(y - r) - half * np.abs(r) - TOL * np.abs(r).max() - (2.0 ** -10 * terms if terms is not None and n == "o" else 0.0)
         assert over.max() <= 0, (n, over.max(), np.abs(r).max(), np.linalg.norm(y - r) / np.linalg.norm(r))
 
 
@@ -99,7 +103,7 @@ SHAPES = [  # B, H, Hk, L, dk, dv
 def test_forward(io, shape):
     x, _ = _make(*shape, io)
     o, S = O.forward(**x, scale=0.25)
-    check(Run(x, io, 0.25).fwd(), {"o": o, "S": S})
+    check(Run(x, io, 0.25).fwd(), {"o": o, "S": S}, dict(x, scale=0.25))
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -185,8 +189,8 @@ def test_states_chain_and_may_be_updated_in_place(io):
         r.S = r.S_out = S
         parts.append((r.fwd() if hi < 96 else r.step())["o"])
     o, Sf = O.forward(**x, scale=1.0)
-    check({"o": torch.cat(parts, 2), "S": S}, {"o": o, "S": Sf})
-    check(whole, {"o": o, "S": Sf})
+    check({"o": torch.cat(parts, 2), "S": S}, {"o": o, "S": Sf}, dict(x, scale=1.0))
+    check(whole, {"o": o, "S": Sf}, dict(x, scale=1.0))
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -258,7 +262,7 @@ def test_two_streams_with_workspaces_of_their_own():
     torch.cuda.synchronize()
     for x, r, _ in runs:
         o, S = O.forward(**x, scale=1.0)
-        check({"o": r.o, "S": r.S_out}, {"o": o, "S": S})
+        check({"o": r.o, "S": r.S_out}, {"o": o, "S": S}, dict(x, scale=1.0))
 
 
 def test_prepared_tokens_run_through_the_rule_and_back():
@@ -276,4 +280,4 @@ def test_prepared_tokens_run_through_the_rule_and_back():
     x = {"q": q.float().cpu().numpy(), "k": k.float().cpu().numpy(), "v": rnd(B, H, L, d).bfloat16().float().cpu().numpy(),
          "eta": eta.cpu().numpy(), "log_gamma": gamma.log().cpu().numpy(), "S": None}
     o, S = O.forward(**x, scale=1.0)
-    check(Run(x, "bf16", 1.0).fwd(), {"o": o, "S": S})
+    check(Run(x, "bf16", 1.0).fwd(), {"o": o, "S": S}, dict(x, scale=1.0))
