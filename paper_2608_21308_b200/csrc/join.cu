@@ -2,7 +2,7 @@
 //   y = o / rms(o per head) w_post,   z = gate(a) y,   x_out = x + res_scale z,   n = x_out / rms(x_out) w_pre.
 // Every tensor is read once and written once: HBM bounds both passes.  A CTA takes a token at a time, a thread V neighbouring values of
 // it (16 bytes where widths and addresses allow); a head's sum is a few shuffles where a head's pieces fill an aligned part of a
-// warp, else it goes through shared memory.  The loads of the next token are issued before the sums of this one.
+// warp, else it goes through shared memory.
 // Reverse pass, with r = gate(a) y0, y0 = o / rms(o):  d x = d x_out + (adjoint of the second norm),  d w_post = res_scale sum_tokens(dx r),
 // d res_scale = w_post sum_tokens(dx r): one column sum serves both, a second one is d w_pre.  A CTA keeps its tokens' column sums in
 // registers; the CTAs' sums are added by a second launch in a fixed order, so that results repeat bit for bit.
@@ -100,37 +100,75 @@ __device__ __forceinline__ Sums make_sums(char* smem, int cols, int G, int H) {
     return s;
 }
 
-template <typename IO, int V, int NC>
-__global__ void __launch_bounds__(512) join_fwd_kernel(const JoinArgs a) {
+// A thread's pieces of the tokens to come wait in shared memory, `depth` tokens deep: cp.async needs no registers for what is in flight, and as
+// every thread reads back only what it copied itself, no barrier either.
+template <int BYTES> __device__ __forceinline__ void copy_piece(void* dst, const void* src) {
+    if constexpr (BYTES >= 4) {
+        const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+        if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+    } else {
+        *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(src);
+    }
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait(int pending) {  // until at most that many groups are under way
+    switch (pending) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    }
+}
+template <int V> struct alignas(V >= 4 ? 16 : 4 * V) Weights {
+    float x[V];
+};
+template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, int c) { return reinterpret_cast<const Weights<V>*>(w)[c]; }
+
+template <typename IO, int V, int NC, int TMAX>
+__global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinArgs a, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
-    Sums sums = make_sums(smem, cols, a.d / V, a.H);
+    P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][3][NC][T]
+    Sums sums = make_sums(smem + (size_t)depth * 3 * NC * T * sizeof(P), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
-    P po[NC], pa[NC], px[NC];
-    auto load = [&](int64_t tok) {
+    auto at_o = [&](int64_t tok, int c) {
         const int64_t b = tok / a.L, l = tok % a.L;
+        const int h = c / sums.G;
+        return ((b * a.H + h) * a.L + l) * sums.G + (c - h * sums.G);
+    };
+    auto load = [&](int64_t tok, int slot) {
+        if (tok < tokens) {
+            P* r = ring + slot * 3 * NC * T;
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = tid + i * T;
-            if (c >= cols) continue;
-            const int h = c / sums.G, in = c - h * sums.G;
-            po[i] = reinterpret_cast<const P*>(a.o)[((b * a.H + h) * a.L + l) * sums.G + in];
-            px[i] = reinterpret_cast<const P*>(a.x)[tok * cols + c];
-            if (a.a) pa[i] = reinterpret_cast<const P*>(a.a)[tok * cols + c];
+            for (int i = 0; i < NC; ++i) {
+                const int c = tid + i * T;
+                if (c >= cols) continue;
+                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + at_o(tok, c));
+                copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
+                if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
+            }
         }
+        copy_commit();
     };
     int64_t tok = blockIdx.x;
-    if (tok < tokens) load(tok);
+    for (int i = 0; i + 1 < depth; ++i) load(tok + i * (int64_t)gridDim.x, i);
+    int slot = 0;
     for (; tok < tokens; tok += gridDim.x) {
+        load(tok + (depth - 1) * (int64_t)gridDim.x, slot == 0 ? depth - 1 : slot - 1);
+        copy_wait(depth - 1);
+        const P* r = ring + slot * 3 * NC * T;
+        slot = slot + 1 == depth ? 0 : slot + 1;
         float y[NC][V], hs[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             hs[i] = 0.0f;
             if (tid + i * T >= cols) continue;
+            const P po = r[i * T];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                y[i][j] = ldf(po[i].x[j]);
+                y[i][j] = ldf(po.x[j]);
                 hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
             }
         }
@@ -141,15 +179,16 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(const JoinArgs a) {
             const int c = tid + i * T;
             if (c >= cols) continue;
             const float inv = rsqrtf(hs[i] / a.d + a.post_eps);
+            const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T];
+            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float dg, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
-                y[i][j] = fmaf(a.res_scale[c * V + j] * g, y[i][j] * inv * a.w_post[c * V + j], ldf(px[i].x[j]));
+                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
+                y[i][j] = fmaf(wr.x[j] * g, y[i][j] * inv * wp.x[j], ldf(px.x[j]));
                 s2 = fmaf(y[i][j], y[i][j], s2);
             }
         }
-        if (tok + gridDim.x < tokens) load(tok + gridDim.x);
         if (a.w_pre) row_sums(sums, s2, none);
         const float m = rsqrtf(s2 / D + a.pre_eps);
 #pragma unroll
@@ -158,57 +197,70 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(const JoinArgs a) {
             if (c >= cols) continue;
             P xo, nn;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                stf(xo.x[j], y[i][j]);
-                if (a.w_pre) stf(nn.x[j], y[i][j] * m * a.w_pre[c * V + j]);
-            }
+            for (int j = 0; j < V; ++j) stf(xo.x[j], y[i][j]);
             reinterpret_cast<P*>(a.x_out)[tok * cols + c] = xo;
-            if (a.w_pre) reinterpret_cast<P*>(a.n_out)[tok * cols + c] = nn;
+            if (a.w_pre) {
+                const Weights<V> w = weights<V>(a.w_pre, c);
+#pragma unroll
+                for (int j = 0; j < V; ++j) stf(nn.x[j], y[i][j] * m * w.x[j]);
+                reinterpret_cast<P*>(a.n_out)[tok * cols + c] = nn;
+            }
         }
     }
 }
 
-template <typename IO, int V, int NC>
-__global__ void __launch_bounds__(512) join_bwd_kernel(const JoinBwdArgs ba) {
+template <typename IO, int V, int NC, int TMAX>
+__global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(const JoinBwdArgs ba, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
     const JoinArgs& a = ba.f;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
-    Sums sums = make_sums(smem, cols, a.d / V, a.H);
+    P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][5][NC][T]
+    Sums sums = make_sums(smem + (size_t)depth * 5 * NC * T * sizeof(P), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
-    P po[NC], pa[NC], px[NC], pd[NC], pn[NC];
     auto at_o = [&](int64_t tok, int c) {
         const int64_t b = tok / a.L, l = tok % a.L;
         const int h = c / sums.G;
         return ((b * a.H + h) * a.L + l) * sums.G + (c - h * sums.G);
     };
-    auto load = [&](int64_t tok) {
+    auto load = [&](int64_t tok, int slot) {
+        if (tok < tokens) {
+            P* r = ring + slot * 5 * NC * T;
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int c = tid + i * T;
-            if (c >= cols) continue;
-            po[i] = reinterpret_cast<const P*>(a.o)[at_o(tok, c)];
-            px[i] = reinterpret_cast<const P*>(a.x)[tok * cols + c];
-            pd[i] = reinterpret_cast<const P*>(ba.d_x_out)[tok * cols + c];
-            if (a.a) pa[i] = reinterpret_cast<const P*>(a.a)[tok * cols + c];
-            if (a.w_pre) pn[i] = reinterpret_cast<const P*>(ba.d_n)[tok * cols + c];
+            for (int i = 0; i < NC; ++i) {
+                const int c = tid + i * T;
+                if (c >= cols) continue;
+                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + at_o(tok, c));
+                copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
+                if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
+                copy_piece<sizeof(P)>(r + (3 * NC + i) * T, reinterpret_cast<const P*>(ba.d_x_out) + tok * cols + c);
+                if (a.w_pre) copy_piece<sizeof(P)>(r + (4 * NC + i) * T, reinterpret_cast<const P*>(ba.d_n) + tok * cols + c);
+            }
         }
+        copy_commit();
     };
     float R[NC][V], W[NC][V];  // column sums: dx gate y0, and dn x_out / rms
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) R[i][j] = W[i][j] = 0.0f;
-    for (int64_t tok = blockIdx.x; tok < tokens; tok += gridDim.x) {
-        load(tok);
+    int64_t tok = blockIdx.x;
+    for (int i = 0; i + 1 < depth; ++i) load(tok + i * (int64_t)gridDim.x, i);
+    int slot = 0;
+    for (; tok < tokens; tok += gridDim.x) {
+        load(tok + (depth - 1) * (int64_t)gridDim.x, slot == 0 ? depth - 1 : slot - 1);
+        copy_wait(depth - 1);
+        const P* r = ring + slot * 5 * NC * T;
+        slot = slot + 1 == depth ? 0 : slot + 1;
         float y[NC][V], xo[NC][V], hs[NC], inv[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             hs[i] = 0.0f;
             if (tid + i * T >= cols) continue;
+            const P po = r[i * T];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                y[i][j] = ldf(po[i].x[j]);
+                y[i][j] = ldf(po.x[j]);
                 hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
             }
         }
@@ -219,14 +271,20 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(const JoinBwdArgs ba) {
             const int c = tid + i * T;
             if (c >= cols) continue;
             inv[i] = rsqrtf(hs[i] / a.d + a.post_eps);
+            const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T], pn = r[(4 * NC + i) * T];
+            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 float dg, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
+                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
                 y[i][j] *= inv[i];
-                xo[i][j] = fmaf(a.res_scale[c * V + j] * g, y[i][j] * a.w_post[c * V + j], ldf(px[i].x[j]));
+                xo[i][j] = fmaf(wr.x[j] * g, y[i][j] * wp.x[j], ldf(px.x[j]));
                 s2 = fmaf(xo[i][j], xo[i][j], s2);
-                if (a.w_pre) sd = fmaf(ldf(pn[i].x[j]) * a.w_pre[c * V + j], xo[i][j], sd);
+            }
+            if (a.w_pre) {
+                const Weights<V> w = weights<V>(a.w_pre, c);
+#pragma unroll
+                for (int j = 0; j < V; ++j) sd = fmaf(ldf(pn.x[j]) * w.x[j], xo[i][j], sd);
             }
         }
         float m = 0.0f, mean = 0.0f;
@@ -240,22 +298,30 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(const JoinBwdArgs ba) {
             const int c = tid + i * T;
             hs[i] = 0.0f;
             if (c >= cols) continue;
+            const P pa = r[(2 * NC + i) * T], pd = r[(3 * NC + i) * T], pn = r[(4 * NC + i) * T];
+            float dx[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) dx[j] = ldf(pd.x[j]);
+            if (a.w_pre) {
+                const Weights<V> w = weights<V>(a.w_pre, c);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float dn = ldf(pn.x[j]), h = xo[i][j] * m;
+                    W[i][j] = fmaf(dn, h, W[i][j]);
+                    dx[j] = fmaf(m, fmaf(-h, mean, dn * w.x[j]), dx[j]);
+                }
+            }
             P dx_p, da_p;
+            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                float dx = ldf(pd[i].x[j]);
-                if (a.w_pre) {
-                    const float dn = ldf(pn[i].x[j]), h = xo[i][j] * m;
-                    W[i][j] = fmaf(dn, h, W[i][j]);
-                    dx = fmaf(m, fmaf(-h, mean, dn * a.w_pre[c * V + j]), dx);
-                }
-                stf(dx_p.x[j], dx);
+                stf(dx_p.x[j], dx[j]);
                 float dg = 0.0f, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa[i].x[j]), a.gate, dg);
-                const float cw = a.res_scale[c * V + j] * a.w_post[c * V + j];
-                R[i][j] = fmaf(dx * g, y[i][j], R[i][j]);
-                stf(da_p.x[j], dx * cw * y[i][j] * dg);
-                xo[i][j] = dx * cw * g;  // adjoint of y0
+                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
+                const float cw = wr.x[j] * wp.x[j];
+                R[i][j] = fmaf(dx[j] * g, y[i][j], R[i][j]);
+                stf(da_p.x[j], dx[j] * cw * y[i][j] * dg);
+                xo[i][j] = dx[j] * cw * g;  // adjoint of y0
                 hs[i] = fmaf(xo[i][j], y[i][j], hs[i]);
             }
             reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
@@ -314,54 +380,66 @@ __global__ void __launch_bounds__(256) join_sum_kernel(const JoinBwdArgs ba, con
 int piece_of(const JoinArgs& a, std::initializer_list<const void*> ptrs) {
     const int size = a.f32 ? 4 : 2;
     int v = 16 / size;
-    uintptr_t all = 0;
+    uintptr_t all = 0, w = 0;
     for (const void* p : ptrs) all |= reinterpret_cast<uintptr_t>(p);
-    while (v > 1 && (a.d % v || all % (size * v))) v >>= 1;
+    for (const void* p : {a.w_post, a.res_scale, a.w_pre}) w |= reinterpret_cast<uintptr_t>(p);
+    while (v > 1 && (a.d % v || all % (size * v) || w % (v >= 4 ? 16 : 4 * v))) v >>= 1;
     return v;
 }
 
 struct Shape {
-    int threads, smem;
+    int threads, depth, smem;
 };
-Shape shape_of(const JoinArgs& a, int V, int NC) {
-    const int cols = a.H * a.d / V, t = (cols + NC - 1) / NC;
-    return {(t + 31) / 32 * 32, (128 + cols + a.H) * 4};
+// tensors: how many are read per token; room: shared memory that a CTA may take for its ring where more than one token is to be under way
+Shape shape_of(const JoinArgs& a, int V, int NC, int tensors, int room) {
+    const int cols = a.H * a.d / V, t = ((cols + NC - 1) / NC + 31) / 32 * 32;
+    const int stage = tensors * NC * t * V * (a.f32 ? 4 : 2), G = a.d / V;
+    const bool lanes = G <= 32 && (G & (G - 1)) == 0;
+    int depth = room / stage;
+    depth = depth > 4 ? 4 : (depth < 1 ? 1 : depth);
+    return {t, depth, depth * stage + (128 + (lanes ? 0 : cols + a.H)) * 4};
 }
 
-template <typename IO, int V, int NC> int launch_fwd(const JoinArgs& a, cudaStream_t st) {
-    const Shape s = shape_of(a, V, NC);
-    auto kernel = join_fwd_kernel<IO, V, NC>;
-    if (s.smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
-        if (e != cudaSuccess) return (int)e;
-    }
-    const int64_t tokens = join_tokens(a), most = 148 * (2048 / s.threads > 32 ? 32 : 2048 / s.threads);
-    kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a);
+template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a, const Shape& s, cudaStream_t st) {
+    auto kernel = join_fwd_kernel<IO, V, NC, TMAX>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+    if (e != cudaSuccess) return (int)e;
+    const int64_t tokens = (int64_t)a.B * a.L, most = 148 * (1024 / s.threads > 16 ? 16 : 1024 / s.threads);
+    kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a, s.depth);
     return (int)cudaGetLastError();
 }
-template <typename IO, int V, int NC> int launch_bwd(const JoinBwdArgs& b, cudaStream_t st) {
-    const Shape s = shape_of(b.f, V, NC);
-    auto kernel = join_bwd_kernel<IO, V, NC>;
-    if (s.smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
-        if (e != cudaSuccess) return (int)e;
-    }
-    const int grid = join_bwd_grid(join_tokens(b.f));
-    kernel<<<grid, s.threads, s.smem, st>>>(b);
-    cudaError_t e = cudaGetLastError();
+template <typename IO, int V, int NC, int TMAX> int launch_bwd(const JoinBwdArgs& b, const Shape& s, cudaStream_t st) {
+    auto kernel = join_bwd_kernel<IO, V, NC, TMAX>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+    if (e != cudaSuccess) return (int)e;
+    const int grid = join_bwd_grid((int64_t)b.f.B * b.f.L, b.f.H * b.f.d);
+    kernel<<<grid, s.threads, s.smem, st>>>(b, s.depth);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return (int)e;
     join_sum_kernel<<<(b.f.H * b.f.d + 31) / 32, 256, 0, st>>>(b, grid);
     return (int)cudaGetLastError();
 }
 
+template <typename IO, int V, int NC> int sized(const JoinArgs& a, cudaStream_t st) {
+    const Shape s = shape_of(a, V, NC, 3, 56 * 1024);
+    if constexpr (V * NC == 8)
+        if (s.threads <= 256) return launch_fwd<IO, V, NC, 256>(a, s, st);
+    return launch_fwd<IO, V, NC, 512>(a, s, st);
+}
+template <typename IO, int V, int NC> int sized(const JoinBwdArgs& b, cudaStream_t st) {
+    const Shape s = shape_of(b.f, V, NC, 5, 72 * 1024);
+    if constexpr (V * NC == 8)
+        if (s.threads <= 256) return launch_bwd<IO, V, NC, 256>(b, s, st);
+    return launch_bwd<IO, V, NC, 512>(b, s, st);
+}
 // 8 values a thread up to 4096 columns (512 threads), 16 above
-#define JOIN_DISPATCH(launch, IO, v, wide, args)                                                           \
-    switch (v) {                                                                                           \
-        case 8: if constexpr (sizeof(IO) == 2) return wide ? launch<IO, 8, 2>(args, st) : launch<IO, 8, 1>(args, st); else return -1; \
-        case 4: return wide ? launch<IO, 4, 4>(args, st) : launch<IO, 4, 2>(args, st);                     \
-        case 2: return wide ? launch<IO, 2, 8>(args, st) : launch<IO, 2, 4>(args, st);                     \
-        default: return wide ? launch<IO, 1, 16>(args, st) : launch<IO, 1, 8>(args, st);                   \
-    }
+template <typename IO, typename Args> int dispatch(const Args& args, int v, bool wide, cudaStream_t st) {
+    if constexpr (sizeof(IO) == 2)
+        if (v == 8) return wide ? sized<IO, 8, 2>(args, st) : sized<IO, 8, 1>(args, st);
+    if (v == 4) return wide ? sized<IO, 4, 4>(args, st) : sized<IO, 4, 2>(args, st);
+    if (v == 2) return wide ? sized<IO, 2, 8>(args, st) : sized<IO, 2, 4>(args, st);
+    return wide ? sized<IO, 1, 16>(args, st) : sized<IO, 1, 8>(args, st);
+}
 
 }  // namespace
 
@@ -369,16 +447,14 @@ int join_fwd_launch(const JoinArgs& a, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int v = piece_of(a, {a.o, a.a, a.x, a.x_out, a.n_out});
     const bool wide = a.H * a.d > 4096;
-    if (a.f32) { JOIN_DISPATCH(launch_fwd, float, v, wide, a) }
-    JOIN_DISPATCH(launch_fwd, __nv_bfloat16, v, wide, a)
+    return a.f32 ? dispatch<float>(a, v, wide, st) : dispatch<__nv_bfloat16>(a, v, wide, st);
 }
 
 int join_bwd_launch(const JoinBwdArgs& b, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const int v = piece_of(b.f, {b.f.o, b.f.a, b.f.x, b.d_x_out, b.d_n, b.d_o, b.d_a, b.d_x});
     const bool wide = b.f.H * b.f.d > 4096;
-    if (b.f.f32) { JOIN_DISPATCH(launch_bwd, float, v, wide, b) }
-    JOIN_DISPATCH(launch_bwd, __nv_bfloat16, v, wide, b)
+    return b.f.f32 ? dispatch<float>(b, v, wide, st) : dispatch<__nv_bfloat16>(b, v, wide, st);
 }
 
 }  // namespace e2ttt
@@ -414,7 +490,7 @@ JoinArgs args_of(const e2ttt_join_params* p, const void* o, const void* a, const
 }
 
 size_t bytes_of(const e2ttt_join_params* p) {
-    return kStatusBytes + (size_t)join_bwd_grid((int64_t)p->B * p->L) * 2 * p->H * p->d * 4;
+    return kStatusBytes + (size_t)join_bwd_grid((int64_t)p->B * p->L, p->H * p->d) * 2 * p->H * p->d * 4;
 }
 
 }  // namespace

@@ -6,7 +6,6 @@
 namespace e2ttt {
 
 constexpr int kJoinMaxWidth = 8192;  // H d: 16 values a thread, 512 threads
-constexpr int kJoinMaxGrid = 592;    // CTAs of the reverse pass, each with partial sums of the parameters' gradients: four per SM
 
 struct JoinArgs {
     int B, H, L, d;
@@ -25,8 +24,11 @@ struct JoinBwdArgs {
     float* part;                                  // [grid][2][H d]
 };
 
-inline int64_t join_tokens(const JoinArgs& a) { return (int64_t)a.B * a.L; }
-inline int join_bwd_grid(int64_t tokens) { return (int)(tokens < kJoinMaxGrid ? tokens : kJoinMaxGrid); }
+// CTAs of the reverse pass, each with partial sums of the parameters' gradients: as many as an SM holds, three of up to 2048 columns
+inline int join_bwd_grid(int64_t tokens, int width) {
+    const int most = 148 * (width <= 512 ? 8 : width <= 2048 ? 3 : 1);
+    return (int)(tokens < most ? tokens : most);
+}
 
 // return a cudaError_t value as int
 int join_fwd_launch(const JoinArgs& a, void* stream);
