@@ -29,15 +29,42 @@ template <typename IO, int V> struct alignas(sizeof(IO) * V) Piece {
     IO x[V];
 };
 
-// gate and its derivative.  With bf16 I/O both are rounded to 2^-9 right after, the hardware's exponential and division (2^-21) serve.
-template <typename IO> __device__ __forceinline__ float gate_of(float a, int kind, float& deriv) {
-    if (kind == E2TTT_GATE_NONE) { deriv = 0.0f; return 1.0f; }
-    const float e = sizeof(IO) == 2 ? __expf(-a) : expf(-a);  // a -> -inf: e = inf, sig = 0
-    const float sig = sizeof(IO) == 2 ? __fdividef(1.0f, 1.0f + e) : 1.0f / (1.0f + e);
-    if (kind == E2TTT_GATE_SIGMOID) { deriv = sig * (1.0f - sig); return sig; }
-    deriv = sig * fmaf(a, 1.0f - sig, 1.0f);
-    return a * sig;
+// 1 / (1 + exp(-a)).  With bf16 I/O what it enters is rounded to 2^-9 right after: the hardware's exponential and reciprocal (2^-22) serve.
+// a -> -inf: the exponential is inf, the result 0.
+template <typename IO> __device__ __forceinline__ float sigmoid(float a) {
+    if (sizeof(IO) == 4) return 1.0f / (1.0f + expf(-a));
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
 }
+
+// Where a token's rows of o start: its batch and position, moved on by the grid's size without a division.
+struct Place {
+    int64_t base;  // first piece of (batch, head 0, position)
+    int l;
+    __device__ __forceinline__ Place(const JoinArgs& a, int64_t tok, int G) {
+        const int64_t b = tok / a.L;
+        l = (int)(tok - b * a.L);
+        base = (b * a.H * a.L + l) * G;
+    }
+};
+struct Stride {
+    int64_t step, wrap;  // pieces to move on, and more when the position wraps into the next batch row
+    int dl, L;
+    __device__ __forceinline__ Stride(const JoinArgs& a, int64_t by, int G) {
+        const int64_t db = by / a.L;
+        L = a.L;
+        dl = (int)(by - db * a.L);
+        step = (db * a.H * a.L + dl) * G;
+        wrap = (int64_t)(a.H - 1) * a.L * G;
+    }
+    __device__ __forceinline__ void move(Place& p) const {
+        p.base += step;
+        p.l += dl;
+        if (p.l >= L) { p.l -= L; p.base += wrap; }
+    }
+};
 
 // Sums over a token's heads and over the token.  `cols` pieces of V values; a head has G of them.
 struct Sums {
@@ -133,11 +160,16 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
     P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][3][NC][T]
     Sums sums = make_sums(smem + (size_t)depth * 3 * NC * T * sizeof(P), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
-    auto at_o = [&](int64_t tok, int c) {
-        const int64_t b = tok / a.L, l = tok % a.L;
-        const int h = c / sums.G;
-        return ((b * a.H + h) * a.L + l) * sums.G + (c - h * sums.G);
-    };
+    int64_t own[NC];  // a piece of o within its token: head and place in the head
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = tid + i * T, h = c / sums.G;
+        own[i] = (int64_t)h * a.L * sums.G + (c - h * sums.G);
+    }
+    const float per_d = 1.0f / a.d, per_D = 1.0f / D;
+    const bool silu = a.gate == E2TTT_GATE_SILU;
+    Place ahead(a, blockIdx.x, sums.G);
+    const Stride stride(a, gridDim.x, sums.G);
     auto load = [&](int64_t tok, int slot) {
         if (tok < tokens) {
             P* r = ring + slot * 3 * NC * T;
@@ -145,11 +177,12 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
             for (int i = 0; i < NC; ++i) {
                 const int c = tid + i * T;
                 if (c >= cols) continue;
-                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + at_o(tok, c));
+                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + ahead.base + own[i]);
                 copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
                 if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
             }
         }
+        stride.move(ahead);
         copy_commit();
     };
     int64_t tok = blockIdx.x;
@@ -178,19 +211,24 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
             if (c >= cols) continue;
-            const float inv = rsqrtf(hs[i] / a.d + a.post_eps);
+            const float inv = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
             const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T];
             const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
+            if (a.a) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av);
+                    y[i][j] *= silu ? av * sig : sig;
+                }
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                float dg, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
-                y[i][j] = fmaf(wr.x[j] * g, y[i][j] * inv * wp.x[j], ldf(px.x[j]));
+                y[i][j] = fmaf(wr.x[j] * inv, y[i][j] * wp.x[j], ldf(px.x[j]));
                 s2 = fmaf(y[i][j], y[i][j], s2);
             }
         }
         if (a.w_pre) row_sums(sums, s2, none);
-        const float m = rsqrtf(s2 / D + a.pre_eps);
+        const float m = rsqrtf(fmaf(s2, per_D, a.pre_eps));
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
@@ -218,11 +256,16 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
     P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][5][NC][T]
     Sums sums = make_sums(smem + (size_t)depth * 5 * NC * T * sizeof(P), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
-    auto at_o = [&](int64_t tok, int c) {
-        const int64_t b = tok / a.L, l = tok % a.L;
-        const int h = c / sums.G;
-        return ((b * a.H + h) * a.L + l) * sums.G + (c - h * sums.G);
-    };
+    int64_t own[NC];  // a piece of o within its token: head and place in the head
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = tid + i * T, h = c / sums.G;
+        own[i] = (int64_t)h * a.L * sums.G + (c - h * sums.G);
+    }
+    const float per_d = 1.0f / a.d, per_D = 1.0f / D;
+    const bool silu = a.gate == E2TTT_GATE_SILU;
+    Place ahead(a, blockIdx.x, sums.G);
+    const Stride stride(a, gridDim.x, sums.G);
     auto load = [&](int64_t tok, int slot) {
         if (tok < tokens) {
             P* r = ring + slot * 5 * NC * T;
@@ -230,15 +273,17 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
             for (int i = 0; i < NC; ++i) {
                 const int c = tid + i * T;
                 if (c >= cols) continue;
-                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + at_o(tok, c));
+                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + ahead.base + own[i]);
                 copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
                 if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
                 copy_piece<sizeof(P)>(r + (3 * NC + i) * T, reinterpret_cast<const P*>(ba.d_x_out) + tok * cols + c);
                 if (a.w_pre) copy_piece<sizeof(P)>(r + (4 * NC + i) * T, reinterpret_cast<const P*>(ba.d_n) + tok * cols + c);
             }
         }
+        stride.move(ahead);
         copy_commit();
     };
+    Place here = ahead;
     float R[NC][V], W[NC][V];  // column sums: dx gate y0, and dn x_out / rms
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -270,15 +315,22 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
             if (c >= cols) continue;
-            inv[i] = rsqrtf(hs[i] / a.d + a.post_eps);
+            inv[i] = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
             const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T], pn = r[(4 * NC + i) * T];
             const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
 #pragma unroll
+            for (int j = 0; j < V; ++j) xo[i][j] = 1.0f;
+            if (a.a) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av);
+                    xo[i][j] = silu ? av * sig : sig;
+                }
+            }
+#pragma unroll
             for (int j = 0; j < V; ++j) {
-                float dg, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
                 y[i][j] *= inv[i];
-                xo[i][j] = fmaf(wr.x[j] * g, y[i][j] * wp.x[j], ldf(px.x[j]));
+                xo[i][j] = fmaf(wr.x[j] * xo[i][j], y[i][j] * wp.x[j], ldf(px.x[j]));
                 s2 = fmaf(xo[i][j], xo[i][j], s2);
             }
             if (a.w_pre) {
@@ -290,8 +342,8 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
         float m = 0.0f, mean = 0.0f;
         if (a.w_pre) {
             row_sums(sums, s2, sd);
-            m = rsqrtf(s2 / D + a.pre_eps);
-            mean = sd * m / D;
+            m = rsqrtf(fmaf(s2, per_D, a.pre_eps));
+            mean = sd * m * per_D;
         }
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -311,33 +363,40 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
                     dx[j] = fmaf(m, fmaf(-h, mean, dn * w.x[j]), dx[j]);
                 }
             }
-            P dx_p, da_p;
+            P dx_p;
             const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
 #pragma unroll
+            for (int j = 0; j < V; ++j) stf(dx_p.x[j], dx[j]);
+            reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
+            if (a.a) {
+                P da_p;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av), dev = silu ? fmaf(av, 1.0f - sig, 1.0f) : 1.0f - sig;
+                    stf(da_p.x[j], dx[j] * wr.x[j] * wp.x[j] * y[i][j] * (sig * dev));
+                    dx[j] *= silu ? av * sig : sig;
+                }
+                reinterpret_cast<P*>(ba.d_a)[tok * cols + c] = da_p;
+            }
+#pragma unroll
             for (int j = 0; j < V; ++j) {
-                stf(dx_p.x[j], dx[j]);
-                float dg = 0.0f, g = 1.0f;
-                if (a.a) g = gate_of<IO>(ldf(pa.x[j]), a.gate, dg);
-                const float cw = wr.x[j] * wp.x[j];
-                R[i][j] = fmaf(dx[j] * g, y[i][j], R[i][j]);
-                stf(da_p.x[j], dx[j] * cw * y[i][j] * dg);
-                xo[i][j] = dx[j] * cw * g;  // adjoint of y0
+                R[i][j] = fmaf(dx[j], y[i][j], R[i][j]);
+                xo[i][j] = dx[j] * wr.x[j] * wp.x[j];  // adjoint of y0
                 hs[i] = fmaf(xo[i][j], y[i][j], hs[i]);
             }
-            reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
-            if (a.a) reinterpret_cast<P*>(ba.d_a)[tok * cols + c] = da_p;
         }
         head_sums<NC>(sums, hs);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
             if (c >= cols) continue;
-            const float mh = hs[i] / a.d;
+            const float mh = hs[i] * per_d;
             P do_p;
 #pragma unroll
             for (int j = 0; j < V; ++j) stf(do_p.x[j], inv[i] * fmaf(-y[i][j], mh, xo[i][j]));
-            reinterpret_cast<P*>(ba.d_o)[at_o(tok, c)] = do_p;
+            reinterpret_cast<P*>(ba.d_o)[here.base + own[i]] = do_p;
         }
+        stride.move(here);
     }
     float* part = ba.part + (size_t)blockIdx.x * 2 * D;
 #pragma unroll
@@ -352,15 +411,15 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
     }
 }
 
-// column sums over the CTAs: 32 columns by 8 row groups a CTA
-__global__ void __launch_bounds__(256) join_sum_kernel(const JoinBwdArgs ba, const int rows) {
-    __shared__ float red[2][8][32];
+// column sums over the CTAs: 32 columns by 32 row groups a CTA
+__global__ void __launch_bounds__(1024) join_sum_kernel(const JoinBwdArgs ba, const int rows) {
+    __shared__ float red[2][32][32];
     const JoinArgs& a = ba.f;
     const int D = a.H * a.d, lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float r = 0.0f, w = 0.0f;
     if (c < D) {
-#pragma unroll 4
-        for (int i = group; i < rows; i += 8) {
+#pragma unroll 8
+        for (int i = group; i < rows; i += 32) {
             r += ba.part[(size_t)i * 2 * D + c];
             if (a.w_pre) w += ba.part[(size_t)i * 2 * D + D + c];
         }
@@ -370,7 +429,7 @@ __global__ void __launch_bounds__(256) join_sum_kernel(const JoinBwdArgs ba, con
     __syncthreads();
     if (group != 0 || c >= D) return;
     r = w = 0.0f;
-    for (int i = 0; i < 8; ++i) { r += red[0][i][lane]; w += red[1][i][lane]; }
+    for (int i = 0; i < 32; ++i) { r += red[0][i][lane]; w += red[1][i][lane]; }
     ba.d_w_post[c] = r * a.res_scale[c];
     ba.d_res_scale[c] = r * a.w_post[c];
     if (a.w_pre) ba.d_w_pre[c] = w;
@@ -416,7 +475,7 @@ template <typename IO, int V, int NC, int TMAX> int launch_bwd(const JoinBwdArgs
     kernel<<<grid, s.threads, s.smem, st>>>(b, s.depth);
     e = cudaGetLastError();
     if (e != cudaSuccess) return (int)e;
-    join_sum_kernel<<<(b.f.H * b.f.d + 31) / 32, 256, 0, st>>>(b, grid);
+    join_sum_kernel<<<(b.f.H * b.f.d + 31) / 32, 1024, 0, st>>>(b, grid);
     return (int)cudaGetLastError();
 }
 

@@ -26,7 +26,7 @@ struct JoinBwdArgs {
 
 // CTAs of the reverse pass, each with partial sums of the parameters' gradients: as many as an SM holds, three of up to 2048 columns
 inline int join_bwd_grid(int64_t tokens, int width) {
-    const int most = 148 * (width <= 512 ? 8 : width <= 2048 ? 3 : 1);
+    const int most = 148 * (width <= 512 ? 8 : width <= 1024 ? 6 : width <= 2048 ? 3 : 1);
     return (int)(tokens < most ? tokens : most);
 }
 
