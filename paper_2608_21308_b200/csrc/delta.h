@@ -19,7 +19,7 @@ constexpr int kDeltaMaxD = 128;  // a slice of 16 state rows of 128 columns is a
 constexpr int kDeltaRecBytes = 9216;
 constexpr int kDeltaRecSkip = 4096;
 // rows of a record's scalars
-enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecHead = 7 };
+enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecW = 4, kRecHead = 7 };
 // the last row: decay of the whole chunk; what undoes the scales of T, A, K, Q and the reverse pass' T; then bounds of the chunk's operands:
 // max b |k| (2-norm), row sums of T, max |eta|, max |eta| D_end (in units of the K tile), sum |eta| D_end |k|
 enum { kHeadEnd = 0, kHeadT = 1, kHeadA = 2, kHeadK = 3, kHeadQ = 4, kHeadR = 5, kHeadKn = 6, kHeadTsum = 7, kHeadUmax = 8, kHeadWmax = 9, kHeadWsum = 10 };

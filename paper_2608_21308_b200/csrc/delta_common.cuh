@@ -42,6 +42,23 @@ __device__ __forceinline__ void pow2_bound(float m, float& s, float& inv) {
     s = __uint_as_float((uint32_t)(127 + e) << 23);
     inv = __uint_as_float((uint32_t)(127 - e) << 23);
 }
+// two fp32 values at a time (one instruction on this architecture)
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pack2(a0, a1)), "l"(pack2(b0, b1)), "l"(pack2(c0, c1)));
+    unpack2(r, d0, d1);
+}
+__device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, float b0, float b1) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a0, a1)), "l"(pack2(b0, b1)));
+    unpack2(r, d0, d1);
+}
 __device__ __forceinline__ float quad_sum(float m) {
     m += __shfl_xor_sync(kAll, m, 1);
     return m + __shfl_xor_sync(kAll, m, 2);
@@ -69,7 +86,16 @@ __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& 
     const __half2 h = __floats2half2_rn(x, y);
     const float2 f = __half22float2(h);
     hi = *reinterpret_cast<const uint32_t*>(&h);
-    lo = pack_half(x - f.x, y - f.y);
+    float r, q;
+    fma2(r, q, f.x, f.y, -1.0f, -1.0f, x, y);
+    lo = pack_half(r, q);
+}
+// an operand that carries its scale already
+__device__ __forceinline__ void split_a(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+    split(x[0], x[1], hi[0], lo[0]);
+    split(x[2], x[3], hi[1], lo[1]);
+    split(y[0], y[1], hi[2], lo[2]);
+    split(y[2], y[3], hi[3], lo[3]);
 }
 
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -79,6 +105,9 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
 }
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void stsm4_t(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -117,6 +146,22 @@ __device__ __forceinline__ void to_a(const float (&x)[4], const float (&y)[4], f
     split(x[2] * s1, x[3] * s1, hi[1], lo[1]);
     split(y[0] * s0, y[1] * s0, hi[2], lo[2]);
     split(y[2] * s1, y[3] * s1, hi[3], lo[3]);
+}
+
+// Tiles of 32 tokens x 16 value rows in bf16 (32 bytes a token, the two pieces of tokens 4-7 of eight exchanged): lane's address for the
+// transposing ldmatrix / stmatrix of tokens 16 half .. 16 half + 15, which give and take pairs of tokens in accumulator order
+__device__ __forceinline__ uint32_t tok_at(int t, int piece) { return (uint32_t)(t * 32 + ((piece ^ ((t >> 2) & 1)) << 4)); }
+__device__ __forceinline__ uint32_t addr_tok(uint32_t base, int half, int lane) {
+    const int m = lane >> 3, r = lane & 7;
+    return base + tok_at(half * 16 + (m >> 1) * 8 + r, m & 1);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// wait for a phase that has usually come: the bounded wait only if it has not
+__device__ __forceinline__ void wait_phase(uint64_t* bar, uint32_t parity, const sm100::WaitCtx& w, int where) {
+    if (!sm100::mbar_try_wait<false>(bar, parity)) sm100::mbar_wait(bar, parity, w, where);
 }
 
 __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {

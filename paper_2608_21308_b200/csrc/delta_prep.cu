@@ -151,7 +151,21 @@ __device__ __forceinline__ float invert(const float* Nm, char* out, int lane, fl
         most = fmaxf(most, fabsf(x[t]));
     }
     float s, inv;
-    rows = warp_sum(most);  // no row's sum of magnitudes is larger
+    // the largest sum of magnitudes of a row: lane t's column sums in 31 exchanges
+    float part[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float keep = fabsf(lane & 16 ? x[i + 16] : x[i]), give = fabsf(lane & 16 ? x[i] : x[i + 16]);
+        part[i] = keep + __shfl_xor_sync(kAll, give, 16);
+    }
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1)
+#pragma unroll
+        for (int i = 0; i < w; ++i) {
+            const float keep = lane & w ? part[i + w] : part[i], give = lane & w ? part[i] : part[i + w];
+            part[i] = keep + __shfl_xor_sync(kAll, give, w);
+        }
+    rows = warp_max(part[0]);
     pow2_scale(warp_max(most), s, inv);
 #pragma unroll
     for (int t = 0; t < 32; ++t) {
@@ -217,6 +231,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         sc[kRecBq * 32 + lane] = bt * iq * s.scale;
         sc[kRecEta * 32 + lane] = eta;
         sc[kRecDend * 32 + lane] = dend * ik;
+        sc[kRecW * 32 + lane] = eta * dend * ik;
         // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
         float amax = 0.0f, av[6][4];
 #pragma unroll
