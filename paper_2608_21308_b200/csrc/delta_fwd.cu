@@ -273,53 +273,42 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 // S = b_end S + (D_end u) K, 32 columns at a time: the sum of the chunk apart from the state (the MMAs truncate what they add to),
                 // then one rounding.  A piece's columns go on into the next chunk's S K^T while the next piece is summed.  (Behind the last
                 // chunk that product is of whatever the ring holds, and unused.)
+                // Fragments are fetched a piece ahead of the products that they are for.
+                constexpr int NJ = DC / 32;
                 float y[2][4][4];
-                auto sum = [&](int j4, float (&t)[4][4]) {
+                uint32_t fs[2][2][KT][4], fk[2][2 * KT][4];
+                auto load_s = [&](int j4) {
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int k = 0; k < KT; ++k) ldsm4_t(fs[kk][h][k], addr_kn<DK>(ks + k * 64 * DK, part * (DC / 8) + 4 * j4 + 2 * h, kk, lane));
+                };
+                auto sum = [&](float (&t)[4][4]) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int z = 0; z < 4; ++z) t[i][z] = 0.0f;
 #pragma unroll
                     for (int kk = 0; kk < 2; ++kk) {
-                        uint32_t b[2][KT][4];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wh[kk], fs[kk][h][0][0], fs[kk][h][0][1]); mma(t[2 * h + 1], wh[kk], fs[kk][h][0][2], fs[kk][h][0][3]); }
 #pragma unroll
-                            for (int k = 0; k < KT; ++k) ldsm4_t(b[h][k], addr_kn<DK>(ks + k * 64 * DK, part * (DC / 8) + 4 * j4 + 2 * h, kk, lane));
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wh[kk], b[h][0][0], b[h][0][1]); mma(t[2 * h + 1], wh[kk], b[h][0][2], b[h][0][3]); }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wl[kk], b[h][0][0], b[h][0][1]); mma(t[2 * h + 1], wl[kk], b[h][0][2], b[h][0][3]); }
+                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wl[kk], fs[kk][h][0][0], fs[kk][h][0][1]); mma(t[2 * h + 1], wl[kk], fs[kk][h][0][2], fs[kk][h][0][3]); }
                         if (KT == 2)
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                mma(t[2 * h], wh[kk], b[h][KT - 1][0], b[h][KT - 1][1]);
-                                mma(t[2 * h + 1], wh[kk], b[h][KT - 1][2], b[h][KT - 1][3]);
+                                mma(t[2 * h], wh[kk], fs[kk][h][KT - 1][0], fs[kk][h][KT - 1][1]);
+                                mma(t[2 * h + 1], wh[kk], fs[kk][h][KT - 1][2], fs[kk][h][KT - 1][3]);
                             }
                     }
                 };
-                sum(0, y[0]);
-#pragma unroll
-                for (int j4 = 0; j4 < DC / 32; ++j4) {
-                    if (j4 + 1 < DC / 32) sum(j4 + 1, y[(j4 + 1) & 1]);
-                    uint32_t b0[2 * KT][4], b1[2 * KT][4];
-                    load_k(kn, 2 * j4, b0);
-                    load_k(kn, 2 * j4 + 1, b1);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float (&d)[4] = S[4 * j4 + i];
-                        const float (&t)[4] = y[j4 & 1][i];
-#pragma unroll
-                        for (int z = 0; z < 4; z += 2) {
-                            float m0, m1;
-                            mul2(m0, m1, d[z], d[z + 1], w_old, w_old);
-                            fma2(d[z], d[z + 1], t[z], t[z + 1], w_new, w_new, m0, m1);
-                        }
-                    }
-                    with_k(2 * j4, xn, b0);
-                    with_k(2 * j4 + 1, xn, b1);
-                }
-                hand(xn);
+                load_s(0);
+                sum(y[0]);
+                if (NJ > 1) load_s(1);
+                load_k(kn, 0, fk[0]);
+                load_k(kn, 1, fk[1]);
                 // u's fragments for the outputs, and what the reverse pass reads: shared out between the parts
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
@@ -346,6 +335,31 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                         }
                     }
                 }
+#pragma unroll
+                for (int j4 = 0; j4 < NJ; ++j4) {
+                    if (j4 + 1 < NJ) {
+                        sum(y[(j4 + 1) & 1]);
+                        if (j4 + 2 < NJ) load_s(j4 + 2);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float (&d)[4] = S[4 * j4 + i];
+                        const float (&t)[4] = y[j4 & 1][i];
+#pragma unroll
+                        for (int z = 0; z < 4; z += 2) {
+                            float m0, m1;
+                            mul2(m0, m1, d[z], d[z + 1], w_old, w_old);
+                            fma2(d[z], d[z + 1], t[z], t[z + 1], w_new, w_new, m0, m1);
+                        }
+                    }
+                    with_k(2 * j4, xn, fk[0]);
+                    with_k(2 * j4 + 1, xn, fk[1]);
+                    if (j4 + 1 < NJ) {
+                        load_k(kn, 2 * j4 + 2, fk[0]);
+                        load_k(kn, 2 * j4 + 3, fk[1]);
+                    }
+                }
+                hand(xn);
                 if (a.save && part == 0) {
                     float m = 0.0f;
 #pragma unroll
@@ -380,41 +394,40 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     const char* qk_src = a.ws + a.l.qk + (size_t)nk * nch * a.l.qk_bytes;
     const char* rec_src = a.ws + a.l.rec + (size_t)n * nch * a.l.rec_bytes;
     const bool fetches = mine == 0 && lane == 0;
-    auto fetch = [&](int c) {
-        const uint32_t dst = ring + (c % NS) * SB;
-        uint64_t* bar = &full[c % NS];
+    auto fetch = [&](int c, int st) {
+        const uint32_t dst = ring + st * SB;
+        uint64_t* bar = &full[st];
         sm100::mbar_expect_tx(bar, SB);
         bulk_copy(dst, qk_src + (size_t)c * a.l.qk_bytes, 2 * KT * 64 * DK, bar);
         bulk_copy(dst + 2 * KT * 64 * DK, rec_src + (size_t)c * a.l.rec_bytes, kDeltaRecBytes, bar);
     };
     if (fetches)
-        for (int c = 0; c < NS && c < nch; ++c) fetch(c);
+        for (int c = 0; c < NS && c < nch; ++c) fetch(c, c);
     __syncwarp();
     const IO* v = reinterpret_cast<const IO*>(a.v) + (size_t)n * s.L * s.dv + slice * 16;
     IO* o = a.o ? reinterpret_cast<IO*>(a.o) + (size_t)n * s.L * s.dv + slice * 16 : nullptr;
     const int rows = active ? min(16, s.dv - slice * 16) : 0;  // value rows of the slice
-    // the values of a chunk: bf16, lane = token, its 16 rows in two pieces; fp32, in fragment order
-    uint4 vp[2];
-    float vf[KT == 1 ? 1 : 4][4];
+    // The values of a chunk: bf16, lane = token, its 16 rows in two pieces; fp32, in fragment order.  Asynchronous copies, so that nothing
+    // that the warp waits for on the way to the outputs waits for them (rows of odd widths go through registers)
+    uint32_t odd[8];
     auto load_v = [&](int c) {
+        X& x = xb[c & 1];
         if (KT == 1) {
             const int t = c * kDeltaChunk + lane;
-            vp[0] = vp[1] = make_uint4(0, 0, 0, 0);
-            if (t >= s.L) return;
             const IO* p = v + (size_t)t * s.dv;
+            const int here = t < s.L ? rows : 0;
             if (vec) {
-                if (rows > 0) vp[0] = reinterpret_cast<const uint4*>(p)[0];
-                if (rows > 8) vp[1] = reinterpret_cast<const uint4*>(p)[1];
+                const uint32_t tile = sm100::smem_u32(x.v);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tile + tok_at(lane, i)), "l"(here > 8 * i ? p + 8 * i : v), "r"(here > 8 * i ? 16 : 0) : "memory");
             } else {
-                uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t x = 2 * i < rows ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u;
-                    const uint32_t y = 2 * i + 1 < rows ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0u;
-                    w[i] = x | y << 16;
+                    const uint32_t y = 2 * i < here ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u;
+                    const uint32_t z = 2 * i + 1 < here ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0u;
+                    odd[i] = y | z << 16;
                 }
-                vp[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                vp[1] = make_uint4(w[4], w[5], w[6], w[7]);
             }
         } else {
 #pragma unroll
@@ -422,35 +435,40 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (i & 1), r = g + (i < 2 ? 0 : 8);
-                    vf[KT == 1 ? 0 : j][i] = t < s.L && r < rows ? to_f32(v[(size_t)t * s.dv + r]) : 0.0f;
+                    const bool ok = t < s.L && r < rows;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(sm100::smem_u32(&x.v[KT == 1 ? 0 : j][lane]) + 4 * i), "l"(ok ? v + (size_t)t * s.dv + r : v), "r"(ok ? 4 : 0) : "memory");
                 }
         }
     };
-    auto hand_v = [&](int c) {
+    auto hand_v = [&](int c) {  // the copies have come; a bound on the values
         X& x = xb[c & 1];
         float m = 0.0f;
         if (KT == 1) {
             char* tile = reinterpret_cast<char*>(x.v);
-            *reinterpret_cast<uint4*>(tile + tok_at(lane, 0)) = vp[0];
-            *reinterpret_cast<uint4*>(tile + tok_at(lane, 1)) = vp[1];
+            if (!vec) {
+                *reinterpret_cast<uint4*>(tile + tok_at(lane, 0)) = make_uint4(odd[0], odd[1], odd[2], odd[3]);
+                *reinterpret_cast<uint4*>(tile + tok_at(lane, 1)) = make_uint4(odd[4], odd[5], odd[6], odd[7]);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            const uint4 y = *reinterpret_cast<const uint4*>(tile + tok_at(lane, 0)), z = *reinterpret_cast<const uint4*>(tile + tok_at(lane, 1));
             uint32_t top = 0;  // largest magnitude on the bits: both halves of a word at a time
-            const uint32_t w[8] = {vp[0].x, vp[0].y, vp[0].z, vp[0].w, vp[1].x, vp[1].y, vp[1].z, vp[1].w};
+            const uint32_t w[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
             m = __uint_as_float(max(top << 16, top & 0xffff0000u));
         } else {
+            asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float (&y)[4] = vf[KT == 1 ? 0 : j];
-                x.v[KT == 1 ? 0 : j][lane] = make_float4(y[0], y[1], y[2], y[3]);
-                m = fmaxf(m, fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])), fmaxf(fabsf(y[2]), fabsf(y[3]))));
+                const float4 y = x.v[KT == 1 ? 0 : j][lane];
+                m = fmaxf(m, fmaxf(fmaxf(fabsf(y.x), fabsf(y.y)), fmaxf(fabsf(y.z), fabsf(y.w))));
             }
         }
         m = warp_max(m);
         if (lane == 0) x.v_max = m;
     };
-    auto product = [&](int c, float (&sq)[4][4]) {  // S Q^T, in S's scale
-        const uint32_t qs = ring + c % NS * SB + KT * 64 * DK;
+    auto product = [&](int c, int st, float (&sq)[4][4]) {  // S Q^T, in S's scale
+        const uint32_t qs = ring + st * SB + KT * 64 * DK;
         const X& x = xb[c & 1];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -475,9 +493,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, b[h][KT - 1][0], b[h][KT - 1][1]); mma(sq[2 * h + 1], hi, b[h][KT - 1][2], b[h][KT - 1][3]); }
         }
     };
-    auto finish = [&](int c, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + u A^T
-        const uint32_t as = ring + c % NS * SB + 2 * KT * 64 * DK + 4096;
-        const float* sc = reinterpret_cast<const float*>(smem + c % NS * SB + 2 * KT * 64 * DK + 8192);
+    auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + u A^T
+        const uint32_t as = ring + st * SB + 2 * KT * 64 * DK + 4096;
+        const float* sc = reinterpret_cast<const float*>(smem + st * SB + 2 * KT * 64 * DK + 8192);
         X& x = xb[c & 1];
         float in[4][4] = {};
 #pragma unroll
@@ -553,22 +571,23 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     load_v(0);
     hand_v(0);
     __syncthreads();
-    if (nch > 1) load_v(1);
     float sq[4][4], s_inv = 1.0f;
+    int st = 0, phase = 0;
     for (int i = 0; i <= nch; ++i) {
-        if (active && i > 0) finish(i - 1, sq, s_inv);
+        if (i + 1 < nch) load_v(i + 1);  // the chain reads chunk i's
+        if (active && i > 0) finish(i - 1, st == 0 ? NS - 1 : st - 1, sq, s_inv);
         if (i < nch) {
-            wait_phase(&full[i % NS], (i / NS) & 1, wait, 903);
+            wait_phase(&full[st], phase, wait, 903);
             if (active) {
-                product(i, sq);
+                product(i, st, sq);
                 s_inv = xb[i & 1].s_inv;
             }
+            if (i + 1 < nch) hand_v(i + 1);
+            __syncthreads();  // chunk i is through the chain, chunk i - 1 through here
         }
-        if (i + 1 < nch) hand_v(i + 1);  // the chain reads chunk i's now
-        if (i + 2 < nch) load_v(i + 2);
-        if (i < nch) __syncthreads();    // chunk i is through the chain, chunk i - 1 through here
-        if (fetches && i > 0 && i - 1 + NS < nch) fetch(i - 1 + NS);
+        if (fetches && i > 0 && i - 1 + NS < nch) fetch(i - 1 + NS, st == 0 ? NS - 1 : st - 1);
         __syncwarp();
+        if (++st == NS) { st = 0; phase ^= 1; }
     }
 }
 
