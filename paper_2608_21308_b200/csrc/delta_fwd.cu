@@ -90,25 +90,31 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         // With |S| the slice's 2-norm:  |P| <= max |v| + max b |k| |S|,  |e| <= sum |T| |P|,  |S_next| <= b_end |S| + sum (|eta| D_end |k|) |e|
         // for every row.  |S| itself is summed beside the products, scaled, so that squares stay in range.
         float sk[4][4], squares0 = 0.0f, squares1 = 0.0f;  // S K^T of the next chunk
-        // column tiles 2 kk, 2 kk + 1 of the warp's part of S: fragments to the outputs' warp and into S K^T
-        auto with_k = [&](int kk, X& x, const uint32_t (&b)[2 * KT][4]) {
-            uint32_t hi[4], lo[4];
-            const float (&y)[4] = S[2 * kk], (&z)[4] = S[2 * kk + 1];
-            fma2(squares0, squares1, y[0], y[1], y[0], y[1], squares0, squares1);
-            fma2(squares0, squares1, y[2], y[3], y[2], y[3], squares0, squares1);
-            fma2(squares0, squares1, z[0], z[1], z[0], z[1], squares0, squares1);
-            fma2(squares0, squares1, z[2], z[3], z[2], z[3], squares0, squares1);
-            split_a(y, z, hi, lo);
-            x.s[0][part * (DC / 16) + kk][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            if (PREC) x.s[PREC ? 1 : 0][part * (DC / 16) + kk][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            mma(sk[0], hi, b[0][0], b[0][1]); mma(sk[1], hi, b[0][2], b[0][3]);
-            mma(sk[2], hi, b[1][0], b[1][1]); mma(sk[3], hi, b[1][2], b[1][3]);
-            mma(sk[0], lo, b[0][0], b[0][1]); mma(sk[1], lo, b[0][2], b[0][3]);
-            mma(sk[2], lo, b[1][0], b[1][1]); mma(sk[3], lo, b[1][2], b[1][3]);
-            if (KT == 2) {
-                constexpr int f = KT == 2 ? 2 : 0, h = KT == 2 ? 3 : 0;
-                mma(sk[0], hi, b[f][0], b[f][1]); mma(sk[1], hi, b[f][2], b[f][3]);
-                mma(sk[2], hi, b[h][0], b[h][1]); mma(sk[3], hi, b[h][2], b[h][3]);
+        uint32_t fh[2][4], fl[2][4];                       // fragments of two column tiles of S each: even and odd
+        constexpr int TERMS = KT == 2 ? 3 : 2;             // products of an operand in two terms with a tile of the ring
+        // a pair of columns of column tiles 2 kk, 2 kk + 1 of the warp's part of S into its fragment
+        auto split_s = [&](int kk, int r) {
+            const float (&y)[4] = S[2 * kk + (r >> 1)];
+            const float y0 = y[2 * (r & 1)], y1 = y[2 * (r & 1) + 1];
+            fma2(squares0, squares1, y0, y1, y0, y1, squares0, squares1);
+            split(y0, y1, fh[kk & 1][r], fl[kk & 1][r]);
+        };
+        auto leave_s = [&](int kk, X& x) {  // for the outputs' warp
+            const uint32_t (&h)[4] = fh[kk & 1], (&l)[4] = fl[kk & 1];
+            x.s[0][part * (DC / 16) + kk][lane] = make_uint4(h[0], h[1], h[2], h[3]);
+            if (PREC) x.s[PREC ? 1 : 0][part * (DC / 16) + kk][lane] = make_uint4(l[0], l[1], l[2], l[3]);
+        };
+        // the i-th two MMAs (of 2 TERMS) of those column tiles with a key tile
+        auto times_k = [&](int kk, int i, bool first, const uint32_t (&b)[2 * KT][4]) {
+            const int term = i >> 1, h = i & 1;
+            const uint32_t (&x)[4] = term == 1 ? fl[kk & 1] : fh[kk & 1];
+            const uint32_t (&y)[4] = b[term == 2 ? 2 * KT - 2 + h : h];
+            if (first && term == 0) {
+                mma0(sk[2 * h], x, y[0], y[1]);
+                mma0(sk[2 * h + 1], x, y[2], y[3]);
+            } else {
+                mma(sk[2 * h], x, y[0], y[1]);
+                mma(sk[2 * h + 1], x, y[2], y[3]);
             }
         };
         auto load_k = [&](uint32_t ks, int kk, uint32_t (&b)[2 * KT][4]) {
@@ -118,15 +124,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 ldsm4(b[2 * t + 1], addr_nk<DK>(ks + t * 64 * DK, 2, part * (DC / 16) + kk, lane));
             }
         };
-        auto begin = [&]() {
-            squares0 = squares1 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) sk[j][y] = 0.0f;
-        };
-        auto hand = [&](X& x) {  // the warp's part of S K^T and of the norm
-            const float y = warp_sum(squares0 + squares1);
+        auto hand = [&](X& x) {  // the warp's part of S K^T and of the norm: 32 times the largest of the lanes' sums bounds their sum
+            const float y = 32.0f * warp_most(squares0 + squares1);
             if (KS == 1) {
                 norm = y;
             } else {
@@ -162,7 +161,6 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 if (ok1) m = fmaxf(m, fabsf(a.S_init[((size_t)n * s.dv + r1) * s.dk + col]));
             }
             pow2_bound(warp_max(m), s_now, s_inv);
-            begin();
 #pragma unroll
             for (int j = 0; j < DC / 8; ++j)
 #pragma unroll
@@ -171,7 +169,11 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             for (int kk = 0; kk < DC / 16; ++kk) {
                 uint32_t b[2 * KT][4];
                 load_k(ring, kk, b);
-                with_k(kk, xb[0], b);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) split_s(kk, r);
+                leave_s(kk, xb[0]);
+#pragma unroll
+                for (int i = 0; i < 2 * TERMS; ++i) times_k(kk, i, kk == 0, b);
             }
             hand(xb[0]);
         }
@@ -185,6 +187,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             X& xn = xb[(c + 1) & 1];
             float e[4][4], uf = 0.0f, w_old = 0.0f, w_new = 0.0f, qe = 0.0f;
             uint32_t wh[2][4], wl[2][4];
+            const bool come = c + 1 == nch || probe_phase(&full[st_next], phase_next);
             if (active) {
                 take(x);
                 if (a.save && (c & 1) == 0) save_state(c >> 1);
@@ -226,14 +229,12 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                     mul2(y0, y1, bk.x, bk.y, fs, fs);
                     fma2(p[j][0], p[j][1], sk[j][0], sk[j][1], y0, y1, p[j][0], p[j][1]);
                     fma2(p[j][2], p[j][3], sk[j][2], sk[j][3], y0, y1, p[j][2], p[j][3]);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) e[j][y] = 0.0f;
                 }
                 {
                     uint32_t h0[4], l0[4], h1[4], l1[4];
                     split_a(p[0], p[1], h0, l0);
-                    mma(e[0], h0, th[0][0], th[0][1]); mma(e[1], h0, th[0][2], th[0][3]);
-                    mma(e[2], h0, th[1][0], th[1][1]); mma(e[3], h0, th[1][2], th[1][3]);
+                    mma0(e[0], h0, th[0][0], th[0][1]); mma0(e[1], h0, th[0][2], th[0][3]);
+                    mma0(e[2], h0, th[1][0], th[1][1]); mma0(e[3], h0, th[1][2], th[1][3]);
                     split_a(p[2], p[3], h1, l1);
                     mma(e[0], l0, th[0][0], th[0][1]); mma(e[1], l0, th[0][2], th[0][3]);
                     mma(e[2], l0, th[1][0], th[1][1]); mma(e[3], l0, th[1][2], th[1][3]);
@@ -266,14 +267,15 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 }
                 split_a(w[0], w[1], wh[0], wl[0]);
                 split_a(w[2], w[3], wh[1], wl[1]);
-                begin();
             }
-            if (c + 1 < nch) wait_phase(&full[st_next], phase_next, wait, 901);
+            if (!come) sm100::mbar_wait(&full[st_next], phase_next, wait, 901);
             if (active) {
                 // S = b_end S + (D_end u) K, 32 columns at a time: the sum of the chunk apart from the state (the MMAs truncate what they add to),
                 // then one rounding.  A piece's columns go on into the next chunk's S K^T while the next piece is summed.  (Behind the last
                 // chunk that product is of whatever the ring holds, and unused.)
-                // Fragments are fetched a piece ahead of the products that they are for.
+                // A warp issues in order, and an MMA that finds the pipe busy holds up what stands behind it: the arithmetic of a piece is cut into
+                // twelve steps (a column tile of S, four times, and its fragments' pairs, eight times), with the MMAs in twos between
+                // them.  Fragments are fetched a piece ahead of the products that they are for.
                 constexpr int NJ = DC / 32;
                 float y[2][4][4];
                 uint32_t fs[2][2][KT][4], fk[2][2 * KT][4];
@@ -285,33 +287,25 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 #pragma unroll
                             for (int k = 0; k < KT; ++k) ldsm4_t(fs[kk][h][k], addr_kn<DK>(ks + k * 64 * DK, part * (DC / 8) + 4 * j4 + 2 * h, kk, lane));
                 };
-                auto sum = [&](float (&t)[4][4]) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int z = 0; z < 4; ++z) t[i][z] = 0.0f;
-#pragma unroll
-                    for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wh[kk], fs[kk][h][0][0], fs[kk][h][0][1]); mma(t[2 * h + 1], wh[kk], fs[kk][h][0][2], fs[kk][h][0][3]); }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { mma(t[2 * h], wl[kk], fs[kk][h][0][0], fs[kk][h][0][1]); mma(t[2 * h + 1], wl[kk], fs[kk][h][0][2], fs[kk][h][0][3]); }
-                        if (KT == 2)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                mma(t[2 * h], wh[kk], fs[kk][h][KT - 1][0], fs[kk][h][KT - 1][1]);
-                                mma(t[2 * h + 1], wh[kk], fs[kk][h][KT - 1][2], fs[kk][h][KT - 1][3]);
-                            }
+                auto sum = [&](float (&t)[4][4], int i) {  // the i-th two MMAs (of 4 TERMS)
+                    const int kk = i / (2 * TERMS), term = i % (2 * TERMS) >> 1, h = i & 1;
+                    const uint32_t (&w)[4] = term == 1 ? wl[kk] : wh[kk];
+                    const uint32_t (&b)[4] = fs[kk][h][term == 2 ? KT - 1 : 0];
+                    if (kk == 0 && term == 0) {
+                        mma0(t[2 * h], w, b[0], b[1]);
+                        mma0(t[2 * h + 1], w, b[2], b[3]);
+                    } else {
+                        mma(t[2 * h], w, b[0], b[1]);
+                        mma(t[2 * h + 1], w, b[2], b[3]);
                     }
                 };
                 load_s(0);
-                sum(y[0]);
-                if (NJ > 1) load_s(1);
-                load_k(kn, 0, fk[0]);
-                load_k(kn, 1, fk[1]);
-                // u's fragments for the outputs, and what the reverse pass reads: shared out between the parts
+                squares0 = squares1 = 0.0f;
+                // u's fragments for the outputs, and what the reverse pass reads, shared out between the parts; beside the first piece's sum
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+                    for (int i = 0; i < 2 * TERMS; ++i) sum(y[0], kk * 2 * TERMS + i);
                     if (KS > 1 && part != kk) continue;
                     float u[2][4];
 #pragma unroll
@@ -335,30 +329,47 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                         }
                     }
                 }
+                if (NJ > 1) load_s(1);
+                load_k(kn, 0, fk[0]);
 #pragma unroll
                 for (int j4 = 0; j4 < NJ; ++j4) {
-                    if (j4 + 1 < NJ) {
-                        sum(y[(j4 + 1) & 1]);
-                        if (j4 + 2 < NJ) load_s(j4 + 2);
-                    }
+                    // the MMAs beside this piece: the odd column tiles of the one before with the keys, the next one's sum, the even tiles of this one
+                    const int before = j4 > 0 ? 2 * TERMS : 0, next = j4 + 1 < NJ ? 4 * TERMS : 0, all = before + next + 2 * TERMS;
+                    auto upto = [&](int m) {  // how many behind step m; the even tiles' fragments are whole behind step 5
+                        const int most = m < 5 ? before + next : all;
+                        return (m + 1) * all / 12 < most ? (m + 1) * all / 12 : most;
+                    };
+                    auto issue = [&](int i) {
+                        if (i < before) times_k(2 * j4 - 1, i, false, fk[1]);
+                        else if (i < before + next) sum(y[(j4 + 1) & 1], i - before);
+                        else times_k(2 * j4, i - before - next, j4 == 0, fk[0]);
+                        if (i + 1 == before || (i == 0 && before == 0)) load_k(kn, 2 * j4 + 1, fk[1]);
+                        if (next > 0 && i + 1 == before + next && j4 + 2 < NJ) load_s(j4 + 2);
+                    };
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float (&d)[4] = S[4 * j4 + i];
-                        const float (&t)[4] = y[j4 & 1][i];
+                    for (int m = 0; m < 12; ++m) {
+                        if (m == 0 || m == 1 || m == 6 || m == 7) {  // a column tile of S
+                            const int i = m < 2 ? m : m - 4;
+                            float (&d)[4] = S[4 * j4 + i];
+                            const float (&t)[4] = y[j4 & 1][i];
 #pragma unroll
-                        for (int z = 0; z < 4; z += 2) {
-                            float m0, m1;
-                            mul2(m0, m1, d[z], d[z + 1], w_old, w_old);
-                            fma2(d[z], d[z + 1], t[z], t[z + 1], w_new, w_new, m0, m1);
+                            for (int z = 0; z < 4; z += 2) {
+                                float m0, m1;
+                                mul2(m0, m1, d[z], d[z + 1], w_old, w_old);
+                                fma2(d[z], d[z + 1], t[z], t[z + 1], w_new, w_new, m0, m1);
+                            }
+                        } else {
+                            const int r = m < 6 ? m - 2 : m - 8;
+                            split_s(2 * j4 + (m < 6 ? 0 : 1), r);
+                            if (r == 3) leave_s(2 * j4 + (m < 6 ? 0 : 1), xn);
                         }
+#pragma unroll
+                        for (int i = upto(m - 1); i < upto(m); ++i) issue(i);
                     }
-                    with_k(2 * j4, xn, fk[0]);
-                    with_k(2 * j4 + 1, xn, fk[1]);
-                    if (j4 + 1 < NJ) {
-                        load_k(kn, 2 * j4 + 2, fk[0]);
-                        load_k(kn, 2 * j4 + 3, fk[1]);
-                    }
+                    if (j4 + 1 < NJ) load_k(kn, 2 * j4 + 2, fk[0]);
                 }
+#pragma unroll
+                for (int i = 0; i < 2 * TERMS; ++i) times_k(2 * NJ - 1, i, false, fk[1]);
                 hand(xn);
                 if (a.save && part == 0) {
                     float m = 0.0f;
@@ -464,33 +475,40 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 m = fmaxf(m, fmaxf(fmaxf(fabsf(y.x), fabsf(y.y)), fmaxf(fabsf(y.z), fabsf(y.w))));
             }
         }
-        m = warp_max(m);
+        m = warp_most(m);
         if (lane == 0) x.v_max = m;
     };
     auto product = [&](int c, int st, float (&sq)[4][4]) {  // S Q^T, in S's scale
         const uint32_t qs = ring + st * SB + KT * 64 * DK;
         const X& x = xb[c & 1];
+        uint4 f[2][PREC ? 2 : 1];
+        uint32_t b[2][2][KT][4];
+        auto load = [&](int kk) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) sq[j][y] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < DK / 16; ++kk) {
-            const uint4 h4 = x.s[0][kk][lane], l4 = x.s[PREC ? 1 : 0][kk][lane];
-            const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
-            uint32_t b[2][KT][4];
+            for (int t = 0; t < (PREC ? 2 : 1); ++t) f[kk & 1][t] = x.s[t][kk][lane];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < KT; ++t) ldsm4(b[h][t], addr_nk<DK>(qs + t * 64 * DK, 2 * h, kk, lane));
+                for (int t = 0; t < KT; ++t) ldsm4(b[kk & 1][h][t], addr_nk<DK>(qs + t * 64 * DK, 2 * h, kk, lane));
+        };
+        load(0);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, b[h][0][0], b[h][0][1]); mma(sq[2 * h + 1], hi, b[h][0][2], b[h][0][3]); }
+        for (int kk = 0; kk < DK / 16; ++kk) {
+            if (kk + 1 < DK / 16) load(kk + 1);
+            const uint4 h4 = f[kk & 1][0], l4 = f[kk & 1][PREC ? 1 : 0];
+            const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
+            const uint32_t (&q)[2][KT][4] = b[kk & 1];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (kk == 0) { mma0(sq[2 * h], hi, q[h][0][0], q[h][0][1]); mma0(sq[2 * h + 1], hi, q[h][0][2], q[h][0][3]); }
+                else { mma(sq[2 * h], hi, q[h][0][0], q[h][0][1]); mma(sq[2 * h + 1], hi, q[h][0][2], q[h][0][3]); }
+            }
             if (PREC)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], lo, b[h][0][0], b[h][0][1]); mma(sq[2 * h + 1], lo, b[h][0][2], b[h][0][3]); }
+                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], lo, q[h][0][0], q[h][0][1]); mma(sq[2 * h + 1], lo, q[h][0][2], q[h][0][3]); }
             if (KT == 2)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, b[h][KT - 1][0], b[h][KT - 1][1]); mma(sq[2 * h + 1], hi, b[h][KT - 1][2], b[h][KT - 1][3]); }
+                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, q[h][KT - 1][0], q[h][KT - 1][1]); mma(sq[2 * h + 1], hi, q[h][KT - 1][2], q[h][KT - 1][3]); }
         }
     };
     auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + u A^T
