@@ -68,3 +68,31 @@ def backward(q, k, v, eta, log_gamma, S, scale, d_o, dS_final):
         X = np.exp(log_gamma[:, :, t])[..., None, None] * X
     group = lambda x: x.reshape(B, Hk, r, L, dk).sum(2)  # noqa: E731
     return {"dq": group(dq), "dk": group(d_k), "dv": d_v, "d_eta": d_eta, "d_log_gamma": d_lg, "dS": X}
+
+
+def gradient_magnitudes(q, k, v, eta, log_gamma, S, scale, d_o, dS_final):
+    """Sums of the magnitudes of the terms of dq and dk: every token's part in the state and in its adjoint with its magnitude."""
+    de = np.abs(backward(q, k, v, eta, log_gamma, S, scale, d_o, dS_final)["dv"])
+    q, k, v, eta, log_gamma, d_o = (np.asarray(x, np.float64) for x in (q, k, v, eta, log_gamma, d_o))
+    B, H, L, dv = v.shape
+    Hk, dk = q.shape[1], q.shape[-1]
+    r = H // Hk
+    q, k, scale, d_o = np.abs(np.repeat(q, r, 1)), np.repeat(k, r, 1), abs(scale), np.abs(d_o)
+    S = np.zeros((B, H, dv, dk)) if S is None else np.array(S, np.float64)
+    A, decayed, after, us = np.abs(S), [], [], []
+    for t in range(L):
+        g = np.exp(log_gamma[:, :, t])[..., None, None]
+        S, A = g * S, g * A
+        u = eta[:, :, t, None] * (v[:, :, t] - np.einsum("bhij,bhj->bhi", S, k[:, :, t]))
+        step = u[..., :, None] * k[:, :, t, None, :]
+        decayed.append(A)
+        S, A = S + step, A + np.abs(step)
+        after.append(A), us.append(np.abs(u))
+    X = np.zeros((B, H, dv, dk)) if dS_final is None else np.abs(np.array(dS_final, np.float64))
+    dq, d_k = np.zeros_like(q), np.zeros_like(k)
+    for t in range(L - 1, -1, -1):
+        dq[:, :, t] = scale * np.einsum("bhi,bhij->bhj", d_o[:, :, t], after[t])
+        X = X + scale * d_o[:, :, t, :, None] * q[:, :, t, None, :]
+        d_k[:, :, t] = np.einsum("bhi,bhij->bhj", us[t], X) + np.einsum("bhi,bhij->bhj", de[:, :, t], decayed[t])
+        X = np.exp(log_gamma[:, :, t])[..., None, None] * (X + de[:, :, t, :, None] * np.abs(k[:, :, t, None, :]))
+    return {"dq": dq.reshape(B, Hk, r, L, dk).sum(2), "dk": d_k.reshape(B, Hk, r, L, dk).sum(2)}

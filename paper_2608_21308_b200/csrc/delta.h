@@ -14,15 +14,16 @@ namespace e2ttt {
 constexpr int kDeltaChunk = 32;  // tokens per chunk: a warp's row for its gates, two k-steps of the MMAs
 constexpr int kDeltaBlock = 64;  // tokens per saved state (two chunks)
 constexpr int kDeltaMaxD = 128;  // a slice of 16 state rows of 128 columns is a quarter of a warp's registers
-// A chunk's record: T and A (two fp16 terms each, 2 KB a term), eight rows of 32 floats; with saved states also the T of the reverse
+constexpr int kDeltaSuper = 8;   // blocks between two inner products <X, S> of the reverse pass
+// A chunk's record: T and A eta (two fp16 terms each, 2 KB a term), eight rows of 32 floats; with saved states also A and the T of the reverse
 // pass, (I + eta strict(D (K K^T)))^-1.  The forward fetches the first 9 KB, the reverse pass the last 9.
 constexpr int kDeltaRecBytes = 9216;
-constexpr int kDeltaRecSkip = 4096;
-// rows of a record's scalars
+constexpr int kDeltaRecSkip = 8192;
+// rows of a record's scalars: b of K and Q (with the scales of their tiles), eta, D_end, eta D_end
 enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecW = 4, kRecHead = 7 };
-// the last row: decay of the whole chunk; what undoes the scales of T, A, K, Q and the reverse pass' T; then bounds of the chunk's operands:
-// max b |k| (2-norm), row sums of T, max |eta|, max |eta| D_end (in units of the K tile), sum |eta| D_end |k|
-enum { kHeadEnd = 0, kHeadT = 1, kHeadA = 2, kHeadK = 3, kHeadQ = 4, kHeadR = 5, kHeadKn = 6, kHeadTsum = 7, kHeadUmax = 8, kHeadWmax = 9, kHeadWsum = 10 };
+// the last row: decay of the whole chunk; what undoes the scales of T, A eta, K, Q, the reverse pass' T and A; then bounds of the chunk's
+// operands: max b |k| (2-norm), row sums of T, max |eta| D_end (in units of the K tile), sum |eta| D_end |k|
+enum { kHeadEnd = 0, kHeadT = 1, kHeadA = 2, kHeadK = 3, kHeadQ = 4, kHeadR = 5, kHeadKn = 6, kHeadTsum = 7, kHeadAr = 8, kHeadWmax = 9, kHeadWsum = 10 };
 
 struct DeltaShape {
     int B, H, Hk, L, dk, dv;
@@ -39,9 +40,24 @@ struct DeltaLayout {
     int64_t N, Nk;     // sequences (value heads), query / key heads
     size_t qk_bytes;   // query and key tiles of a chunk
     size_t rec_bytes;  // record of a chunk
-    // offsets in bytes
-    size_t qk, rec, e, o, S, dp, X, part_eta, part_gate, hx, max_u, max_s, max_dp, max_x, max_do, total;
+    int nsup;          // sums of the decays' gradients: kDeltaSuper blocks each
+    size_t state_bytes;  // a slice of a state: one term of its fragments
+    // offsets in bytes.  Saved for the reverse pass, all in fragment order (a lane's 16 bytes of one product's A operand together), per slice:
+    // the state before every block (first term; the second one where it is needed in 32 bits), e of every chunk, the outputs in fp32; by its
+    // chain: X behind every block, dP of every chunk; what undoes the fragments' scales
+    size_t qk, rec, S, S_lo, s_inv, e, e_inv, o, X, x_inv, dp, dp_inv, max_do, part_eta, part_gate, hx, total;
 };
+
+// where the second term of the state in `slot` (before block `slot`; behind the last one) is kept: -1 nowhere.  With fp32 I/O all are
+inline
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+int delta_lo_slot(int slot, int nblk, int f32) {
+    if (f32) return slot;
+    if (slot == 0 || (slot % kDeltaSuper && slot != nblk)) return -1;
+    return (slot + kDeltaSuper - 1) / kDeltaSuper - 1;
+}
 
 inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
     DeltaLayout l{};
@@ -54,27 +70,29 @@ inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
     l.N = (int64_t)s.B * s.H;
     l.Nk = (int64_t)s.B * s.Hk;
     l.qk_bytes = (size_t)2 * l.terms * 64 * l.DK;
-    l.rec_bytes = kDeltaRecBytes + (save ? 4096 : 0);
+    l.rec_bytes = kDeltaRecBytes + (save ? 8192 : 0);
+    l.nsup = (l.nblk + kDeltaSuper - 1) / kDeltaSuper;
+    l.state_bytes = (size_t)32 * l.DK;
     size_t at = 256;  // the status block
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     l.qk = take((size_t)l.Nk * l.nch * l.qk_bytes);
     l.rec = take((size_t)l.N * l.nch * l.rec_bytes);
     if (save) {
-        const size_t tok = (size_t)l.N * l.nch * l.dvp * kDeltaChunk * 4, part = (size_t)l.N * l.nch * l.slices * kDeltaChunk * 4;
-        l.e = take(tok);
-        l.o = take(tok);
-        l.S = take((size_t)l.N * (l.nblk + 1) * l.dvp * l.DK * 4);
-        l.dp = take(tok);
-        l.X = take((size_t)l.N * l.nblk * l.dvp * l.DK * 4);
-        l.part_eta = take(part);
-        l.part_gate = take(part);
-        l.hx = take((size_t)l.N * l.nblk * l.slices * 4);
-        // largest magnitudes per slice: the scales of dq's and dk's operands
-        l.max_u = take((size_t)l.N * l.nch * l.slices * 4);
-        l.max_dp = take((size_t)l.N * l.nch * l.slices * 4);
-        l.max_do = take((size_t)l.N * l.nch * l.slices * 4);
-        l.max_s = take((size_t)l.N * (l.nblk + 1) * l.slices * 4);
-        l.max_x = take((size_t)l.N * l.nblk * l.slices * 4);
+        const size_t chunks = (size_t)l.N * l.nch * l.slices, blocks = (size_t)l.N * (l.nblk + 1) * l.slices;
+        l.S = take(blocks * l.state_bytes);
+        l.S_lo = take((s.f32 ? blocks : (size_t)l.N * l.nsup * l.slices) * l.state_bytes);
+        l.s_inv = take(blocks * 4);
+        l.e = take(chunks * 2048);
+        l.e_inv = take(chunks * 4);
+        l.o = take(chunks * 2048);
+        l.X = take(blocks * l.state_bytes * l.terms);
+        l.x_inv = take(blocks * 4);
+        l.dp = take(chunks * 1024 * l.terms);
+        l.dp_inv = take(chunks * 4);
+        l.max_do = take(chunks * 4);
+        l.part_eta = take(chunks * kDeltaChunk * 4);
+        l.part_gate = take(chunks * kDeltaChunk * 4);
+        l.hx = take((size_t)l.N * l.nsup * l.slices * 4);
     }
     l.total = at;
     return l;

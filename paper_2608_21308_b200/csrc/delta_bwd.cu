@@ -3,7 +3,7 @@
 //   dQ = (D dO^T U) K + scale b S_0^T dO,   dK = (D dO^T U)^T Q - (W + W^T) K - b S_0^T dP + D_end X^T U,  W = strict(D dP^T U)   (delta_qk_kernel)
 //   d eta = Z . e,   d log_gamma_t = sum over s >= t (o_s . do_s - v_s . dv_s) + <X, S> at the end of the sum         (delta_gate_kernel)
 // The last line is the scaling of everything before token t by g_t: outputs and state are linear in the start state and the values, so
-// no difference of nearly equal sums over keys is formed.  Sums run over blocks of 64 tokens, <X, S> is taken at each block's end.
+// no difference of nearly equal sums over keys is formed.  Sums run over 512 tokens, <X, S> is taken behind each of them.
 // The chain walks the chunks from the last to the first as the forward does, a warp per 16 value rows; dQ and dK contract over the
 // value rows of all warps and are left to a kernel that takes the blocks side by side.
 #include "delta_common.cuh"
@@ -90,44 +90,38 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
                 x[j][i] = (t < s.L && (i < 2 ? ok0 : ok1)) ? to_f32(p[(size_t)t * s.dv + (i < 2 ? r0 : r1)]) : 0.0f;
             }
     };
-    auto load_ws = [&](size_t off, int c, float (&x)[4][4]) {
-        const float* p = reinterpret_cast<const float*>(a.ws + off) + ((size_t)n * nch + c) * a.l.dvp * kDeltaChunk;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float2 y = *reinterpret_cast<const float2*>(p + r0 * kDeltaChunk + j * 8 + 2 * c4);
-            const float2 z = *reinterpret_cast<const float2*>(p + r1 * kDeltaChunk + j * 8 + 2 * c4);
-            x[j][0] = y.x; x[j][1] = y.y; x[j][2] = z.x; x[j][3] = z.y;
-        }
-    };
     float don[4][4];
     load_tok(d_o, nch - 1, don);
     for (int i = 0; i < nch; ++i) {
         const int c = nch - 1 - i, st = i % kStages;
         sm100::mbar_wait(&full[st], (i / kStages) & 1, wait, 902);
         if (active) {
-            const uint32_t ks = sm100::smem_u32(smem) + st * stage_bytes<DK, KT>(), qs = ks + KT * 64 * DK, as = qs + KT * 64 * DK, ts = as + 4096 + 1024;
-            const float* sc = reinterpret_cast<const float*>(smem + st * stage_bytes<DK, KT>() + 2 * KT * 64 * DK + 4096);
-            if ((c & 1) || c == nch - 1) {  // the end of a block: its X, and <X, S>
-                const int blk = c >> 1;
-                float* dst = reinterpret_cast<float*>(a.ws + a.l.X) + ((size_t)n * a.l.nblk + blk) * a.l.dvp * DK;
-                const float* src = reinterpret_cast<const float*>(a.ws + a.l.S) + ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.dvp * DK;
-                float m = 0.0f, h = 0.0f;
+            const uint32_t ks = sm100::smem_u32(smem) + st * stage_bytes<DK, KT>(), qs = ks + KT * 64 * DK, as = qs + KT * 64 * DK + 1024, ts = as + 4096;
+            const float* sc = reinterpret_cast<const float*>(smem + st * stage_bytes<DK, KT>() + 2 * KT * 64 * DK);
+            const int blk = c >> 1;
+            const bool block_end = (c & 1) || c == nch - 1;
+            if (block_end && ((blk + 1) % kDeltaSuper == 0 || blk + 1 == a.l.nblk)) {  // <X, S> behind a superblock
+                const int lo = delta_lo_slot(blk + 1, a.l.nblk, s.f32);
+                const size_t at = ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.slices + slice;
+                const size_t at_lo = s.f32 ? at : ((size_t)n * a.l.nsup + lo) * a.l.slices + slice;
+                const uint4* hi4 = reinterpret_cast<const uint4*>(a.ws + a.l.S + at * a.l.state_bytes);
+                const uint4* lo4 = reinterpret_cast<const uint4*>(a.ws + a.l.S_lo + at_lo * a.l.state_bytes);
+                float h = 0.0f;
 #pragma unroll
-                for (int j = 0; j < DK / 8; ++j) {
-                    const size_t at0 = (size_t)r0 * DK + j * 8 + 2 * c4, at1 = (size_t)r1 * DK + j * 8 + 2 * c4;
-                    *reinterpret_cast<float2*>(dst + at0) = make_float2(X[j][0], X[j][1]);
-                    *reinterpret_cast<float2*>(dst + at1) = make_float2(X[j][2], X[j][3]);
-                    const float2 y = *reinterpret_cast<const float2*>(src + at0), z = *reinterpret_cast<const float2*>(src + at1);
-                    h = fmaf(X[j][0], y.x, h); h = fmaf(X[j][1], y.y, h); h = fmaf(X[j][2], z.x, h); h = fmaf(X[j][3], z.y, h);
-                    m = fmaxf(m, fmaxf(fmaxf(fabsf(X[j][0]), fabsf(X[j][1])), fmaxf(fabsf(X[j][2]), fabsf(X[j][3]))));
-                }
-                m = warp_max(m);
+                for (int kk = 0; kk < DK / 16; ++kk) {
+                    const uint4 u = hi4[kk * 32 + lane], v2 = lo4[kk * 32 + lane];
+                    const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v2.x, v2.y, v2.z, v2.w};
 #pragma unroll
-                for (int x = 16; x > 0; x >>= 1) h += __shfl_xor_sync(kAll, h, x);
-                if (lane == 0) {
-                    reinterpret_cast<float*>(a.ws + a.l.hx)[((size_t)n * a.l.nblk + blk) * a.l.slices + slice] = h;
-                    reinterpret_cast<float*>(a.ws + a.l.max_x)[((size_t)n * a.l.nblk + blk) * a.l.slices + slice] = m;
+                    for (int r = 0; r < 4; ++r) {
+                        float s0, s1;
+                        join_terms(uw[r], vw[r], s0, s1);
+                        const float (&x)[4] = X[2 * kk + (r >> 1)];
+                        h = fmaf(x[2 * (r & 1)], s0, h);
+                        h = fmaf(x[2 * (r & 1) + 1], s1, h);
+                    }
                 }
+                h = warp_sum(h) * reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at];
+                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.hx)[((size_t)n * a.l.nsup + blk / kDeltaSuper) * a.l.slices + slice] = h;
             }
             float xk[4][4], in[4][4], z[4][4], d_out[4][4];
             float m0 = 0.0f, m1 = 0.0f;
@@ -142,13 +136,19 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
                 m0 = fmaxf(m0, fmaxf(fabsf(X[j][0]), fabsf(X[j][1])));
                 m1 = fmaxf(m1, fmaxf(fabsf(X[j][2]), fabsf(X[j][3])));
             }
-            float s0, s1, i0, i1;
-            pow2_scale(quad_max(m0), s0, i0);
-            pow2_scale(quad_max(m1), s1, i1);
+            float s0, i0;
+            pow2_scale(warp_max(fmaxf(m0, m1)), s0, i0);
+            const size_t at_x = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + slice;
+            uint4* x_out = reinterpret_cast<uint4*>(a.ws + a.l.X + at_x * a.l.state_bytes * KT);
+            if (block_end && lane == 0) reinterpret_cast<float*>(a.ws + a.l.x_inv)[at_x] = i0;
 #pragma unroll
             for (int kk = 0; kk < DK / 16; ++kk) {
                 uint32_t hi[4], lo[4];
-                to_a(X[2 * kk], X[2 * kk + 1], s0, s1, hi, lo);
+                to_a(X[2 * kk], X[2 * kk + 1], s0, s0, hi, lo);
+                if (block_end) {
+                    x_out[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    if (KT == 2) x_out[(DK / 16 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t b[4];
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
             pow2_scale(m0, f0, h0);
             pow2_scale(m1, f1, h1);
             lower_t(in, as, d_out, f0, f1);
-            const float ainv = sc[kRecHead * 32 + 2], rinv = sc[kRecHead * 32 + 5], bend = sc[kRecHead * 32 + 0];
+            const float ainv = sc[kRecHead * 32 + kHeadAr], rinv = sc[kRecHead * 32 + kHeadR], bend = sc[kRecHead * 32 + kHeadEnd];
             // dU, then Z
             h0 *= ainv; h1 *= ainv;
             m0 = m1 = 0.0f;
@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
             for (int j = 0; j < 4; ++j) {
                 const float2 de = *reinterpret_cast<const float2*>(sc + kRecDend * 32 + j * 8 + 2 * c4);
                 in[j][0] = fmaf(xk[j][0] * i0, de.x, in[j][0] * h0); in[j][1] = fmaf(xk[j][1] * i0, de.y, in[j][1] * h0);
-                in[j][2] = fmaf(xk[j][2] * i1, de.x, in[j][2] * h1); in[j][3] = fmaf(xk[j][3] * i1, de.y, in[j][3] * h1);
+                in[j][2] = fmaf(xk[j][2] * i0, de.x, in[j][2] * h1); in[j][3] = fmaf(xk[j][3] * i0, de.y, in[j][3] * h1);
                 m0 = fmaxf(m0, fmaxf(fabsf(in[j][0]), fabsf(in[j][1])));
                 m1 = fmaxf(m1, fmaxf(fabsf(in[j][2]), fabsf(in[j][3])));
             }
@@ -214,30 +214,38 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
             for (int j = 0; j < 4; ++j) { z[j][0] *= h0; z[j][1] *= h0; z[j][2] *= h1; z[j][3] *= h1; }
             // sums over the slice's value rows for d eta and d log_gamma
             {
-                float e[4][4], part[8], ov[4][4], vv[4][4];
-                load_ws(a.l.e, c, e);
+                float part[8], vv[4][4];
+                const uint4* ef = reinterpret_cast<const uint4*>(a.ws + a.l.e) + at_max * 128;
+                const float e_inv = reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at_max];
+                const float4* ov = reinterpret_cast<const float4*>(a.ws + a.l.o) + at_max * 128;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    part[2 * j] = fmaf(z[j][0], e[j][0], z[j][2] * e[j][2]);
-                    part[2 * j + 1] = fmaf(z[j][1], e[j][1], z[j][3] * e[j][3]);
+                for (int kk = 0; kk < 2; ++kk) {
+                    const uint4 u = ef[kk * 32 + lane], w = ef[(2 + kk) * 32 + lane];
+                    const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
+                    float e[4][2];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) join_terms(uw[r], ww[r], e[r][0], e[r][1]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const float (&zz)[4] = z[2 * kk + j];
+                            part[4 * kk + 2 * j + y] = fmaf(zz[y], e[2 * j][y], zz[2 + y] * e[2 * j + 1][y]) * e_inv;
+                        }
                 }
                 // lane 4 g + c4 holds the sum of value g of its c4 group: token (g >> 1) * 8 + 2 c4 + (g & 1)
                 const size_t at = at_max * kDeltaChunk + (g >> 1) * 8 + 2 * c4 + (g & 1);
                 reinterpret_cast<float*>(a.ws + a.l.part_eta)[at] = sum_rows(part, lane);
-                load_ws(a.l.o, c, ov);
                 load_tok(v, c, vv);
-                float w0 = 0.0f, w1 = 0.0f;
-                float* dst = reinterpret_cast<float*>(a.ws + a.l.dp) + ((size_t)n * nch + c) * a.l.dvp * kDeltaChunk;
+                float w = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 et = *reinterpret_cast<const float2*>(sc + kRecEta * 32 + j * 8 + 2 * c4);
+                    const float4 o4 = ov[j * 32 + lane];
                     z[j][0] *= et.x; z[j][1] *= et.y; z[j][2] *= et.x; z[j][3] *= et.y;  // dP = dV
-                    part[2 * j] = ov[j][0] * d_out[j][0] - vv[j][0] * z[j][0] + (ov[j][2] * d_out[j][2] - vv[j][2] * z[j][2]);
-                    part[2 * j + 1] = ov[j][1] * d_out[j][1] - vv[j][1] * z[j][1] + (ov[j][3] * d_out[j][3] - vv[j][3] * z[j][3]);
-                    w0 = fmaxf(w0, fmaxf(fabsf(z[j][0]), fabsf(z[j][1])));
-                    w1 = fmaxf(w1, fmaxf(fabsf(z[j][2]), fabsf(z[j][3])));
-                    *reinterpret_cast<float2*>(dst + r0 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(z[j][0], z[j][1]);
-                    *reinterpret_cast<float2*>(dst + r1 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(z[j][2], z[j][3]);
+                    part[2 * j] = o4.x * d_out[j][0] - vv[j][0] * z[j][0] + (o4.z * d_out[j][2] - vv[j][2] * z[j][2]);
+                    part[2 * j + 1] = o4.y * d_out[j][1] - vv[j][1] * z[j][1] + (o4.w * d_out[j][3] - vv[j][3] * z[j][3]);
+                    w = fmaxf(w, fmaxf(fmaxf(fabsf(z[j][0]), fabsf(z[j][1])), fmaxf(fabsf(z[j][2]), fabsf(z[j][3]))));
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (x & 1);
@@ -245,8 +253,17 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
                     }
                 }
                 reinterpret_cast<float*>(a.ws + a.l.part_gate)[at] = sum_rows(part, lane);
-                const float m = warp_max(fmaxf(w0, w1));
-                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_dp)[at_max] = m;
+                float sp, ip;
+                pow2_scale(warp_max(w), sp, ip);
+                uint4* dst = reinterpret_cast<uint4*>(a.ws + a.l.dp) + at_max * 64 * KT;
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    uint32_t hi[4], lo[4];
+                    to_a(z[2 * kk], z[2 * kk + 1], sp, sp, hi, lo);
+                    dst[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    if (KT == 2) dst[(2 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.dp_inv)[at_max] = ip;
             }
             // X = b_end X + (dO b scale) Q - (dP b) K
             m0 = m1 = 0.0f;
@@ -309,83 +326,92 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
         }
 }
 
-// d eta and d log_gamma from the slices' sums: one warp per block of 64 tokens
-__global__ void __launch_bounds__(128) delta_gate_kernel(const DeltaBwdArgs ba) {
+// d eta and d log_gamma from the slices' sums: a CTA per superblock of 512 tokens, a warp per chunk, lane = token.  Sums of many terms in 64 bits:
+// what is left of them counts
+__global__ void __launch_bounds__(kDeltaSuper * 64) delta_gate_kernel(const DeltaBwdArgs ba) {
+    __shared__ double total[2 * kDeltaSuper];
     const DeltaArgs& a = ba.f;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (item >= a.l.N * a.l.nblk) return;
-    const int64_t n = item / a.l.nblk;
-    const int blk = (int)(item % a.l.nblk);
-    float carry = 0.0f;
-    const float* hx = reinterpret_cast<const float*>(a.ws + a.l.hx) + (size_t)item * a.l.slices;
-    for (int i = 0; i < a.l.slices; ++i) carry += hx[i];
-    for (int k = 1; k >= 0; --k) {
-        const int c = 2 * blk + k;
-        if (c >= a.l.nch) continue;
+    const int64_t item = blockIdx.x, n = item / a.l.nsup;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = (int)(item % a.l.nsup) * kDeltaSuper * 2, c = first + warp;
+    const int last = min(a.l.nch, first + kDeltaSuper * 2) - 1;
+    float de = 0.0f, dg = 0.0f;
+    if (c <= last) {
         const size_t at = ((size_t)n * a.l.nch + c) * a.l.slices * kDeltaChunk + lane;
-        float de = 0.0f, dg = 0.0f;
+#pragma unroll 4
         for (int i = 0; i < a.l.slices; ++i) {
             de += reinterpret_cast<const float*>(a.ws + a.l.part_eta)[at + i * kDeltaChunk];
             dg += reinterpret_cast<const float*>(a.ws + a.l.part_gate)[at + i * kDeltaChunk];
         }
+    }
+    double sum = dg;
 #pragma unroll
-        for (int i = 1; i < 32; i <<= 1) {  // suffix sums
-            const float y = __shfl_down_sync(kAll, dg, i);
-            if (lane + i < 32) dg += y;
-        }
-        dg += carry;
-        carry = __shfl_sync(kAll, dg, 0);
-        const int t = c * kDeltaChunk + lane;
-        if (t < a.s.L) {
-            const size_t out = (size_t)n * a.s.L + t;
-            ba.d_eta[out] = de;
-            ba.d_log_gamma[out] = a.log_gamma[out] < -104.0f ? 0.0f : dg;  // a decay that is 0 in 32 bits has none
-        }
+    for (int i = 1; i < 32; i <<= 1) {  // suffix sums
+        const double y = __shfl_down_sync(kAll, sum, i);
+        if (lane + i < 32) sum += y;
+    }
+    if (lane == 0) total[warp] = sum;
+    __syncthreads();
+    if (c > last) return;
+    const float* hx = reinterpret_cast<const float*>(a.ws + a.l.hx) + (size_t)item * a.l.slices;
+    for (int i = 0; i < a.l.slices; ++i) sum += hx[i];
+    for (int i = warp + 1; i <= last - first; ++i) sum += total[i];
+    const int t = c * kDeltaChunk + lane;
+    if (t < a.s.L) {
+        const size_t out = (size_t)n * a.s.L + t;
+        ba.d_eta[out] = de;
+        ba.d_log_gamma[out] = a.log_gamma[out] < -104.0f ? 0.0f : (float)sum;  // a decay that is 0 in 32 bits has none
     }
 }
 
 // ---- dQ and dK ----------------------------------------------------------------------------------------------------
-// A CTA takes 64 tokens of one query / key head and adds up the value heads of its group.  Eight warps: 16 tokens times half of the key
-// columns each.  Value rows come through shared memory 32 at a time, twice: with S_0 (dQ's and dK's first part, both token-by-token
-// matrices), then with X.
-template <int DK, int KT> constexpr int qk_tiles() { return 2 * KT * 128 * DK; }
-template <int DK, int KT> constexpr int qk_smem() { return qk_tiles<DK, KT>() + 2 * 64 * DK + KT * 4096 + 2 * 2 * 4096 + 2 * 2 * 8192 + 5 * 256 + 128; }
+// A CTA takes 64 tokens of one query / key head and adds up the value heads of its group.  Sixteen warps: 16 tokens times a quarter of the key
+// columns each.  The value rows come through shared memory ROWS at a time, with S_0 (dQ's and dK's first part, both token-by-token matrices) and
+// again with X; what the chains left in fragment order goes into tiles of rows here, at one scale for all slices.  With bf16 I/O one term of every
+// operand serves: dQ and dK are off by 2^-11 of their terms before they are rounded to 2^-8.
+template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? 128 : 32; }
+template <int DK, int KT> constexpr int qk_smem() {
+    return 2 * KT * 128 * DK + KT * qk_rows<DK, KT>() * (2 * DK + 3 * 128) + 2 * KT * 8192 + 64 * 8 + 3 * 256 + 256;
+}
 
 template <typename IO, int DK, int KT>
-__global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, const bool vec) {
+__global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
+    constexpr int ROWS = qk_rows<DK, KT>(), SL = ROWS / 16;  // value rows and slices at a time
+    constexpr int TS = ROWS * DK * 2, TT = ROWS * 128;       // bytes of a term: state tile [ROWS][DK]; token tiles [ROWS][64], [64][ROWS]
     const DeltaArgs& a = ba.f;
     const DeltaShape& s = a.s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c4 = lane & 3;
-    const int tw = warp >> 1, hw = warp & 1;
+    const int tw = warp >> 2, hw = warp & 3;
     const int64_t nk = blockIdx.x / a.l.nblk;
     const int blk = (int)(blockIdx.x % a.l.nblk), t0 = blk * kDeltaBlock, r = s.H / s.Hk;
-    // shared memory: K, Q [64][DK]; S or X slab [32][DK] in two terms; dO [64][32]; U, dP [32][64] in two terms; the two 64 x 64 matrices
-    char* kq = smem;
-    char* st_s = kq + qk_tiles<DK, KT>();
-    char* st_o = st_s + 2 * 64 * DK;
-    char* st_u = st_o + KT * 4096;
-    char* st_p = st_u + 2 * 4096;
-    char* mat = st_p + 2 * 4096;                              // sigma (two terms of 8 KB), then kappa
-    double* run = reinterpret_cast<double*>(mat + 4 * 8192);  // 64
-    float* bt = reinterpret_cast<float*>(run + 64);           // 64
-    float* dend = bt + 64;                                    // 64
-    float* eta = dend + 64;                                   // 64
-    float* red = eta + 64;                                    // 32
+    char* kq = smem;                    // K, then Q: [64][DK]
+    char* st_s = kq + 2 * KT * 128 * DK;  // S or X
+    char* st_o = st_s + KT * TS;        // dO [64][ROWS]
+    char* st_u = st_o + KT * TT;        // e [ROWS][64]
+    char* st_p = st_u + KT * TT;        // dP [ROWS][64]
+    char* mat = st_p + KT * TT;         // sigma, then kappa + kappa^T
+    double* run = reinterpret_cast<double*>(mat + 2 * KT * 8192);  // 64
+    float* bt = reinterpret_cast<float*>(run + 64);                // 64
+    float* dend = bt + 64;                                         // 64, times eta
+    float* eta = dend + 64;                                        // 64
+    float* red = eta + 64;                                         // 32, and the scales
     const uint32_t ks = sm100::smem_u32(kq), qs = ks + KT * 128 * DK, ss = sm100::smem_u32(st_s), os = sm100::smem_u32(st_o),
                    us = sm100::smem_u32(st_u), ps = sm100::smem_u32(st_p), ms = sm100::smem_u32(mat);
     const int nchunks = min(2, a.l.nch - 2 * blk);
+    auto times_half = [](uint32_t x, __half2 y) {
+        const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&x), y);
+        return *reinterpret_cast<const uint32_t*>(&z);
+    };
     // the two chunks' tiles at one scale
     float ik, iq;
     {
         const int64_t n0 = (nk / s.Hk) * s.H + (nk % s.Hk) * r;
         const float* h0 = reinterpret_cast<const float*>(a.ws + a.l.rec + ((size_t)n0 * a.l.nch + 2 * blk) * a.l.rec_bytes + 8192) + kRecHead * 32;
         const float* h1 = nchunks > 1 ? h0 + a.l.rec_bytes / 4 : h0;
-        ik = fmaxf(h0[3], h1[3]); iq = fmaxf(h0[4], h1[4]);
-        const float f[2][2] = {{h0[3] / ik, h0[4] / iq}, {h1[3] / ik, h1[4] / iq}};  // powers of two, at most 1
+        ik = fmaxf(h0[kHeadK], h1[kHeadK]); iq = fmaxf(h0[kHeadQ], h1[kHeadQ]);
+        const float f[2][2] = {{h0[kHeadK] / ik, h0[kHeadQ] / iq}, {h1[kHeadK] / ik, h1[kHeadQ] / iq}};  // powers of two, at most 1
         constexpr int P = DK / 8;
-        for (int i = tid; i < 2 * KT * 64 * P; i += 256) {
+        for (int i = tid; i < 2 * KT * 64 * P; i += 512) {
             const int piece = i % P, row = (i / P) % 64, term = (i / P / 64) % KT, which = i / P / 64 / KT;
             uint4 x = make_uint4(0, 0, 0, 0);
             if (row / 32 < nchunks) {
@@ -394,14 +420,13 @@ __global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, co
                 const float y = f[row / 32][which];
                 if (y != 1.0f) {
                     const __half2 m = __float2half2_rn(y);
-                    __half2* w = reinterpret_cast<__half2*>(&x);
-                    for (int j = 0; j < 4; ++j) w[j] = __hmul2(w[j], m);
+                    x = make_uint4(times_half(x.x, m), times_half(x.y, m), times_half(x.z, m), times_half(x.w, m));
                 }
             }
             *reinterpret_cast<uint4*>(kq + which * KT * 128 * DK + term * 128 * DK + (row * P + piece) * 16) = x;
         }
     }
-    constexpr int NT = DK / 16;  // n-tiles of a warp's half of the columns
+    constexpr int NT = DK / 32;  // n-tiles of a warp's quarter of the columns
     float tq[NT][4], tk[NT][4];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -435,141 +460,132 @@ __global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, co
                 const double x = before + sum[k];
                 run[2 * lane + k] = x;
                 bt[2 * lane + k] = expf((float)x);
-                dend[2 * lane + k] = expf((float)(end - x));
+                dend[2 * lane + k] = expf((float)(end - x)) * et[k];
                 eta[2 * lane + k] = et[k];
             }
+        } else if (tid < 64) {  // the largest of the slices' scales; lane = slice and chunk
+            const int sl = lane & 7, ch = lane >> 3;
+            const bool ok = sl < a.l.slices;
+            const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl;
+            const bool tok = ok && ch < nchunks;
+            const float iu = warp_most(tok ? reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at] : 0.0f);
+            const float ip = warp_most(tok ? reinterpret_cast<const float*>(a.ws + a.l.dp_inv)[at] : 0.0f);
+            const float mo = warp_max(tok ? reinterpret_cast<const float*>(a.ws + a.l.max_do)[at] : 0.0f);
+            const size_t at_s = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl;
+            const float iS = warp_most(ok ? reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at_s] : 0.0f);
+            const float iX = warp_most(ok ? reinterpret_cast<const float*>(a.ws + a.l.x_inv)[at_s] : 0.0f);
+            float so, io;
+            pow2_scale(mo, so, io);
+            if (lane == 0) { red[32] = iu; red[33] = ip; red[34] = so; red[35] = io; red[36] = iS; red[37] = iX; }
         }
-        // scales of the operands, from the slices' maxima
-        float mu = 0.0f, mp = 0.0f, mo = 0.0f, msx = 0.0f, mx = 0.0f;
-        for (int i = 0; i < a.l.slices; ++i) {
-            for (int k = 0; k < nchunks; ++k) {
-                const size_t at = ((size_t)n * a.l.nch + 2 * blk + k) * a.l.slices + i;
-                mu = fmaxf(mu, reinterpret_cast<const float*>(a.ws + a.l.max_u)[at]);
-                mp = fmaxf(mp, reinterpret_cast<const float*>(a.ws + a.l.max_dp)[at]);
-                mo = fmaxf(mo, reinterpret_cast<const float*>(a.ws + a.l.max_do)[at]);
-            }
-            msx = fmaxf(msx, reinterpret_cast<const float*>(a.ws + a.l.max_s)[((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + i]);
-            mx = fmaxf(mx, reinterpret_cast<const float*>(a.ws + a.l.max_x)[((size_t)n * a.l.nblk + blk) * a.l.slices + i]);
-        }
-        float su, sp, so, sS, sX, iu, ip, io, iS, iX;
-        pow2_scale(mu, su, iu); pow2_scale(mp, sp, ip); pow2_scale(mo, so, io); pow2_scale(msx, sS, iS); pow2_scale(mx, sX, iX);
         __syncthreads();
-        auto stage_tok = [&](size_t off, float f, bool times_eta, char* dst, int d0) {  // [32 value rows][64 tokens] in two terms
-            const int row = tid >> 3, piece = tid & 7;
-            float x[8];
+        const float iu = red[32], ip = red[33], so = red[34], io = red[35], iS = red[36], iX = red[37];
+        // fragments [16 value rows][16 columns] of a slice to rows of a tile
+        auto put = [&](char* tile, int cols, int row, int piece, const uint4& x, float ratio) {
+            const __half2 m = __float2half2_rn(ratio);
+            const uint32_t w[4] = {times_half(x.x, m), times_half(x.y, m), times_half(x.z, m), times_half(x.w, m)};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.0f;
-            if (d0 + row < a.l.dvp && piece / 4 < nchunks) {
-                const float* p = reinterpret_cast<const float*>(a.ws + off) +
-                                 (((size_t)n * a.l.nch + 2 * blk + piece / 4) * a.l.dvp + d0 + row) * kDeltaChunk + (piece & 3) * 8;
-                const float4 y = reinterpret_cast<const float4*>(p)[0], z = reinterpret_cast<const float4*>(p)[1];
-                x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w; x[4] = z.x; x[5] = z.y; x[6] = z.z; x[7] = z.w;
-                if (times_eta)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] *= eta[piece * 8 + j];
+            for (int i = 0; i < 4; ++i) {
+                const int rr = row + (i & 1) * 8, pp = piece + (i >> 1);
+                const uint32_t at = cols == 64 ? tile_at<64>(rr, pp) : tile_at<DK>(rr, pp);
+                *reinterpret_cast<uint32_t*>(tile + at + c4 * 4) = w[i];
             }
-            uint4 hi, lo;
-            split(x[0] * f, x[1] * f, hi.x, lo.x); split(x[2] * f, x[3] * f, hi.y, lo.y);
-            split(x[4] * f, x[5] * f, hi.z, lo.z); split(x[6] * f, x[7] * f, hi.w, lo.w);
-            const uint32_t at = tile_at<64>(row, piece);
-            *reinterpret_cast<uint4*>(dst + at) = hi;
-            *reinterpret_cast<uint4*>(dst + 4096 + at) = lo;
         };
-        auto stage_state = [&](const float* src, float f, int d0) {  // [32 value rows][DK] in two terms
+        auto stage_tok = [&](size_t off, size_t off_inv, int terms, float most, char* dst, int sl0) {
 #pragma unroll
-            for (int i = 0; i < 32 * DK / 8 / 256; ++i) {
-                const int p = tid + i * 256, row = p / (DK / 8), piece = p % (DK / 8);
-                float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f), z = y;
-                if (d0 + row < a.l.dvp) {
-                    const float4* q = reinterpret_cast<const float4*>(src + (size_t)(d0 + row) * DK + piece * 8);
-                    y = q[0]; z = q[1];
+            for (int q = 0; q < SL * 4 * KT * 32 / 512; ++q) {  // (term, slice, chunk, kk), a warp each
+                const int i = warp + 16 * q, kk = i & 1, ch = (i >> 1) & 1, sl = (i >> 2) % SL, term = (i >> 2) / SL;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                float ratio = 1.0f;
+                if (sl0 + sl < a.l.slices && ch < nchunks) {
+                    const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl0 + sl;
+                    x = reinterpret_cast<const uint4*>(a.ws + off)[(at * terms + term) * 64 + kk * 32 + lane];
+                    ratio = reinterpret_cast<const float*>(a.ws + off_inv)[at] / most;
+                }
+                put(dst + term * TT, 64, sl * 16 + g, (ch * 2 + kk) * 2, x, ratio);
+            }
+        };
+        auto stage_state = [&](size_t off, size_t off_lo, int terms, size_t off_inv, float most, int sl0) {
+#pragma unroll
+            for (int q = 0; q < SL * KT * (DK / 16) / 16; ++q) {
+                const int i = warp + 16 * q, kk = i % (DK / 16), sl = i / (DK / 16) % SL, term = i / (DK / 16) / SL;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                float ratio = 1.0f;
+                if (sl0 + sl < a.l.slices) {
+                    const size_t at = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl0 + sl;
+                    const char* src = off_lo ? a.ws + (term ? off_lo : off) + at * a.l.state_bytes : a.ws + off + (at * terms + term) * a.l.state_bytes;
+                    x = reinterpret_cast<const uint4*>(src)[kk * 32 + lane];
+                    ratio = reinterpret_cast<const float*>(a.ws + off_inv)[at] / most;
+                }
+                put(st_s + term * TS, DK, sl * 16 + g, kk * 2, x, ratio);
+            }
+        };
+        auto stage_do = [&](int d0) {  // [64 tokens][ROWS value rows]
+#pragma unroll
+            for (int q = 0; q < 64 * ROWS / 8 / 512 + (64 * ROWS / 8 < 512); ++q) {
+                const int i = tid + 512 * q, row = i / (ROWS / 8), piece = i % (ROWS / 8), t = t0 + row, d = d0 + piece * 8;
+                if (row >= 64) continue;
+                float x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+                if (t < s.L && d < s.dv) {
+                    const IO* p = reinterpret_cast<const IO*>(ba.d_o) + ((size_t)n * s.L + t) * s.dv + d;
+                    if (vec && sizeof(IO) == 2) {
+                        const uint4 raw = *reinterpret_cast<const uint4*>(p);
+                        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (d + j < s.dv) x[j] = to_f32(p[j]);
+                    }
                 }
                 uint4 hi, lo;
-                split(y.x * f, y.y * f, hi.x, lo.x); split(y.z * f, y.w * f, hi.y, lo.y);
-                split(z.x * f, z.y * f, hi.z, lo.z); split(z.z * f, z.w * f, hi.w, lo.w);
-                const uint32_t at = tile_at<DK>(row, piece);
-                *reinterpret_cast<uint4*>(st_s + at) = hi;
-                *reinterpret_cast<uint4*>(st_s + 64 * DK + at) = lo;
+                split(x[0] * so, x[1] * so, hi.x, lo.x); split(x[2] * so, x[3] * so, hi.y, lo.y);
+                split(x[4] * so, x[5] * so, hi.z, lo.z); split(x[6] * so, x[7] * so, hi.w, lo.w);
+                const uint32_t at = tile_at<ROWS>(row, piece);
+                *reinterpret_cast<uint4*>(st_o + at) = hi;
+                if (KT == 2) *reinterpret_cast<uint4*>(st_o + TT + at) = lo;
             }
         };
-        auto stage_do = [&](int d0) {  // [64 tokens][32 value rows]
-            const int row = tid >> 2, piece = tid & 3, t = t0 + row, d = d0 + piece * 8;
-            float x[8];
+        // two terms each, without the product of the second ones
+        auto product = [&](float (&c)[4], const uint32_t (&x)[KT][4], const uint32_t (&b)[KT][4], int y) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.0f;
-            if (t < s.L && d < s.dv) {
-                const IO* p = reinterpret_cast<const IO*>(ba.d_o) + ((size_t)n * s.L + t) * s.dv + d;
-                if (vec && sizeof(IO) == 2) {
-                    const uint4 raw = *reinterpret_cast<const uint4*>(p);
-                    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (d + j < s.dv) x[j] = to_f32(p[j]);
-                }
-            }
-            uint4 hi, lo;
-            split(x[0] * so, x[1] * so, hi.x, lo.x); split(x[2] * so, x[3] * so, hi.y, lo.y);
-            split(x[4] * so, x[5] * so, hi.z, lo.z); split(x[6] * so, x[7] * so, hi.w, lo.w);
-            const uint32_t at = tile_at<32>(row, piece);
-            *reinterpret_cast<uint4*>(st_o + at) = hi;
-            if (KT == 2) *reinterpret_cast<uint4*>(st_o + 4096 + at) = lo;
+                for (int u = 0; u + t < KT; ++u) mma(c, x[t], b[u][2 * y], b[u][2 * y + 1]);
         };
-        float sg[4][4], kp[4][4], aq[NT][4], ak[NT][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) sg[j][x] = kp[j][x] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) aq[j][x] = ak[j][x] = 0.0f;
-        const float* S0 = reinterpret_cast<const float*>(a.ws + a.l.S) + ((size_t)n * (a.l.nblk + 1) + blk) * a.l.dvp * DK;
-        const float* X1 = reinterpret_cast<const float*>(a.ws + a.l.X) + ((size_t)n * a.l.nblk + blk) * a.l.dvp * DK;
-        for (int d0 = 0; d0 < a.l.dvp; d0 += 32) {
-            stage_do(d0);
-            stage_tok(a.l.e, su, true, st_u, d0);
-            stage_tok(a.l.dp, sp, false, st_p, d0);
-            stage_state(S0, sS, d0);
+        float sg[2][4] = {}, kp[2][4] = {}, aq[NT][4] = {}, ak[NT][4] = {};
+        for (int sl0 = 0; sl0 < a.l.slices; sl0 += SL) {
+            stage_state(a.l.S, KT == 2 ? a.l.S_lo : 0, 1, a.l.s_inv, iS, sl0);
+            stage_tok(a.l.e, a.l.e_inv, 2, iu, st_u, sl0);
+            stage_tok(a.l.dp, a.l.dp_inv, KT, ip, st_p, sl0);
+            stage_do(sl0 * 16);
             __syncthreads();
+            const int steps = min(SL, a.l.slices - sl0);
+#pragma unroll 2
+            for (int kk = 0; kk < steps; ++kk) {
+                uint32_t ao[KT][4], ap[KT][4], b[KT][4];
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                uint32_t ao[2][4], ap[2][4];
-                ldsm4(ao[0], addr_mk<32>(os, tw * 16, kk, lane));
-                if (KT == 2) ldsm4(ao[1], addr_mk<32>(os + 4096, tw * 16, kk, lane));
-                ldsm4_t(ap[0], addr_km<64>(ps, tw * 16, kk, lane));
-                ldsm4_t(ap[1], addr_km<64>(ps + 4096, tw * 16, kk, lane));
+                for (int t = 0; t < KT; ++t) {
+                    ldsm4(ao[t], addr_mk<ROWS>(os + t * TT, tw * 16, kk, lane));
+                    ldsm4_t(ap[t], addr_km<64>(ps + t * TT, tw * 16, kk, lane));
+                }
+                if (hw <= tw) {  // not the tokens after these
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (hw * 32 + h * 16 > tw * 16) continue;  // tokens after these
-                    uint32_t bh[4], bl[4];
-                    ldsm4_t(bh, addr_kn<64>(us, hw * 4 + 2 * h, kk, lane));
-                    ldsm4_t(bl, addr_kn<64>(us + 4096, hw * 4 + 2 * h, kk, lane));
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        mma(sg[2 * h + y], ao[0], bh[2 * y], bh[2 * y + 1]);
-                        mma(sg[2 * h + y], ao[0], bl[2 * y], bl[2 * y + 1]);
-                        if (KT == 2) mma(sg[2 * h + y], ao[1], bh[2 * y], bh[2 * y + 1]);
-                        mma(kp[2 * h + y], ap[0], bh[2 * y], bh[2 * y + 1]);
-                        mma(kp[2 * h + y], ap[0], bl[2 * y], bl[2 * y + 1]);
-                        mma(kp[2 * h + y], ap[1], bh[2 * y], bh[2 * y + 1]);
-                    }
+                    for (int t = 0; t < KT; ++t) ldsm4_t(b[t], addr_kn<64>(us + t * TT, hw * 2, kk, lane));
+                    product(sg[0], ao, b, 0); product(sg[1], ao, b, 1);
+                    product(kp[0], ap, b, 0); product(kp[1], ap, b, 1);
                 }
 #pragma unroll
                 for (int h = 0; h < NT / 2; ++h) {
-                    uint32_t bh[4], bl[4];
-                    ldsm4_t(bh, addr_kn<DK>(ss, hw * NT + 2 * h, kk, lane));
-                    ldsm4_t(bl, addr_kn<DK>(ss + 64 * DK, hw * NT + 2 * h, kk, lane));
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) ldsm4_t(b[t], addr_kn<DK>(ss + t * TS, hw * NT + 2 * h, kk, lane));
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        mma(aq[2 * h + y], ao[0], bh[2 * y], bh[2 * y + 1]);
-                        mma(aq[2 * h + y], ao[0], bl[2 * y], bl[2 * y + 1]);
-                        if (KT == 2) mma(aq[2 * h + y], ao[1], bh[2 * y], bh[2 * y + 1]);
-                        mma(ak[2 * h + y], ap[0], bh[2 * y], bh[2 * y + 1]);
-                        mma(ak[2 * h + y], ap[0], bl[2 * y], bl[2 * y + 1]);
-                        mma(ak[2 * h + y], ap[1], bh[2 * y], bh[2 * y + 1]);
+                        product(aq[2 * h + y], ao, b, y);
+                        product(ak[2 * h + y], ap, b, y);
                     }
                 }
             }
@@ -587,76 +603,74 @@ __global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, co
                 for (int x = 0; x < 4; ++x) aq[j][x] = ak[j][x] = 0.0f;
             }
         }
-        // D on both token-by-token matrices, their largest magnitudes
+        // D and eta on both token-by-token matrices, their largest magnitudes
         float m0 = 0.0f, m1 = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int t = x < 2 ? row0 : row1, u = hw * 32 + j * 8 + 2 * c4 + (x & 1);
-                const float D = u <= t ? expf((float)(run[t] - run[u])) : 0.0f;
+                const int t = x < 2 ? row0 : row1, u = hw * 16 + j * 8 + 2 * c4 + (x & 1);
+                const float D = u <= t ? expf((float)(run[t] - run[u])) * eta[u] : 0.0f;
                 sg[j][x] = u <= t ? sg[j][x] * (io * iu) * (D * s.scale) : 0.0f;
                 kp[j][x] = u < t ? -kp[j][x] * (ip * iu) * D : 0.0f;
                 m0 = fmaxf(m0, fabsf(sg[j][x]));
                 m1 = fmaxf(m1, fabsf(kp[j][x]));
             }
         m0 = warp_max(m0); m1 = warp_max(m1);
-        if (lane == 0) { red[warp] = m0; red[8 + warp] = m1; }
+        if (lane == 0) { red[warp] = m0; red[16 + warp] = m1; }
+        if (a.l.slices <= SL) stage_state(a.l.X, 0, KT, a.l.x_inv, iX, 0);  // everything has been read
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { m0 = fmaxf(m0, red[i]); m1 = fmaxf(m1, red[8 + i]); }
+        for (int i = 0; i < 16; ++i) { m0 = fmaxf(m0, red[i]); m1 = fmaxf(m1, red[16 + i]); }
         float fs, gs, fk, gk;
         pow2_scale(m0, fs, gs);
         pow2_scale(m1, fk, gk);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int t = x ? row1 : row0, u = hw * 32 + j * 8 + 2 * c4;
-                uint32_t hi, lo;
-                split(sg[j][2 * x] * fs, sg[j][2 * x + 1] * fs, hi, lo);
+                const int t = x ? row1 : row0, u = hw * 16 + j * 8 + 2 * c4;
+                uint32_t w[2];
+                split(sg[j][2 * x] * fs, sg[j][2 * x + 1] * fs, w[0], w[1]);
                 const uint32_t at = tile_at<64>(t, u >> 3) + (u & 7) * 2;
-                *reinterpret_cast<uint32_t*>(mat + at) = hi;
-                *reinterpret_cast<uint32_t*>(mat + 8192 + at) = lo;
-                split(kp[j][2 * x] * fk, kp[j][2 * x + 1] * fk, hi, lo);
+                char* kap = mat + KT * 8192;
+#pragma unroll
+                for (int term = 0; term < KT; ++term) *reinterpret_cast<uint32_t*>(mat + term * 8192 + at) = w[term];
+                split(kp[j][2 * x] * fk, kp[j][2 * x + 1] * fk, w[0], w[1]);
                 // kappa + kappa^T: the strictly lower half, its mirror image and a zero diagonal
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    if (u + y <= t) {
-                        *reinterpret_cast<uint16_t*>(mat + 16384 + at + 2 * y) = (uint16_t)(hi >> (16 * y));
-                        *reinterpret_cast<uint16_t*>(mat + 24576 + at + 2 * y) = (uint16_t)(lo >> (16 * y));
-                    }
-                    if (u + y < t) {
-                        const uint32_t mt = tile_at<64>(u + y, t >> 3) + (t & 7) * 2;
-                        *reinterpret_cast<uint16_t*>(mat + 16384 + mt) = (uint16_t)(hi >> (16 * y));
-                        *reinterpret_cast<uint16_t*>(mat + 24576 + mt) = (uint16_t)(lo >> (16 * y));
+                    const uint32_t mt = tile_at<64>(u + y, t >> 3) + (t & 7) * 2;
+#pragma unroll
+                    for (int term = 0; term < KT; ++term) {
+                        const uint16_t z = (uint16_t)(w[term] >> (16 * y));
+                        if (u + y <= t) *reinterpret_cast<uint16_t*>(kap + term * 8192 + at + 2 * y) = z;
+                        if (u + y < t) *reinterpret_cast<uint16_t*>(kap + term * 8192 + mt) = z;
                     }
                 }
             }
-        // D_end X^T U
-        for (int d0 = 0; d0 < a.l.dvp; d0 += 32) {
-            stage_tok(a.l.e, su, true, st_u, d0);
-            stage_state(X1, sX, d0);
+        // eta D_end X^T e
+        for (int sl0 = 0; sl0 < a.l.slices; sl0 += SL) {
+            if (a.l.slices > SL) {
+                stage_tok(a.l.e, a.l.e_inv, 2, iu, st_u, sl0);
+                stage_state(a.l.X, 0, KT, a.l.x_inv, iX, sl0);
+            }
             __syncthreads();
+            const int steps = min(SL, a.l.slices - sl0);
+#pragma unroll 2
+            for (int kk = 0; kk < steps; ++kk) {
+                uint32_t au[KT][4], b[KT][4];
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                uint32_t au[2][4];
-                ldsm4_t(au[0], addr_km<64>(us, tw * 16, kk, lane));
-                ldsm4_t(au[1], addr_km<64>(us + 4096, tw * 16, kk, lane));
+                for (int t = 0; t < KT; ++t) ldsm4_t(au[t], addr_km<64>(us + t * TT, tw * 16, kk, lane));
 #pragma unroll
                 for (int h = 0; h < NT / 2; ++h) {
-                    uint32_t bh[4], bl[4];
-                    ldsm4_t(bh, addr_kn<DK>(ss, hw * NT + 2 * h, kk, lane));
-                    ldsm4_t(bl, addr_kn<DK>(ss + 64 * DK, hw * NT + 2 * h, kk, lane));
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        mma(ak[2 * h + y], au[0], bh[2 * y], bh[2 * y + 1]);
-                        mma(ak[2 * h + y], au[0], bl[2 * y], bl[2 * y + 1]);
-                        mma(ak[2 * h + y], au[1], bh[2 * y], bh[2 * y + 1]);
-                    }
+                    for (int t = 0; t < KT; ++t) ldsm4_t(b[t], addr_kn<DK>(ss + t * TS, hw * NT + 2 * h, kk, lane));
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) product(ak[2 * h + y], au, b, y);
                 }
             }
-            __syncthreads();
+            if (a.l.slices > SL) __syncthreads();
         }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
@@ -668,25 +682,20 @@ __global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, co
         }
         // sigma K, sigma^T Q, (kappa + kappa^T) K: three sums with scales of their own
         auto times = [&](float (&acc)[NT][4], uint32_t rows, uint32_t tile, bool transposed, int k0, int k1) {
-#pragma unroll 1
+#pragma unroll 2
             for (int kk = k0; kk < k1; ++kk) {
-                uint32_t ah[4], al[4];
-                if (transposed) { ldsm4_t(ah, addr_km<64>(rows, tw * 16, kk, lane)); ldsm4_t(al, addr_km<64>(rows + 8192, tw * 16, kk, lane)); }
-                else { ldsm4(ah, addr_mk<64>(rows, tw * 16, kk, lane)); ldsm4(al, addr_mk<64>(rows + 8192, tw * 16, kk, lane)); }
+                uint32_t x[KT][4], b[KT][4];
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    if (transposed) ldsm4_t(x[t], addr_km<64>(rows + t * 8192, tw * 16, kk, lane));
+                    else ldsm4(x[t], addr_mk<64>(rows + t * 8192, tw * 16, kk, lane));
+                }
 #pragma unroll
                 for (int h = 0; h < NT / 2; ++h) {
-                    uint32_t b[4];
-                    ldsm4_t(b, addr_kn<DK>(tile, hw * NT + 2 * h, kk, lane));
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        mma(acc[2 * h + y], ah, b[2 * y], b[2 * y + 1]);
-                        mma(acc[2 * h + y], al, b[2 * y], b[2 * y + 1]);
-                    }
-                    if (KT == 2) {
-                        ldsm4_t(b, addr_kn<DK>(tile + 128 * DK, hw * NT + 2 * h, kk, lane));
+                    for (int t = 0; t < KT; ++t) ldsm4_t(b[t], addr_kn<DK>(tile + t * 128 * DK, hw * NT + 2 * h, kk, lane));
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) mma(acc[2 * h + y], ah, b[2 * y], b[2 * y + 1]);
-                    }
+                    for (int y = 0; y < 2; ++y) product(acc[2 * h + y], x, b, y);
                 }
             }
         };
@@ -700,7 +709,7 @@ __global__ void __launch_bounds__(256) delta_qk_kernel(const DeltaBwdArgs ba, co
                 tk[j][x] = fmaf(ak[j][x], gs * iq, tk[j][x]);
                 ak[j][x] = 0.0f;
             }
-        times(ak, ms + 16384, ks, false, 0, 4);
+        times(ak, ms + KT * 8192, ks, false, 0, 4);
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -740,11 +749,11 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess) return (int)e;
         const bool vec = a.s.dv % 8 == 0 && reinterpret_cast<uintptr_t>(b.d_o) % 16 == 0;
-        kernel<<<(unsigned)(a.l.Nk * a.l.nblk), 256, bytes, st>>>(b, vec);
+        kernel<<<(unsigned)(a.l.Nk * a.l.nblk), 512, bytes, st>>>(b, vec);
         e = cudaGetLastError();
         if (e != cudaSuccess) return (int)e;
     }
-    delta_gate_kernel<<<(unsigned)((a.l.N * a.l.nblk + 3) / 4), 128, 0, st>>>(b);
+    delta_gate_kernel<<<(unsigned)(a.l.N * a.l.nsup), kDeltaSuper * 64, 0, st>>>(b);
     return (int)cudaGetLastError();
 }
 

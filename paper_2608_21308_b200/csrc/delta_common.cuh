@@ -90,6 +90,12 @@ __device__ __forceinline__ void split(float x, float y, uint32_t& hi, uint32_t& 
     fma2(r, q, f.x, f.y, -1.0f, -1.0f, x, y);
     lo = pack_half(r, q);
 }
+// the two values of a word of first and of second terms
+__device__ __forceinline__ void join_terms(uint32_t hi, uint32_t lo, float& x, float& y) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi)), e = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+    x = f.x + e.x;
+    y = f.y + e.y;
+}
 // an operand that carries its scale already
 __device__ __forceinline__ void split_a(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
     split(x[0], x[1], hi[0], lo[0]);
@@ -169,6 +175,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// bulk stores from shared memory, by one lane; their reads, and the stores themselves, waited for by the same lane (others have none under way)
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // wait for a phase that has usually come: the bounded wait only if it has not
 __device__ __forceinline__ void wait_phase(uint64_t* bar, uint32_t parity, const sm100::WaitCtx& w, int where) {
     if (!sm100::mbar_try_wait<false>(bar, parity)) sm100::mbar_wait(bar, parity, w, where);

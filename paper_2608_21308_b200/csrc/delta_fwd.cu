@@ -1,10 +1,10 @@
 // Gated delta rule, the walk over the chunks.  A slice of 16 value rows of a sequence's state, [16, dk], stays in registers from the first
 // token to the last (64 a lane of one warp at dk = 128, or shared out by columns over KS warps), and the slices of a sequence never meet but
 // for the tiles that they share.
-// Per chunk of 32 tokens, rows = value rows:  P = V - b S K^T,  e = P T^T,  O = b S Q^T + u A^T,  S = b_end S + (D_end u) K.
+// Per chunk of 32 tokens, rows = value rows:  P = V - b S K^T,  e = P T^T,  O = b S Q^T + e (A eta)^T,  S = b_end S + (D_end u) K.
 // Each product's result is the next one's A operand in place.  The chunk's tiles (queries, keys, T, A, scalars; written by
 // delta_prep.cu) arrive by bulk copies, several chunks ahead.
-// The chain P, e, S is what a chunk waits for; one more warp per slice does what hangs off it, a chunk behind: O from the state's and u's
+// The chain P, e, S is what a chunk waits for; one more warp per slice does what hangs off it, a chunk behind: O from the state's and e's
 // fragments (which the chain leaves in shared memory), and the values' loads and the outputs' stores.  One barrier a chunk.
 // A chain is bound by the instructions of a chunk one after the other (an MMA every 8 cycles, 146 of them, and splitting the operands into
 // terms), so scales are one per slice, folded into the scalars that the values are multiplied with anyway, and come from bounds that are known
@@ -18,7 +18,7 @@ using namespace delta;
 template <int DK, int KT> constexpr int stage_bytes() { return 2 * KT * 64 * DK + kDeltaRecBytes; }
 template <int KT, bool PREC> constexpr int stages() { return KT == 1 && !PREC ? 4 : 3; }
 
-// what the warps of a slice hand over, a buffer per parity of the chunk: fragments of S and u (a second term each with PREC), what undoes their
+// what the warps of a slice hand over, a buffer per parity of the chunk: fragments of S and e (a second term each with PREC), what undoes their
 // scales, the values of the next chunk (fp32 in fragment order, or bf16 tokens x rows) and a bound on them, the outputs on their way out
 template <int DK, int KT, int KS, bool PREC> struct alignas(128) Exchange {
     uint4 s[PREC ? 2 : 1][DK / 16][32];
@@ -77,16 +77,6 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 const bool ok = a.S_init && col < s.dk && (x < 2 ? ok0 : ok1);
                 S[j][x] = ok ? a.S_init[((size_t)n * s.dv + (x < 2 ? r0 : r1)) * s.dk + col] : 0.0f;
             }
-        auto save_state = [&](int slot) {
-            float* dst = reinterpret_cast<float*>(a.ws + a.l.S) + ((size_t)n * (a.l.nblk + 1) + slot) * a.l.dvp * DK + col0;
-#pragma unroll
-            for (int j = 0; j < DC / 8; ++j) {
-                *reinterpret_cast<float2*>(dst + (size_t)r0 * DK + j * 8 + 2 * c4) = make_float2(S[j][0] * s_inv, S[j][1] * s_inv);
-                *reinterpret_cast<float2*>(dst + (size_t)r1 * DK + j * 8 + 2 * c4) = make_float2(S[j][2] * s_inv, S[j][3] * s_inv);
-            }
-            // the slice's norm bounds its values
-            if (lane == 0 && part == 0) reinterpret_cast<float*>(a.ws + a.l.max_s)[((size_t)n * (a.l.nblk + 1) + slot) * a.l.slices + slice] = norm;
-        };
         // With |S| the slice's 2-norm:  |P| <= max |v| + max b |k| |S|,  |e| <= sum |T| |P|,  |S_next| <= b_end |S| + sum (|eta| D_end |k|) |e|
         // for every row.  |S| itself is summed beside the products, scaled, so that squares stay in range.
         float sk[4][4], squares0 = 0.0f, squares1 = 0.0f;  // S K^T of the next chunk
@@ -176,6 +166,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 for (int i = 0; i < 2 * TERMS; ++i) times_k(kk, i, kk == 0, b);
             }
             hand(xb[0]);
+            if (a.save) sm100::fence_proxy_async_smem();
         }
         __syncthreads();  // the values of chunk 0
         int st = 0, st_next = 1, phase_next = 0;
@@ -185,12 +176,11 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             const float* head = sc + kRecHead * 32;
             X& x = xb[c & 1];
             X& xn = xb[(c + 1) & 1];
-            float e[4][4], uf = 0.0f, w_old = 0.0f, w_new = 0.0f, qe = 0.0f;
+            float e[4][4], uf = 0.0f, w_old = 0.0f, w_new = 0.0f;
             uint32_t wh[2][4], wl[2][4];
             const bool come = c + 1 == nch || probe_phase(&full[st_next], phase_next);
             if (active) {
                 take(x);
-                if (a.save && (c & 1) == 0) save_state(c >> 1);
                 // T's blocks (the one above the diagonal is zero)
                 uint32_t th[3][4], tl[3][4];  // (rows 0-15, k 0), (rows 16-31, k 0), (rows 16-31, k 1)
                 ldsm4(th[0], addr_nk<32>(ts, 0, 0, lane)); ldsm4(th[1], addr_nk<32>(ts, 2, 0, lane)); ldsm4(th[2], addr_nk<32>(ts, 2, 1, lane));
@@ -244,11 +234,11 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                     mma(e[2], l1, th[2][0], th[2][1]); mma(e[3], l1, th[2][2], th[2][3]);
                     mma(e[2], h1, tl[2][0], tl[2][1]); mma(e[3], h1, tl[2][2], tl[2][3]);
                 }
-                // e times qe is the error itself.  u = eta e goes to the outputs' warp, D_end u into the state, each with a scale of its own;
+                // e times qe is the error itself.  It goes to the outputs' warp, eta D_end e into the state, each with a scale of its own;
                 // the state moves to its next scale on the way
-                qe = q * head[kHeadT];
+                const float qe = q * head[kHeadT];
                 float pu, u_inv, fw, w_inv;
-                pow2_bound(eb * head[kHeadUmax], pu, u_inv);
+                pow2_bound(eb, pu, u_inv);
                 pow2_bound(eb * head[kHeadWmax], fw, w_inv);
                 uf = pu * qe;
                 const float wf = fw * qe, old_inv = s_inv;
@@ -301,33 +291,21 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 };
                 load_s(0);
                 squares0 = squares1 = 0.0f;
-                // u's fragments for the outputs, and what the reverse pass reads, shared out between the parts; beside the first piece's sum
+                // e's fragments for the outputs, shared out between the parts; beside the first piece's sum
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
                     for (int i = 0; i < 2 * TERMS; ++i) sum(y[0], kk * 2 * TERMS + i);
                     if (KS > 1 && part != kk) continue;
-                    float u[2][4];
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float2 et = *reinterpret_cast<const float2*>(sc + kRecEta * 32 + (2 * kk + j) * 8 + 2 * c4);
-                        float y0, y1;
-                        mul2(y0, y1, et.x, et.y, uf, uf);
-                        mul2(u[j][0], u[j][1], e[2 * kk + j][0], e[2 * kk + j][1], y0, y1);
-                        mul2(u[j][2], u[j][3], e[2 * kk + j][2], e[2 * kk + j][3], y0, y1);
+                    for (int j = 2 * kk; j < 2 * kk + 2; ++j) {
+                        mul2(e[j][0], e[j][1], e[j][0], e[j][1], uf, uf);
+                        mul2(e[j][2], e[j][3], e[j][2], e[j][3], uf, uf);
                     }
                     uint32_t hi[4], lo[4];
-                    split_a(u[0], u[1], hi, lo);
+                    split_a(e[2 * kk], e[2 * kk + 1], hi, lo);
                     x.u[0][kk][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     if (PREC) x.u[PREC ? 1 : 0][kk][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    if (a.save) {
-                        float* dst = reinterpret_cast<float*>(a.ws + a.l.e) + ((size_t)n * nch + c) * a.l.dvp * kDeltaChunk;
-#pragma unroll
-                        for (int j = 2 * kk; j < 2 * kk + 2; ++j) {
-                            *reinterpret_cast<float2*>(dst + r0 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(e[j][0] * qe, e[j][1] * qe);
-                            *reinterpret_cast<float2*>(dst + r1 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(e[j][2] * qe, e[j][3] * qe);
-                        }
-                    }
                 }
                 if (NJ > 1) load_s(1);
                 load_k(kn, 0, fk[0]);
@@ -371,23 +349,13 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 #pragma unroll
                 for (int i = 0; i < 2 * TERMS; ++i) times_k(2 * NJ - 1, i, false, fk[1]);
                 hand(xn);
-                if (a.save && part == 0) {
-                    float m = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fmaxf(fabsf(e[j][0]), fabsf(e[j][1])), fmaxf(fabsf(e[j][2]), fabsf(e[j][3]))));
-                    m = warp_max(m) * qe * head[kHeadUmax];  // bounds u
-                    if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_u)[((size_t)n * nch + c) * a.l.slices + slice] = m;
-                }
+                if (a.save) sm100::fence_proxy_async_smem();  // the outputs' warp has the fragments copied from there
             }
             st = st_next;
             if (++st_next == NS) { st_next = 0; phase_next ^= 1; }
             __syncthreads();
         }
         if (active) {
-            if (a.save) {
-                take(xb[nch & 1]);
-                save_state(a.l.nblk);
-            }
             if (a.S_final) {
 #pragma unroll
                 for (int j = 0; j < DC / 8; ++j)
@@ -511,7 +479,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, q[h][KT - 1][0], q[h][KT - 1][1]); mma(sq[2 * h + 1], hi, q[h][KT - 1][2], q[h][KT - 1][3]); }
         }
     };
-    auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + u A^T
+    auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + e (A eta)^T
         const uint32_t as = ring + st * SB + 2 * KT * 64 * DK + 4096;
         const float* sc = reinterpret_cast<const float*>(smem + st * SB + 2 * KT * 64 * DK + 8192);
         X& x = xb[c & 1];
@@ -545,12 +513,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             }
         }
         if (a.save) {
-            float* dst = reinterpret_cast<float*>(a.ws + a.l.o) + ((size_t)n * nch + c) * a.l.dvp * kDeltaChunk;
+            float4* dst = reinterpret_cast<float4*>(a.ws + a.l.o) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                *reinterpret_cast<float2*>(dst + r0 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(in[j][0], in[j][1]);
-                *reinterpret_cast<float2*>(dst + r1 * kDeltaChunk + j * 8 + 2 * c4) = make_float2(in[j][2], in[j][3]);
-            }
+            for (int j = 0; j < 4; ++j) dst[j * 32 + lane] = make_float4(in[j][0], in[j][1], in[j][2], in[j][3]);
         }
         if (!o) return;
         if (KT == 1) {  // through shared memory to lane = token
@@ -586,6 +551,24 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 }
         }
     };
+    // what the reverse pass reads of S and e: their fragments as they lie in shared memory
+    auto save_s = [&](int slot, const X& x) {
+        if (lane != 0) return;
+        const size_t at = ((size_t)n * (a.l.nblk + 1) + slot) * a.l.slices + slice;
+        bulk_store(a.ws + a.l.S + at * a.l.state_bytes, sm100::smem_u32(x.s[0]), (uint32_t)a.l.state_bytes);
+        const int lo = delta_lo_slot(slot, a.l.nblk, s.f32);
+        if (lo >= 0) {
+            const size_t to = s.f32 ? at : ((size_t)n * a.l.nsup + lo) * a.l.slices + slice;
+            bulk_store(a.ws + a.l.S_lo + to * a.l.state_bytes, sm100::smem_u32(x.s[PREC ? 1 : 0]), (uint32_t)a.l.state_bytes);
+        }
+        reinterpret_cast<float*>(a.ws + a.l.s_inv)[at] = x.s_inv;
+    };
+    auto save_e = [&](int c, const X& x) {
+        if (lane != 0) return;
+        const size_t at = ((size_t)n * nch + c) * a.l.slices + slice;
+        bulk_store(a.ws + a.l.e + at * 2048, sm100::smem_u32(x.u), 2048);
+        reinterpret_cast<float*>(a.ws + a.l.e_inv)[at] = x.u_inv;
+    };
     load_v(0);
     hand_v(0);
     __syncthreads();
@@ -593,6 +576,12 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     int st = 0, phase = 0;
     for (int i = 0; i <= nch; ++i) {
         if (i + 1 < nch) load_v(i + 1);  // the chain reads chunk i's
+        if (a.save && active) {
+            if (i > 0) save_e(i - 1, xb[(i - 1) & 1]);
+            if (i == nch) save_s(a.l.nblk, xb[i & 1]);
+            else if ((i & 1) == 0) save_s(i >> 1, xb[i & 1]);
+            bulk_store_commit();
+        }
         if (active && i > 0) finish(i - 1, st == 0 ? NS - 1 : st - 1, sq, s_inv);
         if (i < nch) {
             wait_phase(&full[st], phase, wait, 903);
@@ -601,12 +590,14 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 s_inv = xb[i & 1].s_inv;
             }
             if (i + 1 < nch) hand_v(i + 1);
+            if (a.save) bulk_store_read();  // the chain may write there again
             __syncthreads();  // chunk i is through the chain, chunk i - 1 through here
         }
         if (fetches && i > 0 && i - 1 + NS < nch) fetch(i - 1 + NS, st == 0 ? NS - 1 : st - 1);
         __syncwarp();
         if (++st == NS) { st = 0; phase ^= 1; }
     }
+    if (a.save) bulk_store_done();
 }
 
 template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const DeltaArgs& a, int per, cudaStream_t st) {

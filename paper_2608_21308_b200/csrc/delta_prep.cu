@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         sc[kRecDend * 32 + lane] = dend * ik;
         sc[kRecW * 32 + lane] = eta * dend * ik;
         // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
-        float amax = 0.0f, av[6][4];
+        float amax = 0.0f, emax = 0.0f, av[6][4];
 #pragma unroll
         for (int i = 0; i < 6; ++i) {
             const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
@@ -245,20 +245,28 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
                 Nm[t * 36 + u] = u < t ? D * kk[i][x] * (ik * ik) * eta_s[u] : 0.0f;
                 av[i][x] = u <= t ? D * qk[i][x] * (iq * ik * s.scale) : 0.0f;
                 amax = fmaxf(amax, fabsf(av[i][x]));
+                emax = fmaxf(emax, fabsf(av[i][x] * eta_s[u]));
             }
         }
-        float as, ai;
+        float as, ai, es, ei;
         pow2_scale(warp_max(amax), as, ai);
+        pow2_scale(warp_max(emax), es, ei);
 #pragma unroll
         for (int i = 0; i < 6; ++i) {  // the block above the diagonal is read by no product
             const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i : i - 2;
+            const float e0 = eta_s[n0 * 8 + 2 * c4] * es, e1 = eta_s[n0 * 8 + 2 * c4 + 1] * es;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint32_t hi, lo;
-                split(av[i][2 * x] * as, av[i][2 * x + 1] * as, hi, lo);
                 const uint32_t at = tile_at<32>(m0 + g + x * 8, n0) + c4 * 4;
+                split(av[i][2 * x] * e0, av[i][2 * x + 1] * e1, hi, lo);
                 *reinterpret_cast<uint32_t*>(rec + 4096 + at) = hi;
                 *reinterpret_cast<uint32_t*>(rec + 6144 + at) = lo;
+                if (a.save) {
+                    split(av[i][2 * x] * as, av[i][2 * x + 1] * as, hi, lo);
+                    *reinterpret_cast<uint32_t*>(rec + 9216 + at) = hi;
+                    *reinterpret_cast<uint32_t*>(rec + 11264 + at) = lo;
+                }
             }
         }
         __syncwarp();
@@ -277,21 +285,21 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
                 }
             }
             __syncwarp();
-            ri = invert(Nm, rec + kDeltaRecBytes, lane, rsum);
+            ri = invert(Nm, rec + 13312, lane, rsum);
         }
         const float kn = sqrtf(norm_s[lane]);
-        const float b_kn = warp_max(bt * kn), umax = warp_max(fabsf(eta)), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
+        const float b_kn = warp_max(bt * kn), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
         if (lane == 0) {
             float* head = sc + kRecHead * 32;
             head[kHeadEnd] = expf((float)end);
             head[kHeadT] = ti;
-            head[kHeadA] = ai;
+            head[kHeadA] = ei;
             head[kHeadK] = ik;
             head[kHeadQ] = iq;
             head[kHeadR] = ri;
             head[kHeadKn] = b_kn;
             head[kHeadTsum] = tsum;
-            head[kHeadUmax] = umax;
+            head[kHeadAr] = ai;
             head[kHeadWmax] = wmax;
             head[kHeadWsum] = wsum;
         }

@@ -7,6 +7,8 @@ per chunk: 4 (2 x 2^-22 + 30 x 2^-23) = 1.6e-5 of the sum of the magnitudes if a
 largest magnitude's row by more than sqrt(128): 2e-5 of the largest magnitude holds for the worst value.
 bf16 outputs of a forward without saved states come from products with one fp16 term (half a step: 2^-11) of the start state, of u and of A: an output
 is off by at most 2^-11 of the magnitudes of what the state puts into it and 2 x 2^-11 of what the chunk's tokens do: 2^-10 of the sum of magnitudes.
+The gradients of bf16 queries and keys come from products with one term as well: dq's of the state, or of e and then of their product's matrix (2 x 2^-11);
+dk's of dP, of e or the state or its adjoint, and of their products' matrices (3 x 2^-11 at most), of the sum of magnitudes.
 """
 import numpy as np
 import pytest
@@ -81,13 +83,19 @@ class Run:
 
 
 def check(got, ref, single=None):
-    """single: the inputs, where the outputs are of products with one term."""
-    terms = None if single is None or got["o"].dtype != torch.bfloat16 else O.magnitudes(**single)
+    """single: the inputs, where the outputs (with `d_o` among them: dq and dk) are of products with one term."""
+    terms = {}
+    if single is not None and next(iter(got.values())).dtype == torch.bfloat16:
+        if "d_o" in single:
+            m = O.gradient_magnitudes(**single)
+            terms = {"dq": 2.0 ** -10 * m["dq"], "dk": 3 * 2.0 ** -11 * m["dk"]}
+        else:
+            terms = {"o": 2.0 ** -10 * O.magnitudes(**single)}
     for n, t in got.items():
         y, r = t.double().cpu().numpy(), ref[n]
         half = torch.finfo(t.dtype).eps / 2
         assert np.isfinite(y).all(), n
-        over = np.abs(y - r) - half * np.abs(r) - TOL * np.abs(r).max() - (2.0 ** -10 * terms if terms is not None and n == "o" else 0.0)
+        over = np.abs(y - r) - half * np.abs(r) - TOL * np.abs(r).max() - terms.get(n, 0.0)
         assert over.max() <= 0, (n, over.max(), np.abs(r).max(), np.linalg.norm(y - r) / np.linalg.norm(r))
 
 
@@ -114,7 +122,7 @@ def test_backward(io, shape):
     r = Run(x, io, 0.25)
     check(r.fwd(1), {"o": o, "S": S})
     got = r.bwd(d)
-    check(got, O.backward(**x, scale=0.25, **d))
+    check(got, O.backward(**x, scale=0.25, **d), dict(x, scale=0.25, **d))
     again = r.bwd(d, saved=0)
     for n in got:
         assert torch.equal(got[n], again[n]), n
@@ -137,7 +145,7 @@ def test_edges_of_the_gates(io, start):
     o, S = O.forward(**x, scale=1.0)
     r = Run(x, io, 1.0)
     check(r.fwd(1), {"o": o, "S": S})
-    check(r.bwd(d), O.backward(**x, scale=1.0, **d))
+    check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
     if start:
         check(r.step(), {"o": o, "S": S})
 
@@ -150,7 +158,7 @@ def test_no_decay_over_many_chunks(io):
     o, S = O.forward(**x, scale=1.0)
     r = Run(x, io, 1.0)
     check(r.fwd(1), {"o": o, "S": S})
-    check(r.bwd(d), O.backward(**x, scale=1.0, **d))
+    check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
 
 
 @pytest.mark.parametrize("size", [1e-12, 1e-4, 1e4])
@@ -164,7 +172,7 @@ def test_magnitudes_far_from_one(size):
         o, S = O.forward(**x, scale=1.0)
         r = Run(x, io, 1.0)
         check(r.fwd(1), {"o": o, "S": S})
-        check(r.bwd(d), O.backward(**x, scale=1.0, **d))
+        check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
 
 
 def test_small_keys_of_one_chunk_beside_large_ones():
@@ -175,7 +183,7 @@ def test_small_keys_of_one_chunk_beside_large_ones():
     o, S = O.forward(**x, scale=1.0)
     r = Run(x, "f32", 1.0)
     check(r.fwd(1), {"o": o, "S": S})
-    check(r.bwd(d), O.backward(**x, scale=1.0, **d))
+    check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -245,7 +253,8 @@ def test_graph_replay_on_a_side_stream_with_new_inputs():
     graph.replay()
     torch.cuda.synchronize()
     o, S = O.forward(**y, scale=1.0)
-    check({"o": r.o, "S": r.S_out, **out}, {"o": o, "S": S, **O.backward(**y, scale=1.0, **d)})
+    check({"o": r.o, "S": r.S_out}, {"o": o, "S": S})
+    check(out, O.backward(**y, scale=1.0, **d), dict(y, scale=1.0, **d))
 
 
 def test_two_streams_with_workspaces_of_their_own():
