@@ -14,7 +14,7 @@ namespace e2ttt {
 constexpr int kDeltaChunk = 32;  // tokens per chunk: a warp's row for its gates, two k-steps of the MMAs
 constexpr int kDeltaBlock = 64;  // tokens per saved state (two chunks)
 constexpr int kDeltaMaxD = 128;  // a slice of 16 state rows of 128 columns is a quarter of a warp's registers
-constexpr int kDeltaSuper = 8;   // blocks between two inner products <X, S> of the reverse pass
+constexpr int kDeltaSuper = 2;   // blocks between two inner products <X, S> of the reverse pass
 // A chunk's record: T and A eta (two fp16 terms each, 2 KB a term), eight rows of 32 floats; with saved states also A and the T of the reverse
 // pass, (I + eta strict(D (K K^T)))^-1.  The forward fetches the first 9 KB, the reverse pass the last 9.
 constexpr int kDeltaRecBytes = 9216;

@@ -3,7 +3,7 @@
 //   dQ = (D dO^T U) K + scale b S_0^T dO,   dK = (D dO^T U)^T Q - (W + W^T) K - b S_0^T dP + D_end X^T U,  W = strict(D dP^T U)   (delta_qk_kernel)
 //   d eta = Z . e,   d log_gamma_t = sum over s >= t (o_s . do_s - v_s . dv_s) + <X, S> at the end of the sum         (delta_gate_kernel)
 // The last line is the scaling of everything before token t by g_t: outputs and state are linear in the start state and the values, so
-// no difference of nearly equal sums over keys is formed.  Sums run over 512 tokens, <X, S> is taken behind each of them.
+// no difference of nearly equal sums over keys is formed.  Sums run over 128 tokens, <X, S> is taken behind each of them.
 // The chain walks the chunks from the last to the first as the forward does, a warp per 16 value rows; dQ and dK contract over the
 // value rows of all warps and are left to a kernel that takes the blocks side by side.
 #include "delta_common.cuh"
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba,
         }
 }
 
-// d eta and d log_gamma from the slices' sums: a CTA per superblock of 512 tokens, a warp per chunk, lane = token.  Sums of many terms in 64 bits:
+// d eta and d log_gamma from the slices' sums: a CTA per superblock of 128 tokens, a warp per chunk, lane = token.  Sums of many terms in 64 bits:
 // what is left of them counts
 __global__ void __launch_bounds__(kDeltaSuper * 64) delta_gate_kernel(const DeltaBwdArgs ba) {
     __shared__ double total[2 * kDeltaSuper];

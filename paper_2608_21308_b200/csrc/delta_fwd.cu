@@ -450,6 +450,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         const uint32_t qs = ring + st * SB + KT * 64 * DK;
         const X& x = xb[c & 1];
         uint4 f[2][PREC ? 2 : 1];
+        float sl[4][4] = {};  // the second terms' products apart: an MMA truncates the sum that it adds to
         uint32_t b[2][2][KT][4];
         auto load = [&](int kk) {
 #pragma unroll
@@ -473,17 +474,22 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             }
             if (PREC)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], lo, q[h][0][0], q[h][0][1]); mma(sq[2 * h + 1], lo, q[h][0][2], q[h][0][3]); }
+                for (int h = 0; h < 2; ++h) { mma(sl[2 * h], lo, q[h][0][0], q[h][0][1]); mma(sl[2 * h + 1], lo, q[h][0][2], q[h][0][3]); }
             if (KT == 2)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) { mma(sq[2 * h], hi, q[h][KT - 1][0], q[h][KT - 1][1]); mma(sq[2 * h + 1], hi, q[h][KT - 1][2], q[h][KT - 1][3]); }
+                for (int h = 0; h < 2; ++h) { mma(sl[2 * h], hi, q[h][KT - 1][0], q[h][KT - 1][1]); mma(sl[2 * h + 1], hi, q[h][KT - 1][2], q[h][KT - 1][3]); }
         }
+        if (PREC)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) sq[j][y] += sl[j][y];
     };
     auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + e (A eta)^T
         const uint32_t as = ring + st * SB + 2 * KT * 64 * DK + 4096;
         const float* sc = reinterpret_cast<const float*>(smem + st * SB + 2 * KT * 64 * DK + 8192);
         X& x = xb[c & 1];
-        float in[4][4] = {};
+        float in[4][4] = {}, il[4][4] = {};
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             const uint4 h4 = x.u[0][kk][lane], l4 = x.u[PREC ? 1 : 0][kk][lane];
@@ -495,11 +501,16 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 mma(in[2 * h], hi, bh[0], bh[1]); mma(in[2 * h + 1], hi, bh[2], bh[3]);
                 if (PREC) {
                     ldsm4(bl, addr_nk<32>(as + 2048, 2 * h, kk, lane));
-                    mma(in[2 * h], lo, bh[0], bh[1]); mma(in[2 * h + 1], lo, bh[2], bh[3]);
-                    mma(in[2 * h], hi, bl[0], bl[1]); mma(in[2 * h + 1], hi, bl[2], bl[3]);
+                    mma(il[2 * h], lo, bh[0], bh[1]); mma(il[2 * h + 1], lo, bh[2], bh[3]);
+                    mma(il[2 * h], hi, bl[0], bl[1]); mma(il[2 * h + 1], hi, bl[2], bl[3]);
                 }
             }
         }
+        if (PREC)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) in[j][y] += il[j][y];
         const float q = x.u_inv * sc[kRecHead * 32 + kHeadA];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

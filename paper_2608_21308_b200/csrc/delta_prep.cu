@@ -133,48 +133,59 @@ template <int DK, int KT> __device__ __forceinline__ void gram(uint32_t rows, ui
     }
 }
 
-// (I + N)^-1 of a strictly lower N column by column, lane = column: x_t = [t == lane] - sum_{i < t} N_ti x_i; two terms to `out`
-__device__ __forceinline__ float invert(const float* Nm, char* out, int lane, float& rows) {
-    float x[32], most = 0.0f;
+// (I + N)^-1 of a strictly lower N column by column, lane = column: x_t = [t == lane] - sum_{i < t} N_ti x_i, four rows at a time; the columns
+// in shared memory (rows of 33).  Rolled: with all rows written out the warps of an SM, each at a place of its own, waited for instructions a
+// third of their time.  Two terms to `out`, then by rows; the largest sum of magnitudes of a row.
+__device__ __forceinline__ float invert(const float* Nm, float* xs, char* out, int lane, float& rows) {
+#pragma unroll 1
+    for (int t = 0; t < 32; t += 4) {
+        float y[4];
 #pragma unroll
-    for (int t = 0; t < 32; ++t) {
-        float y[4] = {t == lane ? 1.0f : 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = t + k == lane ? 1.0f : 0.0f;
+#pragma unroll 2
         for (int i = 0; i < t; i += 4) {
-            const float4 w = *reinterpret_cast<const float4*>(Nm + t * 36 + i);
-            y[0] = fmaf(-w.x, x[i], y[0]);
-            if (i + 1 < t) y[1] = fmaf(-w.y, x[i + 1], y[1]);
-            if (i + 2 < t) y[2] = fmaf(-w.z, x[i + 2], y[2]);
-            if (i + 3 < t) y[3] = fmaf(-w.w, x[i + 3], y[3]);
+            float x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = xs[(i + k) * 33 + lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 w = *reinterpret_cast<const float4*>(Nm + (t + k) * 36 + i);
+                y[k] = fmaf(-w.x, x[0], y[k]); y[k] = fmaf(-w.y, x[1], y[k]);
+                y[k] = fmaf(-w.z, x[2], y[k]); y[k] = fmaf(-w.w, x[3], y[k]);
+            }
         }
-        x[t] = (y[0] + y[1]) + (y[2] + y[3]);
-        most = fmaxf(most, fabsf(x[t]));
+        const float* d = Nm + t * 36 + t;
+        y[1] = fmaf(-d[36], y[0], y[1]);
+        y[2] = fmaf(-d[72], y[0], y[2]); y[2] = fmaf(-d[73], y[1], y[2]);
+        y[3] = fmaf(-d[108], y[0], y[3]); y[3] = fmaf(-d[109], y[1], y[3]); y[3] = fmaf(-d[110], y[2], y[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) xs[(t + k) * 33 + lane] = y[k];
     }
+    __syncwarp();
+    const float* row = xs + lane * 33;  // lane = row
+    float sum = 0.0f, most = 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+        const float x = fabsf(row[i]);
+        sum += x;
+        most = fmaxf(most, x);
+    }
+    rows = warp_max(sum);
     float s, inv;
-    // the largest sum of magnitudes of a row: lane t's column sums in 31 exchanges
-    float part[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float keep = fabsf(lane & 16 ? x[i + 16] : x[i]), give = fabsf(lane & 16 ? x[i] : x[i + 16]);
-        part[i] = keep + __shfl_xor_sync(kAll, give, 16);
-    }
-#pragma unroll
-    for (int w = 8; w > 0; w >>= 1)
-#pragma unroll
-        for (int i = 0; i < w; ++i) {
-            const float keep = lane & w ? part[i + w] : part[i], give = lane & w ? part[i] : part[i + w];
-            part[i] = keep + __shfl_xor_sync(kAll, give, w);
-        }
-    rows = warp_max(part[0]);
     pow2_scale(warp_max(most), s, inv);
-#pragma unroll
-    for (int t = 0; t < 32; ++t) {
-        const float y = x[t] * s;
-        const __half hi = __float2half_rn(y), lo = __float2half_rn(y - __half2float(hi));
-        const uint32_t at = tile_at<32>(t, lane >> 3) + (lane & 7) * 2;
-        *reinterpret_cast<__half*>(out + at) = hi;
-        *reinterpret_cast<__half*>(out + 2048 + at) = lo;
+#pragma unroll 1
+    for (int piece = 0; piece < 4; ++piece) {
+        uint4 hi, lo;
+        const float* x = row + piece * 8;
+        split(x[0] * s, x[1] * s, hi.x, lo.x);
+        split(x[2] * s, x[3] * s, hi.y, lo.y);
+        split(x[4] * s, x[5] * s, hi.z, lo.z);
+        split(x[6] * s, x[7] * s, hi.w, lo.w);
+        const uint32_t at = tile_at<32>(lane, piece);
+        *reinterpret_cast<uint4*>(out + at) = hi;
+        *reinterpret_cast<uint4*>(out + 2048 + at) = lo;
     }
+    __syncwarp();
     return inv;
 }
 
@@ -196,8 +207,13 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     float* norm_s = eta_s + 32;  // |k|^2
     char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
     const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
-    const float ik = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(a.k) + row0, rows, s.dk, vec, sm, out, lane);
-    const float iq = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(a.q) + row0, rows, s.dk, vec, sm + KT * 64 * DK, out + KT * 64 * DK, lane);
+    float ik = 1.0f, iq = 1.0f;
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        ik = iq;
+        iq = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(which ? a.q : a.k) + row0, rows, s.dk, vec, sm + which * KT * 64 * DK,
+                                    out + which * KT * 64 * DK, lane);
+    }
     __syncwarp();
     const uint32_t ks = sm100::smem_u32(sm), qs = ks + KT * 64 * DK;
     float kk[6][4], qk[6][4];
@@ -233,7 +249,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         sc[kRecDend * 32 + lane] = dend * ik;
         sc[kRecW * 32 + lane] = eta * dend * ik;
         // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
-        float amax = 0.0f, emax = 0.0f, av[6][4];
+        float amax = 0.0f, emax = 0.0f, av[6][4], gk[6][4];  // gk: strict(D (k k^T))
 #pragma unroll
         for (int i = 0; i < 6; ++i) {
             const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
@@ -242,7 +258,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
                 const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
                 const float D = u <= t ? expf((float)(run[t] - run[u])) : 0.0f;
                 if (u == t) norm_s[t] = kk[i][x] * (ik * ik);
-                Nm[t * 36 + u] = u < t ? D * kk[i][x] * (ik * ik) * eta_s[u] : 0.0f;
+                gk[i][x] = u < t ? D * kk[i][x] * (ik * ik) : 0.0f;
+                Nm[t * 36 + u] = gk[i][x] * eta_s[u];
                 av[i][x] = u <= t ? D * qk[i][x] * (iq * ik * s.scale) : 0.0f;
                 amax = fmaxf(amax, fabsf(av[i][x]));
                 emax = fmaxf(emax, fabsf(av[i][x] * eta_s[u]));
@@ -270,22 +287,25 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             }
         }
         __syncwarp();
-        float tsum, rsum;
-        const float ti = invert(Nm, rec, lane, tsum);
-        float ri = 0.0f;
-        if (a.save) {  // the same with eta on the rows: what the reverse pass multiplies with
-            __syncwarp();
+        // T, and with saved states the same with eta on the rows: what the reverse pass multiplies with
+        float tsum = 0.0f, ti = 0.0f, ri = 0.0f, rsum;
+#pragma unroll 1
+        for (int pass = 0; pass <= a.save; ++pass) {
+            const float y = invert(Nm, reinterpret_cast<float*>(sm), rec + (pass ? 13312 : 0), lane, rsum);
+            if (pass) { ri = y; break; }
+            ti = y;
+            tsum = rsum;
+            if (!a.save) break;
 #pragma unroll
             for (int i = 0; i < 6; ++i) {
                 const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                     const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
-                    Nm[t * 36 + u] = u < t ? expf((float)(run[t] - run[u])) * kk[i][x] * (ik * ik) * eta_s[t] : 0.0f;
+                    Nm[t * 36 + u] = gk[i][x] * eta_s[t];
                 }
             }
             __syncwarp();
-            ri = invert(Nm, rec + 13312, lane, rsum);
         }
         const float kn = sqrtf(norm_s[lane]);
         const float b_kn = warp_max(bt * kn), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
