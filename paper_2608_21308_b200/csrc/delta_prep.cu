@@ -10,7 +10,10 @@ using namespace delta;
 
 constexpr int kWarps = 4;
 
-template <int DK, int KT> constexpr int prep_warp_bytes() { return 2 * KT * 64 * DK + 4608 + 256 + 256; }
+// the tiles, and over them, once their products are in registers, N (32 rows of 36) and its inverse (32 rows of 33); then the tokens' scalars
+constexpr int kTriangles = 4608 + 4224;
+template <int DK, int KT> constexpr int prep_work_bytes() { return 2 * KT * 64 * DK > kTriangles ? 2 * KT * 64 * DK : kTriangles; }
+template <int DK, int KT> constexpr int prep_warp_bytes() { return prep_work_bytes<DK, KT>() + 256 + 256; }
 
 // largest magnitude of a row tile, then its scaled terms to shared memory and to the workspace
 template <typename IO, int DK, int KT>
@@ -201,9 +204,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     const int c = (int)(item % a.l.nch);
     const int t0 = c * kDeltaChunk, rows = min(kDeltaChunk, s.L - t0);
     char* sm = smem + warp * prep_warp_bytes<DK, KT>();
-    float* Nm = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK);  // 32 x 32, rows of 36
-    double* run = reinterpret_cast<double*>(sm + 2 * KT * 64 * DK + 4608);
-    float* eta_s = reinterpret_cast<float*>(sm + 2 * KT * 64 * DK + 4608 + 256);
+    float* Nm = reinterpret_cast<float*>(sm);
+    float* xs = reinterpret_cast<float*>(sm + 4608);
+    double* run = reinterpret_cast<double*>(sm + prep_work_bytes<DK, KT>());
+    float* eta_s = reinterpret_cast<float*>(run + 32);
     float* norm_s = eta_s + 32;  // |k|^2
     char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
     const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
@@ -219,6 +223,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     float kk[6][4], qk[6][4];
     gram<DK, KT>(ks, ks, kk, lane);
     gram<DK, KT>(qs, ks, qk, lane);
+    __syncwarp();
     const int g = lane >> 2, c4 = lane & 3, r = s.H / s.Hk;
     const int64_t b = nk / s.Hk, hk = nk % s.Hk;
     for (int j = 0; j < r; ++j) {
@@ -291,7 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         float tsum = 0.0f, ti = 0.0f, ri = 0.0f, rsum;
 #pragma unroll 1
         for (int pass = 0; pass <= a.save; ++pass) {
-            const float y = invert(Nm, reinterpret_cast<float*>(sm), rec + (pass ? 13312 : 0), lane, rsum);
+            const float y = invert(Nm, xs, rec + (pass ? 13312 : 0), lane, rsum);
             if (pass) { ri = y; break; }
             ti = y;
             tsum = rsum;
