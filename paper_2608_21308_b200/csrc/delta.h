@@ -19,11 +19,13 @@ constexpr int kDeltaSuper = 2;   // blocks between two inner products <X, S> of 
 // pass, (I + eta strict(D (K K^T)))^-1.  The forward fetches the first 9 KB, the reverse pass the last 9.
 constexpr int kDeltaRecBytes = 9216;
 constexpr int kDeltaRecSkip = 8192;
-// rows of a record's scalars: b of K and Q (with the scales of their tiles), eta, D_end, eta D_end
-enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecW = 4, kRecHead = 7 };
+// rows of a record's scalars: b of K and Q (with the scales of their tiles), eta, D_end, eta D_end, eta b
+enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecW = 4, kRecZ = 5, kRecHead = 7 };
 // the last row: decay of the whole chunk; what undoes the scales of T, A eta, K, Q, the reverse pass' T and A; then bounds of the chunk's
 // operands: max b |k| (2-norm), row sums of T, max |eta| D_end (in units of the K tile), sum |eta| D_end |k|
-enum { kHeadEnd = 0, kHeadT = 1, kHeadA = 2, kHeadK = 3, kHeadQ = 4, kHeadR = 5, kHeadKn = 6, kHeadTsum = 7, kHeadAr = 8, kHeadWmax = 9, kHeadWsum = 10 };
+enum { kHeadEnd = 0, kHeadT = 1, kHeadA = 2, kHeadK = 3, kHeadQ = 4, kHeadR = 5, kHeadKn = 6, kHeadTsum = 7, kHeadAr = 8, kHeadWmax = 9, kHeadWsum = 10,
+       // and of the reverse pass: max D_end |k|, column sums of its T, max |eta| b (in units of the K tile), sum |eta| b |k|, sum b scale |q|
+       kHeadKe = 11, kHeadRsum = 12, kHeadZmax = 13, kHeadZsum = 14, kHeadQsum = 15 };
 
 struct DeltaShape {
     int B, H, Hk, L, dk, dv;
@@ -92,7 +94,7 @@ inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
         l.max_do = take(chunks * 4);
         l.part_eta = take(chunks * kDeltaChunk * 4);
         l.part_gate = take(chunks * kDeltaChunk * 4);
-        l.hx = take((size_t)l.N * l.nsup * l.slices * 4);
+        l.hx = take((size_t)l.N * l.nsup * l.slices * 16);
     }
     l.total = at;
     return l;

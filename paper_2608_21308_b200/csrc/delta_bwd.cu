@@ -33,297 +33,652 @@ __device__ __forceinline__ float sum_rows(const float (&v)[8], int lane) {
     return keep + __shfl_xor_sync(kAll, give, 4);
 }
 
-template <typename IO, int DK, int KT>
-__global__ void __launch_bounds__(128) delta_chain_kernel(const DeltaBwdArgs ba, const int warps) {
+// what the warps of a slice hand over, a buffer per parity of the step: from the side warp A^T dO, the fragments of b dO and bounds on both; from the
+// chain Z, X's fragments behind a block (first term, with fp32 I/O both); and what the side warp has fetched
+template <int DK, int KT, int KS> struct alignas(128) ReverseExchange {
+    uint4 x[KT][DK / 16][32];
+    uint4 q[2][2][32];        // [term][k-step]
+    float4 in[4][32], z[4][32];
+    float4 part[KS > 1 ? KS : 1][4][KS > 1 ? 32 : 1];
+    uint4 e[2][2][32];        // e's fragments
+    float4 o[4][32];
+    float4 d_o[KT == 1 ? 2 : 4][32], v[KT == 1 ? 2 : 4][32];
+    uint4 out[KT == 1 ? 64 : 1];
+    float norm[KS];
+    float x_inv, in_max, q_max, q_inv, q_sum;
+};
+template <int DK, int KT, int KS> constexpr int chain_smem(int slices) {
+    return kStages * stage_bytes<DK, KT>() + 2 * slices * (int)sizeof(ReverseExchange<DK, KT, KS>);
+}
+
+// The chain X, Z, X runs as the forward's does (a warp per slice, or KS by columns; scales from bounds; the products of a chunk between the steps of
+// its arithmetic).  A side warp per slice, a chunk ahead, makes what does not depend on X (A^T dO, the fragments of b dO, o . dO), and, a chunk
+// behind, what hangs off Z (dV, dP's fragments, the sums for d eta and d log_gamma).
+template <typename IO, int DK, int KT, int KS>
+__global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(const DeltaBwdArgs ba, const int per, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
-    __shared__ uint64_t full[kStages];
+    constexpr int NS = kStages, DC = DK / KS, SB = stage_bytes<DK, KT>(), TERMS = KT == 2 ? 3 : 2;
+    __shared__ uint64_t full[NS];
     __shared__ int dead_flag;
+    using X = ReverseExchange<DK, KT, KS>;
     const DeltaArgs& a = ba.f;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
     const DeltaShape& s = a.s;
-    const int groups = (a.l.slices + warps - 1) / warps;
+    const int groups = (a.l.slices + per - 1) / per;
     const int64_t n = blockIdx.x / groups, nk = (n / s.H) * s.Hk + (n % s.H) / (s.H / s.Hk);
-    const int slice = (int)(blockIdx.x % groups) * warps + warp;
+    const bool chain = warp < per * KS;
+    const int mine = chain ? warp / KS : warp - per * KS, part = chain ? warp % KS : 0;
+    const int slice = (int)(blockIdx.x % groups) * per + mine;
     const bool active = slice < a.l.slices;
     const int nch = a.l.nch;
+    X* xb = reinterpret_cast<X*>(smem + NS * SB) + 2 * mine;
     sm100::WaitCtx wait{&dead_flag, reinterpret_cast<int*>(a.ws)};
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) sm100::mbar_init(&full[i], 1);
+        for (int i = 0; i < NS; ++i) sm100::mbar_init(&full[i], 1);
         dead_flag = 0;
         sm100::fence_mbar_init();
     }
     __syncthreads();
+    const int r0 = slice * 16 + g, r1 = r0 + 8;
+    const bool ok0 = active && r0 < s.dv, ok1 = active && r1 < s.dv;
+    const uint32_t ring = sm100::smem_u32(smem);
+    // a stage: K, Q, then the record's scalars, A, T
+    constexpr int AT_SC = 2 * KT * 64 * DK, AT_A = AT_SC + 1024, AT_T = AT_A + 4096;
+
+    if (chain) {
+        const int col0 = part * DC;
+        float S[DC / 8][4], s_now = 1.0f, s_inv = 1.0f, norm = 0.0f;  // X times its scale
+#pragma unroll
+        for (int j = 0; j < DC / 8; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int col = col0 + j * 8 + 2 * c4 + (x & 1);
+                const bool ok = ba.dS_final && col < s.dk && (x < 2 ? ok0 : ok1);
+                S[j][x] = ok ? ba.dS_final[((size_t)n * s.dv + (x < 2 ? r0 : r1)) * s.dk + col] : 0.0f;
+            }
+        // |dU| <= max |A^T dO| + max D_end |k| |X|,  |Z| <= column sums of |T| |dU|,  |X_before| <= b_end |X| + max |dO| sum b |q| + |Z| sum |eta| b |k|
+        float sk[4][4], squares0 = 0.0f, squares1 = 0.0f;  // X K^T of the next chunk
+        uint32_t fh[2][4], fl[2][4];
+        auto split_s = [&](int kk, int r) {
+            const float (&y)[4] = S[2 * kk + (r >> 1)];
+            const float y0 = y[2 * (r & 1)], y1 = y[2 * (r & 1) + 1];
+            fma2(squares0, squares1, y0, y1, y0, y1, squares0, squares1);
+            split(y0, y1, fh[kk & 1][r], fl[kk & 1][r]);
+        };
+        auto leave_s = [&](int kk, X& x) {
+            const uint32_t (&h)[4] = fh[kk & 1], (&l)[4] = fl[kk & 1];
+            x.x[0][part * (DC / 16) + kk][lane] = make_uint4(h[0], h[1], h[2], h[3]);
+            if (KT == 2) x.x[KT - 1][part * (DC / 16) + kk][lane] = make_uint4(l[0], l[1], l[2], l[3]);
+        };
+        auto times_k = [&](int kk, int i, bool first, const uint32_t (&b)[2 * KT][4]) {
+            const int term = i >> 1, h = i & 1;
+            const uint32_t (&x)[4] = term == 1 ? fl[kk & 1] : fh[kk & 1];
+            const uint32_t (&y)[4] = b[term == 2 ? 2 * KT - 2 + h : h];
+            if (first && term == 0) {
+                mma0(sk[2 * h], x, y[0], y[1]);
+                mma0(sk[2 * h + 1], x, y[2], y[3]);
+            } else {
+                mma(sk[2 * h], x, y[0], y[1]);
+                mma(sk[2 * h + 1], x, y[2], y[3]);
+            }
+        };
+        auto load_k = [&](uint32_t ks, int kk, uint32_t (&b)[2 * KT][4]) {
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+                ldsm4(b[2 * t], addr_nk<DK>(ks + t * 64 * DK, 0, part * (DC / 16) + kk, lane));
+                ldsm4(b[2 * t + 1], addr_nk<DK>(ks + t * 64 * DK, 2, part * (DC / 16) + kk, lane));
+            }
+        };
+        auto hand = [&](X& x) {
+            const float y = 32.0f * warp_most(squares0 + squares1);
+            if (KS == 1) {
+                norm = y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.part[part][j][lane] = make_float4(sk[j][0], sk[j][1], sk[j][2], sk[j][3]);
+                if (lane == 0) x.norm[part] = y;
+            }
+            if (lane == 0 && part == 0) x.x_inv = s_inv;
+        };
+        auto take = [&](const X& x) {
+            if (KS > 1) {
+                norm = 0.0f;
+#pragma unroll
+                for (int h = 0; h < KS; ++h) {
+                    norm += x.norm[h];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 z = x.part[KS > 1 ? h : 0][j][lane];
+                        if (h == 0) { sk[j][0] = z.x; sk[j][1] = z.y; sk[j][2] = z.z; sk[j][3] = z.w; }
+                        else { sk[j][0] += z.x; sk[j][1] += z.y; sk[j][2] += z.z; sk[j][3] += z.w; }
+                    }
+                }
+            }
+            float root;
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(norm));
+            norm = root * s_inv;
+        };
+        wait_phase(&full[0], 0, wait, 902);
+        if (active) {
+            float m = 0.0f;
+            for (int col = c4; col < s.dk && ba.dS_final; col += 4) {
+                if (ok0) m = fmaxf(m, fabsf(ba.dS_final[((size_t)n * s.dv + r0) * s.dk + col]));
+                if (ok1) m = fmaxf(m, fabsf(ba.dS_final[((size_t)n * s.dv + r1) * s.dk + col]));
+            }
+            pow2_bound(warp_max(m), s_now, s_inv);
+#pragma unroll
+            for (int j = 0; j < DC / 8; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) S[j][x] *= s_now;
+#pragma unroll
+            for (int kk = 0; kk < DC / 16; ++kk) {
+                uint32_t b[2 * KT][4];
+                load_k(ring, kk, b);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) split_s(kk, r);
+                leave_s(kk, xb[0]);
+#pragma unroll
+                for (int i = 0; i < 2 * TERMS; ++i) times_k(kk, i, kk == 0, b);
+            }
+            hand(xb[0]);
+            sm100::fence_proxy_async_smem();  // X behind the last chunk is copied from there
+        }
+        __syncthreads();  // the side warp's part of the last chunk
+        int st = 0, st_next = 1, phase_next = 0;
+        for (int i = 0; i < nch; ++i) {
+            const int c = nch - 1 - i;
+            const uint32_t ks = ring + st * SB, qs = ks + KT * 64 * DK, ts = ks + AT_T, kn = ring + st_next * SB;
+            const float* sc = reinterpret_cast<const float*>(smem + st * SB + AT_SC);
+            const float* head = sc + kRecHead * 32;
+            X& x = xb[i & 1];
+            X& xn = xb[(i + 1) & 1];
+            float w_old = 0.0f, w_new = 0.0f;
+            uint32_t wh[2][4], wl[2][4], qh[2][4], ql[2][4];
+            const bool come = i + 1 == nch || probe_phase(&full[st_next], phase_next);
+            if (active) {
+                take(x);
+                const int blk = c >> 1;
+                if (((c & 1) || c == nch - 1) && ((blk + 1) % kDeltaSuper == 0 || blk + 1 == a.l.nblk)) {  // <X, S> behind a superblock
+                    const int lo = delta_lo_slot(blk + 1, a.l.nblk, s.f32);
+                    const size_t at = ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.slices + slice;
+                    const size_t at_lo = s.f32 ? at : ((size_t)n * a.l.nsup + lo) * a.l.slices + slice;
+                    const uint4* hi4 = reinterpret_cast<const uint4*>(a.ws + a.l.S + at * a.l.state_bytes) + part * (DC / 16) * 32 + lane;
+                    const uint4* lo4 = reinterpret_cast<const uint4*>(a.ws + a.l.S_lo + at_lo * a.l.state_bytes) + part * (DC / 16) * 32 + lane;
+                    float h = 0.0f;
+#pragma unroll
+                    for (int kk = 0; kk < DC / 16; ++kk) {
+                        const uint4 u = hi4[kk * 32], v2 = lo4[kk * 32];
+                        const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v2.x, v2.y, v2.z, v2.w};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float y0, y1;
+                            join_terms(uw[r], vw[r], y0, y1);
+                            const float (&y)[4] = S[2 * kk + (r >> 1)];
+                            h = fmaf(y[2 * (r & 1)], y0, h);
+                            h = fmaf(y[2 * (r & 1) + 1], y1, h);
+                        }
+                    }
+                    h = warp_sum(h) * (s_inv * reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at]);
+                    float* hx = reinterpret_cast<float*>(a.ws + a.l.hx) + (((size_t)n * a.l.nsup + blk / kDeltaSuper) * a.l.slices + slice) * 4;
+                    if (lane == 0) hx[part] = h;
+                    if (lane >= KS && lane < 4 && part == 0) hx[lane] = 0.0f;
+                }
+                uint32_t th[3][4], tl[3][4];  // (tokens 0-15 x 0-15), (16-31 x 0-15), (16-31 x 16-31)
+                ldsm4_t(th[0], addr_kn<32>(ts, 0, 0, lane)); ldsm4_t(th[1], addr_kn<32>(ts, 0, 1, lane)); ldsm4_t(th[2], addr_kn<32>(ts, 2, 1, lane));
+                ldsm4_t(tl[0], addr_kn<32>(ts + 2048, 0, 0, lane)); ldsm4_t(tl[1], addr_kn<32>(ts + 2048, 0, 1, lane));
+                ldsm4_t(tl[2], addr_kn<32>(ts + 2048, 2, 1, lane));
+                const float bend = head[kHeadEnd];
+                const float ub = fmaf(head[kHeadKe], norm, x.in_max), zb = ub * head[kHeadRsum];
+                float f, q;
+                pow2_bound(ub, f, q);
+                // dU, times its scale f
+                float p[4][4], z[4][4];
+                const float fs = f * s_inv;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 in = x.in[j][lane];
+                    const float2 de = *reinterpret_cast<const float2*>(sc + kRecDend * 32 + j * 8 + 2 * c4);
+                    float y0, y1;
+                    mul2(y0, y1, de.x, de.y, fs, fs);
+                    mul2(p[j][0], p[j][1], in.x, in.y, f, f);
+                    mul2(p[j][2], p[j][3], in.z, in.w, f, f);
+                    fma2(p[j][0], p[j][1], sk[j][0], sk[j][1], y0, y1, p[j][0], p[j][1]);
+                    fma2(p[j][2], p[j][3], sk[j][2], sk[j][3], y0, y1, p[j][2], p[j][3]);
+                }
+                {
+                    uint32_t h0[4], l0[4], h1[4], l1[4];
+                    split_a(p[2], p[3], h1, l1);
+                    mma0(z[0], h1, th[1][0], th[1][1]); mma0(z[1], h1, th[1][2], th[1][3]);
+                    mma0(z[2], h1, th[2][0], th[2][1]); mma0(z[3], h1, th[2][2], th[2][3]);
+                    split_a(p[0], p[1], h0, l0);
+                    mma(z[0], l1, th[1][0], th[1][1]); mma(z[1], l1, th[1][2], th[1][3]);
+                    mma(z[2], l1, th[2][0], th[2][1]); mma(z[3], l1, th[2][2], th[2][3]);
+                    mma(z[0], h1, tl[1][0], tl[1][1]); mma(z[1], h1, tl[1][2], tl[1][3]);
+                    mma(z[2], h1, tl[2][0], tl[2][1]); mma(z[3], h1, tl[2][2], tl[2][3]);
+                    mma(z[0], h0, th[0][0], th[0][1]); mma(z[1], h0, th[0][2], th[0][3]);
+                    mma(z[0], l0, th[0][0], th[0][1]); mma(z[1], l0, th[0][2], th[0][3]);
+                    mma(z[0], h0, tl[0][0], tl[0][1]); mma(z[1], h0, tl[0][2], tl[0][3]);
+                }
+                // z times qe is Z.  - eta b Z and b dO go into the state at one scale, fw: the fragments of b dO, which are there at their own, move to it
+                const float qe = q * head[kHeadR];
+                float fw, w_inv;
+                pow2_bound(fmaxf(zb * head[kHeadZmax], x.q_max), fw, w_inv);
+                const __half2 move = __float2half2_rn(fw * x.q_inv);
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const uint4 h4 = x.q[0][kk][lane], l4 = x.q[1][kk][lane];
+                    const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&hw[r]), move), y2 = __hmul2(*reinterpret_cast<const __half2*>(&lw[r]), move);
+                        qh[kk][r] = *reinterpret_cast<const uint32_t*>(&y);
+                        ql[kk][r] = *reinterpret_cast<const uint32_t*>(&y2);
+                    }
+                }
+                const float wf = -fw * qe, old_inv = s_inv;
+                pow2_bound(fmaf(bend, norm, fmaf(zb, head[kHeadZsum], x.q_sum)), s_now, s_inv);
+                w_old = bend * (s_now * old_inv);
+                w_new = w_inv * s_now;
+                float w[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 ze = *reinterpret_cast<const float2*>(sc + kRecZ * 32 + j * 8 + 2 * c4);
+                    float y0, y1;
+                    mul2(y0, y1, ze.x, ze.y, wf, wf);
+                    mul2(w[j][0], w[j][1], z[j][0], z[j][1], y0, y1);
+                    mul2(w[j][2], w[j][3], z[j][2], z[j][3], y0, y1);
+                    if (KS == 1 || part == (j >> 1)) {
+                        float4 t;
+                        mul2(t.x, t.y, z[j][0], z[j][1], qe, qe);
+                        mul2(t.z, t.w, z[j][2], z[j][3], qe, qe);
+                        x.z[j][lane] = t;
+                    }
+                }
+                split_a(w[0], w[1], wh[0], wl[0]);
+                split_a(w[2], w[3], wh[1], wl[1]);
+            }
+            if (!come) sm100::mbar_wait(&full[st_next], phase_next, wait, 902);
+            if (active) {
+                constexpr int NJ = DC / 32;
+                float y[2][4][4];
+                uint32_t fs[2][2][KT][4], fk[2][2 * KT][4];
+                auto load_s = [&](uint32_t tile, int j4) {
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int k = 0; k < KT; ++k) ldsm4_t(fs[kk][h][k], addr_kn<DK>(tile + k * 64 * DK, part * (DC / 8) + 4 * j4 + 2 * h, kk, lane));
+                };
+                // the i-th two MMAs: 4 TERMS with the keys, then as many with the queries
+                auto sum = [&](float (&t)[4][4], int i) {
+                    const bool keys = i < 4 * TERMS;
+                    const int m = keys ? i : i - 4 * TERMS, kk = m / (2 * TERMS), term = m % (2 * TERMS) >> 1, h = m & 1;
+                    const uint32_t (&w)[4] = keys ? (term == 1 ? wl[kk] : wh[kk]) : (term == 1 ? ql[kk] : qh[kk]);
+                    const uint32_t (&b)[4] = fs[kk][h][term == 2 ? KT - 1 : 0];
+                    if (i < 2) {
+                        mma0(t[2 * h], w, b[0], b[1]);
+                        mma0(t[2 * h + 1], w, b[2], b[3]);
+                    } else {
+                        mma(t[2 * h], w, b[0], b[1]);
+                        mma(t[2 * h + 1], w, b[2], b[3]);
+                    }
+                };
+                load_s(ks, 0);
+                squares0 = squares1 = 0.0f;
+#pragma unroll
+                for (int m = 0; m < 4 * TERMS; ++m) sum(y[0], m);
+                load_s(qs, 0);
+                load_k(kn, 0, fk[0]);
+#pragma unroll
+                for (int m = 4 * TERMS; m < 8 * TERMS; ++m) sum(y[0], m);
+                if (NJ > 1) load_s(ks, 1);
+                const bool kept = c & 1 ? false : c > 0;  // X before this chunk is X behind a block
+#pragma unroll
+                for (int j4 = 0; j4 < NJ; ++j4) {
+                    const int before = j4 > 0 ? 2 * TERMS : 0, next = j4 + 1 < NJ ? 8 * TERMS : 0, all = before + next + 2 * TERMS;
+                    auto upto = [&](int m) {
+                        const int most = m < 5 ? before + next : all;
+                        return (m + 1) * all / 12 < most ? (m + 1) * all / 12 : most;
+                    };
+                    auto issue = [&](int m) {
+                        if (m < before) times_k(2 * j4 - 1, m, false, fk[1]);
+                        else if (m < before + next) sum(y[(j4 + 1) & 1], m - before);
+                        else times_k(2 * j4, m - before - next, j4 == 0, fk[0]);
+                        if (m + 1 == before || (m == 0 && before == 0)) load_k(kn, 2 * j4 + 1, fk[1]);
+                        if (next > 0 && m + 1 == before + next / 2) load_s(qs, j4 + 1);
+                        if (next > 0 && m + 1 == before + next && j4 + 2 < NJ) load_s(ks, j4 + 2);
+                    };
+#pragma unroll
+                    for (int m = 0; m < 12; ++m) {
+                        if (m == 0 || m == 1 || m == 6 || m == 7) {
+                            const int k = m < 2 ? m : m - 4;
+                            float (&d)[4] = S[4 * j4 + k];
+                            const float (&t)[4] = y[j4 & 1][k];
+#pragma unroll
+                            for (int z = 0; z < 4; z += 2) {
+                                float m0, m1;
+                                mul2(m0, m1, d[z], d[z + 1], w_old, w_old);
+                                fma2(d[z], d[z + 1], t[z], t[z + 1], w_new, w_new, m0, m1);
+                            }
+                        } else {
+                            const int r = m < 6 ? m - 2 : m - 8;
+                            split_s(2 * j4 + (m < 6 ? 0 : 1), r);
+                            if (r == 3 && kept) leave_s(2 * j4 + (m < 6 ? 0 : 1), xn);
+                        }
+#pragma unroll
+                        for (int k = upto(m - 1); k < upto(m); ++k) issue(k);
+                    }
+                    if (j4 + 1 < NJ) load_k(kn, 2 * j4 + 2, fk[0]);
+                }
+#pragma unroll
+                for (int k = 0; k < 2 * TERMS; ++k) times_k(2 * NJ - 1, k, false, fk[1]);
+                hand(xn);
+                if (kept) sm100::fence_proxy_async_smem();
+            }
+            st = st_next;
+            if (++st_next == NS) { st_next = 0; phase_next ^= 1; }
+            __syncthreads();
+        }
+        if (active) {
+#pragma unroll
+            for (int j = 0; j < DC / 8; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const int col = col0 + j * 8 + 2 * c4 + (x & 1);
+                    if (col < s.dk && (x < 2 ? ok0 : ok1)) ba.dS_init[((size_t)n * s.dv + (x < 2 ? r0 : r1)) * s.dk + col] = S[j][x] * s_inv;
+                }
+        }
+        return;
+    }
+
+    // ---- the side warp of a slice; step i is chunk nch - 1 - i
     const char* qk_src = a.ws + a.l.qk + (size_t)nk * nch * a.l.qk_bytes;
     const char* rec_src = a.ws + a.l.rec + (size_t)n * nch * a.l.rec_bytes + kDeltaRecSkip;
-    auto fetch = [&](int i) {  // the i-th chunk from the end
+    const bool fetches = mine == 0 && lane == 0;
+    auto fetch = [&](int i, int st) {
         const int c = nch - 1 - i;
-        const uint32_t dst = sm100::smem_u32(smem) + (i % kStages) * stage_bytes<DK, KT>();
-        uint64_t* bar = &full[i % kStages];
-        sm100::mbar_expect_tx(bar, stage_bytes<DK, KT>());
+        const uint32_t dst = ring + st * SB;
+        uint64_t* bar = &full[st];
+        sm100::mbar_expect_tx(bar, SB);
         bulk_copy(dst, qk_src + (size_t)c * a.l.qk_bytes, 2 * KT * 64 * DK, bar);
         bulk_copy(dst + 2 * KT * 64 * DK, rec_src + (size_t)c * a.l.rec_bytes, kDeltaRecBytes, bar);
     };
-    if (threadIdx.x == 0)
-        for (int i = 0; i < kStages && i < nch; ++i) fetch(i);
-
-    const int r0 = slice * 16 + g, r1 = r0 + 8;
-    const bool ok0 = active && r0 < s.dv, ok1 = active && r1 < s.dv;
-    float X[DK / 8][4];
-#pragma unroll
-    for (int j = 0; j < DK / 8; ++j)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int col = j * 8 + 2 * c4 + (x & 1);
-            const bool ok = ba.dS_final && col < s.dk && (x < 2 ? ok0 : ok1);
-            X[j][x] = ok ? ba.dS_final[((size_t)n * s.dv + (x < 2 ? r0 : r1)) * s.dk + col] : 0.0f;
-        }
-    const size_t seq = (size_t)n * s.L * s.dv;
+    if (fetches)
+        for (int i = 0; i < NS && i < nch; ++i) fetch(i, i);
+    __syncwarp();
+    const int rows = active ? min(16, s.dv - slice * 16) : 0;
+    const size_t seq = (size_t)n * s.L * s.dv + slice * 16;
     const IO* v = reinterpret_cast<const IO*>(a.v) + seq;
     const IO* d_o = reinterpret_cast<const IO*>(ba.d_o) + seq;
     IO* dv = reinterpret_cast<IO*>(ba.dv) + seq;
-    auto load_tok = [&](const IO* p, int c, float (&x)[4][4]) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (i & 1);
-                x[j][i] = (t < s.L && (i < 2 ? ok0 : ok1)) ? to_f32(p[(size_t)t * s.dv + (i < 2 ? r0 : r1)]) : 0.0f;
-            }
+    auto copy16 = [&](const void* dst, const void* src, int bytes) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sm100::smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
     };
-    float don[4][4];
-    load_tok(d_o, nch - 1, don);
-    for (int i = 0; i < nch; ++i) {
-        const int c = nch - 1 - i, st = i % kStages;
-        sm100::mbar_wait(&full[st], (i / kStages) & 1, wait, 902);
-        if (active) {
-            const uint32_t ks = sm100::smem_u32(smem) + st * stage_bytes<DK, KT>(), qs = ks + KT * 64 * DK, as = qs + KT * 64 * DK + 1024, ts = as + 4096;
-            const float* sc = reinterpret_cast<const float*>(smem + st * stage_bytes<DK, KT>() + 2 * KT * 64 * DK);
-            const int blk = c >> 1;
-            const bool block_end = (c & 1) || c == nch - 1;
-            if (block_end && ((blk + 1) % kDeltaSuper == 0 || blk + 1 == a.l.nblk)) {  // <X, S> behind a superblock
-                const int lo = delta_lo_slot(blk + 1, a.l.nblk, s.f32);
-                const size_t at = ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.slices + slice;
-                const size_t at_lo = s.f32 ? at : ((size_t)n * a.l.nsup + lo) * a.l.slices + slice;
-                const uint4* hi4 = reinterpret_cast<const uint4*>(a.ws + a.l.S + at * a.l.state_bytes);
-                const uint4* lo4 = reinterpret_cast<const uint4*>(a.ws + a.l.S_lo + at_lo * a.l.state_bytes);
-                float h = 0.0f;
+    // a chunk's rows of v or dO to a tile of tokens (bf16) or to fragment order (fp32)
+    auto load_tok = [&](float4* dst, const IO* src, int c) {
+        if (KT == 1) {
+            const int t = c * kDeltaChunk + lane;
+            const IO* p = src + (size_t)t * s.dv;
+            const int here = t < s.L ? rows : 0;
+            if (vec) {
 #pragma unroll
-                for (int kk = 0; kk < DK / 16; ++kk) {
-                    const uint4 u = hi4[kk * 32 + lane], v2 = lo4[kk * 32 + lane];
-                    const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, vw[4] = {v2.x, v2.y, v2.z, v2.w};
+                for (int i = 0; i < 2; ++i) copy16(reinterpret_cast<char*>(dst) + tok_at(lane, i), here > 8 * i ? p + 8 * i : src, here > 8 * i ? 16 : 0);
+            } else {
+                uint32_t w[8];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float s0, s1;
-                        join_terms(uw[r], vw[r], s0, s1);
-                        const float (&x)[4] = X[2 * kk + (r >> 1)];
-                        h = fmaf(x[2 * (r & 1)], s0, h);
-                        h = fmaf(x[2 * (r & 1) + 1], s1, h);
-                    }
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t y = 2 * i < here ? reinterpret_cast<const uint16_t*>(p)[2 * i] : 0u;
+                    const uint32_t z = 2 * i + 1 < here ? reinterpret_cast<const uint16_t*>(p)[2 * i + 1] : 0u;
+                    w[i] = y | z << 16;
                 }
-                h = warp_sum(h) * reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at];
-                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.hx)[((size_t)n * a.l.nsup + blk / kDeltaSuper) * a.l.slices + slice] = h;
+                *reinterpret_cast<uint4*>(reinterpret_cast<char*>(dst) + tok_at(lane, 0)) = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<uint4*>(reinterpret_cast<char*>(dst) + tok_at(lane, 1)) = make_uint4(w[4], w[5], w[6], w[7]);
             }
-            float xk[4][4], in[4][4], z[4][4], d_out[4][4];
-            float m0 = 0.0f, m1 = 0.0f;
+        } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) { xk[j][x] = in[j][x] = z[j][x] = 0.0f; d_out[j][x] = don[j][x]; }
-            if (c > 0) load_tok(d_o, c - 1, don);
-            // X K^T
-#pragma unroll
-            for (int j = 0; j < DK / 8; ++j) {
-                m0 = fmaxf(m0, fmaxf(fabsf(X[j][0]), fabsf(X[j][1])));
-                m1 = fmaxf(m1, fmaxf(fabsf(X[j][2]), fabsf(X[j][3])));
-            }
-            float s0, i0;
-            pow2_scale(warp_max(fmaxf(m0, m1)), s0, i0);
-            const size_t at_x = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + slice;
-            uint4* x_out = reinterpret_cast<uint4*>(a.ws + a.l.X + at_x * a.l.state_bytes * KT);
-            if (block_end && lane == 0) reinterpret_cast<float*>(a.ws + a.l.x_inv)[at_x] = i0;
-#pragma unroll
-            for (int kk = 0; kk < DK / 16; ++kk) {
-                uint32_t hi[4], lo[4];
-                to_a(X[2 * kk], X[2 * kk + 1], s0, s0, hi, lo);
-                if (block_end) {
-                    x_out[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    if (KT == 2) x_out[(DK / 16 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                for (int i = 0; i < 4; ++i) {
+                    const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (i & 1), r = g + (i < 2 ? 0 : 8);
+                    const bool ok = t < s.L && r < rows;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(sm100::smem_u32(&dst[j * 32 + lane]) + 4 * i), "l"(ok ? src + (size_t)t * s.dv + r : src), "r"(ok ? 4 : 0) : "memory");
                 }
+        }
+    };
+    auto frag_tok = [&](const float4* src, float (&x)[4][4]) {  // in accumulator order: rows g, g + 8, pairs of tokens
+        if (KT == 1) {
+            uint32_t w[2][4];
+            ldsm4_t(w[0], addr_tok(sm100::smem_u32(src), 0, lane));
+            ldsm4_t(w[1], addr_tok(sm100::smem_u32(src), 1, lane));
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t b[4];
-                    ldsm4(b, addr_nk<DK>(ks, 2 * h, kk, lane));
-                    mma(xk[2 * h], hi, b[0], b[1]); mma(xk[2 * h + 1], hi, b[2], b[3]);
-                    mma(xk[2 * h], lo, b[0], b[1]); mma(xk[2 * h + 1], lo, b[2], b[3]);
-                    if (KT == 2) {
-                        ldsm4(b, addr_nk<DK>(ks + 64 * DK, 2 * h, kk, lane));
-                        mma(xk[2 * h], hi, b[0], b[1]); mma(xk[2 * h + 1], hi, b[2], b[3]);
-                    }
-                }
-            }
-            // y M for a lower M [t][i] (two terms): contraction over t >= i
-            auto lower_t = [&](float (&acc)[4][4], uint32_t tile, const float (&y)[4][4], float f0, float f1) {
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    uint32_t hi[4], lo[4];
-                    to_a(y[2 * kk], y[2 * kk + 1], f0, f1, hi, lo);
-#pragma unroll
-                    for (int h = 0; h <= kk; ++h) {
-                        uint32_t bh[4], bl[4];
-                        ldsm4_t(bh, addr_kn<32>(tile, 2 * h, kk, lane));
-                        ldsm4_t(bl, addr_kn<32>(tile + 2048, 2 * h, kk, lane));
-                        mma(acc[2 * h], hi, bh[0], bh[1]); mma(acc[2 * h + 1], hi, bh[2], bh[3]);
-                        mma(acc[2 * h], lo, bh[0], bh[1]); mma(acc[2 * h + 1], lo, bh[2], bh[3]);
-                        mma(acc[2 * h], hi, bl[0], bl[1]); mma(acc[2 * h + 1], hi, bl[2], bl[3]);
-                    }
-                }
-            };
-            m0 = m1 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                m0 = fmaxf(m0, fmaxf(fabsf(d_out[j][0]), fabsf(d_out[j][1])));
-                m1 = fmaxf(m1, fmaxf(fabsf(d_out[j][2]), fabsf(d_out[j][3])));
-            }
-            m0 = quad_max(m0); m1 = quad_max(m1);
-            const size_t at_max = ((size_t)n * nch + c) * a.l.slices + slice;
-            {
-                const float m = warp_max(fmaxf(m0, m1));
-                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_do)[at_max] = m;
-            }
-            float f0, f1, h0, h1;
-            pow2_scale(m0, f0, h0);
-            pow2_scale(m1, f1, h1);
-            lower_t(in, as, d_out, f0, f1);
-            const float ainv = sc[kRecHead * 32 + kHeadAr], rinv = sc[kRecHead * 32 + kHeadR], bend = sc[kRecHead * 32 + kHeadEnd];
-            // dU, then Z
-            h0 *= ainv; h1 *= ainv;
-            m0 = m1 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 de = *reinterpret_cast<const float2*>(sc + kRecDend * 32 + j * 8 + 2 * c4);
-                in[j][0] = fmaf(xk[j][0] * i0, de.x, in[j][0] * h0); in[j][1] = fmaf(xk[j][1] * i0, de.y, in[j][1] * h0);
-                in[j][2] = fmaf(xk[j][2] * i0, de.x, in[j][2] * h1); in[j][3] = fmaf(xk[j][3] * i0, de.y, in[j][3] * h1);
-                m0 = fmaxf(m0, fmaxf(fabsf(in[j][0]), fabsf(in[j][1])));
-                m1 = fmaxf(m1, fmaxf(fabsf(in[j][2]), fabsf(in[j][3])));
-            }
-            pow2_scale(quad_max(m0), f0, h0);
-            pow2_scale(quad_max(m1), f1, h1);
-            lower_t(z, ts, in, f0, f1);
-            h0 *= rinv; h1 *= rinv;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { z[j][0] *= h0; z[j][1] *= h0; z[j][2] *= h1; z[j][3] *= h1; }
-            // sums over the slice's value rows for d eta and d log_gamma
-            {
-                float part[8], vv[4][4];
-                const uint4* ef = reinterpret_cast<const uint4*>(a.ws + a.l.e) + at_max * 128;
-                const float e_inv = reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at_max];
-                const float4* ov = reinterpret_cast<const float4*>(a.ws + a.l.o) + at_max * 128;
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    const uint4 u = ef[kk * 32 + lane], w = ef[(2 + kk) * 32 + lane];
-                    const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
-                    float e[4][2];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) join_terms(uw[r], ww[r], e[r][0], e[r][1]);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const float (&zz)[4] = z[2 * kk + j];
-                            part[4 * kk + 2 * j + y] = fmaf(zz[y], e[2 * j][y], zz[2 + y] * e[2 * j + 1][y]) * e_inv;
-                        }
-                }
-                // lane 4 g + c4 holds the sum of value g of its c4 group: token (g >> 1) * 8 + 2 c4 + (g & 1)
-                const size_t at = at_max * kDeltaChunk + (g >> 1) * 8 + 2 * c4 + (g & 1);
-                reinterpret_cast<float*>(a.ws + a.l.part_eta)[at] = sum_rows(part, lane);
-                load_tok(v, c, vv);
-                float w = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 et = *reinterpret_cast<const float2*>(sc + kRecEta * 32 + j * 8 + 2 * c4);
-                    const float4 o4 = ov[j * 32 + lane];
-                    z[j][0] *= et.x; z[j][1] *= et.y; z[j][2] *= et.x; z[j][3] *= et.y;  // dP = dV
-                    part[2 * j] = o4.x * d_out[j][0] - vv[j][0] * z[j][0] + (o4.z * d_out[j][2] - vv[j][2] * z[j][2]);
-                    part[2 * j + 1] = o4.y * d_out[j][1] - vv[j][1] * z[j][1] + (o4.w * d_out[j][3] - vv[j][3] * z[j][3]);
-                    w = fmaxf(w, fmaxf(fmaxf(fabsf(z[j][0]), fabsf(z[j][1])), fmaxf(fabsf(z[j][2]), fabsf(z[j][3]))));
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (x & 1);
-                        if (t < s.L && (x < 2 ? ok0 : ok1)) dv[(size_t)t * s.dv + (x < 2 ? r0 : r1)] = from_f32<IO>(z[j][x]);
-                    }
-                }
-                reinterpret_cast<float*>(a.ws + a.l.part_gate)[at] = sum_rows(part, lane);
-                float sp, ip;
-                pow2_scale(warp_max(w), sp, ip);
-                uint4* dst = reinterpret_cast<uint4*>(a.ws + a.l.dp) + at_max * 64 * KT;
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    uint32_t hi[4], lo[4];
-                    to_a(z[2 * kk], z[2 * kk + 1], sp, sp, hi, lo);
-                    dst[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    if (KT == 2) dst[(2 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                }
-                if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.dp_inv)[at_max] = ip;
-            }
-            // X = b_end X + (dO b scale) Q - (dP b) K
-            m0 = m1 = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 bq = *reinterpret_cast<const float2*>(sc + kRecBq * 32 + j * 8 + 2 * c4);
-                const float2 bk = *reinterpret_cast<const float2*>(sc + kRecBk * 32 + j * 8 + 2 * c4);
-                d_out[j][0] *= bq.x; d_out[j][1] *= bq.y; d_out[j][2] *= bq.x; d_out[j][3] *= bq.y;
-                z[j][0] *= -bk.x; z[j][1] *= -bk.y; z[j][2] *= -bk.x; z[j][3] *= -bk.y;
-                m0 = fmaxf(m0, fmaxf(fmaxf(fabsf(z[j][0]), fabsf(z[j][1])), fmaxf(fabsf(d_out[j][0]), fabsf(d_out[j][1]))));
-                m1 = fmaxf(m1, fmaxf(fmaxf(fabsf(z[j][2]), fabsf(z[j][3])), fmaxf(fabsf(d_out[j][2]), fabsf(d_out[j][3]))));
-            }
-            pow2_scale(quad_max(m0), f0, h0);
-            pow2_scale(quad_max(m1), f1, h1);
-            uint32_t qh[2][4], ql[2][4], ph[2][4], pl[2][4];
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                to_a(d_out[2 * kk], d_out[2 * kk + 1], f0, f1, qh[kk], ql[kk]);
-                to_a(z[2 * kk], z[2 * kk + 1], f0, f1, ph[kk], pl[kk]);
-            }
-#pragma unroll
-            for (int j2 = 0; j2 < DK / 16; ++j2) {
-                float x[2][4] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    uint32_t b[4];
-                    ldsm4_t(b, addr_kn<DK>(ks, 2 * j2, kk, lane));
-                    mma(x[0], ph[kk], b[0], b[1]); mma(x[1], ph[kk], b[2], b[3]);
-                    mma(x[0], pl[kk], b[0], b[1]); mma(x[1], pl[kk], b[2], b[3]);
-                    if (KT == 2) {
-                        ldsm4_t(b, addr_kn<DK>(ks + 64 * DK, 2 * j2, kk, lane));
-                        mma(x[0], ph[kk], b[0], b[1]); mma(x[1], ph[kk], b[2], b[3]);
-                    }
-                    ldsm4_t(b, addr_kn<DK>(qs, 2 * j2, kk, lane));
-                    mma(x[0], qh[kk], b[0], b[1]); mma(x[1], qh[kk], b[2], b[3]);
-                    mma(x[0], ql[kk], b[0], b[1]); mma(x[1], ql[kk], b[2], b[3]);
-                    if (KT == 2) {
-                        ldsm4_t(b, addr_kn<DK>(qs + 64 * DK, 2 * j2, kk, lane));
-                        mma(x[0], qh[kk], b[0], b[1]); mma(x[1], qh[kk], b[2], b[3]);
-                    }
-                }
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    float (&d)[4] = X[2 * j2 + y];
-                    d[0] = fmaf(x[y][0], h0, bend * d[0]); d[1] = fmaf(x[y][1], h0, bend * d[1]);
-                    d[2] = fmaf(x[y][2], h1, bend * d[2]); d[3] = fmaf(x[y][3], h1, bend * d[3]);
+                    const uint32_t z = w[j >> 1][(j & 1) * 2 + y];
+                    x[j][2 * y] = __uint_as_float(z << 16);
+                    x[j][2 * y + 1] = __uint_as_float(z & 0xffff0000u);
                 }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 y = src[j * 32 + lane];
+                x[j][0] = y.x; x[j][1] = y.y; x[j][2] = y.z; x[j][3] = y.w;
             }
         }
-        __syncthreads();
-        if (threadIdx.x == 0 && i + kStages < nch) fetch(i + kStages);
-    }
-    if (!active) return;
+    };
+    auto load_ahead = [&](int i) {  // dO and o of step i
+        if (i >= nch || !active) return;
+        const int c = nch - 1 - i;
+        X& x = xb[i & 1];
+        load_tok(x.d_o[0], d_o, c);
+        const float4* src = reinterpret_cast<const float4*>(a.ws + a.l.o) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
 #pragma unroll
-    for (int j = 0; j < DK / 8; ++j)
+        for (int j = 0; j < 4; ++j) copy16(&x.o[j][lane], src + j * 32 + lane, 16);
+    };
+    auto load_behind = [&](int i) {  // e and v of step i
+        if (i >= nch || !active) return;
+        const int c = nch - 1 - i;
+        X& x = xb[i & 1];
+        load_tok(x.v[0], v, c);
+        const uint4* src = reinterpret_cast<const uint4*>(a.ws + a.l.e) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int col = j * 8 + 2 * c4 + (x & 1);
-            if (col < s.dk && (x < 2 ? ok0 : ok1)) ba.dS_init[((size_t)n * s.dv + (x < 2 ? r0 : r1)) * s.dk + col] = X[j][x];
+        for (int j = 0; j < 4; ++j) copy16(&x.e[j >> 1][j & 1][lane], src + j * 32 + lane, 16);
+    };
+    float od[2] = {0.0f, 0.0f}, et[2][4][2];  // o . dO and eta of the last two chunks prepared
+    auto prepare = [&](int i, int st) {
+        X& x = xb[i & 1];
+        const uint32_t as = ring + st * SB + AT_A;
+        const float* sc = reinterpret_cast<const float*>(smem + st * SB + AT_SC);
+        const float* head = sc + kRecHead * 32;
+        float d[4][4], sums[8], m = 0.0f;
+        frag_tok(x.d_o[0], d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 o = x.o[j][lane];
+            sums[2 * j] = fmaf(d[j][0], o.x, d[j][2] * o.z);
+            sums[2 * j + 1] = fmaf(d[j][1], o.y, d[j][3] * o.w);
+            m = fmaxf(m, fmaxf(fmaxf(fabsf(d[j][0]), fabsf(d[j][1])), fmaxf(fabsf(d[j][2]), fabsf(d[j][3]))));
         }
+        m = warp_most(m);
+        if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_do)[((size_t)n * nch + nch - 1 - i) * a.l.slices + slice] = m;
+        od[0] = od[1];
+        od[1] = sum_rows(sums, lane);
+        float f, q;
+        pow2_scale(m, f, q);
+        float in[4][4] = {}, il[4][4] = {};
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint32_t hi[4], lo[4];
+            to_a(d[2 * kk], d[2 * kk + 1], f, f, hi, lo);  // with bf16 one term, exactly
+#pragma unroll
+            for (int h = 0; h <= kk; ++h) {
+                uint32_t bh[4], bl[4];
+                ldsm4_t(bh, addr_kn<32>(as, 2 * h, kk, lane));
+                ldsm4_t(bl, addr_kn<32>(as + 2048, 2 * h, kk, lane));
+                mma(in[2 * h], hi, bh[0], bh[1]); mma(in[2 * h + 1], hi, bh[2], bh[3]);
+                mma(il[2 * h], hi, bl[0], bl[1]); mma(il[2 * h + 1], hi, bl[2], bl[3]);
+                if (KT == 2) { mma(il[2 * h], lo, bh[0], bh[1]); mma(il[2 * h + 1], lo, bh[2], bh[3]); }
+            }
+        }
+        q *= head[kHeadAr];
+        float most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 y = make_float4((in[j][0] + il[j][0]) * q, (in[j][1] + il[j][1]) * q, (in[j][2] + il[j][2]) * q, (in[j][3] + il[j][3]) * q);
+            x.in[j][lane] = y;
+            most = fmaxf(most, fmaxf(fmaxf(fabsf(y.x), fabsf(y.y)), fmaxf(fabsf(y.z), fabsf(y.w))));
+        }
+        most = warp_most(most);
+        const float qm = m * warp_most(fabsf(sc[kRecBq * 32 + lane]));
+        float fq, q_inv;
+        pow2_bound(qm, fq, q_inv);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 bq = *reinterpret_cast<const float2*>(sc + kRecBq * 32 + j * 8 + 2 * c4);
+            const float2 e2 = *reinterpret_cast<const float2*>(sc + kRecEta * 32 + j * 8 + 2 * c4);
+            et[0][j][0] = et[1][j][0]; et[0][j][1] = et[1][j][1];
+            et[1][j][0] = e2.x; et[1][j][1] = e2.y;
+            d[j][0] *= bq.x * fq; d[j][1] *= bq.y * fq; d[j][2] *= bq.x * fq; d[j][3] *= bq.y * fq;
+        }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint32_t hi[4], lo[4];
+            split_a(d[2 * kk], d[2 * kk + 1], hi, lo);
+            x.q[0][kk][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            x.q[1][kk][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        if (lane == 0) { x.in_max = most; x.q_max = qm; x.q_inv = q_inv; x.q_sum = m * head[kHeadQsum]; }
+    };
+    // step i's dV, sums and fragments; `older`: one more chunk has been prepared since
+    auto finish = [&](int i, bool older) {
+        const int c = nch - 1 - i;
+        X& x = xb[i & 1];
+        const size_t at_max = ((size_t)n * nch + c) * a.l.slices + slice;
+        float z[4][4], part_[8], vv[4][4], m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 y = x.z[j][lane];
+            z[j][0] = y.x; z[j][1] = y.y; z[j][2] = y.z; z[j][3] = y.w;
+        }
+        const float e_inv = reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at_max];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const uint4 u = x.e[0][kk][lane], w = x.e[1][kk][lane];
+            const uint32_t uw[4] = {u.x, u.y, u.z, u.w}, ww[4] = {w.x, w.y, w.z, w.w};
+            float e[4][2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) join_terms(uw[r], ww[r], e[r][0], e[r][1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float (&zz)[4] = z[2 * kk + j];
+                    part_[4 * kk + 2 * j + y] = fmaf(zz[y], e[2 * j][y], zz[2 + y] * e[2 * j + 1][y]);
+                }
+        }
+        // lane 4 g + c4 holds the sum of value g of its c4 group: token (g >> 1) * 8 + 2 c4 + (g & 1)
+        const size_t at = at_max * kDeltaChunk + (g >> 1) * 8 + 2 * c4 + (g & 1);
+        reinterpret_cast<float*>(a.ws + a.l.part_eta)[at] = sum_rows(part_, lane) * e_inv;
+        frag_tok(x.v[0], vv);
+        const float (&eta)[4][2] = et[older ? 0 : 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            z[j][0] *= eta[j][0]; z[j][1] *= eta[j][1]; z[j][2] *= eta[j][0]; z[j][3] *= eta[j][1];  // dP = dV
+            part_[2 * j] = fmaf(vv[j][0], z[j][0], vv[j][2] * z[j][2]);
+            part_[2 * j + 1] = fmaf(vv[j][1], z[j][1], vv[j][3] * z[j][3]);
+            m = fmaxf(m, fmaxf(fmaxf(fabsf(z[j][0]), fabsf(z[j][1])), fmaxf(fabsf(z[j][2]), fabsf(z[j][3]))));
+        }
+        reinterpret_cast<float*>(a.ws + a.l.part_gate)[at] = od[older ? 0 : 1] - sum_rows(part_, lane);
+        float sp, ip;
+        pow2_scale(warp_most(m), sp, ip);
+        uint4* dst = reinterpret_cast<uint4*>(a.ws + a.l.dp) + at_max * 64 * KT;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            uint32_t hi[4], lo[4];
+            to_a(z[2 * kk], z[2 * kk + 1], sp, sp, hi, lo);
+            dst[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            if (KT == 2) dst[(2 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.dp_inv)[at_max] = ip;
+        if (KT == 1) {
+            const uint32_t tile = sm100::smem_u32(x.out);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                stsm4_t(addr_tok(tile, h, lane), pack_bf16(z[2 * h][0], z[2 * h][1]), pack_bf16(z[2 * h][2], z[2 * h][3]),
+                        pack_bf16(z[2 * h + 1][0], z[2 * h + 1][1]), pack_bf16(z[2 * h + 1][2], z[2 * h + 1][3]));
+            __syncwarp();
+            const int t = c * kDeltaChunk + lane;
+            const char* row = reinterpret_cast<const char*>(x.out);
+            const uint4 y0 = *reinterpret_cast<const uint4*>(row + tok_at(lane, 0)), y1 = *reinterpret_cast<const uint4*>(row + tok_at(lane, 1));
+            if (t < s.L) {
+                IO* p = dv + (size_t)t * s.dv;
+                if (vec) {
+                    reinterpret_cast<uint4*>(p)[0] = y0;
+                    if (rows > 8) reinterpret_cast<uint4*>(p)[1] = y1;
+                } else {
+                    const uint32_t w[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (2 * k < rows) reinterpret_cast<uint16_t*>(p)[2 * k] = (uint16_t)w[k];
+                        if (2 * k + 1 < rows) reinterpret_cast<uint16_t*>(p)[2 * k + 1] = (uint16_t)(w[k] >> 16);
+                    }
+                }
+            }
+            __syncwarp();
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int t = c * kDeltaChunk + j * 8 + 2 * c4 + (y & 1), r = g + (y < 2 ? 0 : 8);
+                    if (t < s.L && r < rows) dv[(size_t)t * s.dv + r] = from_f32<IO>(z[j][y]);
+                }
+        }
+    };
+    auto save_x = [&](int i) {  // X behind step i's chunk, where a block ends there
+        const int c = nch - 1 - i;
+        if (lane != 0 || !((c & 1) || c == nch - 1)) return;
+        const X& x = xb[i & 1];
+        const size_t at = ((size_t)n * (a.l.nblk + 1) + (c >> 1)) * a.l.slices + slice;
+        bulk_store(a.ws + a.l.X + at * a.l.state_bytes * KT, sm100::smem_u32(x.x), (uint32_t)a.l.state_bytes * KT);
+        reinterpret_cast<float*>(a.ws + a.l.x_inv)[at] = x.x_inv;
+    };
+    load_ahead(0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    load_ahead(1);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+    wait_phase(&full[0], 0, wait, 904);
+    if (active) prepare(0, 0);
+    __syncthreads();
+    int st = 0, phase_next = 0;
+    for (int i = 0; i < nch; ++i) {
+        const int st_next = st + 1 == NS ? 0 : st + 1;
+        if (st_next == 0) phase_next ^= 1;
+        load_ahead(i + 2);
+        load_behind(i);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        if (active) save_x(i);
+        bulk_store_commit();
+        if (active && i > 0) finish(i - 1, true);
+        if (i + 1 < nch) {
+            wait_phase(&full[st_next], phase_next, wait, 904);
+            if (active) prepare(i + 1, st_next);
+        }
+        bulk_store_read();  // the chain may write X there again
+        __syncthreads();
+        if (fetches && i + NS < nch) fetch(i + NS, st);
+        __syncwarp();
+        st = st_next;
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    if (active) finish(nch - 1, false);
+    bulk_store_done();
 }
 
 // d eta and d log_gamma from the slices' sums: a CTA per superblock of 128 tokens, a warp per chunk, lane = token.  Sums of many terms in 64 bits:
@@ -352,8 +707,8 @@ __global__ void __launch_bounds__(kDeltaSuper * 64) delta_gate_kernel(const Delt
     if (lane == 0) total[warp] = sum;
     __syncthreads();
     if (c > last) return;
-    const float* hx = reinterpret_cast<const float*>(a.ws + a.l.hx) + (size_t)item * a.l.slices;
-    for (int i = 0; i < a.l.slices; ++i) sum += hx[i];
+    const float4* hx = reinterpret_cast<const float4*>(a.ws + a.l.hx) + (size_t)item * a.l.slices;
+    for (int i = 0; i < a.l.slices; ++i) sum += (hx[i].x + hx[i].y) + (hx[i].z + hx[i].w);
     for (int i = warp + 1; i <= last - first; ++i) sum += total[i];
     const int t = c * kDeltaChunk + lane;
     if (t < a.s.L) {
@@ -729,18 +1084,30 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
         }
 }
 
+template <typename IO, int DK, int KT, int KS> int launch_chain(const DeltaBwdArgs& b, int per, bool vec, cudaStream_t st) {
+    static_assert(chain_smem<DK, KT, KS>(KS > 1 ? 1 : KT == 1 ? 4 : 2) <= 226 * 1024, "shared memory of the chain");
+    const int bytes = chain_smem<DK, KT, KS>(per);
+    auto kernel = delta_chain_kernel<IO, DK, KT, KS>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return (int)e;
+    kernel<<<(unsigned)(b.f.l.N * ((b.f.l.slices + per - 1) / per)), per * (KS + 1) * 32, bytes, st>>>(b, per, vec);
+    return (int)cudaGetLastError();
+}
+
 template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStream_t st) {
     const DeltaArgs& a = b.f;
     {
-        constexpr int bytes = kStages * stage_bytes<DK, KT>();
-        auto kernel = delta_chain_kernel<IO, DK, KT>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != cudaSuccess) return (int)e;
-        int w = 4;
-        while (w > 1 && a.l.N * ((a.l.slices + w - 1) / w) < 96) w >>= 1;
-        kernel<<<(unsigned)(a.l.N * ((a.l.slices + w - 1) / w)), w * 32, bytes, st>>>(b, w);
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return (int)e;
+        constexpr int most = KT == 1 ? 4 : 2;
+        const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(b.d_o) | reinterpret_cast<uintptr_t>(b.dv)) % 16 == 0;
+        int rc;
+        if (a.l.N * a.l.slices <= 148) {
+            rc = launch_chain<IO, DK, KT, DK / 32>(b, 1, vec, st);
+        } else {
+            int per = most;
+            while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
+            rc = launch_chain<IO, DK, KT, 1>(b, per, vec, st);
+        }
+        if (rc != 0) return rc;
     }
     {
         constexpr int bytes = qk_smem<DK, KT>();

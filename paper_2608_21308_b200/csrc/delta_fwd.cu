@@ -25,7 +25,7 @@ template <int DK, int KT, int KS, bool PREC> struct alignas(128) Exchange {
     uint4 u[PREC ? 2 : 1][2][32];
     float4 v[KT == 1 ? 2 : 4][32];
     uint4 o[KT == 1 ? 64 : 1];
-    float4 part[KS > 1 ? KS : 1][4][32];  // S K^T over a warp's columns (KS > 1)
+    float4 part[KS > 1 ? KS : 1][4][KS > 1 ? 32 : 1];  // S K^T over a warp's columns (KS > 1)
     float norm[KS];                       // the sum of squares of its part of S, scaled
     float s_inv, u_inv, v_max;
 };

@@ -15,9 +15,9 @@ constexpr int kTriangles = 4608 + 4224;
 template <int DK, int KT> constexpr int prep_work_bytes() { return 2 * KT * 64 * DK > kTriangles ? 2 * KT * 64 * DK : kTriangles; }
 template <int DK, int KT> constexpr int prep_warp_bytes() { return prep_work_bytes<DK, KT>() + 256 + 256; }
 
-// largest magnitude of a row tile, then its scaled terms to shared memory and to the workspace
+// largest magnitude of a row tile, then its scaled terms to shared memory and to the workspace; norm: the 2-norm of the whole tile
 template <typename IO, int DK, int KT>
-__device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool vec, char* sm, char* out, int lane) {
+__device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool vec, char* sm, char* out, int lane, float& norm) {
     constexpr int P = DK / 8;  // 16-byte pieces of a tile row
     float m = 0.0f;
     auto load = [&](int i, float (&x)[8]) {
@@ -45,12 +45,18 @@ __device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool
                 if (c + j < d) x[j] = to_f32(p[j]);
         }
     };
-    auto put = [&](int i, const float (&x)[8], float s) {
+    float sq0 = 0.0f, sq1 = 0.0f;  // squares, scaled
+    auto put = [&](int i, float (&x)[8], float s) {
         uint4 hi, lo;
-        split(x[0] * s, x[1] * s, hi.x, lo.x);
-        split(x[2] * s, x[3] * s, hi.y, lo.y);
-        split(x[4] * s, x[5] * s, hi.z, lo.z);
-        split(x[6] * s, x[7] * s, hi.w, lo.w);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            mul2(x[j], x[j + 1], x[j], x[j + 1], s, s);
+            fma2(sq0, sq1, x[j], x[j + 1], x[j], x[j + 1], sq0, sq1);
+        }
+        split(x[0], x[1], hi.x, lo.x);
+        split(x[2], x[3], hi.y, lo.y);
+        split(x[4], x[5], hi.z, lo.z);
+        split(x[6], x[7], hi.w, lo.w);
         const uint32_t at = tile_at<DK>(i / P, i % P);
         *reinterpret_cast<uint4*>(sm + at) = hi;
         *reinterpret_cast<uint4*>(out + at) = hi;
@@ -87,6 +93,7 @@ __device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool
             for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
             put(i * 32 + lane, x, s);
         }
+        norm = sqrtf(warp_sum(sq0 + sq1)) * inv;
         return inv;
     }
 #pragma unroll 4
@@ -103,6 +110,7 @@ __device__ __forceinline__ float stage_rows(const IO* src, int rows, int d, bool
         load(i, x);  // from L1
         put(i, x, s);
     }
+    norm = sqrtf(warp_sum(sq0 + sq1)) * inv;
     return inv;
 }
 
@@ -138,8 +146,9 @@ template <int DK, int KT> __device__ __forceinline__ void gram(uint32_t rows, ui
 
 // (I + N)^-1 of a strictly lower N column by column, lane = column: x_t = [t == lane] - sum_{i < t} N_ti x_i, four rows at a time; the columns
 // in shared memory (rows of 33).  Rolled: with all rows written out the warps of an SM, each at a place of its own, waited for instructions a
-// third of their time.  Two terms to `out`, then by rows; the largest sum of magnitudes of a row.
-__device__ __forceinline__ float invert(const float* Nm, float* xs, char* out, int lane, float& rows) {
+// third of their time.  Two terms to `out`, then by rows; the largest sums of magnitudes of a row and of a column.
+__device__ __forceinline__ float invert(const float* Nm, float* xs, char* out, int lane, float& rows, float& cols) {
+    float col = 0.0f;
 #pragma unroll 1
     for (int t = 0; t < 32; t += 4) {
         float y[4];
@@ -162,7 +171,10 @@ __device__ __forceinline__ float invert(const float* Nm, float* xs, char* out, i
         y[2] = fmaf(-d[72], y[0], y[2]); y[2] = fmaf(-d[73], y[1], y[2]);
         y[3] = fmaf(-d[108], y[0], y[3]); y[3] = fmaf(-d[109], y[1], y[3]); y[3] = fmaf(-d[110], y[2], y[3]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) xs[(t + k) * 33 + lane] = y[k];
+        for (int k = 0; k < 4; ++k) {
+            xs[(t + k) * 33 + lane] = y[k];
+            col += fabsf(y[k]);
+        }
     }
     __syncwarp();
     const float* row = xs + lane * 33;  // lane = row
@@ -174,6 +186,7 @@ __device__ __forceinline__ float invert(const float* Nm, float* xs, char* out, i
         most = fmaxf(most, x);
     }
     rows = warp_max(sum);
+    cols = warp_max(col);
     float s, inv;
     pow2_scale(warp_max(most), s, inv);
 #pragma unroll 1
@@ -211,12 +224,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     float* norm_s = eta_s + 32;  // |k|^2
     char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
     const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
-    float ik = 1.0f, iq = 1.0f;
+    float ik = 1.0f, iq = 1.0f, q_norm = 0.0f;
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         ik = iq;
         iq = stage_rows<IO, DK, KT>(reinterpret_cast<const IO*>(which ? a.q : a.k) + row0, rows, s.dk, vec, sm + which * KT * 64 * DK,
-                                    out + which * KT * 64 * DK, lane);
+                                    out + which * KT * 64 * DK, lane, q_norm);
     }
     __syncwarp();
     const uint32_t ks = sm100::smem_u32(sm), qs = ks + KT * 64 * DK;
@@ -253,6 +266,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         sc[kRecEta * 32 + lane] = eta;
         sc[kRecDend * 32 + lane] = dend * ik;
         sc[kRecW * 32 + lane] = eta * dend * ik;
+        sc[kRecZ * 32 + lane] = eta * bt * ik;
         // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
         float amax = 0.0f, emax = 0.0f, av[6][4], gk[6][4];  // gk: strict(D (k k^T))
 #pragma unroll
@@ -293,10 +307,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         }
         __syncwarp();
         // T, and with saved states the same with eta on the rows: what the reverse pass multiplies with
-        float tsum = 0.0f, ti = 0.0f, ri = 0.0f, rsum;
+        float tsum = 0.0f, ti = 0.0f, ri = 0.0f, rsum, csum;
 #pragma unroll 1
         for (int pass = 0; pass <= a.save; ++pass) {
-            const float y = invert(Nm, xs, rec + (pass ? 13312 : 0), lane, rsum);
+            const float y = invert(Nm, xs, rec + (pass ? 13312 : 0), lane, rsum, csum);
             if (pass) { ri = y; break; }
             ti = y;
             tsum = rsum;
@@ -314,6 +328,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         }
         const float kn = sqrtf(norm_s[lane]);
         const float b_kn = warp_max(bt * kn), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
+        const float ke = warp_max(dend * kn), zmax = warp_max(fabsf(eta) * bt * ik), zsum = warp_sum(fabsf(eta) * bt * kn);
+        const float qsum = fabsf(s.scale) * sqrtf(warp_sum(bt * bt)) * q_norm;
         if (lane == 0) {
             float* head = sc + kRecHead * 32;
             head[kHeadEnd] = expf((float)end);
@@ -327,6 +343,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             head[kHeadAr] = ai;
             head[kHeadWmax] = wmax;
             head[kHeadWsum] = wsum;
+            head[kHeadKe] = ke;
+            head[kHeadRsum] = csum;
+            head[kHeadZmax] = zmax;
+            head[kHeadZsum] = zsum;
+            head[kHeadQsum] = qsum;
         }
         __syncwarp();
     }
