@@ -725,7 +725,7 @@ __global__ void __launch_bounds__(kDeltaSuper * 64) delta_gate_kernel(const Delt
 // operand serves: dQ and dK are off by 2^-11 of their terms before they are rounded to 2^-8.
 template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? 128 : 32; }
 template <int DK, int KT> constexpr int qk_smem() {
-    return 2 * KT * 128 * DK + KT * qk_rows<DK, KT>() * (2 * DK + 3 * 128) + 2 * KT * 8192 + 64 * 8 + 3 * 256 + 256;
+    return 2 * KT * 128 * DK + KT * qk_rows<DK, KT>() * (2 * DK + 3 * 128) + 2 * KT * 8192 + 64 * 8 + 3 * 256 + 384;
 }
 
 template <typename IO, int DK, int KT>
@@ -749,7 +749,7 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
     float* bt = reinterpret_cast<float*>(run + 64);                // 64
     float* dend = bt + 64;                                         // 64, times eta
     float* eta = dend + 64;                                        // 64
-    float* red = eta + 64;                                         // 32, and the scales
+    float* red = eta + 64;                                         // 32, then the scales and the slices' ratios to them
     const uint32_t ks = sm100::smem_u32(kq), qs = ks + KT * 128 * DK, ss = sm100::smem_u32(st_s), os = sm100::smem_u32(st_o),
                    us = sm100::smem_u32(st_u), ps = sm100::smem_u32(st_p), ms = sm100::smem_u32(mat);
     const int nchunks = min(2, a.l.nch - 2 * blk);
@@ -832,6 +832,15 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
             float so, io;
             pow2_scale(mo, so, io);
             if (lane == 0) { red[32] = iu; red[33] = ip; red[34] = so; red[35] = io; red[36] = iS; red[37] = iX; }
+            // what brings a slice's fragments to these scales: powers of two, at most 1
+            if (lane < 16) {
+                red[38 + lane] = tok ? reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at] / iu : 1.0f;
+                red[54 + lane] = tok ? reinterpret_cast<const float*>(a.ws + a.l.dp_inv)[at] / ip : 1.0f;
+            }
+            if (lane < 8) {
+                red[70 + lane] = ok ? reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at_s] / iS : 1.0f;
+                red[78 + lane] = ok ? reinterpret_cast<const float*>(a.ws + a.l.x_inv)[at_s] / iX : 1.0f;
+            }
         }
         __syncthreads();
         const float iu = red[32], ip = red[33], so = red[34], io = red[35], iS = red[36], iX = red[37];
@@ -846,35 +855,40 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
                 *reinterpret_cast<uint32_t*>(tile + at + c4 * 4) = w[i];
             }
         };
-        auto stage_tok = [&](size_t off, size_t off_inv, int terms, float most, char* dst, int sl0) {
+        // the loads of a tile, all under way before the first is looked at, and what then becomes of them; a warp per (term, slice, ..)
+        constexpr int QT = SL * 4 * KT * 32 / 512, QS = SL * KT * (DK / 16) / 16;
+        auto load_tok = [&](size_t off, int terms, uint4 (&x)[QT], int sl0) {
 #pragma unroll
-            for (int q = 0; q < SL * 4 * KT * 32 / 512; ++q) {  // (term, slice, chunk, kk), a warp each
+            for (int q = 0; q < QT; ++q) {
                 const int i = warp + 16 * q, kk = i & 1, ch = (i >> 1) & 1, sl = (i >> 2) % SL, term = (i >> 2) / SL;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                float ratio = 1.0f;
-                if (sl0 + sl < a.l.slices && ch < nchunks) {
-                    const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl0 + sl;
-                    x = reinterpret_cast<const uint4*>(a.ws + off)[(at * terms + term) * 64 + kk * 32 + lane];
-                    ratio = reinterpret_cast<const float*>(a.ws + off_inv)[at] / most;
-                }
-                put(dst + term * TT, 64, sl * 16 + g, (ch * 2 + kk) * 2, x, ratio);
+                const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl0 + sl;
+                x[q] = sl0 + sl < a.l.slices && ch < nchunks ? reinterpret_cast<const uint4*>(a.ws + off)[(at * terms + term) * 64 + kk * 32 + lane] : make_uint4(0, 0, 0, 0);
             }
         };
-        auto stage_state = [&](size_t off, size_t off_lo, int terms, size_t off_inv, float most, int sl0) {
+        auto put_tok = [&](const float* ratios, char* dst, const uint4 (&x)[QT], int sl0) {
 #pragma unroll
-            for (int q = 0; q < SL * KT * (DK / 16) / 16; ++q) {
-                const int i = warp + 16 * q, kk = i % (DK / 16), sl = i / (DK / 16) % SL, term = i / (DK / 16) / SL;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                float ratio = 1.0f;
-                if (sl0 + sl < a.l.slices) {
-                    const size_t at = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl0 + sl;
-                    const char* src = off_lo ? a.ws + (term ? off_lo : off) + at * a.l.state_bytes : a.ws + off + (at * terms + term) * a.l.state_bytes;
-                    x = reinterpret_cast<const uint4*>(src)[kk * 32 + lane];
-                    ratio = reinterpret_cast<const float*>(a.ws + off_inv)[at] / most;
-                }
-                put(st_s + term * TS, DK, sl * 16 + g, kk * 2, x, ratio);
+            for (int q = 0; q < QT; ++q) {
+                const int i = warp + 16 * q, kk = i & 1, ch = (i >> 1) & 1, sl = (i >> 2) % SL, term = (i >> 2) / SL;
+                put(dst + term * TT, 64, sl * 16 + g, (ch * 2 + kk) * 2, x[q], ratios[ch * 8 + ((sl0 + sl) & 7)]);
             }
         };
+        auto load_state = [&](size_t off, size_t off_lo, int terms, uint4 (&x)[QS], int sl0) {
+#pragma unroll
+            for (int q = 0; q < QS; ++q) {
+                const int i = warp + 16 * q, kk = i % (DK / 16), sl = i / (DK / 16) % SL, term = i / (DK / 16) / SL;
+                const size_t at = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl0 + sl;
+                const char* src = off_lo ? a.ws + (term ? off_lo : off) + at * a.l.state_bytes : a.ws + off + (at * terms + term) * a.l.state_bytes;
+                x[q] = sl0 + sl < a.l.slices ? reinterpret_cast<const uint4*>(src)[kk * 32 + lane] : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto put_state = [&](const float* ratios, const uint4 (&x)[QS], int sl0) {
+#pragma unroll
+            for (int q = 0; q < QS; ++q) {
+                const int i = warp + 16 * q, kk = i % (DK / 16), sl = i / (DK / 16) % SL, term = i / (DK / 16) / SL;
+                put(st_s + term * TS, DK, sl * 16 + g, kk * 2, x[q], ratios[(sl0 + sl) & 7]);
+            }
+        };
+        uint4 raw_s[QS], raw_e[QT], raw_p[QT];
         auto stage_do = [&](int d0) {  // [64 tokens][ROWS value rows]
 #pragma unroll
             for (int q = 0; q < 64 * ROWS / 8 / 512 + (64 * ROWS / 8 < 512); ++q) {
@@ -913,10 +927,14 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
         };
         float sg[2][4] = {}, kp[2][4] = {}, aq[NT][4] = {}, ak[NT][4] = {};
         for (int sl0 = 0; sl0 < a.l.slices; sl0 += SL) {
-            stage_state(a.l.S, KT == 2 ? a.l.S_lo : 0, 1, a.l.s_inv, iS, sl0);
-            stage_tok(a.l.e, a.l.e_inv, 2, iu, st_u, sl0);
-            stage_tok(a.l.dp, a.l.dp_inv, KT, ip, st_p, sl0);
+            load_state(a.l.S, KT == 2 ? a.l.S_lo : 0, 1, raw_s, sl0);
+            load_tok(a.l.e, 2, raw_e, sl0);
+            load_tok(a.l.dp, KT, raw_p, sl0);
             stage_do(sl0 * 16);
+            put_state(red + 70, raw_s, sl0);
+            put_tok(red + 38, st_u, raw_e, sl0);
+            put_tok(red + 54, st_p, raw_p, sl0);
+            if (a.l.slices <= SL) load_state(a.l.X, 0, KT, raw_s, 0);  // for behind these products
             __syncthreads();
             const int steps = min(SL, a.l.slices - sl0);
 #pragma unroll 2
@@ -973,7 +991,7 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
             }
         m0 = warp_max(m0); m1 = warp_max(m1);
         if (lane == 0) { red[warp] = m0; red[16 + warp] = m1; }
-        if (a.l.slices <= SL) stage_state(a.l.X, 0, KT, a.l.x_inv, iX, 0);  // everything has been read
+        if (a.l.slices <= SL) put_state(red + 78, raw_s, 0);  // everything has been read
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 16; ++i) { m0 = fmaxf(m0, red[i]); m1 = fmaxf(m1, red[16 + i]); }
@@ -1007,8 +1025,10 @@ __global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba,
         // eta D_end X^T e
         for (int sl0 = 0; sl0 < a.l.slices; sl0 += SL) {
             if (a.l.slices > SL) {
-                stage_tok(a.l.e, a.l.e_inv, 2, iu, st_u, sl0);
-                stage_state(a.l.X, 0, KT, a.l.x_inv, iX, sl0);
+                load_tok(a.l.e, 2, raw_e, sl0);
+                load_state(a.l.X, 0, KT, raw_s, sl0);
+                put_tok(red + 38, st_u, raw_e, sl0);
+                put_state(red + 78, raw_s, sl0);
             }
             __syncthreads();
             const int steps = min(SL, a.l.slices - sl0);

@@ -103,6 +103,8 @@ SHAPES = [  # B, H, Hk, L, dk, dv
     (1, 1, 1, 1, 64, 64), (1, 2, 1, 31, 128, 128), (2, 2, 2, 32, 64, 64), (1, 3, 3, 33, 128, 128), (1, 4, 2, 64, 72, 100), (1, 2, 2, 65, 128, 16),
     (2, 6, 2, 97, 72, 100), (1, 1, 1, 200, 128, 128), (1, 2, 1, 130, 1, 1), (1, 1, 1, 70, 17, 33), (3, 5, 5, 129, 65, 127), (9, 16, 4, 96, 64, 64),
     (1, 13, 13, 128, 128, 128),
+    # more slices than SMs: a warp for all of a slice's columns, four slices (two with fp32) or fewer in a CTA, the last CTA not full
+    (2, 16, 16, 70, 128, 128), (3, 16, 4, 100, 128, 100), (5, 8, 2, 96, 96, 80),
 ]
 
 
