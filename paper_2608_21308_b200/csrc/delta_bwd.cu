@@ -723,13 +723,14 @@ __global__ void __launch_bounds__(kDeltaSuper * 64) delta_gate_kernel(const Delt
 // columns each.  The value rows come through shared memory ROWS at a time, with S_0 (dQ's and dK's first part, both token-by-token matrices) and
 // again with X; what the chains left in fragment order goes into tiles of rows here, at one scale for all slices.  With bf16 I/O one term of every
 // operand serves: dQ and dK are off by 2^-11 of their terms before they are rounded to 2^-8.
-template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? 128 : 32; }
+template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? DK : 32; }
+template <int DK, int KT> constexpr int qk_ctas() { return KT == 1 && DK == 64 ? 2 : 1; }  // per SM
 template <int DK, int KT> constexpr int qk_smem() {
     return 2 * KT * 128 * DK + KT * qk_rows<DK, KT>() * (2 * DK + 3 * 128) + 2 * KT * 8192 + 64 * 8 + 3 * 256 + 384;
 }
 
 template <typename IO, int DK, int KT>
-__global__ void __launch_bounds__(512, 1) delta_qk_kernel(const DeltaBwdArgs ba, const bool vec) {
+__global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const DeltaBwdArgs ba, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
     constexpr int ROWS = qk_rows<DK, KT>(), SL = ROWS / 16;  // value rows and slices at a time
     constexpr int TS = ROWS * DK * 2, TT = ROWS * 128;       // bytes of a term: state tile [ROWS][DK]; token tiles [ROWS][64], [64][ROWS]
