@@ -356,8 +356,16 @@ def e2ttt_delta_workspace_bytes(p: e2ttt_delta_params, save_states: int) -> int:
     return int(n.value)
 
 
+_one_device = None
+
+
 def _here(*tensors):
     """A call runs on the current device: tensors of another one are refused."""
+    global _one_device
+    if _one_device is None:
+        _one_device = torch.cuda.device_count() == 1
+    if _one_device:
+        return
     dev = torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:

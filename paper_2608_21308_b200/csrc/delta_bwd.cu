@@ -6,6 +6,7 @@
 // no difference of nearly equal sums over keys is formed.  Sums run over 128 tokens, <X, S> is taken behind each of them.
 // The chain walks the chunks from the last to the first as the forward does, a warp per 16 value rows; dQ and dK contract over the
 // value rows of all warps and are left to a kernel that takes the blocks side by side.
+#include "api_checks.h"
 #include "delta_common.cuh"
 
 namespace e2ttt {
@@ -1106,10 +1107,10 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
 }
 
 template <typename IO, int DK, int KT, int KS> int launch_chain(const DeltaBwdArgs& b, int per, bool vec, cudaStream_t st) {
-    static_assert(chain_smem<DK, KT, KS>(KS > 1 ? 1 : KT == 1 ? 4 : 2) <= 226 * 1024, "shared memory of the chain");
+    static_assert(chain_smem<DK, KT, KS>(KS > 1 ? 1 : KT == 1 ? 4 : 2) <= kMostSharedMemory, "shared memory of the chain");
     const int bytes = chain_smem<DK, KT, KS>(per);
     auto kernel = delta_chain_kernel<IO, DK, KT, KS>;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    const cudaError_t e = allow_shared_memory<delta_chain_kernel<IO, DK, KT, KS>>();
     if (e != cudaSuccess) return (int)e;
     kernel<<<(unsigned)(b.f.l.N * ((b.f.l.slices + per - 1) / per)), per * (KS + 1) * 32, bytes, st>>>(b, per, vec);
     return (int)cudaGetLastError();
@@ -1132,9 +1133,9 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
     }
     {
         constexpr int bytes = qk_smem<DK, KT>();
-        static_assert(bytes <= 227 * 1024, "shared memory of the dq / dk kernel");
+        static_assert(bytes <= kMostSharedMemory, "shared memory of the dq / dk kernel");
         auto kernel = delta_qk_kernel<IO, DK, KT>;
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        cudaError_t e = allow_shared_memory<delta_qk_kernel<IO, DK, KT>>();
         if (e != cudaSuccess) return (int)e;
         const bool vec = a.s.dv % 8 == 0 && reinterpret_cast<uintptr_t>(b.d_o) % 16 == 0;
         kernel<<<(unsigned)(a.l.Nk * a.l.nblk), 512, bytes, st>>>(b, vec);

@@ -9,6 +9,7 @@
 // A chain is bound by the instructions of a chunk one after the other (an MMA every 8 cycles, 146 of them, and splitting the operands into
 // terms), so scales are one per slice, folded into the scalars that the values are multiplied with anyway, and come from bounds that are known
 // before the values are.
+#include "api_checks.h"
 #include "delta_common.cuh"
 
 namespace e2ttt {
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const DeltaArgs& a, int per, cudaStream_t st) {
     auto kernel = delta_fwd_kernel<IO, DK, KT, KS, PREC>;
     const int bytes = fwd_smem<DK, KT, KS, PREC>(per);
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    cudaError_t e = allow_shared_memory<delta_fwd_kernel<IO, DK, KT, KS, PREC>>();
     if (e != cudaSuccess) return (int)e;
     const unsigned grid = (unsigned)(a.l.N * ((a.l.slices + per - 1) / per));
     const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o)) % 16 == 0;
@@ -624,7 +625,7 @@ template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const Delta
 
 template <typename IO, int DK, int KT, bool PREC> int dispatch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int most = KT == 1 ? 4 : 2;
-    static_assert(fwd_smem<DK, KT, 1, PREC>(most) <= 226 * 1024 && fwd_smem<DK, KT, DK / 32, PREC>(1) <= 226 * 1024, "shared memory");
+    static_assert(fwd_smem<DK, KT, 1, PREC>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32, PREC>(1) <= kMostSharedMemory, "shared memory");
     if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, PREC>(a, 1, st);
     int per = most;
     while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;

@@ -2,6 +2,7 @@
 // It writes the chunk's queries and keys as fp16 tiles (scaled by powers of two, zero-padded, swizzled: the kernels that walk the chunks fetch
 // them with bulk copies whatever the caller's width and alignment), and for every value head of the group the record of delta.h:
 // T, A and the products of the decays.  All chunks run side by side.
+#include "api_checks.h"
 #include "delta_common.cuh"
 
 namespace e2ttt {
@@ -356,7 +357,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
 template <typename IO, int DK, int KT> int launch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int bytes = kWarps * prep_warp_bytes<DK, KT>();
     auto kernel = delta_prep_kernel<IO, DK, KT>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    cudaError_t e = allow_shared_memory<delta_prep_kernel<IO, DK, KT>>();
     if (e != cudaSuccess) return (int)e;
     const bool vec = a.s.dk % 8 == 0 && (reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k)) % 16 == 0;
     const unsigned grid = (unsigned)((a.l.Nk * a.l.nch + kWarps - 1) / kWarps);

@@ -461,7 +461,7 @@ Shape shape_of(const JoinArgs& a, int V, int NC, int tensors, int room) {
 
 template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a, const Shape& s, cudaStream_t st) {
     auto kernel = join_fwd_kernel<IO, V, NC, TMAX>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+    cudaError_t e = allow_shared_memory<join_fwd_kernel<IO, V, NC, TMAX>>();
     if (e != cudaSuccess) return (int)e;
     const int64_t tokens = (int64_t)a.B * a.L, most = 148 * (1024 / s.threads > 16 ? 16 : 1024 / s.threads);
     kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a, s.depth);
@@ -469,7 +469,7 @@ template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a
 }
 template <typename IO, int V, int NC, int TMAX> int launch_bwd(const JoinBwdArgs& b, const Shape& s, cudaStream_t st) {
     auto kernel = join_bwd_kernel<IO, V, NC, TMAX>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+    cudaError_t e = allow_shared_memory<join_bwd_kernel<IO, V, NC, TMAX>>();
     if (e != cudaSuccess) return (int)e;
     const int grid = join_bwd_grid((int64_t)b.f.B * b.f.L, b.f.H * b.f.d);
     kernel<<<grid, s.threads, s.smem, st>>>(b, s.depth);
