@@ -526,6 +526,7 @@ int check(const e2ttt_join_params* p) {
     if (!p) return E2TTT_ERR_NULL;
     if (p->io_dtype != E2TTT_F32 && p->io_dtype != E2TTT_BF16) return E2TTT_ERR_DTYPE;
     if (p->B <= 0 || p->H <= 0 || p->L <= 0 || p->d <= 0) return E2TTT_ERR_SHAPE;
+    if (p->L > (1 << 30)) return E2TTT_ERR_SHAPE;  // positions are stepped on in 32 bits
     if ((int64_t)p->H * p->d > kJoinMaxWidth || (int64_t)p->B * p->L > (int64_t)1 << 40) return E2TTT_ERR_SHAPE;
     if (p->gate != E2TTT_GATE_NONE && p->gate != E2TTT_GATE_SIGMOID && p->gate != E2TTT_GATE_SILU) return E2TTT_ERR_SHAPE;
     if (!(p->post_eps >= 0.0f) || !(p->pre_eps >= 0.0f)) return E2TTT_ERR_SHAPE;

@@ -20,7 +20,7 @@ WS = vp(0x100000)
 
 
 @pytest.mark.parametrize("field,value,status", [
-    ("B", 0, -2), ("H", 0, -2), ("L", 0, -2), ("d", 0, -2), ("d", 8193, -2), ("H", 129, -2), ("io_dtype", 3, -3), ("gate", 3, -2),
+    ("B", 0, -2), ("H", 0, -2), ("L", 0, -2), ("L", (1 << 30) + 1, -2), ("d", 0, -2), ("d", 8193, -2), ("H", 129, -2), ("io_dtype", 3, -3), ("gate", 3, -2),
     ("post_eps", -1.0, -2), ("pre_eps", float("nan"), -2),
 ])
 def test_bad_parameters(L, field, value, status):
