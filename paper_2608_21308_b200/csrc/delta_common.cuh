@@ -2,11 +2,13 @@
 //
 // Products run as mma.m16n8k16 with fp16 operands and fp32 sums.  A state is cut into slices of 16 value rows, one warp each: the slice
 // stays in a warp's accumulators for the whole sequence, an accumulator tile is the next product's A operand as it is, and no value
-// crosses a warp.  A 128-lane tensor-memory tile would hold one sequence per SM and send the state through tensor memory and back
-// between any two of the four dependent products of a chunk.
-// Operands in 32 bits are used as two fp16 terms, x = 2^-s (hi + lo): 22 bits, and s (a power of two per row or tile, from its largest
-// value) keeps both terms inside fp16's exponents.  What is bf16 on input is one term, exactly.  (Two bf16 terms, 16 bits, leave 3e-6
-// in every product: the fp32 outputs would be ten times less exact.)
+// crosses a warp.  Measured on B200: an m16n8k16 takes 8.1 cycles of its scheduler (1024 multiply-adds per cycle and SM), its result 21, and
+// other arithmetic does not run beside it (one MMA and four FMAs take 12.1 cycles, with six 14.1), so a chain of dependent chunks is bound by what
+// its warp issues.  A 128-row tensor-memory tile would hold one sequence per SM (64 sequences: 64 of 148 SMs), and send the state through tensor
+// memory and back, and through the splitting into terms, between any two of the four dependent products of a chunk.
+// Operands in 32 bits are used as two fp16 terms, x = 2^-s (hi + lo): 22 bits, and s (a power of two per slice or tile, from its largest
+// value or a bound on it) keeps both terms inside fp16's exponents.  What is bf16 on input is one term, exactly down to 2^-24 of its tile's largest
+// value.  (Two bf16 terms, 16 bits, leave 3e-6 in every product: the fp32 outputs would be ten times less exact.)
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -59,18 +61,15 @@ __device__ __forceinline__ void mul2(float& d0, float& d1, float a0, float a1, f
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(a0, a1)), "l"(pack2(b0, b1)));
     unpack2(r, d0, d1);
 }
-__device__ __forceinline__ float quad_sum(float m) {
-    m += __shfl_xor_sync(kAll, m, 1);
-    return m + __shfl_xor_sync(kAll, m, 2);
+__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pack2(d0, d1)), "l"(pack2(a0, a1)));
+    unpack2(r, d0, d1);
 }
 __device__ __forceinline__ float warp_sum(float m) {
 #pragma unroll
     for (int i = 16; i > 0; i >>= 1) m += __shfl_xor_sync(kAll, m, i);
     return m;
-}
-__device__ __forceinline__ float quad_max(float m) {  // over the four lanes that share a fragment row
-    m = fmaxf(m, __shfl_xor_sync(kAll, m, 1));
-    return fmaxf(m, __shfl_xor_sync(kAll, m, 2));
 }
 __device__ __forceinline__ float warp_max(float m) {
 #pragma unroll

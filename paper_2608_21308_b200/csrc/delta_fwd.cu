@@ -9,6 +9,9 @@
 // A chain is bound by the instructions of a chunk one after the other (an MMA every 8 cycles, 146 of them, and splitting the operands into
 // terms), so scales are one per slice, folded into the scalars that the values are multiplied with anyway, and come from bounds that are known
 // before the values are.
+// 4 x 16 sequences of 4096 tokens, 128 x 128, bf16: 226 us (128 chunks, one after the other: 1.8 us each), 355 us with saved states (540 MB of states,
+// errors and fp32 outputs to write, and the outputs' products with both terms); 16 sequences of 32768 tokens: 1180 us (1024 chunks: 1.15 us each,
+// the columns of a slice over four warps); 8 x 12 sequences of 2048 tokens, 64 x 64, with saved states: 135 us.
 #include "api_checks.h"
 #include "delta_common.cuh"
 
@@ -227,13 +230,20 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                     mma0(e[0], h0, th[0][0], th[0][1]); mma0(e[1], h0, th[0][2], th[0][3]);
                     mma0(e[2], h0, th[1][0], th[1][1]); mma0(e[3], h0, th[1][2], th[1][3]);
                     split_a(p[2], p[3], h1, l1);
-                    mma(e[0], l0, th[0][0], th[0][1]); mma(e[1], l0, th[0][2], th[0][3]);
-                    mma(e[2], l0, th[1][0], th[1][1]); mma(e[3], l0, th[1][2], th[1][3]);
-                    mma(e[0], h0, tl[0][0], tl[0][1]); mma(e[1], h0, tl[0][2], tl[0][3]);
-                    mma(e[2], h0, tl[1][0], tl[1][1]); mma(e[3], h0, tl[1][2], tl[1][3]);
+                    // the second terms' products apart: an MMA truncates the sum that it adds to
+                    float t[4][4];
+                    mma0(t[0], l0, th[0][0], th[0][1]); mma0(t[1], l0, th[0][2], th[0][3]);
+                    mma0(t[2], l0, th[1][0], th[1][1]); mma0(t[3], l0, th[1][2], th[1][3]);
                     mma(e[2], h1, th[2][0], th[2][1]); mma(e[3], h1, th[2][2], th[2][3]);
-                    mma(e[2], l1, th[2][0], th[2][1]); mma(e[3], l1, th[2][2], th[2][3]);
-                    mma(e[2], h1, tl[2][0], tl[2][1]); mma(e[3], h1, tl[2][2], tl[2][3]);
+                    mma(t[0], h0, tl[0][0], tl[0][1]); mma(t[1], h0, tl[0][2], tl[0][3]);
+                    mma(t[2], h0, tl[1][0], tl[1][1]); mma(t[3], h0, tl[1][2], tl[1][3]);
+                    mma(t[2], l1, th[2][0], th[2][1]); mma(t[3], l1, th[2][2], th[2][3]);
+                    mma(t[2], h1, tl[2][0], tl[2][1]); mma(t[3], h1, tl[2][2], tl[2][3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        add2(e[j][0], e[j][1], t[j][0], t[j][1]);
+                        add2(e[j][2], e[j][3], t[j][2], t[j][3]);
+                    }
                 }
                 // e times qe is the error itself.  It goes to the outputs' warp, eta D_end e into the state, each with a scale of its own;
                 // the state moves to its next scale on the way
@@ -568,11 +578,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         if (lane != 0) return;
         const size_t at = ((size_t)n * (a.l.nblk + 1) + slot) * a.l.slices + slice;
         bulk_store(a.ws + a.l.S + at * a.l.state_bytes, sm100::smem_u32(x.s[0]), (uint32_t)a.l.state_bytes);
-        const int lo = delta_lo_slot(slot, a.l.nblk, s.f32);
-        if (lo >= 0) {
-            const size_t to = s.f32 ? at : ((size_t)n * a.l.nsup + lo) * a.l.slices + slice;
-            bulk_store(a.ws + a.l.S_lo + to * a.l.state_bytes, sm100::smem_u32(x.s[PREC ? 1 : 0]), (uint32_t)a.l.state_bytes);
-        }
+        if (slot > 0 || KT == 2)  // with bf16 the start state's second term enters no inner product
+            bulk_store(a.ws + a.l.S_lo + at * a.l.state_bytes, sm100::smem_u32(x.s[PREC ? 1 : 0]), (uint32_t)a.l.state_bytes);
         reinterpret_cast<float*>(a.ws + a.l.s_inv)[at] = x.s_inv;
     };
     auto save_e = [&](int c, const X& x) {
@@ -626,6 +633,10 @@ template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const Delta
 template <typename IO, int DK, int KT, bool PREC> int dispatch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int most = KT == 1 ? 4 : 2;
     static_assert(fwd_smem<DK, KT, 1, PREC>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32, PREC>(1) <= kMostSharedMemory, "shared memory");
+    // Few slices, as many as SMs at most: one per CTA, its columns over DK / 32 warps; with more of them the warps share an SM's schedulers and a chain
+    // per warp is faster.  Then slices of a sequence share the tiles that they fetch, as long as 96 CTAs are left.  Forward and reverse pass
+    // together, us: 8 x 12 x 2048 tokens, 64 x 64, bf16: 4 slices per CTA 554, 2: 563, 1: 647, one over two warps 744.  Forward alone, 128 x 128,
+    // 16 heads x 4096 tokens: B = 4: 4 slices 310, 2: 421; B = 2: 2 slices 220, 4: 269.  fp32 tiles leave room for two.
     if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, PREC>(a, 1, st);
     int per = most;
     while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
