@@ -269,13 +269,18 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  *   S            [B,H,dv,dk] fp32           rows are outputs, as in the fast-weight matrices
  * e2ttt_delta_fwd runs whole sequences in chunks of 32 tokens on the tensor cores; e2ttt_delta_step is the recurrent form for a few
  * tokens (decoding), without a workspace; both move the same state and may follow each other.
- * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly; outputs are rounded once.  A NaN or an
- * infinity at one token reaches all outputs and gradients of its chunk of 32 tokens (of its block of 64 in the reverse pass) and what follows it.
+ * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly; outputs are rounded once.  Bits are counted
+ * from the largest value of a chunk's queries or keys, of 16 neighbouring value rows of a state: a value 2^-10 of it has 10 bits fewer.  bf16
+ * outputs without saved states, and bf16 dq and dk, are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.
+ * Magnitudes should stay below 2^100.  A NaN or an infinity at one token of a sequence makes all outputs of its chunk of 32 tokens and what follows
+ * them (NaN or without meaning), and in the reverse pass all gradients of its block of 64 tokens and what depends on them; tokens before its chunk,
+ * and other heads with queries and keys of their own, keep their outputs bit for bit.
+ * Calls that may run at the same time need workspaces of their own; calls one after the other may share one (but for saved states in it).
  * Arguments are refused as everywhere: E2TTT_ERR_NULL / _SHAPE / _DTYPE / _WORKSPACE / _ALIGN / _ARCH / _CUDA.  Tensors need the
  * alignment of their elements only; 16 bytes, and widths that are a multiple of 8, load faster. */
 typedef struct {
     int32_t B, H, Hk; /* batch, value heads, query / key heads (H a multiple of Hk) */
-    int32_t L;        /* tokens per sequence, any number */
+    int32_t L;        /* tokens per sequence, 1 .. 2^30, no multiple of anything; B H L up to 2^35 */
     int32_t dk, dv;   /* widths of a query / key and of a value, 1..128 */
     int32_t io_dtype; /* e2ttt_dtype of q, k, v, o and their gradients */
     float scale;      /* of the outputs; 1 / sqrt(dk) is usual, 1 for the library's normalised queries */
@@ -313,7 +318,7 @@ E2TTT_API int e2ttt_delta_step(const e2ttt_delta_params* p, const void* q, const
  *   a, x, x_out, n           [B,L,H d] io_dtype, head h at columns h d .. (h + 1) d
  *   w_post, res_scale, w_pre [H d] fp32
  * a is NULL with E2TTT_GATE_NONE and required otherwise; w_pre and n_out (d_n, d_w_pre) are given together or not at all (no second norm).
- * x_out may alias x, n_out may alias a.  H d <= 8192.  fp32 arithmetic, each output rounded once; n is of the unrounded x_out.
+ * x_out may alias x, n_out may alias a.  H d <= 8192, L <= 2^30.  fp32 arithmetic, each output rounded once; n is of the unrounded x_out.
  * Returns E2TTT_OK or E2TTT_ERR_NULL / _SHAPE / _DTYPE / _ALIGN / _WORKSPACE / _ARCH / _CUDA; alignment as for e2ttt_delta_fwd. */
 typedef enum { E2TTT_GATE_NONE = 0, E2TTT_GATE_SIGMOID = 1, E2TTT_GATE_SILU = 2 } e2ttt_gate;
 typedef struct {

@@ -276,6 +276,114 @@ def test_two_streams_with_workspaces_of_their_own():
         check({"o": r.o, "S": r.S_out}, {"o": o, "S": S}, dict(x, scale=1.0))
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("eta", [1.0, 1.5])
+def test_one_key_in_all_tokens(io, eta):
+    """What is written is read, and taken out, by every token: T's rows alternate in sign, their magnitudes sum to 1 + eta / (1 - |1 - eta|) <= 4,
+    which times the operands' 2^-22 and the three products in a row stays below the tolerance."""
+    x, d = _make(1, 2, 1, 100, 64, 48, io, seed=14)
+    x["k"][:] = x["k"][:, :, :1]
+    x["eta"][:], x["log_gamma"][:] = eta, 0
+    o, S = O.forward(**x, scale=1.0)
+    r = Run(x, io, 1.0)
+    check(r.fwd(1), {"o": o, "S": S})
+    check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
+
+
+def test_gradient_of_the_start_state_over_that_of_the_end():
+    x, d = _make(3, 16, 4, 100, 128, 100, "bf16", seed=15)
+    r = Run(x, "bf16", 1.0)
+    r.fwd(1)
+    want = r.bwd(d)
+    dS = _dev(d["dS_final"])
+    out = {n: torch.empty_like(t) for n, t in want.items()}
+    out["dS"] = dS
+    E.e2ttt_delta_bwd(r.p, r.q, r.k, r.v, r.eta, r.lg, r.S, _dev(d["d_o"], "bf16"), dS, *out.values(), r.ws, 1)
+    for n in want:
+        assert torch.equal(out[n], want[n]), n
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("shape", [(1, 3, 3, 300, 64, 64), (4, 16, 16, 300, 128, 64)])  # the columns of a slice over two warps; one warp per slice
+def test_a_value_that_is_not_finite(io, bad, shape):
+    """It reaches its own chunk and what follows it, nothing before it and no other head."""
+    x, d = _make(*shape, io, seed=16)
+    clean = Run(x, io, 1.0)
+    good, grads = clean.fwd(1), clean.bwd(d)
+    for name in ("v", "k", "eta"):
+        r = Run(x, io, 1.0)
+        t = getattr(r, name)
+        t[0, 1, 170] = bad
+        got = r.fwd(1)
+        assert not torch.isfinite(got["o"][0, 1, 170]).all() or not torch.isfinite(got["o"][0, 1, 171]).all()
+        assert torch.equal(got["o"][0, 1, :160], good["o"][0, 1, :160])
+        back = r.bwd(d)
+        for m in (0, 2):
+            assert torch.equal(got["o"][0, m], good["o"][0, m]) and torch.equal(got["S"][0, m], good["S"][0, m])
+            for n in back:
+                assert torch.equal(back[n][0, m], grads[n][0, m]), (name, n)
+
+
+def test_more_than_two_to_the_31_elements():
+    """The last head starts 2^31 elements into q, k, v and o; it has to come out as it does alone."""
+    H, L, d = 17, 1 << 20, 128
+    g = torch.Generator(device="cuda").manual_seed(0)
+    p = E.make_delta_params(1, H, H, L, d, d, E.E2TTT_BF16, 1.0)
+    one = E.make_delta_params(1, 1, 1, L, d, d, E.E2TTT_BF16, 1.0)
+    q, k, v = (torch.zeros(1, H, L, d, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    eta, lg = torch.zeros(1, H, L, device="cuda"), torch.zeros(1, H, L, device="cuda")
+    for t in (q, k, v):
+        t[:, -1] = torch.randn(1, L, d, device="cuda", generator=g) / d ** 0.5
+    eta[:, -1], lg[:, -1] = torch.rand(1, L, device="cuda", generator=g), -torch.rand(1, L, device="cuda", generator=g)
+    o, S = torch.empty_like(v), torch.empty(1, H, d, d, device="cuda")
+    ws = torch.empty(E.e2ttt_delta_workspace_bytes(p, 0), dtype=torch.uint8, device="cuda")
+    E.e2ttt_delta_fwd(p, q, k, v, eta, lg, None, o, S, ws, 0)
+    last = [t[:, -1:] for t in (q, k, v, eta, lg)]
+    o1, S1 = torch.empty_like(last[2]), torch.empty(1, 1, d, d, device="cuda")
+    E.e2ttt_delta_fwd(one, *last, None, o1, S1, ws, 0)
+    assert torch.equal(o[:, -1:], o1) and torch.equal(S[:, -1:], S1)
+    assert (o[:, :-1] == 0).all() and bool((o1 != 0).any())
+
+
+def test_a_workspace_of_more_than_two_to_the_32_bytes():
+    """The same for what the reverse pass keeps of the sequences."""
+    H, L, d = 17, 1 << 17, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    q, k, v, d_o = ((rnd(1, H, L, d) / d ** 0.5).bfloat16() for _ in range(4))
+    eta, lg = torch.rand(1, H, L, device="cuda", generator=g), -torch.rand(1, H, L, device="cuda", generator=g)
+
+    def run(h):
+        p = E.make_delta_params(1, h, h, L, d, d, E.E2TTT_BF16, 1.0)
+        x = [t[:, -h:] for t in (q, k, v, eta, lg)]
+        n = E.e2ttt_delta_workspace_bytes(p, 1)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        S = torch.empty(1, h, d, d, device="cuda")
+        out = [torch.empty_like(t) for t in x] + [S.clone()]
+        E.e2ttt_delta_bwd(p, *x, None, d_o[:, -h:], None, *out, ws, 0)
+        assert E.e2ttt_device_status(ws) == 0
+        return n, out
+
+    (n, all_), (_, last) = run(H), run(1)
+    assert n > 1 << 32
+    for a, b in zip(all_, last):
+        assert torch.equal(a[:, -1:], b)
+
+
+def test_step_with_more_than_two_to_the_31_values_of_state():
+    B, H, d = 8200, 16, 128
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    S = torch.empty(B, H, d, d, device="cuda")
+    S[:-1], S[-1] = 0, rnd(H, d, d)
+    x = [(rnd(B, H, 1, d) / d ** 0.5).bfloat16() for _ in range(3)] + [torch.rand(B, H, 1, device="cuda", generator=g), -torch.rand(B, H, 1, device="cuda", generator=g)]
+    one, o, o1, S1 = [t[-1:].contiguous() for t in x], torch.empty_like(x[2]), torch.empty_like(x[2][-1:]), S[-1:].clone()
+    E.e2ttt_delta_step(E.make_delta_params(1, H, H, 1, d, d, E.E2TTT_BF16, 1.0), *one, S1, o1, S1)
+    E.e2ttt_delta_step(E.make_delta_params(B, H, H, 1, d, d, E.E2TTT_BF16, 1.0), *x, S, o, S)
+    assert torch.equal(o[-1:], o1) and torch.equal(S[-1:], S1)
+
+
 def test_prepared_tokens_run_through_the_rule_and_back():
     """e2ttt_prepare_fwd's queries, keys, eta and gamma (its logarithm) are what the rule takes."""
     B, H, L, d = 1, 2, 75, 64

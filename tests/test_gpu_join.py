@@ -140,6 +140,22 @@ def test_a_token_does_not_depend_on_the_others():
             assert torch.equal(t, grads[n][1:2]), n
 
 
+def test_more_than_two_to_the_31_elements():
+    """The last tokens lie 2^31 elements into every tensor; they have to come out as they do alone."""
+    H, L, d, n = 16, (1 << 20) + 64, 128, 64
+    g = torch.Generator(device="cuda").manual_seed(0)
+    o, a, x = (torch.zeros(*s, device="cuda", dtype=torch.bfloat16) for s in ((1, H, L, d), (1, L, H * d), (1, L, H * d)))
+    for t in (o[:, :, -n:], a[:, -n:], x[:, -n:]):
+        t.copy_(torch.randn(t.shape, device="cuda", generator=g))
+    w = [1 + 0.1 * torch.randn(H * d, device="cuda", generator=g) for _ in range(3)]
+    xo, no = torch.empty_like(x), torch.empty_like(x)
+    E.e2ttt_join_fwd(E.make_join_params(1, H, L, d, E.E2TTT_BF16, E.E2TTT_GATE_SILU, **EPS), o, a, x, *w, xo, no)
+    tail = [t.contiguous() for t in (o[:, :, -n:], a[:, -n:], x[:, -n:])]
+    x1, n1 = torch.empty_like(tail[2]), torch.empty_like(tail[2])
+    E.e2ttt_join_fwd(E.make_join_params(1, H, n, d, E.E2TTT_BF16, E.E2TTT_GATE_SILU, **EPS), *tail, *w, x1, n1)
+    assert torch.equal(xo[:, -n:], x1) and torch.equal(no[:, -n:], n1)
+
+
 def test_graph_replay_and_a_side_stream():
     x, d = _make(2, 4, 33, 64, "bf16", "silu", True, seed=4)
     y, _ = _make(2, 4, 33, 64, "bf16", "silu", True, seed=5)
