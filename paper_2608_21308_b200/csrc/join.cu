@@ -68,7 +68,7 @@ struct Stride {
 
 // Sums over a token's heads and over the token.  `cols` pieces of V values; a head has G of them.
 struct Sums {
-    float *part, *head, *row;  // shared memory: [cols], [H], [2][2][32]
+    float *part, *head, *row;  // shared memory: [cols], [H], [2][2][16]
     int cols, G, H, T, flip;
     bool lanes;                // a head is an aligned group of G lanes
 };
@@ -100,27 +100,33 @@ template <int NC> __device__ __forceinline__ void head_sums(Sums& s, float (&v)[
         if (tid + i * s.T < s.cols) v[i] = s.head[(tid + i * s.T) / s.G];
 }
 
-// sums of u and v over the CTA's threads, in a fixed order; two buffers in turn, so that one barrier is enough
-__device__ __forceinline__ void row_sums(Sums& s, float& u, float& v) {
+// sums of u[0] (and u[1]) over the CTA's threads, in a fixed order; two buffers in turn, so that one barrier is enough.  A warp's lanes 0-15 read the
+// warps' first sums, lanes 16-31 the second ones.
+template <int N> __device__ __forceinline__ void row_sums(Sums& s, float (&u)[N]) {
 #pragma unroll
-    for (int x = 16; x > 0; x >>= 1) {
-        u += __shfl_xor_sync(kAll, u, x);
-        v += __shfl_xor_sync(kAll, v, x);
-    }
-    const int warps = s.T >> 5;
+    for (int x = 16; x > 0; x >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) u[k] += __shfl_xor_sync(kAll, u[k], x);
+    const int warps = s.T >> 5, lane = threadIdx.x & 31;
     if (warps == 1) return;
-    float* b = s.row + s.flip * 64;
+    float* b = s.row + s.flip * 32;
     s.flip ^= 1;
-    if ((threadIdx.x & 31) == 0) { b[threadIdx.x >> 5] = u; b[32 + (threadIdx.x >> 5)] = v; }
+    if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) b[16 * k + (threadIdx.x >> 5)] = u[k];
+    }
     __syncthreads();
-    u = v = 0.0f;
-    for (int i = 0; i < warps; ++i) { u += b[i]; v += b[32 + i]; }
+    float y = (lane & 15) < warps ? b[N == 1 ? lane & 15 : lane] : 0.0f;
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) y += __shfl_xor_sync(kAll, y, x);
+    u[0] = N == 1 ? y : __shfl_sync(kAll, y, 0);
+    if (N == 2) u[N - 1] = __shfl_sync(kAll, y, 16);
 }
 
 __device__ __forceinline__ Sums make_sums(char* smem, int cols, int G, int H) {
     Sums s;
     s.row = reinterpret_cast<float*>(smem);
-    s.part = s.row + 128;
+    s.part = s.row + 64;
     s.head = s.part + cols;
     s.cols = cols; s.G = G; s.H = H; s.T = blockDim.x; s.flip = 0;
     s.lanes = G <= 32 && (G & (G - 1)) == 0;
@@ -206,7 +212,7 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
             }
         }
         head_sums<NC>(sums, hs);
-        float s2 = 0.0f, none = 0.0f;
+        float sum[1] = {0.0f};  // of x_out^2
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
@@ -224,11 +230,11 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 y[i][j] = fmaf(wr.x[j] * inv, y[i][j] * wp.x[j], ldf(px.x[j]));
-                s2 = fmaf(y[i][j], y[i][j], s2);
+                sum[0] = fmaf(y[i][j], y[i][j], sum[0]);
             }
         }
-        if (a.w_pre) row_sums(sums, s2, none);
-        const float m = rsqrtf(fmaf(s2, per_D, a.pre_eps));
+        if (a.w_pre) row_sums<1>(sums, sum);
+        const float m = rsqrtf(fmaf(sum[0], per_D, a.pre_eps));
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
             }
         }
         head_sums<NC>(sums, hs);
-        float s2 = 0.0f, sd = 0.0f;
+        float sum[2] = {0.0f, 0.0f};  // of x_out^2 and of dn w x_out
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int c = tid + i * T;
@@ -331,19 +337,19 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
             for (int j = 0; j < V; ++j) {
                 y[i][j] *= inv[i];
                 xo[i][j] = fmaf(wr.x[j] * xo[i][j], y[i][j] * wp.x[j], ldf(px.x[j]));
-                s2 = fmaf(xo[i][j], xo[i][j], s2);
+                sum[0] = fmaf(xo[i][j], xo[i][j], sum[0]);
             }
             if (a.w_pre) {
                 const Weights<V> w = weights<V>(a.w_pre, c);
 #pragma unroll
-                for (int j = 0; j < V; ++j) sd = fmaf(ldf(pn.x[j]) * w.x[j], xo[i][j], sd);
+                for (int j = 0; j < V; ++j) sum[1] = fmaf(ldf(pn.x[j]) * w.x[j], xo[i][j], sum[1]);
             }
         }
         float m = 0.0f, mean = 0.0f;
         if (a.w_pre) {
-            row_sums(sums, s2, sd);
-            m = rsqrtf(fmaf(s2, per_D, a.pre_eps));
-            mean = sd * m * per_D;
+            row_sums<2>(sums, sum);
+            m = rsqrtf(fmaf(sum[0], per_D, a.pre_eps));
+            mean = sum[1] * m * per_D;
         }
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -456,7 +462,7 @@ Shape shape_of(const JoinArgs& a, int V, int NC, int tensors, int room) {
     const bool lanes = G <= 32 && (G & (G - 1)) == 0;
     int depth = room / stage;
     depth = depth > 4 ? 4 : (depth < 1 ? 1 : depth);
-    return {t, depth, depth * stage + (128 + (lanes ? 0 : cols + a.H)) * 4};
+    return {t, depth, depth * stage + (64 + (lanes ? 0 : cols + a.H)) * 4};
 }
 
 template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a, const Shape& s, cudaStream_t st) {
