@@ -158,8 +158,12 @@ template <int V> struct alignas(V >= 4 ? 16 : 4 * V) Weights {
 };
 template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, int c) { return reinterpret_cast<const Weights<V>*>(w)[c]; }
 
+// Whether a thread of the forward keeps its weights in registers from token to token (three CTAs of 256 threads on an SM instead of four).  16384 tokens
+// of 2048 in bf16: 65 us with them, 72 without; fp32, whose threads take two pieces of four, 8 x 2048 tokens of 768: 41 and 35.
+template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256; }
+
 template <typename IO, int V, int NC, int TMAX>
-__global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinArgs a, const int depth) {
+__global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_fwd_kernel(const JoinArgs a, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
@@ -191,6 +195,15 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
         stride.move(ahead);
         copy_commit();
     };
+    Weights<V> wrs[NC], wps[NC], wns[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = tid + i * T;
+        if (!kept<V, TMAX>() || c >= cols) continue;
+        wrs[i] = weights<V>(a.res_scale, c);
+        wps[i] = weights<V>(a.w_post, c);
+        if (a.w_pre) wns[i] = weights<V>(a.w_pre, c);
+    }
     int64_t tok = blockIdx.x;
     for (int i = 0; i + 1 < depth; ++i) load(tok + i * (int64_t)gridDim.x, i);
     int slot = 0;
@@ -219,7 +232,7 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
             if (c >= cols) continue;
             const float inv = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
             const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T];
-            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
+            const Weights<V> wr = kept<V, TMAX>() ? wrs[i] : weights<V>(a.res_scale, c), wp = kept<V, TMAX>() ? wps[i] : weights<V>(a.w_post, c);
             if (a.a) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
@@ -244,7 +257,7 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
             for (int j = 0; j < V; ++j) stf(xo.x[j], y[i][j]);
             reinterpret_cast<P*>(a.x_out)[tok * cols + c] = xo;
             if (a.w_pre) {
-                const Weights<V> w = weights<V>(a.w_pre, c);
+                const Weights<V> w = kept<V, TMAX>() ? wns[i] : weights<V>(a.w_pre, c);
 #pragma unroll
                 for (int j = 0; j < V; ++j) stf(nn.x[j], y[i][j] * m * w.x[j]);
                 reinterpret_cast<P*>(a.n_out)[tok * cols + c] = nn;
@@ -254,9 +267,10 @@ __global__ void __launch_bounds__(TMAX, 1024 / TMAX) join_fwd_kernel(const JoinA
 }
 
 template <typename IO, int V, int NC, int TMAX>
-__global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(const JoinBwdArgs ba, const int depth) {
+__global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBwdArgs ba, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
+    constexpr bool KEPT = TMAX == 256;
     const JoinArgs& a = ba.f;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
     P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][5][NC][T]
@@ -295,6 +309,15 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
     for (int i = 0; i < NC; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) R[i][j] = W[i][j] = 0.0f;
+    Weights<V> wrs[NC], wps[NC], wns[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int c = tid + i * T;
+        if (!KEPT || c >= cols) continue;
+        wrs[i] = weights<V>(a.res_scale, c);
+        wps[i] = weights<V>(a.w_post, c);
+        if (a.w_pre) wns[i] = weights<V>(a.w_pre, c);
+    }
     int64_t tok = blockIdx.x;
     for (int i = 0; i + 1 < depth; ++i) load(tok + i * (int64_t)gridDim.x, i);
     int slot = 0;
@@ -323,7 +346,7 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
             if (c >= cols) continue;
             inv[i] = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
             const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T], pn = r[(4 * NC + i) * T];
-            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
+            const Weights<V> wr = KEPT ? wrs[i] : weights<V>(a.res_scale, c), wp = KEPT ? wps[i] : weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) xo[i][j] = 1.0f;
             if (a.a) {
@@ -340,7 +363,7 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
                 sum[0] = fmaf(xo[i][j], xo[i][j], sum[0]);
             }
             if (a.w_pre) {
-                const Weights<V> w = weights<V>(a.w_pre, c);
+                const Weights<V> w = KEPT ? wns[i] : weights<V>(a.w_pre, c);
 #pragma unroll
                 for (int j = 0; j < V; ++j) sum[1] = fmaf(ldf(pn.x[j]) * w.x[j], xo[i][j], sum[1]);
             }
@@ -361,7 +384,7 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
 #pragma unroll
             for (int j = 0; j < V; ++j) dx[j] = ldf(pd.x[j]);
             if (a.w_pre) {
-                const Weights<V> w = weights<V>(a.w_pre, c);
+                const Weights<V> w = KEPT ? wns[i] : weights<V>(a.w_pre, c);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float dn = ldf(pn.x[j]), h = xo[i][j] * m;
@@ -370,7 +393,7 @@ __global__ void __launch_bounds__(TMAX, TMAX == 256 ? 3 : 1) join_bwd_kernel(con
                 }
             }
             P dx_p;
-            const Weights<V> wr = weights<V>(a.res_scale, c), wp = weights<V>(a.w_post, c);
+            const Weights<V> wr = KEPT ? wrs[i] : weights<V>(a.res_scale, c), wp = KEPT ? wps[i] : weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) stf(dx_p.x[j], dx[j]);
             reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
@@ -469,7 +492,8 @@ template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a
     auto kernel = join_fwd_kernel<IO, V, NC, TMAX>;
     cudaError_t e = allow_shared_memory<join_fwd_kernel<IO, V, NC, TMAX>>();
     if (e != cudaSuccess) return (int)e;
-    const int64_t tokens = (int64_t)a.B * a.L, most = 148 * (1024 / s.threads > 16 ? 16 : 1024 / s.threads);
+    constexpr int threads = kept<V, TMAX>() ? 768 : 1024;  // on an SM
+    const int64_t tokens = (int64_t)a.B * a.L, most = 148 * (threads / s.threads > 16 ? 16 : threads / s.threads);
     kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a, s.depth);
     return (int)cudaGetLastError();
 }
@@ -492,7 +516,7 @@ template <typename IO, int V, int NC> int sized(const JoinArgs& a, cudaStream_t 
     return launch_fwd<IO, V, NC, 512>(a, s, st);
 }
 template <typename IO, int V, int NC> int sized(const JoinBwdArgs& b, cudaStream_t st) {
-    const Shape s = shape_of(b.f, V, NC, 5, 72 * 1024);
+    const Shape s = shape_of(b.f, V, NC, 5, 110 * 1024);
     if constexpr (V * NC == 8)
         if (s.threads <= 256) return launch_bwd<IO, V, NC, 256>(b, s, st);
     return launch_bwd<IO, V, NC, 512>(b, s, st);

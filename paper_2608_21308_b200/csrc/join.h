@@ -24,9 +24,10 @@ struct JoinBwdArgs {
     float* part;                                  // [grid][2][H d]
 };
 
-// CTAs of the reverse pass, each with partial sums of the parameters' gradients: as many as an SM holds, three of up to 2048 columns
+// CTAs of the reverse pass, each with partial sums of the parameters' gradients: 512 threads on an SM, a thread per 8 columns (16 above 4096 columns)
 inline int join_bwd_grid(int64_t tokens, int width) {
-    const int most = 148 * (width <= 512 ? 8 : width <= 1024 ? 6 : width <= 2048 ? 3 : 1);
+    const int threads = width <= 4096 ? (width + 255) / 256 * 32 : 512;
+    const int most = 148 * (threads <= 64 ? 8 : 512 / threads);
     return (int)(tokens < most ? tokens : most);
 }
 
