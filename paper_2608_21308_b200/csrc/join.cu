@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
         copy_wait(depth - 1);
         const P* r = ring + slot * 5 * NC * T;
         slot = slot + 1 == depth ? 0 : slot + 1;
-        float y[NC][V], xo[NC][V], hs[NC], inv[NC];
+        float y[NC][V], xo[NC][V], sg[NC][V], hs[NC], inv[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             hs[i] = 0.0f;
@@ -353,6 +353,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av);
+                    if (KEPT) sg[i][j] = sig;
                     xo[i][j] = silu ? av * sig : sig;
                 }
             }
@@ -401,7 +402,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
                 P da_p;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av), dev = silu ? fmaf(av, 1.0f - sig, 1.0f) : 1.0f - sig;
+                    const float av = ldf(pa.x[j]), sig = KEPT ? sg[i][j] : sigmoid<IO>(av), dev = silu ? fmaf(av, 1.0f - sig, 1.0f) : 1.0f - sig;
                     stf(da_p.x[j], dx[j] * wr.x[j] * wp.x[j] * y[i][j] * (sig * dev));
                     dx[j] *= silu ? av * sig : sig;
                 }
