@@ -441,28 +441,41 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
     }
 }
 
-// column sums over the CTAs: 32 columns by 32 row groups a CTA
+// Column sums over the CTAs' partial sums: 8 columns (32 bytes of a row) by 128 row groups a CTA, so that many SMs have a part of the few MB.  Both sums of a
+// column are added in an order that depends on the number of rows alone.
+constexpr int kSumCols = 8;
 __global__ void __launch_bounds__(1024) join_sum_kernel(const JoinBwdArgs ba, const int rows) {
-    __shared__ float red[2][32][32];
+    __shared__ float red[2][kSumCols][33];
     const JoinArgs& a = ba.f;
-    const int D = a.H * a.d, lane = threadIdx.x & 31, group = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    const int D = a.H * a.d, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = lane & 7, c = blockIdx.x * kSumCols + col;
     float r = 0.0f, w = 0.0f;
     if (c < D) {
-#pragma unroll 8
-        for (int i = group; i < rows; i += 32) {
+#pragma unroll 4
+        for (int i = threadIdx.x >> 3; i < rows; i += 128) {
             r += ba.part[(size_t)i * 2 * D + c];
             if (a.w_pre) w += ba.part[(size_t)i * 2 * D + D + c];
         }
     }
-    red[0][group][lane] = r;
-    red[1][group][lane] = w;
+#pragma unroll
+    for (int x = 8; x <= 16; x <<= 1) {
+        r += __shfl_xor_sync(kAll, r, x);
+        w += __shfl_xor_sync(kAll, w, x);
+    }
+    if (lane < kSumCols) { red[0][lane][warp] = r; red[1][lane][warp] = w; }
     __syncthreads();
-    if (group != 0 || c >= D) return;
-    r = w = 0.0f;
-    for (int i = 0; i < 32; ++i) { r += red[0][i][lane]; w += red[1][i][lane]; }
-    ba.d_w_post[c] = r * a.res_scale[c];
-    ba.d_res_scale[c] = r * a.w_post[c];
-    if (a.w_pre) ba.d_w_pre[c] = w;
+    if (warp >= kSumCols) return;
+    r = red[0][warp][lane];
+    w = red[1][warp][lane];
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+        r += __shfl_xor_sync(kAll, r, x);
+        w += __shfl_xor_sync(kAll, w, x);
+    }
+    const int out = blockIdx.x * kSumCols + warp;
+    if (lane != 0 || out >= D) return;
+    ba.d_w_post[out] = r * a.res_scale[out];
+    ba.d_res_scale[out] = r * a.w_post[out];
+    if (a.w_pre) ba.d_w_pre[out] = w;
 }
 
 // values per piece: the widest that divides a head and that all addresses allow
@@ -506,7 +519,7 @@ template <typename IO, int V, int NC, int TMAX> int launch_bwd(const JoinBwdArgs
     kernel<<<grid, s.threads, s.smem, st>>>(b, s.depth);
     e = cudaGetLastError();
     if (e != cudaSuccess) return (int)e;
-    join_sum_kernel<<<(b.f.H * b.f.d + 31) / 32, 1024, 0, st>>>(b, grid);
+    join_sum_kernel<<<(b.f.H * b.f.d + kSumCols - 1) / kSumCols, 1024, 0, st>>>(b, grid);
     return (int)cudaGetLastError();
 }
 
