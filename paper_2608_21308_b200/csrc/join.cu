@@ -6,6 +6,8 @@
 // Reverse pass, with r = gate(a) y0, y0 = o / rms(o):  d x = d x_out + (adjoint of the second norm),  d w_post = res_scale sum_tokens(dx r),
 // d res_scale = w_post sum_tokens(dx r): one column sum serves both, a second one is d w_pre.  A CTA keeps its tokens' column sums in
 // registers; the CTAs' sums are added by a second launch in a fixed order, so that results repeat bit for bit.
+// 16384 tokens of 2048 in bf16 with a gate and both norms: 64 us forward (336 MB, 5.2 TB/s), 126 us in reverse (537 MB, 4.3 TB/s) and 6 us for the column
+// sums; 8000 tokens of 768 in fp32, sigmoid gate: 34, 66 and 6 us.  What is above the bytes' time is issue: the gate's special functions, bf16 conversions, sums.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -159,7 +161,7 @@ template <int V> struct alignas(V >= 4 ? 16 : 4 * V) Weights {
 template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, int c) { return reinterpret_cast<const Weights<V>*>(w)[c]; }
 
 // Whether a thread of the forward keeps its weights in registers from token to token (three CTAs of 256 threads on an SM instead of four).  16384 tokens
-// of 2048 in bf16: 65 us with them, 72 without; fp32, whose threads take two pieces of four, 8 x 2048 tokens of 768: 41 and 35.
+// of 2048 in bf16: 65 us with them, 72 without; fp32, whose threads take two pieces of four, 8000 tokens of 768: 41 and 35.
 template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256; }
 
 template <typename IO, int V, int NC, int TMAX>
