@@ -105,6 +105,8 @@ SHAPES = [  # B, H, Hk, L, dk, dv
     (1, 13, 13, 128, 128, 128),
     # more slices than SMs: a warp for all of a slice's columns, four slices (two with fp32) or fewer in a CTA, the last CTA not full
     (2, 16, 16, 70, 128, 128), (3, 16, 4, 100, 128, 100), (5, 8, 2, 96, 96, 80),
+    # narrow keys and wide values
+    (2, 4, 2, 130, 48, 120), (6, 8, 4, 70, 64, 128),
 ]
 
 
