@@ -7,7 +7,7 @@
 // d res_scale = w_post sum_tokens(dx r): one column sum serves both, a second one is d w_pre.  A CTA keeps its tokens' column sums in
 // registers; the CTAs' sums are added by a second launch in a fixed order, so that results repeat bit for bit.
 // 16384 tokens of 2048 in bf16 with a gate and both norms: 64 us forward (336 MB, 5.2 TB/s), 126 us in reverse (537 MB, 4.3 TB/s) and 6 us for the column
-// sums; 8000 tokens of 768 in fp32, sigmoid gate: 34, 66 and 6 us.  What is above the bytes' time is issue: the gate's special functions, bf16 conversions, sums.
+// sums; 8000 tokens of 768 in fp32, sigmoid gate: 31, 58 and 6 us.  What is above the bytes' time is issue: the gate's special functions, bf16 conversions, sums.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -31,12 +31,12 @@ template <typename IO, int V> struct alignas(sizeof(IO) * V) Piece {
     IO x[V];
 };
 
-// 1 / (1 + exp(-a)).  With bf16 I/O what it enters is rounded to 2^-9 right after: the hardware's exponential and reciprocal (2^-22) serve.
-// a -> -inf: the exponential is inf, the result 0.
+// 1 / (1 + exp(-a)).  The hardware's reciprocal is off by one step of fp32 (2^-23), which a division would halve.  With bf16 I/O what the gate enters is
+// rounded to 2^-9 right after, and the hardware's exponential (2^-22, and that of its argument) serves as well.  a -> -inf: the exponential is inf, the result 0.
 template <typename IO> __device__ __forceinline__ float sigmoid(float a) {
-    if (sizeof(IO) == 4) return 1.0f / (1.0f + expf(-a));
     float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -1.4426950408889634f));
+    if (sizeof(IO) == 4) e = expf(-a);
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(a * -1.4426950408889634f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return r;
 }
