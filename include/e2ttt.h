@@ -269,12 +269,13 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  *   S            [B,H,dv,dk] fp32           rows are outputs, as in the fast-weight matrices
  * e2ttt_delta_fwd runs whole sequences in chunks of 32 tokens on the tensor cores; e2ttt_delta_step is the recurrent form for a few
  * tokens (decoding), without a workspace; both move the same state and may follow each other.
- * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly; outputs are rounded once.  Bits are counted
- * from the largest value of a chunk's queries or keys, of 16 neighbouring value rows of a state: a value 2^-10 of it has 10 bits fewer.  bf16
- * outputs without saved states, and bf16 dq and dk, are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.
- * Magnitudes should stay below 2^100.  A NaN or an infinity at one token of a sequence makes all outputs of its chunk of 32 tokens and what follows
- * them (NaN or without meaning), and in the reverse pass all gradients of its block of 64 tokens and what depends on them; tokens before its chunk,
- * and other heads with queries and keys of their own, keep their outputs bit for bit.
+ * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly, neither finer than 2^-27 of the largest
+ * value of a chunk's queries or keys, or of 16 neighbouring value rows of a state; outputs are rounded once.  bf16 outputs without saved states, and
+ * bf16 dq and dk, are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  The largest magnitude of a
+ * tensor should be 0 or lie between 2^-90 and 2^100.
+ * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
+ * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
+ * queries and keys of their own, keep their outputs bit for bit.
  * Calls that may run at the same time need workspaces of their own; calls one after the other may share one (but for saved states in it).
  * Arguments are refused as everywhere: E2TTT_ERR_NULL / _SHAPE / _DTYPE / _WORKSPACE / _ALIGN / _ARCH / _CUDA.  Tensors need the
  * alignment of their elements only; 16 bytes, and widths that are a multiple of 8, load faster. */
