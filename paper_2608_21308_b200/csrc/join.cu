@@ -41,6 +41,16 @@ template <typename IO> __device__ __forceinline__ float sigmoid(float a) {
     return r;
 }
 
+// The smaller of sig = sigmoid(a) and 1 - sig: e / (1 + e), e = exp(-|a|).  The reverse pass needs both, and 1 - sig as a difference would lose what an open gate's
+// derivative is made of (all of it from a = 17 on).
+template <typename IO> __device__ __forceinline__ float smaller_part(float a) {
+    float e, r;
+    if (sizeof(IO) == 4) e = expf(-fabsf(a));
+    else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(a) * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return e * r;
+}
+
 // Where a token's rows of o start: its batch and position, moved on by the grid's size without a division.
 struct Place {
     int64_t base;  // first piece of (batch, head 0, position)
@@ -354,8 +364,8 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
             if (a.a) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float av = ldf(pa.x[j]), sig = sigmoid<IO>(av);
-                    if (KEPT) sg[i][j] = sig;
+                    const float av = ldf(pa.x[j]), w = smaller_part<IO>(av), sig = av > 0.0f ? 1.0f - w : w;
+                    if (KEPT) sg[i][j] = w;
                     xo[i][j] = silu ? av * sig : sig;
                 }
             }
@@ -404,7 +414,8 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
                 P da_p;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float av = ldf(pa.x[j]), sig = KEPT ? sg[i][j] : sigmoid<IO>(av), dev = silu ? fmaf(av, 1.0f - sig, 1.0f) : 1.0f - sig;
+                    const float av = ldf(pa.x[j]), w = KEPT ? sg[i][j] : smaller_part<IO>(av);
+                    const float sig = av > 0.0f ? 1.0f - w : w, rest = av > 0.0f ? w : 1.0f - w, dev = silu ? fmaf(av, rest, 1.0f) : rest;
                     stf(da_p.x[j], dx[j] * wr.x[j] * wp.x[j] * y[i][j] * (sig * dev));
                     dx[j] *= silu ? av * sig : sig;
                 }
