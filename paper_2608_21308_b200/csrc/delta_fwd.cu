@@ -20,13 +20,12 @@ namespace {
 using namespace delta;
 
 template <int DK, int KT> constexpr int stage_bytes() { return 2 * KT * 64 * DK + kDeltaRecBytes; }
-template <int KT, bool PREC> constexpr int stages() { return KT == 1 && !PREC ? 4 : 3; }
+template <int KT> constexpr int stages() { return KT == 1 ? 4 : 3; }
 
-// what the warps of a slice hand over, a buffer per parity of the chunk: fragments of S and e (a second term each with PREC), what undoes their
-// scales, the values of the next chunk (fp32 in fragment order, or bf16 tokens x rows) and a bound on them, the outputs on their way out
-template <int DK, int KT, int KS, bool PREC> struct alignas(128) Exchange {
-    uint4 s[PREC ? 2 : 1][DK / 16][32];
-    uint4 u[PREC ? 2 : 1][2][32];
+// what the warps of a slice hand over, a buffer per parity of the chunk: fragments of S and e (both terms), what undoes their scales, the values of the next chunk (fp32 in fragment order, or bf16 tokens x rows) and a bound on them, the outputs on their way out
+template <int DK, int KT, int KS> struct alignas(128) Exchange {
+    uint4 s[2][DK / 16][32];
+    uint4 u[2][2][32];
     float4 v[KT == 1 ? 2 : 4][32];
     uint4 o[KT == 1 ? 64 : 1];
     float4 part[KS > 1 ? KS : 1][4][KS > 1 ? 32 : 1];  // S K^T over a warp's columns (KS > 1)
@@ -34,20 +33,18 @@ template <int DK, int KT, int KS, bool PREC> struct alignas(128) Exchange {
     float s_inv, u_inv, v_max;
 };
 
-template <int DK, int KT, int KS, bool PREC> constexpr int fwd_smem(int slices) {
-    return stages<KT, PREC>() * stage_bytes<DK, KT>() + 2 * slices * (int)sizeof(Exchange<DK, KT, KS, PREC>);
+template <int DK, int KT, int KS> constexpr int fwd_smem(int slices) {
+    return stages<KT>() * stage_bytes<DK, KT>() + 2 * slices * (int)sizeof(Exchange<DK, KT, KS>);
 }
 
-// PREC: both terms in the outputs' products as well (fp32 outputs, or outputs that the reverse pass needs in 32 bits).  Without it an output
-// is off by 2^-11 of its terms at most before it is rounded to bf16's 2^-8.
 // vec: bf16 rows of v and o that allow 16-byte pieces.
-template <typename IO, int DK, int KT, int KS, bool PREC>
+template <typename IO, int DK, int KT, int KS>
 __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const DeltaArgs a, const int per, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
-    constexpr int NS = stages<KT, PREC>(), DC = DK / KS, SB = stage_bytes<DK, KT>();
+    constexpr int NS = stages<KT>(), DC = DK / KS, SB = stage_bytes<DK, KT>();
     __shared__ uint64_t full[NS];
     __shared__ int dead_flag;
-    using X = Exchange<DK, KT, KS, PREC>;
+    using X = Exchange<DK, KT, KS>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
     const DeltaShape& s = a.s;
     const int groups = (a.l.slices + per - 1) / per;  // CTAs per sequence
@@ -96,7 +93,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         auto leave_s = [&](int kk, X& x) {  // for the outputs' warp
             const uint32_t (&h)[4] = fh[kk & 1], (&l)[4] = fl[kk & 1];
             x.s[0][part * (DC / 16) + kk][lane] = make_uint4(h[0], h[1], h[2], h[3]);
-            if (PREC) x.s[PREC ? 1 : 0][part * (DC / 16) + kk][lane] = make_uint4(l[0], l[1], l[2], l[3]);
+            x.s[1][part * (DC / 16) + kk][lane] = make_uint4(l[0], l[1], l[2], l[3]);
         };
         // the i-th two MMAs (of 2 TERMS) of those column tiles with a key tile
         auto times_k = [&](int kk, int i, bool first, const uint32_t (&b)[2 * KT][4]) {
@@ -316,7 +313,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                     uint32_t hi[4], lo[4];
                     split_a(e[2 * kk], e[2 * kk + 1], hi, lo);
                     x.u[0][kk][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    if (PREC) x.u[PREC ? 1 : 0][kk][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    x.u[1][kk][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 }
                 if (NJ > 1) load_s(1);
                 load_k(kn, 0, fk[0]);
@@ -460,12 +457,12 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     auto product = [&](int c, int st, float (&sq)[4][4]) {  // S Q^T, in S's scale
         const uint32_t qs = ring + st * SB + KT * 64 * DK;
         const X& x = xb[c & 1];
-        uint4 f[2][PREC ? 2 : 1];
+        uint4 f[2][2];
         float sl[4][4] = {};  // the second terms' products apart: an MMA truncates the sum that it adds to
         uint32_t b[2][2][KT][4];
         auto load = [&](int kk) {
 #pragma unroll
-            for (int t = 0; t < (PREC ? 2 : 1); ++t) f[kk & 1][t] = x.s[t][kk][lane];
+            for (int t = 0; t < 2; ++t) f[kk & 1][t] = x.s[t][kk][lane];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -475,7 +472,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 #pragma unroll
         for (int kk = 0; kk < DK / 16; ++kk) {
             if (kk + 1 < DK / 16) load(kk + 1);
-            const uint4 h4 = f[kk & 1][0], l4 = f[kk & 1][PREC ? 1 : 0];
+            const uint4 h4 = f[kk & 1][0], l4 = f[kk & 1][1];
             const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
             const uint32_t (&q)[2][KT][4] = b[kk & 1];
 #pragma unroll
@@ -483,18 +480,16 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 if (kk == 0) { mma0(sq[2 * h], hi, q[h][0][0], q[h][0][1]); mma0(sq[2 * h + 1], hi, q[h][0][2], q[h][0][3]); }
                 else { mma(sq[2 * h], hi, q[h][0][0], q[h][0][1]); mma(sq[2 * h + 1], hi, q[h][0][2], q[h][0][3]); }
             }
-            if (PREC)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) { mma(sl[2 * h], lo, q[h][0][0], q[h][0][1]); mma(sl[2 * h + 1], lo, q[h][0][2], q[h][0][3]); }
+            for (int h = 0; h < 2; ++h) { mma(sl[2 * h], lo, q[h][0][0], q[h][0][1]); mma(sl[2 * h + 1], lo, q[h][0][2], q[h][0][3]); }
             if (KT == 2)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) { mma(sl[2 * h], hi, q[h][KT - 1][0], q[h][KT - 1][1]); mma(sl[2 * h + 1], hi, q[h][KT - 1][2], q[h][KT - 1][3]); }
         }
-        if (PREC)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) sq[j][y] += sl[j][y];
+            for (int y = 0; y < 4; ++y) sq[j][y] += sl[j][y];
     };
     auto finish = [&](int c, int st, const float (&sq)[4][4], float s_inv) {  // O = b S Q^T + e (A eta)^T
         const uint32_t as = ring + st * SB + 2 * KT * 64 * DK + 4096;
@@ -503,25 +498,22 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         float in[4][4] = {}, il[4][4] = {};
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            const uint4 h4 = x.u[0][kk][lane], l4 = x.u[PREC ? 1 : 0][kk][lane];
+            const uint4 h4 = x.u[0][kk][lane], l4 = x.u[1][kk][lane];
             const uint32_t hi[4] = {h4.x, h4.y, h4.z, h4.w}, lo[4] = {l4.x, l4.y, l4.z, l4.w};
 #pragma unroll
             for (int h = kk; h < 2; ++h) {
                 uint32_t bh[4], bl[4];
                 ldsm4(bh, addr_nk<32>(as, 2 * h, kk, lane));
                 mma(in[2 * h], hi, bh[0], bh[1]); mma(in[2 * h + 1], hi, bh[2], bh[3]);
-                if (PREC) {
-                    ldsm4(bl, addr_nk<32>(as + 2048, 2 * h, kk, lane));
-                    mma(il[2 * h], lo, bh[0], bh[1]); mma(il[2 * h + 1], lo, bh[2], bh[3]);
-                    mma(il[2 * h], hi, bl[0], bl[1]); mma(il[2 * h + 1], hi, bl[2], bl[3]);
-                }
+                ldsm4(bl, addr_nk<32>(as + 2048, 2 * h, kk, lane));
+                mma(il[2 * h], lo, bh[0], bh[1]); mma(il[2 * h + 1], lo, bh[2], bh[3]);
+                mma(il[2 * h], hi, bl[0], bl[1]); mma(il[2 * h + 1], hi, bl[2], bl[3]);
             }
         }
-        if (PREC)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) in[j][y] += il[j][y];
+            for (int y = 0; y < 4; ++y) in[j][y] += il[j][y];
         const float q = x.u_inv * sc[kRecHead * 32 + kHeadA];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -579,7 +571,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
         const size_t at = ((size_t)n * (a.l.nblk + 1) + slot) * a.l.slices + slice;
         bulk_store(a.ws + a.l.S + at * a.l.state_bytes, sm100::smem_u32(x.s[0]), (uint32_t)a.l.state_bytes);
         if (slot > 0 || KT == 2)  // with bf16 the start state's second term enters no inner product
-            bulk_store(a.ws + a.l.S_lo + at * a.l.state_bytes, sm100::smem_u32(x.s[PREC ? 1 : 0]), (uint32_t)a.l.state_bytes);
+            bulk_store(a.ws + a.l.S_lo + at * a.l.state_bytes, sm100::smem_u32(x.s[1]), (uint32_t)a.l.state_bytes);
         reinterpret_cast<float*>(a.ws + a.l.s_inv)[at] = x.s_inv;
     };
     auto save_e = [&](int c, const X& x) {
@@ -619,10 +611,10 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     if (a.save) bulk_store_done();
 }
 
-template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const DeltaArgs& a, int per, cudaStream_t st) {
-    auto kernel = delta_fwd_kernel<IO, DK, KT, KS, PREC>;
-    const int bytes = fwd_smem<DK, KT, KS, PREC>(per);
-    cudaError_t e = allow_shared_memory<delta_fwd_kernel<IO, DK, KT, KS, PREC>>();
+template <typename IO, int DK, int KT, int KS> int launch(const DeltaArgs& a, int per, cudaStream_t st) {
+    auto kernel = delta_fwd_kernel<IO, DK, KT, KS>;
+    const int bytes = fwd_smem<DK, KT, KS>(per);
+    cudaError_t e = allow_shared_memory<delta_fwd_kernel<IO, DK, KT, KS>>();
     if (e != cudaSuccess) return (int)e;
     const unsigned grid = (unsigned)(a.l.N * ((a.l.slices + per - 1) / per));
     const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o)) % 16 == 0;
@@ -630,26 +622,25 @@ template <typename IO, int DK, int KT, int KS, bool PREC> int launch(const Delta
     return (int)cudaGetLastError();
 }
 
-template <typename IO, int DK, int KT, bool PREC> int dispatch(const DeltaArgs& a, cudaStream_t st) {
+template <typename IO, int DK, int KT> int dispatch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int most = KT == 1 ? 4 : 2;
-    static_assert(fwd_smem<DK, KT, 1, PREC>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32, PREC>(1) <= kMostSharedMemory, "shared memory");
+    static_assert(fwd_smem<DK, KT, 1>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32>(1) <= kMostSharedMemory, "shared memory");
     // Few slices, as many as SMs at most: one per CTA, its columns over DK / 32 warps; with more of them the warps share an SM's schedulers and a chain
     // per warp is faster.  Then slices of a sequence share the tiles that they fetch, as long as 96 CTAs are left.  Forward and reverse pass
     // together, us: 8 x 12 x 2048 tokens, 64 x 64, bf16: 4 slices per CTA 554, 2: 563, 1: 647, one over two warps 744.  Forward alone, 128 x 128,
     // 16 heads x 4096 tokens: B = 4: 4 slices 310, 2: 421; B = 2: 2 slices 220, 4: 269.  fp32 tiles leave room for two.
-    if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, PREC>(a, 1, st);
+    if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32>(a, 1, st);
     int per = most;
     while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
-    return launch<IO, DK, KT, 1, PREC>(a, per, st);
+    return launch<IO, DK, KT, 1>(a, per, st);
 }
 
 }  // namespace
 
 int delta_fwd_launch(const DeltaArgs& a, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (a.s.f32) return a.l.DK == 64 ? dispatch<float, 64, 2, true>(a, st) : dispatch<float, 128, 2, true>(a, st);
-    if (a.save) return a.l.DK == 64 ? dispatch<__nv_bfloat16, 64, 1, true>(a, st) : dispatch<__nv_bfloat16, 128, 1, true>(a, st);
-    return a.l.DK == 64 ? dispatch<__nv_bfloat16, 64, 1, false>(a, st) : dispatch<__nv_bfloat16, 128, 1, false>(a, st);
+    if (a.s.f32) return a.l.DK == 64 ? dispatch<float, 64, 2>(a, st) : dispatch<float, 128, 2>(a, st);
+    return a.l.DK == 64 ? dispatch<__nv_bfloat16, 64, 1>(a, st) : dispatch<__nv_bfloat16, 128, 1>(a, st);
 }
 
 }  // namespace e2ttt
