@@ -12,14 +12,14 @@
 namespace e2ttt {
 
 constexpr int kDeltaChunk = 32;  // tokens per chunk: a warp's row for its gates, two k-steps of the MMAs
-// tokens per saved state (two chunks), and per sum of the decays' gradients: <X, S> ends each.  With sums of 64 and of 128 tokens, at 4 x 16 sequences
-// of 4096 tokens, 128 x 128, bf16, these gradients are off by 0.8e-6 and 1.1e-6 of their norm; forward 355 and 346 us, reverse walk 407 and 384.
-constexpr int kDeltaBlock = 64;
+constexpr int kDeltaBlock = 64;  // tokens per saved state: two chunks
 constexpr int kDeltaMaxD = 128;  // a slice of 16 state rows of 128 columns is a quarter of a warp's registers
 // A chunk's record: T and A eta (two fp16 terms each, 2 KB a term), eight rows of 32 floats; with saved states also A and the T of the reverse
-// pass, (I + eta strict(D (K K^T)))^-1.  The forward fetches the first 9 KB, the reverse pass the last 9.
+// pass, (I + eta strict(D (K K^T)))^-1, and A and strict(D (K K^T)) in fp32, in the order of a product's six 16 x 8 tiles on and below the diagonal blocks.
+// The forward fetches the first 9 KB, the reverse walk 9 KB from the scalars on; the fp32 matrices are for the decays' gradients.
 constexpr int kDeltaRecBytes = 9216;
 constexpr int kDeltaRecSkip = 8192;
+constexpr int kDeltaRecPairs = 17408;
 // rows of a record's scalars: b of K and Q (with the scales of their tiles), eta, D_end, eta D_end, eta b
 enum { kRecBk = 0, kRecBq = 1, kRecEta = 2, kRecDend = 3, kRecW = 4, kRecZ = 5, kRecHead = 7 };
 // the last row: decay of the whole chunk; what undoes the scales of T, A eta, K, Q, the reverse pass' T and A; then bounds of the chunk's
@@ -45,9 +45,9 @@ struct DeltaLayout {
     size_t rec_bytes;  // record of a chunk
     size_t state_bytes;  // a slice of a state: one term of its fragments
     // offsets in bytes.  Saved for the reverse pass, all in fragment order (a lane's 16 bytes of one product's A operand together), per slice:
-    // the state before every block and behind the last (first terms and second terms), e of every chunk, the outputs in fp32; by its
-    // chain: X behind every block, dP of every chunk; what undoes the fragments' scales
-    size_t qk, rec, S, S_lo, s_inv, e, e_inv, o, X, x_inv, dp, dp_inv, max_do, part_eta, part_gate, hx, total;
+    // the state before every block (first terms and second terms), e of every chunk, S Q^T and S K^T of the state before it in
+    // fp32 (at the state's scale); by its chain: X behind every block, dP of every chunk; what undoes the scales; per token, sums over a slice's rows
+    size_t qk, rec, S, S_lo, s_inv, e, e_inv, sq, sk, c_inv, X, x_inv, dp, dp_lo, dp_inv, max_do, part_eta, part_s, part_x, hx, total;
 };
 
 inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
@@ -61,27 +61,31 @@ inline DeltaLayout delta_layout(const DeltaShape& s, bool save) {
     l.N = (int64_t)s.B * s.H;
     l.Nk = (int64_t)s.B * s.Hk;
     l.qk_bytes = (size_t)2 * l.terms * 64 * l.DK;
-    l.rec_bytes = kDeltaRecBytes + (save ? 8192 : 0);
+    l.rec_bytes = save ? kDeltaRecPairs + 2 * 3072 : kDeltaRecBytes;
     l.state_bytes = (size_t)32 * l.DK;
     size_t at = 256;  // the status block
     auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
     l.qk = take((size_t)l.Nk * l.nch * l.qk_bytes);
     l.rec = take((size_t)l.N * l.nch * l.rec_bytes);
     if (save) {
-        const size_t chunks = (size_t)l.N * l.nch * l.slices, blocks = (size_t)l.N * (l.nblk + 1) * l.slices;
+        const size_t chunks = (size_t)l.N * l.nch * l.slices, blocks = (size_t)l.N * l.nblk * l.slices;
         l.S = take(blocks * l.state_bytes);
         l.S_lo = take(blocks * l.state_bytes);
         l.s_inv = take(blocks * 4);
         l.e = take(chunks * 2048);
         l.e_inv = take(chunks * 4);
-        l.o = take(chunks * 2048);
+        l.sq = take(chunks * 2048);
+        l.sk = take(chunks * 2048);
+        l.c_inv = take(chunks * 4);
         l.X = take(blocks * l.state_bytes * l.terms);
         l.x_inv = take(blocks * 4);
         l.dp = take(chunks * 1024 * l.terms);
+        l.dp_lo = l.terms == 1 ? take(chunks * 1024) : 0;  // apart: dq and dk are of first terms with bf16
         l.dp_inv = take(chunks * 4);
         l.max_do = take(chunks * 4);
         l.part_eta = take(chunks * kDeltaChunk * 4);
-        l.part_gate = take(chunks * kDeltaChunk * 4);
+        l.part_s = take(chunks * kDeltaChunk * 4);
+        l.part_x = take(chunks * kDeltaChunk * 4);
         l.hx = take((size_t)l.N * l.nblk * l.slices * 16);
     }
     l.total = at;

@@ -1,9 +1,11 @@
 // Gated delta rule, reverse pass.  With X the adjoint of the state behind a chunk and Z = (I + eta strict(D K K^T))^-T dU:
 //   dU = A^T dO + D_end X K,   dP = eta Z = dV,   X_before = b_end X + scale (b dO) Q^T - (b dP) K^T            (delta_chain_kernel)
 //   dQ = (D dO^T U) K + scale b S_0^T dO,   dK = (D dO^T U)^T Q - (W + W^T) K - b S_0^T dP + D_end X^T U,  W = strict(D dP^T U)   (delta_qk_kernel)
-//   d eta = Z . e,   d log_gamma_t = sum over s >= t (o_s . do_s - v_s . dv_s) + <X, S> at the end of the sum         (delta_gate_kernel)
-// The last line is the scaling of everything before token t by g_t: outputs and state are linear in the start state and the values, so
-// no difference of nearly equal sums over keys is formed.  Sums run over 64 tokens, <X, S> is taken behind each of them.
+//   d eta = Z . e,   d log_gamma_t = <X'_t, g_t S_{t-1}>: what tokens before t hand on to tokens from t on, over a chunk                (delta_gate_kernel)
+//     = sum_{i < t <= s} eta_i (A_si dO_s . e_i - (D K K^T)_si dP_s . e_i) + sum_{s >= t} b_s (scale dO_s . S_0 q_s - dP_s . S_0 k_s)
+//       + sum_{i < t} eta_i D_end,i e_i . X k_i + b_end <X, S_0>,   X'_t the adjoint with what token t reads.
+// Every term carries the decays between its two ends as factors, so a token that forgets the state has an exact small gradient: sums of
+// outputs and values (o_s . do_s - v_s . dv_s and so on) would have to cancel to it.  The walks have S_0 Q^T, S_0 K^T and X K^T at hand.
 // The chain walks the chunks from the last to the first as the forward does, a warp per 16 value rows; dQ and dK contract over the
 // value rows of all warps and are left to a kernel that takes the blocks side by side.
 #include "api_checks.h"
@@ -43,8 +45,10 @@ template <int DK, int KT, int KS> struct alignas(128) ReverseExchange {
     float4 in[4][32], z[4][32];
     float4 part[KS > 1 ? KS : 1][4][KS > 1 ? 32 : 1];
     uint4 e[2][2][32];        // e's fragments
-    float4 o[4][32];
-    float4 d_o[KT == 1 ? 2 : 4][32], v[KT == 1 ? 2 : 4][32];
+    float4 sq[4][32];         // S Q^T of the forward
+    float4 sk[4][32];                            // S K^T of the forward
+    float4 xk[KS > 1 ? 4 : 1][KS > 1 ? 32 : 1];  // X K^T; with one warp it takes the place of `in`, which the same lane has read
+    float4 d_o[KT == 1 ? 2 : 4][32];
     uint4 out[KT == 1 ? 64 : 1];
     float norm[KS];
     float x_inv, in_max, q_max, q_inv, q_sum;
@@ -56,7 +60,7 @@ template <int DK, int KT, int KS> constexpr int chain_smem(int slices) {
 // The chain X, Z, X runs as the forward's does (a warp per slice, or KS by columns; scales from bounds; the products of a chunk between the steps of
 // its arithmetic).  A side warp per slice, a chunk ahead, makes what does not depend on X (A^T dO, the fragments of b dO, o . dO), and, a chunk
 // behind, what hangs off Z (dV, dP's fragments, the sums for d eta and d log_gamma).  Bound by what a chunk's steps issue one after the other:
-// 4 x 16 sequences of 4096 tokens, 128 x 128, bf16, in 407 us (3.2 us a chunk); 8 x 12 of 2048 tokens, 64 x 64, in 157 us.
+// 4 x 16 sequences of 4096 tokens, 128 x 128, bf16, in 423 us (3.3 us a chunk); 8 x 12 of 2048 tokens, 64 x 64, in 162 us.
 template <typename IO, int DK, int KT, int KS>
 __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(const DeltaBwdArgs ba, const int per, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
@@ -200,9 +204,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
             const bool come = i + 1 == nch || probe_phase(&full[st_next], phase_next);
             if (active) {
                 take(x);
-                const int blk = c >> 1;
-                if ((c & 1) || c == nch - 1) {  // <X, S> behind a block
-                    const size_t at = ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.slices + slice;
+                if (!(c & 1)) {  // <X, S>: behind a block's first chunk, before it
+                    const size_t at = ((size_t)n * a.l.nblk + (c >> 1)) * a.l.slices + slice;
                     const uint4* hi4 = reinterpret_cast<const uint4*>(a.ws + a.l.S + at * a.l.state_bytes) + part * (DC / 16) * 32 + lane;
                     const uint4* lo4 = reinterpret_cast<const uint4*>(a.ws + a.l.S_lo + at * a.l.state_bytes) + part * (DC / 16) * 32 + lane;
                     float h = 0.0f;
@@ -220,7 +223,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
                         }
                     }
                     h = warp_sum(h) * (s_inv * reinterpret_cast<const float*>(a.ws + a.l.s_inv)[at]);
-                    float* hx = reinterpret_cast<float*>(a.ws + a.l.hx) + (((size_t)n * a.l.nblk + blk) * a.l.slices + slice) * 4;
+                    float* hx = reinterpret_cast<float*>(a.ws + a.l.hx) + at * 4;
                     if (lane == 0) hx[part] = h;
                     if (lane >= KS && lane < 4 && part == 0) hx[lane] = 0.0f;
                 }
@@ -238,6 +241,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float4 in = x.in[j][lane];
+                    if (KS == 1) x.in[j][lane] = make_float4(sk[j][0], sk[j][1], sk[j][2], sk[j][3]);
+                    else if (part == (j >> 1)) x.xk[KS > 1 ? j : 0][KS > 1 ? lane : 0] = make_float4(sk[j][0], sk[j][1], sk[j][2], sk[j][3]);
                     const float2 de = *reinterpret_cast<const float2*>(sc + kRecDend * 32 + j * 8 + 2 * c4);
                     float y0, y1;
                     mul2(y0, y1, de.x, de.y, fs, fs);
@@ -417,13 +422,12 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
     __syncwarp();
     const int rows = active ? min(16, s.dv - slice * 16) : 0;
     const size_t seq = (size_t)n * s.L * s.dv + slice * 16;
-    const IO* v = reinterpret_cast<const IO*>(a.v) + seq;
     const IO* d_o = reinterpret_cast<const IO*>(ba.d_o) + seq;
     IO* dv = reinterpret_cast<IO*>(ba.dv) + seq;
     auto copy16 = [&](const void* dst, const void* src, int bytes) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(sm100::smem_u32(dst)), "l"(src), "r"(bytes) : "memory");
     };
-    // a chunk's rows of v or dO to a tile of tokens (bf16) or to fragment order (fp32)
+    // a chunk's rows of dO to a tile of tokens (bf16) or to fragment order (fp32)
     auto load_tok = [&](float4* dst, const IO* src, int c) {
         if (KT == 1) {
             const int t = c * kDeltaChunk + lane;
@@ -475,25 +479,30 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
             }
         }
     };
-    auto load_ahead = [&](int i) {  // dO and o of step i
+    auto load_ahead = [&](int i) {  // dO and S Q^T of step i
         if (i >= nch || !active) return;
         const int c = nch - 1 - i;
         X& x = xb[i & 1];
         load_tok(x.d_o[0], d_o, c);
-        const float4* src = reinterpret_cast<const float4*>(a.ws + a.l.o) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
+        const float4* src = reinterpret_cast<const float4*>(a.ws + a.l.sq) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) copy16(&x.o[j][lane], src + j * 32 + lane, 16);
+        for (int j = 0; j < 4; ++j) copy16(&x.sq[j][lane], src + j * 32 + lane, 16);
     };
-    auto load_behind = [&](int i) {  // e and v of step i
+    auto load_behind = [&](int i) {  // e and S K^T of step i
         if (i >= nch || !active) return;
         const int c = nch - 1 - i;
         X& x = xb[i & 1];
-        load_tok(x.v[0], v, c);
-        const uint4* src = reinterpret_cast<const uint4*>(a.ws + a.l.e) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
+        const size_t at = (((size_t)n * nch + c) * a.l.slices + slice) * 128;
+        const uint4* src = reinterpret_cast<const uint4*>(a.ws + a.l.e) + at;
+        const float4* sk = reinterpret_cast<const float4*>(a.ws + a.l.sk) + at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) copy16(&x.sk[j][lane], sk + j * 32 + lane, 16);
 #pragma unroll
         for (int j = 0; j < 4; ++j) copy16(&x.e[j >> 1][j & 1][lane], src + j * 32 + lane, 16);
     };
-    float od[2] = {0.0f, 0.0f}, et[2][4][2];  // o . dO and eta of the last two chunks prepared
+    // Of the last two chunks prepared: eta of the lane's tokens; of token `tok`, scale b dO . S q and the factors of dP . S k and of e . X k
+    const int tok = (g >> 1) * 8 + 2 * c4 + (g & 1);  // sum_rows leaves a lane this token's sum
+    float et[2][4][2], by_q[2] = {0.0f, 0.0f}, by_k[2] = {0.0f, 0.0f}, by_x[2] = {0.0f, 0.0f}, x_inv = 1.0f;
     auto prepare = [&](int i, int st) {
         X& x = xb[i & 1];
         const uint32_t as = ring + st * SB + AT_A;
@@ -503,15 +512,19 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
         frag_tok(x.d_o[0], d);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float4 o = x.o[j][lane];
-            sums[2 * j] = fmaf(d[j][0], o.x, d[j][2] * o.z);
-            sums[2 * j + 1] = fmaf(d[j][1], o.y, d[j][3] * o.w);
+            const float4 y = x.sq[j][lane];
+            sums[2 * j] = fmaf(d[j][0], y.x, d[j][2] * y.z);
+            sums[2 * j + 1] = fmaf(d[j][1], y.y, d[j][3] * y.w);
             m = fmaxf(m, fmaxf(fmaxf(fabsf(d[j][0]), fabsf(d[j][1])), fmaxf(fabsf(d[j][2]), fabsf(d[j][3]))));
         }
         m = warp_most(m);
-        if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_do)[((size_t)n * nch + nch - 1 - i) * a.l.slices + slice] = m;
-        od[0] = od[1];
-        od[1] = sum_rows(sums, lane);
+        const size_t at = ((size_t)n * nch + nch - 1 - i) * a.l.slices + slice;
+        const float c_inv = reinterpret_cast<const float*>(a.ws + a.l.c_inv)[at];
+        if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.max_do)[at] = m;
+        by_q[0] = by_q[1]; by_k[0] = by_k[1]; by_x[0] = by_x[1];
+        by_q[1] = sum_rows(sums, lane) * sc[kRecBq * 32 + tok] * c_inv;
+        by_k[1] = sc[kRecBk * 32 + tok] * c_inv;
+        by_x[1] = sc[kRecW * 32 + tok];
         float f, q;
         pow2_scale(m, f, q);
         float in[4][4] = {}, il[4][4] = {};
@@ -563,11 +576,13 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
         const int c = nch - 1 - i;
         X& x = xb[i & 1];
         const size_t at_max = ((size_t)n * nch + c) * a.l.slices + slice;
-        float z[4][4], part_[8], vv[4][4], m = 0.0f;
+        const int own = older ? 0 : 1;
+        float z[4][4], xk[4][4], part_[8], part_x[8], m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float4 y = x.z[j][lane];
+            const float4 y = x.z[j][lane], w = KS == 1 ? x.in[j][lane] : x.xk[KS > 1 ? j : 0][KS > 1 ? lane : 0];
             z[j][0] = y.x; z[j][1] = y.y; z[j][2] = y.z; z[j][3] = y.w;
+            xk[j][0] = w.x; xk[j][1] = w.y; xk[j][2] = w.z; xk[j][3] = w.w;
         }
         const float e_inv = reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at_max];
 #pragma unroll
@@ -581,23 +596,24 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const float (&zz)[4] = z[2 * kk + j];
+                    const float (&zz)[4] = z[2 * kk + j], (&xx)[4] = xk[2 * kk + j];
                     part_[4 * kk + 2 * j + y] = fmaf(zz[y], e[2 * j][y], zz[2 + y] * e[2 * j + 1][y]);
+                    part_x[4 * kk + 2 * j + y] = fmaf(xx[y], e[2 * j][y], xx[2 + y] * e[2 * j + 1][y]);
                 }
         }
-        // lane 4 g + c4 holds the sum of value g of its c4 group: token (g >> 1) * 8 + 2 c4 + (g & 1)
-        const size_t at = at_max * kDeltaChunk + (g >> 1) * 8 + 2 * c4 + (g & 1);
+        const size_t at = at_max * kDeltaChunk + tok;
         reinterpret_cast<float*>(a.ws + a.l.part_eta)[at] = sum_rows(part_, lane) * e_inv;
-        frag_tok(x.v[0], vv);
-        const float (&eta)[4][2] = et[older ? 0 : 1];
+        reinterpret_cast<float*>(a.ws + a.l.part_x)[at] = sum_rows(part_x, lane) * e_inv * (by_x[own] * x_inv);
+        const float (&eta)[4][2] = et[own];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            const float4 y = x.sk[j][lane];
             z[j][0] *= eta[j][0]; z[j][1] *= eta[j][1]; z[j][2] *= eta[j][0]; z[j][3] *= eta[j][1];  // dP = dV
-            part_[2 * j] = fmaf(vv[j][0], z[j][0], vv[j][2] * z[j][2]);
-            part_[2 * j + 1] = fmaf(vv[j][1], z[j][1], vv[j][3] * z[j][3]);
+            part_[2 * j] = fmaf(y.x, z[j][0], y.z * z[j][2]);
+            part_[2 * j + 1] = fmaf(y.y, z[j][1], y.w * z[j][3]);
             m = fmaxf(m, fmaxf(fmaxf(fabsf(z[j][0]), fabsf(z[j][1])), fmaxf(fabsf(z[j][2]), fabsf(z[j][3]))));
         }
-        reinterpret_cast<float*>(a.ws + a.l.part_gate)[at] = od[older ? 0 : 1] - sum_rows(part_, lane);
+        reinterpret_cast<float*>(a.ws + a.l.part_s)[at] = fmaf(-sum_rows(part_, lane), by_k[own], by_q[own]);
         float sp, ip;
         pow2_scale(warp_most(m), sp, ip);
         uint4* dst = reinterpret_cast<uint4*>(a.ws + a.l.dp) + at_max * 64 * KT;
@@ -606,7 +622,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
             uint32_t hi[4], lo[4];
             to_a(z[2 * kk], z[2 * kk + 1], sp, sp, hi, lo);
             dst[kk * 32 + lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            if (KT == 2) dst[(2 + kk) * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            uint4* second = KT == 2 ? dst + 64 : reinterpret_cast<uint4*>(a.ws + a.l.dp_lo) + at_max * 64;
+            second[kk * 32 + lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         if (lane == 0) reinterpret_cast<float*>(a.ws + a.l.dp_inv)[at_max] = ip;
         if (KT == 1) {
@@ -648,14 +665,14 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
         const int c = nch - 1 - i;
         if (lane != 0 || !((c & 1) || c == nch - 1)) return;
         const X& x = xb[i & 1];
-        const size_t at = ((size_t)n * (a.l.nblk + 1) + (c >> 1)) * a.l.slices + slice;
+        const size_t at = ((size_t)n * a.l.nblk + (c >> 1)) * a.l.slices + slice;
         bulk_store(a.ws + a.l.X + at * a.l.state_bytes * KT, sm100::smem_u32(x.x), (uint32_t)a.l.state_bytes * KT);
         reinterpret_cast<float*>(a.ws + a.l.x_inv)[at] = x.x_inv;
     };
     auto near_s = [&](int i) {  // the state that the chain takes its inner product with in step i, into L2
-        const int c = nch - 1 - i, blk = c >> 1;
-        if (i >= nch || !active || !((c & 1) || i == 0) || lane * 128 >= (int)a.l.state_bytes) return;
-        const size_t at = ((size_t)n * (a.l.nblk + 1) + blk + 1) * a.l.slices + slice;
+        const int c = nch - 1 - i;
+        if (i >= nch || !active || (c & 1) || lane * 128 >= (int)a.l.state_bytes) return;
+        const size_t at = ((size_t)n * a.l.nblk + (c >> 1)) * a.l.slices + slice;
         asm volatile("prefetch.global.L2 [%0];" ::"l"(a.ws + a.l.S + at * a.l.state_bytes + lane * 128));
         asm volatile("prefetch.global.L2 [%0];" ::"l"(a.ws + a.l.S_lo + at * a.l.state_bytes + lane * 128));
     };
@@ -678,9 +695,11 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
         asm volatile("cp.async.commit_group;" ::: "memory");
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
+        const float x_inv_next = xb[i & 1].x_inv;  // the chain gives that place another value while finish(i) runs
         if (active) save_x(i);
         bulk_store_commit();
         if (active && i > 0) finish(i - 1, true);
+        x_inv = x_inv_next;
         if (i + 1 < nch) {
             wait_phase(&full[st_next], phase_next, wait, 904);
             if (active) prepare(i + 1, st_next);
@@ -697,44 +716,156 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
     bulk_store_done();
 }
 
-// d eta and d log_gamma from the slices' sums: a warp per block of 64 tokens, lane = token of each of its chunks.  Sums of many terms in 64 bits: what is
-// left of them counts.
-__global__ void __launch_bounds__(kGateWarps * 32) delta_gate_kernel(const DeltaBwdArgs ba) {
+// d eta and d log_gamma: a warp per chunk, the two chunks of a block beside each other.  dO_s . e_i and dP_s . e_i over all value rows are products of the
+// fragments that the walks left (rows to columns by transposing 8 x 8 matrices in registers), both terms of every operand; A and D K K^T come from
+// the chunk's record.  The sums over i < t <= s are formed as they stand, first over i, then over s.  B = b_end <X, S_0> comes from the walk for a
+// block's first chunk, whose S_0 is kept.  For the second one it is what reaches this chunk at all, which is its first token's gradient and known from the
+// first chunk (B and all X terms there), without what its tokens read (all S terms).  That difference is the one place where terms cancel, down to
+// another token's gradient in 32 bits; where the chunk forgets everything, B is 0.
+// Bound by fetching the fragments: 64 heads of 4096 tokens, 128 x 128, bf16, in 100 us (390 MB: 3.9 TB/s); 96 of 2048, 64 x 64, in 50 us.
+template <typename IO, int KT>
+__global__ void __launch_bounds__(kGateWarps * 32) delta_gate_kernel(const DeltaBwdArgs ba, const bool pairs) {
+    __shared__ float grid[kGateWarps][32][33];
+    __shared__ double handed[kGateWarps / 2];
     const DeltaArgs& a = ba.f;
-    const int64_t item = (int64_t)blockIdx.x * kGateWarps + (threadIdx.x >> 5), n = item / a.l.nblk;
-    if (item >= a.l.N * a.l.nblk) return;
-    const int lane = threadIdx.x & 31, blk = (int)(item % a.l.nblk), nchunks = min(2, a.l.nch - 2 * blk);
+    const DeltaShape& s = a.s;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c4 = lane & 3;
+    const int64_t item = (int64_t)blockIdx.x * (kGateWarps / 2) + (warp >> 1), n = item / a.l.nblk;
+    const int blk = (int)(item % a.l.nblk), c = 2 * blk + (warp & 1), t0 = c * kDeltaChunk;
+    const bool here = item < a.l.N * a.l.nblk && c < a.l.nch;
     const float4* hx = reinterpret_cast<const float4*>(a.ws + a.l.hx) + (size_t)item * a.l.slices;
-    float de[2] = {0.0f, 0.0f};
-    double dg[2] = {0.0, 0.0}, behind = 0.0;
-#pragma unroll 4
-    for (int i = 0; i < a.l.slices; ++i) {
-        behind += (hx[i].x + hx[i].y) + (hx[i].z + hx[i].w);
+    double flow = 0.0, back = 0.0, forth = 0.0, through = 0.0;  // of token t = lane: what is handed on; S terms; X terms; B
+    float de = 0.0f;
+    bool forgets = false;
+    if (here) {
+        const char* rec = a.ws + a.l.rec + ((size_t)n * a.l.nch + c) * a.l.rec_bytes;
+        float wo[6][4], wp[6][4];  // dO_s . e_i and dP_s . e_i
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (k >= nchunks) continue;
-            const size_t at = (((size_t)n * a.l.nch + 2 * blk + k) * a.l.slices + i) * kDeltaChunk + lane;
-            de[k] += reinterpret_cast<const float*>(a.ws + a.l.part_eta)[at];
-            dg[k] += reinterpret_cast<const float*>(a.ws + a.l.part_gate)[at];
+        for (int i = 0; i < 6; ++i)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) wo[i][x] = wp[i][x] = 0.0f;
+        const IO* d_o = reinterpret_cast<const IO*>(ba.d_o) + ((size_t)n * s.L + t0) * s.dv;
+        for (int sl = 0; sl < a.l.slices; ++sl) {
+            const size_t at = ((size_t)n * a.l.nch + c) * a.l.slices + sl;
+            const uint4* e4 = reinterpret_cast<const uint4*>(a.ws + a.l.e) + at * 128 + lane;
+            const uint4* p4 = reinterpret_cast<const uint4*>(a.ws + a.l.dp) + at * 64 * KT + lane;
+            const uint4* q4 = KT == 2 ? p4 + 64 : reinterpret_cast<const uint4*>(a.ws + a.l.dp_lo) + at * 64 + lane;
+            const uint4 raw_e[2][2] = {{e4[0], e4[32]}, {e4[64], e4[96]}}, raw_p[2][2] = {{p4[0], p4[32]}, {q4[0], q4[32]}};
+            const float e_inv = reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at], p_inv = reinterpret_cast<const float*>(a.ws + a.l.dp_inv)[at];
+            de += reinterpret_cast<const float*>(a.ws + a.l.part_eta)[at * kDeltaChunk + lane];
+            back += reinterpret_cast<const float*>(a.ws + a.l.part_s)[at * kDeltaChunk + lane];
+            forth += reinterpret_cast<const float*>(a.ws + a.l.part_x)[at * kDeltaChunk + lane];
+            if (!(c & 1)) through += (hx[sl].x + hx[sl].y) + (hx[sl].z + hx[sl].w);
+            float so, o_inv;
+            pow2_scale(reinterpret_cast<const float*>(a.ws + a.l.max_do)[at], so, o_inv);
+            // A operands: tokens x value rows of the slice.  [term][tokens 0-15, 16-31]
+            uint32_t ao[KT][2][4], ap[2][2][4], b[2][4][2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = m * 16 + (r & 1) * 8 + g, d = sl * 16 + (r >> 1) * 8 + 2 * c4;
+                    const IO* p = d_o + (size_t)t * s.dv + d;
+                    const bool ok = t0 + t < s.L;
+                    float y0 = 0.0f, y1 = 0.0f;
+                    if (sizeof(IO) == 2 && pairs) {
+                        if (ok && d < s.dv) {
+                            const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+                            y0 = __uint_as_float(w << 16);
+                            y1 = __uint_as_float(w & 0xffff0000u);
+                        }
+                    } else {
+                        if (ok && d < s.dv) y0 = to_f32(p[0]);
+                        if (ok && d + 1 < s.dv) y1 = to_f32(p[1]);
+                    }
+                    uint32_t hi, lo;
+                    split(y0 * so, y1 * so, hi, lo);  // with bf16 one term, exactly
+                    ao[0][m][r] = hi;
+                    if (KT == 2) ao[KT - 1][m][r] = lo;
+                }
+            // fragments [value rows][tokens]: register r of k-step kk holds rows 8 (r & 1) .., tokens 16 kk + 8 (r >> 1) ..
+#pragma unroll
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const uint4 x = raw_e[term][kk], y = raw_p[term][kk];
+                    const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        b[term][2 * kk + (r >> 1)][r & 1] = transposed(xw[r]);
+                        ap[term][kk][(r >> 1) + 2 * (r & 1)] = transposed(yw[r]);
+                    }
+                }
+            const float fo = o_inv * e_inv, fp = p_inv * e_inv;
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                const int m = i < 2 ? 0 : 1, j = i < 2 ? i : i - 2;
+                float y[4];
+                mma0(y, ao[0][m], b[1][j][0], b[1][j][1]);
+                if (KT == 2) mma(y, ao[KT - 1][m], b[0][j][0], b[0][j][1]);
+                mma(y, ao[0][m], b[0][j][0], b[0][j][1]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) wo[i][x] = fmaf(y[x], fo, wo[i][x]);
+                mma0(y, ap[0][m], b[1][j][0], b[1][j][1]);
+                mma(y, ap[1][m], b[0][j][0], b[0][j][1]);
+                mma(y, ap[0][m], b[0][j][0], b[0][j][1]);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) wp[i][x] = fmaf(y[x], fp, wp[i][x]);
+            }
         }
-    }
+        const float4* pair = reinterpret_cast<const float4*>(rec + kDeltaRecPairs) + lane;
+        const float* sc = reinterpret_cast<const float*>(rec + kDeltaRecSkip);
+        float (&m)[32][33] = grid[warp];
 #pragma unroll
-    for (int k = 1; k >= 0; --k) {  // suffix sums, the second chunk's first
-        if (k >= nchunks) continue;
-        double sum = dg[k];
+        for (int i = 0; i < 6; ++i) {
+            const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i * 8 : (i - 2) * 8;
+            const float4 q = pair[i * 32], k = pair[(6 + i) * 32];
+            const float qw[4] = {q.x, q.y, q.z, q.w}, kw[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
+                m[t][u] = u < t ? (qw[x] * wo[i][x] - kw[x] * wp[i][x]) * sc[kRecEta * 32 + u] : 0.0f;
+            }
+        }
+        __syncwarp();
+        float run = 0.0f;  // lane = s: sum over i < t for every t up to s
+#pragma unroll 4
+        for (int t = 0; t < 32; ++t) {
+            const float x = t < lane ? m[lane][t] : 0.0f;
+            m[lane][t] = t <= lane ? run : 0.0f;
+            run += x;
+        }
+        __syncwarp();
+#pragma unroll 4
+        for (int t = 0; t < 32; ++t) flow += m[t][lane];  // lane = t: over s >= t
+        // S terms from t on, X terms before t, and all of either
+        double after = back, before = __shfl_up_sync(kAll, forth, 1);
+        if (lane == 0) before = 0.0;
 #pragma unroll
         for (int i = 1; i < 32; i <<= 1) {
-            const double y = __shfl_down_sync(kAll, sum, i);
-            if (lane + i < 32) sum += y;
+            const double y = __shfl_down_sync(kAll, after, i), z = __shfl_up_sync(kAll, before, i);
+            if (lane + i < 32) after += y;
+            if (lane >= i) before += z;
         }
-        sum += behind;
-        behind = __shfl_sync(kAll, sum, 0);
-        const int t = blk * kDeltaBlock + k * kDeltaChunk + lane;
-        if (t >= a.s.L) continue;
-        const size_t out = (size_t)n * a.s.L + t;
-        ba.d_eta[out] = de[k];
-        ba.d_log_gamma[out] = a.log_gamma[out] < -104.0f ? 0.0f : (float)sum;  // a decay that is 0 in 32 bits has none
+        flow += after + before;
+        back = __shfl_sync(kAll, after, 0);
+        forth = __shfl_sync(kAll, before + forth, 31);
+        const float end = sc[kRecHead * 32 + kHeadEnd];
+        forgets = end == 0.0f;
+        if (!(c & 1)) {
+            through *= end;
+            if (lane == 0) handed[warp >> 1] = through + forth;
+        }
     }
+    __syncthreads();
+    if (!here) return;
+    if ((c & 1) && !forgets) through = handed[warp >> 1] - back;
+    flow += through;
+    const int t = t0 + lane;
+    if (t >= s.L) return;
+    const size_t out = (size_t)n * s.L + t;
+    ba.d_eta[out] = de;
+    ba.d_log_gamma[out] = a.log_gamma[out] < -104.0f ? 0.0f : (float)flow;  // a decay that is 0 in 32 bits has none
 }
 
 // ---- dQ and dK ----------------------------------------------------------------------------------------------------
@@ -794,7 +925,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
         if (lane != 0) return;
         const uint32_t bytes = (uint32_t)(a.l.slices * a.l.state_bytes);
         sm100::mbar_expect_tx(bar, bytes);
-        bulk_copy(sm100::smem_u32(raw_s), a.ws + off + ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices * a.l.state_bytes, bytes, bar);
+        bulk_copy(sm100::smem_u32(raw_s), a.ws + off + ((size_t)n * a.l.nblk + blk) * a.l.slices * a.l.state_bytes, bytes, bar);
     };
     auto fetch_tok = [&](int64_t n) {
         const uint32_t rows = vec ? (uint32_t)(min(kDeltaBlock, s.L - t0) * s.dv * 2) : 0;
@@ -867,7 +998,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
         } else {  // lane = slice and chunk
             const int sl = lane & 7, ch = lane >> 3;
             const bool ok = sl < a.l.slices, tok = ok && ch < nchunks;
-            const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl, at_s = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl;
+            const size_t at = ((size_t)n * a.l.nch + 2 * blk + ch) * a.l.slices + sl, at_s = ((size_t)n * a.l.nblk + blk) * a.l.slices + sl;
             x[0] = tok ? reinterpret_cast<const float*>(a.ws + a.l.e_inv)[at] : 0.0f;
             x[1] = tok ? reinterpret_cast<const float*>(a.ws + a.l.dp_inv)[at] : 0.0f;
             x[2] = tok ? reinterpret_cast<const float*>(a.ws + a.l.max_do)[at] : 0.0f;
@@ -959,7 +1090,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
                 const int i = warp + 16 * q, kk = i % (DK / 16), sl = i / (DK / 16) % SL, term = i / (DK / 16) / SL;
                 x[q] = make_uint4(0, 0, 0, 0);
                 if (sl0 + sl >= a.l.slices) continue;
-                const size_t at = ((size_t)n * (a.l.nblk + 1) + blk) * a.l.slices + sl0 + sl;
+                const size_t at = ((size_t)n * a.l.nblk + blk) * a.l.slices + sl0 + sl;
                 const char* src = off_lo ? a.ws + (term ? off_lo : off) + at * a.l.state_bytes : a.ws + off + (at * terms + term) * a.l.state_bytes;
                 x[q] = reinterpret_cast<const uint4*>(AHEAD ? raw_s + sl * 32 * DK : src)[kk * 32 + lane];
             }
@@ -1250,7 +1381,7 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
     const DeltaArgs& a = b.f;
     {
         constexpr int most = KT == 1 ? 4 : 2;
-        const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(b.d_o) | reinterpret_cast<uintptr_t>(b.dv)) % 16 == 0;
+        const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(b.d_o) | reinterpret_cast<uintptr_t>(b.dv)) % 16 == 0;
         int rc;
         if (a.l.N * a.l.slices <= 148) {
             rc = launch_chain<IO, DK, KT, DK / 32>(b, 1, vec, st);
@@ -1268,7 +1399,9 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
     else if constexpr (KT == 1) rc = a.l.slices <= qk_rows<DK, KT>() / 16 ? launch_qk<IO, DK, KT, true>(b, st) : launch_qk<IO, DK, KT, false>(b, st);
     else rc = launch_qk<IO, DK, KT, false>(b, st);
     if (rc != 0) return rc;
-    delta_gate_kernel<<<(unsigned)((a.l.N * a.l.nblk + kGateWarps - 1) / kGateWarps), kGateWarps * 32, 0, st>>>(b);
+    const bool pairs = a.s.dv % 2 == 0 && reinterpret_cast<uintptr_t>(b.d_o) % 4 == 0;
+    constexpr int blocks = kGateWarps / 2;
+    delta_gate_kernel<IO, KT><<<(unsigned)((a.l.N * a.l.nblk + blocks - 1) / blocks), kGateWarps * 32, 0, st>>>(b, pairs);
     return (int)cudaGetLastError();
 }
 

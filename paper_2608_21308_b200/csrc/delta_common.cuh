@@ -127,6 +127,12 @@ __device__ __forceinline__ void stsm4_t(uint32_t addr, uint32_t a, uint32_t b, u
 __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+// an 8 x 8 matrix of 16-bit values over a warp, transposed: lane 4 g + c holds [g][2 c], [g][2 c + 1] before and after
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 
 // Tiles of fp16 in shared memory and in the workspace: rows of COLS values, the 16-byte piece p of row r at place p ^ swz(r), so that
 // eight rows' pieces of one column (an 8 x 8 matrix of ldmatrix) lie in different banks.

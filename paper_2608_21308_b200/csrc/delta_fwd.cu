@@ -9,9 +9,9 @@
 // A chain is bound by the instructions of a chunk one after the other (an MMA every 8 cycles, 146 of them, and splitting the operands into
 // terms), so scales are one per slice, folded into the scalars that the values are multiplied with anyway, and come from bounds that are known
 // before the values are.
-// 4 x 16 sequences of 4096 tokens, 128 x 128, bf16: 226 us (128 chunks, one after the other: 1.8 us each), 355 us with saved states (540 MB of states,
-// errors and fp32 outputs to write, and the outputs' products with both terms); 16 sequences of 32768 tokens: 1180 us (1024 chunks: 1.15 us each,
-// the columns of a slice over four warps); 8 x 12 sequences of 2048 tokens, 64 x 64, with saved states: 135 us.
+// 4 x 16 sequences of 4096 tokens, 128 x 128, bf16: 268 us (128 chunks, one after the other: 2.1 us each), 317 us with saved states (670 MB of states,
+// errors and the states' products with queries and keys to write); 16 sequences of 32768 tokens: 1440 us (1024 chunks: 1.4 us each, the columns of a
+// slice over four warps); 8 x 12 sequences of 2048 tokens, 64 x 64, with saved states: 121 us.
 #include "api_checks.h"
 #include "delta_common.cuh"
 
@@ -38,7 +38,8 @@ template <int DK, int KT, int KS> constexpr int fwd_smem(int slices) {
 }
 
 // vec: bf16 rows of v and o that allow 16-byte pieces.
-template <typename IO, int DK, int KT, int KS>
+// SAVE: what the reverse pass reads is kept.
+template <typename IO, int DK, int KT, int KS, bool SAVE>
 __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const DeltaArgs a, const int per, const bool vec) {
     extern __shared__ __align__(1024) char smem[];
     constexpr int NS = stages<KT>(), DC = DK / KS, SB = stage_bytes<DK, KT>();
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 for (int i = 0; i < 2 * TERMS; ++i) times_k(kk, i, kk == 0, b);
             }
             hand(xb[0]);
-            if (a.save) sm100::fence_proxy_async_smem();
+            if (SAVE) sm100::fence_proxy_async_smem();
         }
         __syncthreads();  // the values of chunk 0
         int st = 0, st_next = 1, phase_next = 0;
@@ -182,6 +183,14 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
             const bool come = c + 1 == nch || probe_phase(&full[st_next], phase_next);
             if (active) {
                 take(x);
+                if (SAVE) {  // S K^T as it is, for the decays' gradients
+                    const size_t at = ((size_t)n * nch + c) * a.l.slices + slice;
+                    float4* dst = reinterpret_cast<float4*>(a.ws + a.l.sk) + at * 128;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (KS == 1 || part == (j >> 1)) dst[j * 32 + lane] = make_float4(sk[j][0], sk[j][1], sk[j][2], sk[j][3]);
+                    if (lane == 0 && part == 0) reinterpret_cast<float*>(a.ws + a.l.c_inv)[at] = s_inv;
+                }
                 // T's blocks (the one above the diagonal is zero)
                 uint32_t th[3][4], tl[3][4];  // (rows 0-15, k 0), (rows 16-31, k 0), (rows 16-31, k 1)
                 ldsm4(th[0], addr_nk<32>(ts, 0, 0, lane)); ldsm4(th[1], addr_nk<32>(ts, 2, 0, lane)); ldsm4(th[2], addr_nk<32>(ts, 2, 1, lane));
@@ -357,7 +366,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
 #pragma unroll
                 for (int i = 0; i < 2 * TERMS; ++i) times_k(2 * NJ - 1, i, false, fk[1]);
                 hand(xn);
-                if (a.save) sm100::fence_proxy_async_smem();  // the outputs' warp has the fragments copied from there
+                if (SAVE) sm100::fence_proxy_async_smem();  // the outputs' warp has the fragments copied from there
             }
             st = st_next;
             if (++st_next == NS) { st_next = 0; phase_next ^= 1; }
@@ -526,10 +535,10 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 fma2(in[j][z], in[j][z + 1], sq[j][z], sq[j][z + 1], y0, y1, in[j][z], in[j][z + 1]);
             }
         }
-        if (a.save) {
-            float4* dst = reinterpret_cast<float4*>(a.ws + a.l.o) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
+        if (SAVE) {
+            float4* dst = reinterpret_cast<float4*>(a.ws + a.l.sq) + (((size_t)n * nch + c) * a.l.slices + slice) * 128;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) dst[j * 32 + lane] = make_float4(in[j][0], in[j][1], in[j][2], in[j][3]);
+            for (int j = 0; j < 4; ++j) dst[j * 32 + lane] = make_float4(sq[j][0], sq[j][1], sq[j][2], sq[j][3]);
         }
         if (!o) return;
         if (KT == 1) {  // through shared memory to lane = token
@@ -568,10 +577,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     // what the reverse pass reads of S and e: their fragments as they lie in shared memory
     auto save_s = [&](int slot, const X& x) {
         if (lane != 0) return;
-        const size_t at = ((size_t)n * (a.l.nblk + 1) + slot) * a.l.slices + slice;
+        const size_t at = ((size_t)n * a.l.nblk + slot) * a.l.slices + slice;
         bulk_store(a.ws + a.l.S + at * a.l.state_bytes, sm100::smem_u32(x.s[0]), (uint32_t)a.l.state_bytes);
-        if (slot > 0 || KT == 2)  // with bf16 the start state's second term enters no inner product
-            bulk_store(a.ws + a.l.S_lo + at * a.l.state_bytes, sm100::smem_u32(x.s[1]), (uint32_t)a.l.state_bytes);
+        bulk_store(a.ws + a.l.S_lo + at * a.l.state_bytes, sm100::smem_u32(x.s[1]), (uint32_t)a.l.state_bytes);
         reinterpret_cast<float*>(a.ws + a.l.s_inv)[at] = x.s_inv;
     };
     auto save_e = [&](int c, const X& x) {
@@ -587,10 +595,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
     int st = 0, phase = 0;
     for (int i = 0; i <= nch; ++i) {
         if (i + 1 < nch) load_v(i + 1);  // the chain reads chunk i's
-        if (a.save && active) {
+        if (SAVE && active) {
             if (i > 0) save_e(i - 1, xb[(i - 1) & 1]);
-            if (i == nch) save_s(a.l.nblk, xb[i & 1]);
-            else if ((i & 1) == 0) save_s(i >> 1, xb[i & 1]);
+            if (i < nch && (i & 1) == 0) save_s(i >> 1, xb[i & 1]);
             bulk_store_commit();
         }
         if (active && i > 0) finish(i - 1, st == 0 ? NS - 1 : st - 1, sq, s_inv);
@@ -601,20 +608,20 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 s_inv = xb[i & 1].s_inv;
             }
             if (i + 1 < nch) hand_v(i + 1);
-            if (a.save) bulk_store_read();  // the chain may write there again
+            if (SAVE) bulk_store_read();  // the chain may write there again
             __syncthreads();  // chunk i is through the chain, chunk i - 1 through here
         }
         if (fetches && i > 0 && i - 1 + NS < nch) fetch(i - 1 + NS, st == 0 ? NS - 1 : st - 1);
         __syncwarp();
         if (++st == NS) { st = 0; phase ^= 1; }
     }
-    if (a.save) bulk_store_done();
+    if (SAVE) bulk_store_done();
 }
 
-template <typename IO, int DK, int KT, int KS> int launch(const DeltaArgs& a, int per, cudaStream_t st) {
-    auto kernel = delta_fwd_kernel<IO, DK, KT, KS>;
+template <typename IO, int DK, int KT, int KS, bool SAVE> int launch(const DeltaArgs& a, int per, cudaStream_t st) {
+    auto kernel = delta_fwd_kernel<IO, DK, KT, KS, SAVE>;
     const int bytes = fwd_smem<DK, KT, KS>(per);
-    cudaError_t e = allow_shared_memory<delta_fwd_kernel<IO, DK, KT, KS>>();
+    cudaError_t e = allow_shared_memory<delta_fwd_kernel<IO, DK, KT, KS, SAVE>>();
     if (e != cudaSuccess) return (int)e;
     const unsigned grid = (unsigned)(a.l.N * ((a.l.slices + per - 1) / per));
     const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o)) % 16 == 0;
@@ -622,25 +629,29 @@ template <typename IO, int DK, int KT, int KS> int launch(const DeltaArgs& a, in
     return (int)cudaGetLastError();
 }
 
-template <typename IO, int DK, int KT> int dispatch(const DeltaArgs& a, cudaStream_t st) {
+template <typename IO, int DK, int KT, bool SAVE> int dispatch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int most = KT == 1 ? 4 : 2;
     static_assert(fwd_smem<DK, KT, 1>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32>(1) <= kMostSharedMemory, "shared memory");
     // Few slices, as many as SMs at most: one per CTA, its columns over DK / 32 warps; with more of them the warps share an SM's schedulers and a chain
     // per warp is faster.  Then slices of a sequence share the tiles that they fetch, as long as 96 CTAs are left.  Forward and reverse pass
     // together, us: 8 x 12 x 2048 tokens, 64 x 64, bf16: 4 slices per CTA 554, 2: 563, 1: 647, one over two warps 744.  Forward alone, 128 x 128,
     // 16 heads x 4096 tokens: B = 4: 4 slices 310, 2: 421; B = 2: 2 slices 220, 4: 269.  fp32 tiles leave room for two.
-    if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32>(a, 1, st);
+    if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, SAVE>(a, 1, st);
     int per = most;
     while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
-    return launch<IO, DK, KT, 1>(a, per, st);
+    return launch<IO, DK, KT, 1, SAVE>(a, per, st);
+}
+
+template <typename IO, int DK, int KT> int either(const DeltaArgs& a, cudaStream_t st) {
+    return a.save ? dispatch<IO, DK, KT, true>(a, st) : dispatch<IO, DK, KT, false>(a, st);
 }
 
 }  // namespace
 
 int delta_fwd_launch(const DeltaArgs& a, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    if (a.s.f32) return a.l.DK == 64 ? dispatch<float, 64, 2>(a, st) : dispatch<float, 128, 2>(a, st);
-    return a.l.DK == 64 ? dispatch<__nv_bfloat16, 64, 1>(a, st) : dispatch<__nv_bfloat16, 128, 1>(a, st);
+    if (a.s.f32) return a.l.DK == 64 ? either<float, 64, 2>(a, st) : either<float, 128, 2>(a, st);
+    return a.l.DK == 64 ? either<__nv_bfloat16, 64, 1>(a, st) : either<__nv_bfloat16, 128, 1>(a, st);
 }
 
 }  // namespace e2ttt

@@ -309,6 +309,14 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
                 }
             }
         }
+        if (a.save) {
+            float4* pairs = reinterpret_cast<float4*>(rec + kDeltaRecPairs);
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                pairs[i * 32 + lane] = make_float4(av[i][0], av[i][1], av[i][2], av[i][3]);
+                pairs[(6 + i) * 32 + lane] = make_float4(gk[i][0], gk[i][1], gk[i][2], gk[i][3]);
+            }
+        }
         __syncwarp();
         // T, and with saved states the same with eta on the rows: what the reverse pass multiplies with
         float tsum = 0.0f, ti = 0.0f, ri = 0.0f, rsum, csum;
