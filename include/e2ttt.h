@@ -271,8 +271,9 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  * tokens (decoding), without a workspace; both move the same state and may follow each other.
  * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly, neither finer than 2^-27 of the largest
  * value of a chunk's queries or keys, or of 16 neighbouring value rows of a state; outputs are rounded once, and the same with and without saved states.
- * bf16 dq and dk are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  The largest magnitude of a
- * tensor should be 0 or lie between 2^-90 and 2^100.
+ * bf16 dq and dk are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  Tensors, and the chunks of a
+ * tensor, may be as far from one another as they like as long as their largest magnitudes are 0 or between 2^-60 and 2^60, and the products that the
+ * formulas form of them are in fp32's range.
  * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
  * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
  * queries and keys of their own, keep their outputs bit for bit.

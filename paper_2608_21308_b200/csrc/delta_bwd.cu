@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
                 pow2_bound(ub, f, q);
                 // dU, times its scale f
                 float p[4][4], z[4][4];
-                const float fs = f * s_inv;
+                const float fs = scales(f, s_inv);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float4 in = x.in[j][lane];
@@ -287,9 +287,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
                         ql[kk][r] = *reinterpret_cast<const uint32_t*>(&y2);
                     }
                 }
-                const float wf = -fw * qe, old_inv = s_inv;
+                const float wf = -scales(fw, qe), old_inv = s_inv;
                 pow2_bound(fmaf(bend, norm, fmaf(zb, head[kHeadZsum], x.q_sum)), s_now, s_inv);
-                w_old = bend * (s_now * old_inv);
+                w_old = scales(bend * old_inv, s_now);
                 w_new = w_inv * s_now;
                 float w[4][4];
 #pragma unroll
@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
             const float2 e2 = *reinterpret_cast<const float2*>(sc + kRecEta * 32 + j * 8 + 2 * c4);
             et[0][j][0] = et[1][j][0]; et[0][j][1] = et[1][j][1];
             et[1][j][0] = e2.x; et[1][j][1] = e2.y;
-            d[j][0] *= bq.x * fq; d[j][1] *= bq.y * fq; d[j][2] *= bq.x * fq; d[j][3] *= bq.y * fq;
+            d[j][0] = d[j][0] * bq.x * fq; d[j][1] = d[j][1] * bq.y * fq; d[j][2] = d[j][2] * bq.x * fq; d[j][3] = d[j][3] * bq.y * fq;
         }
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {

@@ -44,6 +44,9 @@ __device__ __forceinline__ void pow2_bound(float m, float& s, float& inv) {
     s = __uint_as_float((uint32_t)(127 + e) << 23);
     inv = __uint_as_float((uint32_t)(127 - e) << 23);
 }
+// Product of two scales that meets a sum of zeros wherever it is this large (a bound of 0 has the scale 2^100: a state of 2^28 or more beside a chunk without keys
+// and values): kept finite, so that zeros stay zeros.
+__device__ __forceinline__ float scales(float x, float y) { return fminf(x * y, 0x1p120f); }
 // two fp32 values at a time (one instruction on this architecture)
 __device__ __forceinline__ uint64_t pack2(float x, float y) {
     uint64_t r;

@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                         mul2(p[j][2], p[j][3], v.z, v.w, f, f);
                     }
                 }
-                const float fs = -f * s_inv;
+                const float fs = -scales(f, s_inv);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float2 bk = *reinterpret_cast<const float2*>(sc + kRecBk * 32 + j * 8 + 2 * c4);
@@ -258,9 +258,9 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_fwd_kernel(const
                 pow2_bound(eb, pu, u_inv);
                 pow2_bound(eb * head[kHeadWmax], fw, w_inv);
                 uf = pu * qe;
-                const float wf = fw * qe, old_inv = s_inv;
+                const float wf = scales(fw, qe), old_inv = s_inv;
                 pow2_bound(fmaf(bend, norm, eb * head[kHeadWsum]), s_now, s_inv);
-                w_old = bend * (s_now * old_inv);
+                w_old = scales(bend * old_inv, s_now);
                 w_new = w_inv * s_now;
                 if (lane == 0 && part == 0) x.u_inv = u_inv;
                 float w[4][4];

@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     float* xs = reinterpret_cast<float*>(sm + 4608);
     double* run = reinterpret_cast<double*>(sm + prep_work_bytes<DK, KT>());
     float* eta_s = reinterpret_cast<float*>(run + 32);
-    float* norm_s = eta_s + 32;  // |k|^2
+    float* norm_s = eta_s + 32;  // |k|^2, in units of the tile
     char* out = a.ws + a.l.qk + (size_t)item * a.l.qk_bytes;
     const size_t row0 = ((size_t)nk * s.L + t0) * s.dk;
     float ik = 1.0f, iq = 1.0f, q_norm = 0.0f;
@@ -242,6 +242,16 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
     gram<DK, KT>(qs, ks, qk, lane);
     __syncwarp();
     const int g = lane >> 2, c4 = lane & 3, r = s.H / s.Hk;
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int t = (i < 2 ? 0 : 16) + g + (x >> 1) * 8, u = (i < 2 ? i * 8 : (i - 2) * 8) + 2 * c4 + (x & 1);
+            if (u == t) norm_s[t] = kk[i][x];
+        }
+    __syncwarp();
+    const float kn = sqrtf(norm_s[lane]) * ik;
+    const float ik_t = norm_s[lane] == 0.0f ? 0.0f : ik;  // a token without a key has factors of 0: no scale is stretched for it
     const int64_t b = nk / s.Hk, hk = nk % s.Hk;
     for (int j = 0; j < r; ++j) {
         const int64_t n = b * s.H + hk * r + j;
@@ -265,12 +275,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
         char* rec = a.ws + a.l.rec + ((size_t)n * a.l.nch + c) * a.l.rec_bytes;
         float* sc = reinterpret_cast<float*>(rec + 8192);
         const float bt = expf((float)sum), dend = expf((float)(end - sum));
-        sc[kRecBk * 32 + lane] = bt * ik;
+        sc[kRecBk * 32 + lane] = bt * ik_t;
         sc[kRecBq * 32 + lane] = bt * iq * s.scale;
         sc[kRecEta * 32 + lane] = eta;
-        sc[kRecDend * 32 + lane] = dend * ik;
-        sc[kRecW * 32 + lane] = eta * dend * ik;
-        sc[kRecZ * 32 + lane] = eta * bt * ik;
+        sc[kRecDend * 32 + lane] = dend * ik_t;
+        sc[kRecW * 32 + lane] = eta * dend * ik_t;
+        sc[kRecZ * 32 + lane] = eta * bt * ik_t;
         // N = strict(D (k k^T)) eta to shared memory, A = lower(D (q k^T)) scale to the record
         float amax = 0.0f, emax = 0.0f, av[6][4], gk[6][4];  // gk: strict(D (k k^T))
 #pragma unroll
@@ -280,7 +290,6 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             for (int x = 0; x < 4; ++x) {
                 const int t = m0 + g + (x >> 1) * 8, u = n0 + 2 * c4 + (x & 1);
                 const float D = u <= t ? expf((float)(run[t] - run[u])) : 0.0f;
-                if (u == t) norm_s[t] = kk[i][x] * (ik * ik);
                 gk[i][x] = u < t ? D * kk[i][x] * (ik * ik) : 0.0f;
                 Nm[t * 36 + u] = gk[i][x] * eta_s[u];
                 av[i][x] = u <= t ? D * qk[i][x] * (iq * ik * s.scale) : 0.0f;
@@ -294,12 +303,12 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
 #pragma unroll
         for (int i = 0; i < 6; ++i) {  // the block above the diagonal is read by no product
             const int m0 = i < 2 ? 0 : 16, n0 = i < 2 ? i : i - 2;
-            const float e0 = eta_s[n0 * 8 + 2 * c4] * es, e1 = eta_s[n0 * 8 + 2 * c4 + 1] * es;
+            const float e0 = eta_s[n0 * 8 + 2 * c4], e1 = eta_s[n0 * 8 + 2 * c4 + 1];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint32_t hi, lo;
                 const uint32_t at = tile_at<32>(m0 + g + x * 8, n0) + c4 * 4;
-                split(av[i][2 * x] * e0, av[i][2 * x + 1] * e1, hi, lo);
+                split(av[i][2 * x] * e0 * es, av[i][2 * x + 1] * e1 * es, hi, lo);
                 *reinterpret_cast<uint32_t*>(rec + 4096 + at) = hi;
                 *reinterpret_cast<uint32_t*>(rec + 6144 + at) = lo;
                 if (a.save) {
@@ -338,10 +347,10 @@ __global__ void __launch_bounds__(kWarps * 32, 3) delta_prep_kernel(const DeltaA
             }
             __syncwarp();
         }
-        const float kn = sqrtf(norm_s[lane]);
-        const float b_kn = warp_max(bt * kn), wmax = warp_max(fabsf(eta) * dend * ik), wsum = warp_sum(fabsf(eta) * dend * kn);
-        const float ke = warp_max(dend * kn), zmax = warp_max(fabsf(eta) * bt * ik), zsum = warp_sum(fabsf(eta) * bt * kn);
-        const float qsum = fabsf(s.scale) * sqrtf(warp_sum(bt * bt)) * q_norm;
+        const float b_kn = warp_max(bt * kn), wmax = warp_max(fabsf(eta) * dend * ik_t), wsum = warp_sum(fabsf(eta) * dend * kn);
+        const float ke = warp_max(dend * kn), zmax = warp_max(fabsf(eta) * bt * ik_t), zsum = warp_sum(fabsf(eta) * bt * kn);
+        const float up = bt * 0x1p60f;  // squares of decays down to 2^-120 stay in range
+        const float qsum = fabsf(s.scale) * (sqrtf(warp_sum(up * up)) * 0x1p-60f) * q_norm;
         if (lane == 0) {
             float* head = sc + kRecHead * 32;
             head[kHeadEnd] = expf((float)end);
