@@ -269,11 +269,13 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  *   S            [B,H,dv,dk] fp32           rows are outputs, as in the fast-weight matrices
  * e2ttt_delta_fwd runs whole sequences in chunks of 32 tokens on the tensor cores; e2ttt_delta_step is the recurrent form for a few
  * tokens (decoding), without a workspace; both move the same state and may follow each other.
- * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly, neither finer than 2^-27 of the largest
- * value of a chunk's queries or keys, or of 16 neighbouring value rows of a state; outputs are rounded once, and the same with and without saved states.
- * bf16 dq and dk are of products with one term (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  Tensors, and the chunks of a
- * tensor, may be as far from one another as they like as long as their largest magnitudes are 0 or between 2^-60 and 2^60, and the products that the
- * formulas form of them are in fp32's range.
+ * Arithmetic: fp32 sums and states, operands of 32 bits as two fp16 terms (22 bits), bf16 inputs exactly, neither finer than 2^-27 of the largest value of
+ * a chunk's queries or keys, of its errors e or their adjoints, or of 16 neighbouring value rows of a state or its adjoint; outputs are rounded once, and
+ * the same with and without saved states.  dq and dk are formed of 64 tokens (from a multiple of 64) and all value rows of a head: not finer than 2^-27 of the
+ * largest value of the state, its adjoint, the queries, the keys or the products of two tokens there; bf16 dq and dk, moreover, of products with one term
+ * (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  d_log_gamma is off by some 2e-6 of its size whatever the decay, as long as the
+ * decays of a chunk do not differ in size by more than that.
+ * The largest magnitude of a tensor should be 0 or lie between 2^-50 and 2^50; chunks, heads and documents in it may be smaller, or all zeros.
  * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
  * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
  * queries and keys of their own, keep their outputs bit for bit.

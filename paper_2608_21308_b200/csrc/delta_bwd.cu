@@ -275,7 +275,8 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
                 const float qe = q * head[kHeadR];
                 float fw, w_inv;
                 pow2_bound(fmaxf(zb * head[kHeadZmax], x.q_max), fw, w_inv);
-                const __half2 move = __float2half2_rn(fw * x.q_inv);
+                const float ratio = fw * x.q_inv;
+                const __half2 move = __float2half2_rn(ratio);
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk) {
                     const uint4 h4 = x.q[0][kk][lane], l4 = x.q[1][kk][lane];
@@ -285,6 +286,19 @@ __global__ void __launch_bounds__(KS == 1 ? 256 : 160, 1) delta_chain_kernel(con
                         const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&hw[r]), move), y2 = __hmul2(*reinterpret_cast<const __half2*>(&lw[r]), move);
                         qh[kk][r] = *reinterpret_cast<const uint32_t*>(&y);
                         ql[kk][r] = *reinterpret_cast<const uint32_t*>(&y2);
+                    }
+                }
+                if (ratio < 0x1p-14f) {  // dO far below the adjoint: what of it fits this scale, where the ratio itself has few bits in fp16 or none
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk) {
+                        const uint4 h4 = x.q[0][kk][lane], l4 = x.q[1][kk][lane];
+                        const uint32_t hw[4] = {h4.x, h4.y, h4.z, h4.w}, lw[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float y0, y1;
+                            join_terms(hw[r], lw[r], y0, y1);
+                            split(y0 * ratio, y1 * ratio, qh[kk][r], ql[kk][r]);
+                        }
                     }
                 }
                 const float wf = -scales(fw, qe), old_inv = s_inv;
@@ -871,7 +885,7 @@ __global__ void __launch_bounds__(kGateWarps * 32) delta_gate_kernel(const Delta
 // ---- dQ and dK ----------------------------------------------------------------------------------------------------
 // A CTA takes 64 tokens of one query / key head and adds up the value heads of its group.  Sixteen warps: 16 tokens times a quarter of the key
 // columns each.  The value rows come through shared memory ROWS at a time, with S_0 (dQ's and dK's first part, both token-by-token matrices) and
-// again with X; what the chains left in fragment order goes into tiles of rows here, at one scale for all slices.  With bf16 I/O one term of every
+// again with X; what the chains left in fragment order goes into tiles of rows here, at one scale for all slices (S, X) or all of a chunk (e, dP, dO).  With bf16 I/O one term of every
 // operand serves: dQ and dK are off by 2^-11 of their terms before they are rounded to 2^-8.  AHEAD: the next head's raw tiles come by bulk copies.
 // Bound by the dependent phases of a head (tiles, products with S, token matrices, products with X, products with K and Q, a barrier between any
 // two): 20 thousand cycles, of which the MMAs are 5, the tiles 4.  4 x 4 key heads of 4 value heads, 4096 tokens, 128 x 128, bf16: 335 us (470 MB: 1.4
@@ -906,8 +920,8 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
     char* mat = st_p + KT * TT;         // sigma, then kappa + kappa^T
     double* run2 = reinterpret_cast<double*>(mat + 2 * KT * 8192);  // [2][64], of this head and of the next
     float* bt2 = reinterpret_cast<float*>(run2 + 2 * 64);          // [2][3][64]: b, eta D_end, eta
-    float* scl2 = bt2 + 2 * 3 * 64;                                // [2][56]: the scales and the slices' ratios to them
-    float* red = scl2 + 2 * 56;                                    // 32
+    float* scl2 = bt2 + 2 * 3 * 64;                                // [2][64]: the scales and the slices' ratios to them
+    float* red = scl2 + 2 * 64;                                    // 32
     const uint32_t ks = sm100::smem_u32(kq), qs = ks + KT * 128 * DK, ss = sm100::smem_u32(st_s), os = sm100::smem_u32(st_o),
                    us = sm100::smem_u32(st_u), ps = sm100::smem_u32(st_p), ms = sm100::smem_u32(mat);
     const int nchunks = min(2, a.l.nch - 2 * blk);
@@ -950,10 +964,6 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
         fetch_state(n_first, a.l.S, &come[0]);
         fetch_tok(n_first);
     }
-    auto times_half = [](uint32_t x, __half2 y) {
-        const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&x), y);
-        return *reinterpret_cast<const uint32_t*>(&z);
-    };
     // the two chunks' tiles at one scale
     float ik, iq;
     {
@@ -969,10 +979,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
                 const char* src = a.ws + a.l.qk + ((size_t)nk * a.l.nch + 2 * blk + row / 32) * a.l.qk_bytes;
                 x = *reinterpret_cast<const uint4*>(src + (which * KT + term) * 64 * DK + ((row & 31) * P + piece) * 16);
                 const float y = f[row / 32][which];
-                if (y != 1.0f) {
-                    const __half2 m = __float2half2_rn(y);
-                    x = make_uint4(times_half(x.x, m), times_half(x.y, m), times_half(x.z, m), times_half(x.w, m));
-                }
+                if (y != 1.0f) x = times_ratio(x, y);
             }
             *reinterpret_cast<uint4*>(kq + which * KT * 128 * DK + term * 128 * DK + (row * P + piece) * 16) = x;
         }
@@ -1027,19 +1034,32 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
                 bt[128 + 2 * lane + k] = x[2 + k];
             }
         } else {
-            float* scl = scl2 + buf * 56;
-            const float iu = warp_most(x[0]), ip = warp_most(x[1]), mo = warp_max(x[2]), iS = warp_most(x[3]), iX = warp_most(x[4]);
+            float* scl = scl2 + buf * 64;
+            // e, dP and dO: a scale per chunk, as no product sums over tokens of theirs; S and X have one
+            float iu = x[0], ip = x[1], mo = x[2];
+#pragma unroll
+            for (int i = 1; i < 8; i <<= 1) {
+                iu = fmaxf(iu, __shfl_xor_sync(kAll, iu, i));
+                ip = fmaxf(ip, __shfl_xor_sync(kAll, ip, i));
+                mo = fmaxf(mo, __shfl_xor_sync(kAll, mo, i));
+            }
+            if (iu == 0.0f) iu = ip = 1.0f;  // no second chunk
+            const float iS = warp_most(x[3]), iX = warp_most(x[4]);
             float so, io;
             pow2_scale(mo, so, io);
-            if (lane == 0) { scl[0] = iu; scl[1] = ip; scl[2] = so; scl[3] = io; scl[4] = iS; scl[5] = iX; }
+            if (lane < 16 && (lane & 7) == 0) {
+                float* of = scl + (lane >> 3);
+                of[0] = iu; of[2] = ip; of[4] = so; of[6] = io;
+            }
+            if (lane == 0) { scl[8] = iS; scl[9] = iX; }
             // what brings a slice's fragments to these scales: powers of two, at most 1
             if (lane < 16) {
-                scl[8 + lane] = x[0] / iu;
-                scl[24 + lane] = x[1] / ip;
+                scl[16 + lane] = x[0] / iu;
+                scl[32 + lane] = x[1] / ip;
             }
             if (lane < 8) {
-                scl[40 + lane] = x[3] / iS;
-                scl[48 + lane] = x[4] / iX;
+                scl[48 + lane] = x[3] / iS;
+                scl[56 + lane] = x[4] / iX;
             }
         }
     };
@@ -1052,11 +1072,11 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
         const int64_t n = n_first + hd;
         const int buf = AHEAD ? hd & 1 : 0;
         const double* run = run2 + buf * 64;
-        const float *bt = bt2 + buf * 192, *dend = bt + 64, *eta = bt + 128, *scl = scl2 + buf * 56;
+        const float *bt = bt2 + buf * 192, *dend = bt + 64, *eta = bt + 128, *scl = scl2 + buf * 64;
         // fragments [16 value rows][16 columns] of a slice to rows of a tile
         auto put = [&](char* tile, int cols, int row, int piece, const uint4& x, float ratio) {
-            const __half2 m = __float2half2_rn(ratio);
-            const uint32_t w[4] = {times_half(x.x, m), times_half(x.y, m), times_half(x.z, m), times_half(x.w, m)};
+            const uint4 y = times_ratio(x, ratio);
+            const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int rr = row + (i & 1) * 8, pp = piece + (i >> 1);
@@ -1117,7 +1137,8 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
             }
         }
         __syncthreads();  // this head's scales are there, the one before has been read
-        const float iu = scl[0], ip = scl[1], so = scl[2], io = scl[3], iS = scl[4], iX = scl[5];
+        // of the chunk of the warp's rows (with e's of its columns for the token matrices)
+        const float iu = scl[tw >> 1], ip = scl[2 + (tw >> 1)], io = scl[6 + (tw >> 1)], iu_col = scl[hw >> 1], iS = scl[8], iX = scl[9];
         auto stage_do = [&](int d0) {  // [64 tokens][ROWS value rows]
 #pragma unroll
             for (int q = 0; q < 64 * ROWS / 8 / 512 + (64 * ROWS / 8 < 512); ++q) {
@@ -1141,6 +1162,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
                     }
                 }
                 uint4 hi, lo;
+                const float so = scl[4 + (row >> 5)];
                 split(x[0] * so, x[1] * so, hi.x, lo.x); split(x[2] * so, x[3] * so, hi.y, lo.y);
                 split(x[4] * so, x[5] * so, hi.z, lo.z); split(x[6] * so, x[7] * so, hi.w, lo.w);
                 const uint32_t at = tile_at<ROWS>(row, piece);
@@ -1161,18 +1183,18 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
                 wait_phase(&come[0], hd & 1, wait, 905);
                 wait_phase(&come[2], hd & 1, wait, 906);
                 load_state(a.l.S, 0, 1, xs, 0);
-                put_state(scl + 40, xs, 0);
+                put_state(scl + 48, xs, 0);
                 load_tok(a.l.e, 2, raw_e, xe, 0);
-                put_tok(scl + 8, st_u, xe, 0);
+                put_tok(scl + 16, st_u, xe, 0);
                 load_tok(a.l.dp, KT, raw_p, xp, 0);
-                put_tok(scl + 24, st_p, xp, 0);
+                put_tok(scl + 32, st_p, xp, 0);
                 stage_do(0);
             } else {
                 load_all(sl0);
                 stage_do(sl0 * 16);
-                put_state(scl + 40, xs, sl0);
-                put_tok(scl + 8, st_u, xe, sl0);
-                put_tok(scl + 24, st_p, xp, sl0);
+                put_state(scl + 48, xs, sl0);
+                put_tok(scl + 16, st_u, xe, sl0);
+                put_tok(scl + 32, st_p, xp, sl0);
                 if (a.l.slices <= SL) load_state(a.l.X, 0, KT, xs, 0);  // for behind these products
             }
             __syncthreads();
@@ -1231,8 +1253,8 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
             for (int x = 0; x < 4; ++x) {
                 const int t = x < 2 ? row0 : row1, u = hw * 16 + j * 8 + 2 * c4 + (x & 1);
                 const float D = u <= t ? expf((float)(run[t] - run[u])) * eta[u] : 0.0f;
-                sg[j][x] = u <= t ? sg[j][x] * (io * iu) * (D * s.scale) : 0.0f;
-                kp[j][x] = u < t ? -kp[j][x] * (ip * iu) * D : 0.0f;
+                sg[j][x] = u <= t ? sg[j][x] * (io * iu_col) * (D * s.scale) : 0.0f;
+                kp[j][x] = u < t ? -kp[j][x] * (ip * iu_col) * D : 0.0f;
                 m0 = fmaxf(m0, fabsf(sg[j][x]));
                 m1 = fmaxf(m1, fabsf(kp[j][x]));
             }
@@ -1242,7 +1264,7 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
             wait_phase(&come[1], hd & 1, wait, 907);
             load_state(a.l.X, 0, KT, xs, 0);
         }
-        if (a.l.slices <= SL) put_state(scl + 48, xs, 0);  // the products with S are through
+        if (a.l.slices <= SL) put_state(scl + 56, xs, 0);  // the products with S are through
         __syncthreads();
         if (fetches && hd + 1 < r) fetch_state(n + 1, a.l.S, &come[0]);
 #pragma unroll
@@ -1279,8 +1301,8 @@ __global__ void __launch_bounds__(512, qk_ctas<DK, KT>()) delta_qk_kernel(const 
             if (a.l.slices > SL) {
                 load_tok(a.l.e, 2, raw_e, xe, sl0);
                 load_state(a.l.X, 0, KT, xs, sl0);
-                put_tok(scl + 8, st_u, xe, sl0);
-                put_state(scl + 48, xs, sl0);
+                put_tok(scl + 16, st_u, xe, sl0);
+                put_state(scl + 56, xs, sl0);
             }
             __syncthreads();
             const int steps = min(SL, a.l.slices - sl0);

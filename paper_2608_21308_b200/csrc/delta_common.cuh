@@ -98,6 +98,25 @@ __device__ __forceinline__ void join_terms(uint32_t hi, uint32_t lo, float& x, f
     x = f.x + e.x;
     y = f.y + e.y;
 }
+// Eight values of a term brought to another scale by a power of two, at most 1: below 2^-14 that power has fewer bits in fp16 than the values that it leaves, or none.
+__device__ __forceinline__ uint4 times_ratio(const uint4& x, float ratio) {
+    uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    if (ratio >= 0x1p-14f) {
+        const __half2 m = __float2half2_rn(ratio);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 z = __hmul2(*reinterpret_cast<const __half2*>(&w[i]), m);
+            w[i] = *reinterpret_cast<const uint32_t*>(&z);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            w[i] = pack_half(f.x * ratio, f.y * ratio);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // an operand that carries its scale already
 __device__ __forceinline__ void split_a(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
     split(x[0], x[1], hi[0], lo[0]);
