@@ -279,6 +279,7 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
  * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
  * queries and keys of their own, keep their outputs bit for bit.
+ * A call repeats bit for bit; a sequence's last bits depend on how many sequences and heads share the call, not on what is in them.
  * Calls that may run at the same time need workspaces of their own; calls one after the other may share one (but for saved states in it).
  * Arguments are refused as everywhere: E2TTT_ERR_NULL / _SHAPE / _DTYPE / _WORKSPACE / _ALIGN / _ARCH / _CUDA.  Tensors need the
  * alignment of their elements only; 16 bytes, and widths that are a multiple of 8, load faster. */
