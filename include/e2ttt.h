@@ -303,7 +303,8 @@ E2TTT_API int e2ttt_delta_fwd(const e2ttt_delta_params* p, const void* q, const 
 /* Reverse pass: gradients of q, k, v (io_dtype; those of shared query / key heads are summed over the value heads, in a fixed order), eta,
  * log_gamma and S_init from d_o and dS_final (NULL: zeros).  dS_init may alias dS_final.  states_saved != 0: the workspace still
  * holds what e2ttt_delta_fwd(save_states = 1) left for the same inputs; 0: it is computed again first.  Where log_gamma is
- * below -104 (the decay is 0 in 32 bits) its gradient is 0. */
+ * below -104 (the decay is 0 in 32 bits) its gradient is 0.  e2ttt_prepare_bwd takes d_gamma = d_log_gamma / gamma, and zeros for d_beta: the rule
+ * has no momentum. */
 E2TTT_API int e2ttt_delta_bwd(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
                               const float* log_gamma, const float* S_init, const void* d_o, const float* dS_final, void* dq, void* dk,
                               void* dv, float* d_eta, float* d_log_gamma, float* dS_init, void* workspace, size_t workspace_bytes,
@@ -314,12 +315,13 @@ E2TTT_API int e2ttt_delta_bwd(const e2ttt_delta_params* p, const void* q, const 
 E2TTT_API int e2ttt_delta_step(const e2ttt_delta_params* p, const void* q, const void* k, const void* v, const float* eta,
                                const float* log_gamma, const float* S, void* o, float* S_out, void* stream);
 
-/* Block join: what stands between a token-mixing block's heads and the next block (the paper's block ends in a gate and a norm, Fig.
- * "attention_block"): norm after the block, gate, scaled residual sum, norm before the next block, in one pass.  Per token
+/* Block join: what stands between a token-mixing block and the next one: norm after the block, gate, scaled residual sum, norm before the next block, in one
+ * pass.  With H heads it joins a block whose heads go into the residual as they are.  Behind an output projection, as in the paper's block (Fig.
+ * "attention_block": norm of the heads, projection), it is called with H = 1 and d the model's width: a norm of the projection's output.  The first norm is always
+ * there; the projection, and a norm of heads before it, are not part of it.  Per token
  *   y = o / sqrt(mean_d(o^2) + post_eps) * w_post   (per head),   x_out = x + res_scale * gate(a) * y,
  *   n = x_out / sqrt(mean(x_out^2) + pre_eps) * w_pre   (over all H d values).
  *   o                        [B,H,L,d] io_dtype: the block's outputs by heads, as e2ttt_chunk_fwd, e2ttt_apply and e2ttt_delta_* write them
- *                            (H = 1 with d the model's width: the output of a projection)
  *   a, x, x_out, n           [B,L,H d] io_dtype, head h at columns h d .. (h + 1) d
  *   w_post, res_scale, w_pre [H d] fp32
  * a is NULL with E2TTT_GATE_NONE and required otherwise; w_pre and n_out (d_n, d_w_pre) are given together or not at all (no second norm).
