@@ -1404,11 +1404,13 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
     {
         constexpr int most = KT == 1 ? 4 : 2;
         const bool vec = a.s.dv % 8 == 0 && (reinterpret_cast<uintptr_t>(b.d_o) | reinterpret_cast<uintptr_t>(b.dv)) % 16 == 0;
+        // Few slices, as many as SMs at most: the columns of each over DK / 32 warps.  16 heads of 128 x 128, 4096 tokens, bf16, forward and reverse pass: 691 us, with a
+        // warp per slice 727.  More: as the forward's.
         int rc;
         if (a.l.N * a.l.slices <= 148) {
             rc = launch_chain<IO, DK, KT, DK / 32>(b, 1, vec, st);
         } else {
-            int per = most;  // as the forward's
+            int per = most;
             while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
             rc = launch_chain<IO, DK, KT, 1>(b, per, vec, st);
         }

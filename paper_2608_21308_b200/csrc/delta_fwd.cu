@@ -10,8 +10,8 @@
 // terms), so scales are one per slice, folded into the scalars that the values are multiplied with anyway, and come from bounds that are known
 // before the values are.
 // 4 x 16 sequences of 4096 tokens, 128 x 128, bf16: 268 us (128 chunks, one after the other: 2.1 us each), 317 us with saved states (670 MB of states,
-// errors and the states' products with queries and keys to write); 16 sequences of 32768 tokens: 1440 us (1024 chunks: 1.4 us each, the columns of a
-// slice over four warps); 8 x 12 sequences of 2048 tokens, 64 x 64, with saved states: 121 us.
+// errors and the states' products with queries and keys to write); 16 sequences of 32768 tokens: 1280 us (1024 chunks: 1.25 us each, one slice on an
+// SM); 8 x 12 sequences of 2048 tokens, 64 x 64, with saved states: 121 us.
 #include "api_checks.h"
 #include "delta_common.cuh"
 
@@ -631,12 +631,14 @@ template <typename IO, int DK, int KT, int KS, bool SAVE> int launch(const Delta
 
 template <typename IO, int DK, int KT, bool SAVE> int dispatch(const DeltaArgs& a, cudaStream_t st) {
     constexpr int most = KT == 1 ? 4 : 2;
-    static_assert(fwd_smem<DK, KT, 1>(most) <= kMostSharedMemory && fwd_smem<DK, KT, DK / 32>(1) <= kMostSharedMemory, "shared memory");
-    // Few slices, as many as SMs at most: one per CTA, its columns over DK / 32 warps; with more of them the warps share an SM's schedulers and a chain
-    // per warp is faster.  Then slices of a sequence share the tiles that they fetch, as long as 96 CTAs are left.  Forward and reverse pass
-    // together, us: 8 x 12 x 2048 tokens, 64 x 64, bf16: 4 slices per CTA 554, 2: 563, 1: 647, one over two warps 744.  Forward alone, 128 x 128,
-    // 16 heads x 4096 tokens: B = 4: 4 slices 310, 2: 421; B = 2: 2 slices 220, 4: 269.  fp32 tiles leave room for two.
-    if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, SAVE>(a, 1, st);
+    static_assert(fwd_smem<DK, KT, 1>(most) <= kMostSharedMemory && (KT == 1 || fwd_smem<DK, KT, DK / 32>(1) <= kMostSharedMemory), "shared memory");
+    // fp32, few slices, as many as SMs at most: one per CTA, its columns over DK / 32 warps.  Calls of 2048 tokens, us: 16 heads of 128 x 128: 175, with a warp per
+    // slice 188; 12 of 64 x 64: 107 and 115.  With bf16, whose chain has two products where fp32 has three, the outputs' warp would hold up the chain's: 111 and
+    // 103, 76.5 and 76.4.  More slices than SMs: a chain per warp, and slices of a sequence share the tiles that they fetch, as long as 96 CTAs are
+    // left.  bf16, us: forward and reverse pass, 8 x 12 x 2048 tokens, 64 x 64: 4 slices per CTA 604, 2: 679, 1: 734, one over two warps 731.  Forward
+    // alone, 128 x 128, 16 heads x 4096 tokens: B = 4: 4 slices 344, 2: 427; B = 2: 2 slices 222, 4: 302; B = 1: 1 slice 201, 4: 282.  fp32 tiles leave room for two.
+    if constexpr (KT == 2)
+        if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, SAVE>(a, 1, st);
     int per = most;
     while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
     return launch<IO, DK, KT, 1, SAVE>(a, per, st);
