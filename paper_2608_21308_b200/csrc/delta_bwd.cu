@@ -1410,9 +1410,7 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
         if (a.l.N * a.l.slices <= 148) {
             rc = launch_chain<IO, DK, KT, DK / 32>(b, 1, vec, st);
         } else {
-            int per = most;
-            while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
-            rc = launch_chain<IO, DK, KT, 1>(b, per, vec, st);
+            rc = launch_chain<IO, DK, KT, 1>(b, slices_per_cta(a.l, most), vec, st);
         }
         if (rc != 0) return rc;
     }

@@ -639,9 +639,7 @@ template <typename IO, int DK, int KT, bool SAVE> int dispatch(const DeltaArgs& 
     // alone, 128 x 128, 16 heads x 4096 tokens: B = 4: 4 slices 344, 2: 427; B = 2: 2 slices 222, 4: 302; B = 1: 1 slice 201, 4: 282.  fp32 tiles leave room for two.
     if constexpr (KT == 2)
         if (a.l.N * a.l.slices <= 148) return launch<IO, DK, KT, DK / 32, SAVE>(a, 1, st);
-    int per = most;
-    while (per > 1 && a.l.N * ((a.l.slices + per - 1) / per) < 96) per >>= 1;
-    return launch<IO, DK, KT, 1, SAVE>(a, per, st);
+    return launch<IO, DK, KT, 1, SAVE>(a, slices_per_cta(a.l, most), st);
 }
 
 template <typename IO, int DK, int KT> int either(const DeltaArgs& a, cudaStream_t st) {
