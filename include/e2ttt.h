@@ -273,13 +273,14 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  * a chunk's queries or keys, of its errors e or their adjoints, or of 16 neighbouring value rows of a state or its adjoint; outputs are rounded once, and
  * the same with and without saved states.  dq and dk are formed of 64 tokens (from a multiple of 64) and all value rows of a head: not finer than 2^-27 of the
  * largest value of the state, its adjoint, the queries, the keys or the products of two tokens there; bf16 dq and dk, moreover, of products with one term
- * (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  d_log_gamma is off by some 2e-6 of its size whatever the decay, as long as the
- * decays of a chunk do not differ in size by more than that.
+ * (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  d_log_gamma is off by 2e-6 of the
+ * gradients' size among 64 tokens, whatever the decays: where all forget alike that is of its own size.
  * The largest magnitude of a tensor should be 0 or lie between 2^-50 and 2^50; chunks, heads and documents in it may be smaller, or all zeros.
  * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
  * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
  * queries and keys of their own, keep their outputs bit for bit.
- * A call repeats bit for bit; a sequence's last bits depend on how many sequences and heads share the call, not on what is in them.
+ * A call repeats bit for bit; the last bits of a sequence's gradients, and of its fp32 outputs, depend on how many sequences and heads share the call, but not on what
+ * is in them.
  * Calls that may run at the same time need workspaces of their own; calls one after the other may share one (but for saved states in it).
  * Arguments are refused as everywhere: E2TTT_ERR_NULL / _SHAPE / _DTYPE / _WORKSPACE / _ALIGN / _ARCH / _CUDA.  Tensors need the
  * alignment of their elements only; 16 bytes, and widths that are a multiple of 8, load faster. */

@@ -888,8 +888,10 @@ __global__ void __launch_bounds__(kGateWarps * 32) delta_gate_kernel(const Delta
 // again with X; what the chains left in fragment order goes into tiles of rows here, at one scale for all slices (S, X) or all of a chunk (e, dP, dO).  With bf16 I/O one term of every
 // operand serves: dQ and dK are off by 2^-11 of their terms before they are rounded to 2^-8.  AHEAD: the next head's raw tiles come by bulk copies.
 // Bound by the dependent phases of a head (tiles, products with S, token matrices, products with X, products with K and Q, a barrier between any
-// two): 20 thousand cycles, of which the MMAs are 5, the tiles 4.  4 x 4 key heads of 4 value heads, 4096 tokens, 128 x 128, bf16: 335 us (470 MB: 1.4
+// two): 20 thousand cycles, of which the MMAs are 5, the tiles 4.  4 x 4 key heads of 4 value heads, 4096 tokens, 128 x 128, bf16: 348 us (470 MB: 1.35
 // TB/s); 8 x 12 heads, 2048 tokens, 64 x 64: 209 us.
+// One term leaves dq and dk 1.68e-3 from their values in 64 bits where rounding alone leaves 1.66e-3.  Both terms of S, e, dP, X and the token matrices would be 2.5
+// times the MMAs and twice the tiles, without room for the next head's (fp32, which has them: 860 and 390 us).
 template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? DK : 32; }
 template <int DK, int KT> constexpr int qk_ctas() { return KT == 1 && DK == 64 ? 2 : 1; }  // per SM
 template <int DK, int KT> constexpr int qk_work() {
@@ -1415,7 +1417,7 @@ template <typename IO, int DK, int KT> int launch(const DeltaBwdArgs& b, cudaStr
         if (rc != 0) return rc;
     }
     // With bf16 the tiles of a head that fits (all but value rows beyond 64 with keys of up to 64) come ahead.  4 x 4 key heads with 4 value heads each, 4096
-    // tokens, 128 x 128: 335 us, and 416 with loads when they are needed; 8 x 12 heads with one each, 2048 tokens, 64 x 64: 209 and 213.
+    // tokens, 128 x 128: 348 us, and 416 with loads when they are needed; 8 x 12 heads with one each, 2048 tokens, 64 x 64: 209 and 213.
     int rc;
     if constexpr (KT == 1 && DK == 128) rc = launch_qk<IO, DK, KT, true>(b, st);
     else if constexpr (KT == 1) rc = a.l.slices <= qk_rows<DK, KT>() / 16 ? launch_qk<IO, DK, KT, true>(b, st) : launch_qk<IO, DK, KT, false>(b, st);

@@ -4,7 +4,7 @@
 // stays in a warp's accumulators for the whole sequence, an accumulator tile is the next product's A operand as it is, and no value
 // crosses a warp.  Measured on B200: an m16n8k16 takes 8.1 cycles of its scheduler (1024 multiply-adds per cycle and SM), its result 21, and
 // other arithmetic does not run beside it (one MMA and four FMAs take 12.1 cycles, with six 14.1), so a chain of dependent chunks is bound by what
-// its warp issues.  A 128-row tensor-memory tile would hold one sequence per SM (64 sequences: 64 of 148 SMs), and send the state through tensor
+// its warp issues.  A 128-row tensor-memory tile would hold one sequence per SM (64 sequences: 64 of 148 SMs; a 64-row tile half of one), and send the state through tensor
 // memory and back, and through the splitting into terms, between any two of the four dependent products of a chunk.
 // Operands in 32 bits are used as two fp16 terms, x = 2^-s (hi + lo): 22 bits, and s (a power of two per slice or tile, from its largest
 // value or a bound on it) keeps both terms inside fp16's exponents.  What is bf16 on input is one term, exactly down to 2^-24 of its tile's largest

@@ -3,8 +3,8 @@
 // them with bulk copies whatever the caller's width and alignment), and for every value head of the group the record of delta.h:
 // T, A and the products of the decays.  All chunks run side by side.
 // Bound by what it issues and by the latency of a chunk's dependent steps, with 12 chunks at a time on an SM, before memory: 64 heads of 4096 tokens,
-// 128 wide, bf16, each with its own queries and keys, in 90 us (344 MB: 53 us at 6.5 TB/s); 64 value heads on 16 of those with what the reverse
-// pass needs in 95 us (210 MB).
+// 128 wide, bf16, each with its own queries and keys, in 92 us (344 MB: 53 us at 6.5 TB/s); 64 value heads on 16 of those with what the reverse
+// pass needs in 97 us (260 MB), each warp with four value heads one after the other.
 #include "api_checks.h"
 #include "delta_common.cuh"
 

@@ -6,8 +6,9 @@
 // Reverse pass, with r = gate(a) y0, y0 = o / rms(o):  d x = d x_out + (adjoint of the second norm),  d w_post = res_scale sum_tokens(dx r),
 // d res_scale = w_post sum_tokens(dx r): one column sum serves both, a second one is d w_pre.  A CTA keeps its tokens' column sums in
 // registers; the CTAs' sums are added by a second launch in a fixed order, so that results repeat bit for bit.
-// 16384 tokens of 2048 in bf16 with a gate and both norms: 64 us forward (336 MB, 5.2 TB/s), 126 us in reverse (537 MB, 4.3 TB/s) and 6 us for the column
-// sums; 8000 tokens of 768 in fp32, sigmoid gate: 31, 58 and 6 us.  What is above the bytes' time is issue: the gate's special functions, bf16 conversions, sums.
+// 16384 tokens of 2048 in bf16 with a gate and both norms: 64 us forward (336 MB, 5.2 TB/s), 131 us in reverse (537 MB, 4.1 TB/s) and 6 us for the column
+// sums; 8000 tokens of 768 in fp32, sigmoid gate: 31, 58 and 7 us.  What is above the bytes' time is
+// issue with heads that fit a warp (the gate's special functions, bf16 conversions, sums), and the barriers of the sums through shared memory with wider ones.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -45,3 +45,17 @@ def test_a_large_state_over_chunks_of_zeros(io, shape, case):
     check(r.fwd(1), {"o": o, "S": S})
     check(r.bwd(d), ref, dict(x, scale=1.0, **d))
     check(r.fwd(0), {"o": o, "S": S}, dict(x, scale=1.0))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("values,gradients", [(50, 50), (50, -50), (-50, 50), (-50, -50)])
+def test_ends_of_the_range_of_magnitudes(io, shape, values, gradients):
+    x, d = _make(*shape, io, seed=37)
+    for t, n in ((x["v"], values), (x["S"], values), (d["d_o"], gradients), (d["dS_final"], gradients)):
+        t *= np.float32(2.0 ** (n - np.sign(n) * 3))  # the largest of them are within 2^3 of the typical ones
+    o, S = O.forward(**x, scale=1.0)
+    r = Run(x, io, 1.0)
+    check(r.fwd(1), {"o": o, "S": S})
+    check(r.bwd(d), O.backward(**x, scale=1.0, **d), dict(x, scale=1.0, **d))
+    check(r.step(), {"o": o, "S": S})
