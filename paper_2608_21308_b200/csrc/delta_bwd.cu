@@ -890,8 +890,8 @@ __global__ void __launch_bounds__(kGateWarps * 32) delta_gate_kernel(const Delta
 // Bound by the dependent phases of a head (tiles, products with S, token matrices, products with X, products with K and Q, a barrier between any
 // two): 20 thousand cycles, of which the MMAs are 5, the tiles 4.  4 x 4 key heads of 4 value heads, 4096 tokens, 128 x 128, bf16: 348 us (470 MB: 1.35
 // TB/s); 8 x 12 heads, 2048 tokens, 64 x 64: 209 us.
-// One term leaves dq and dk 1.68e-3 from their values in 64 bits where rounding alone leaves 1.66e-3.  Both terms of S, e, dP, X and the token matrices would be 2.5
-// times the MMAs and twice the tiles, without room for the next head's (fp32, which has them: 860 and 390 us).
+// One term leaves dq and dk 1.68e-3 from their values in 64 bits where rounding alone leaves 1.66e-3.  Both terms of S, e, dP, X and the token matrices are 2.5 times
+// the MMAs and twice the tiles, without room for the next head's: 778 and 301 us.  A caller who wants them has fp32 I/O.
 template <int DK, int KT> constexpr int qk_rows() { return KT == 1 ? DK : 32; }
 template <int DK, int KT> constexpr int qk_ctas() { return KT == 1 && DK == 64 ? 2 : 1; }  // per SM
 template <int DK, int KT> constexpr int qk_work() {
