@@ -273,8 +273,8 @@ E2TTT_API int e2ttt_prepare_bwd(const e2ttt_params* p, const e2ttt_gate_params* 
  * a chunk's queries or keys, of its errors e or their adjoints, or of 16 neighbouring value rows of a state or its adjoint; outputs are rounded once, and
  * the same with and without saved states.  dq and dk are formed of 64 tokens (from a multiple of 64) and all value rows of a head: not finer than 2^-27 of the
  * largest value of the state, its adjoint, the queries, the keys or the products of two tokens there; bf16 dq and dk, moreover, of products with one term
- * (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  d_log_gamma is off by 2e-6 of the
- * gradients' size among 64 tokens, whatever the decays: where all forget alike that is of its own size.
+ * (off by 2^-11 of the products' terms) before they are rounded to 2^-8.  d_log_gamma is off by
+ * some 1e-6 of the gradients' size among 64 tokens, whatever the decays: where all forget alike that is of its own size.
  * The largest magnitude of a tensor should be 0 or lie between 2^-50 and 2^50; chunks, heads and documents in it may be smaller, or all zeros.
  * A NaN or an infinity at one token of a sequence reaches all outputs of its chunk of 32 tokens and what follows, and in the reverse pass all
  * gradients of its block of 64 tokens and what depends on them: they are NaN or without meaning.  Tokens before its chunk, and other heads with
