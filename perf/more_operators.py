@@ -12,7 +12,9 @@ The recurrence, per sequence and channel, with learned rates and a logit of deca
 
   a_t = exp(-rate sigmoid(r_t)),   i_t = sigmoid(g_t),   s_t = sqrt(1 - a_t^2),   h_t = a_t h_{t-1} + s_t i_t x_t
 
-(s_t = 1 without unit scale, i_t = 1 without an input gate; a token that starts a document has a_t = 0 and s_t = 1).  8-bit checkpoints: a row is cut into
+(s_t = 1 without unit scale, i_t = 1 without an input gate; a token that starts a document has a_t = 0 and s_t = 1).  With its inputs kept in 8 bits, the reverse
+pass is the adjoint at the inputs that are read back; the states it multiplies are walked again from them, from the forward's own state before every 64th token,
+which is kept in 32 bits.  8-bit checkpoints: a row is cut into
 blocks of 32 values; a block's scale is 2^e, e the smallest integer with 127 2^e >= max |x|, its codes are the integers nearest to x 2^-e (ties to even).
 
 Shapes are those of the benchmark configurations and tests: widths of 768 (12 heads of 64) and 2048 (16 heads of 128), a batch of 1 to 8 (decoding: up to 64
@@ -30,6 +32,7 @@ own = False
 
 EPS = 1e-6
 BLOCK = 32
+SPAN = 64  # tokens between two states that the recurrence keeps
 
 
 def _scan(name, op, B, L, D, io="bf16", gate=True, unit=True, docs=False, save="states"):
@@ -212,8 +215,16 @@ def _run_scan(s):
     if case["save"] == "packed":
         x, r, g = (None if t is None else _plain_packed(t) for t in (x, r, g))
         sg, la, c, i, scale, first = gates()
-        h = states(c, scale * i * x)
+        kept = torch.cat([s["h0"].unsqueeze(1), h[:, SPAN - 1:-1:SPAN]], 1)
+        c1, b = c.clone(), scale * i * x
+        b[:, ::SPAN] += (1.0 - c[:, ::SPAN]) * kept
+        c1[:, ::SPAN] = 1.0
+        h = _plain_prefix(c1, b)
+    else:
+        kept = None
     before = torch.cat([s["h0"].unsqueeze(1), h[:, :-1]], 1)
+    if kept is not None:
+        before[:, ::SPAN] = kept
     d = s["d_h"].float().clone()
     d[:, -1] += s["dh_out"]
     lam = _plain_prefix(torch.cat([c[:, 1:], torch.ones_like(c[:, :1])], 1), d, reverse=True)
@@ -392,7 +403,7 @@ def _exact_scan(s):
     rate, h0 = s["rate"].double(), s["h0"].double()
     start = None if s["starts"] is None else (s["starts"].t() != 0).unsqueeze(-1)
 
-    def walk(x, r, g):
+    def walk(x, r, g, known=None):
         la = -rate * torch.sigmoid(r)
         one_less = -torch.expm1(2.0 * la)  # 1 - a^2
         if not case["unit"]:
@@ -402,19 +413,21 @@ def _exact_scan(s):
             a, one_less = torch.where(start, 0.0, a), torch.where(start, 1.0, one_less)
         u = x if g is None else x * torch.sigmoid(g)
         b = one_less.sqrt() * u
-        h = torch.empty_like(x)
-        last = h0
+        before, last = torch.empty_like(x), h0
         for t in range(L):
-            last = torch.addcmul(b[t], a[t], last, out=h[t])
-        return la, one_less, a, u, h
+            if known is not None and t % SPAN == 0:
+                last = known[t]
+            before[t] = last
+            last = torch.addcmul(b[t], a[t], last)
+        return la, one_less, a, u, before, last
 
-    la, one_less, a, u, h = walk(x, r, g)
-    out = {"h": h.transpose(0, 1), "h_out": h[-1].clone()}
+    la, one_less, a, u, before, last = walk(x, r, g)
+    out = {"h": torch.cat([before[1:], last.unsqueeze(0)]).transpose(0, 1), "h_out": last}
     if not train:
         return out
     if case["save"] == "packed":
         x, r, g = (None if t is None else _exact_packed(t) for t in (x, r, g))
-        la, one_less, a, u, h = walk(x, r, g)
+        la, one_less, a, u, before, _ = walk(x, r, g, before)
     lam = s["d_h"].double().transpose(0, 1).contiguous()
     lam[L - 1] += s["dh_out"].double()
     for t in range(L - 2, -1, -1):
@@ -424,7 +437,7 @@ def _exact_scan(s):
     out["d_x"] = lam * root if g is None else lam * root * torch.sigmoid(g)
     if g is not None:
         out["d_g"] = lam * root * u * torch.sigmoid(-g)
-    to_a = lam * torch.cat([h0.unsqueeze(0), h[:-1]])
+    to_a = lam * before
     if case["unit"]:
         to_a = to_a - lam * u * a / root  # through sqrt(1 - a^2)
     to_la = a * to_a
