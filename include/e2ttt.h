@@ -346,6 +346,78 @@ E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const vo
                              void* d_x, float* d_w_post, float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes,
                              void* stream);
 
+/* Gated linear recurrence: the token mixer without a matrix state, a decay per channel instead of one per head.  Per sequence and channel, with a learned rate
+ * and two logits per token (outputs of the model's linear maps, which stay with the caller):
+ *   a_t = exp(-rate sigmoid(a_decay_t)),   i_t = sigmoid(a_in_t),   s_t = sqrt(1 - a_t^2),   h_t = a_t h_{t-1} + s_t i_t x_t.
+ * With E2TTT_GATE_NONE there is no a_in and i_t is 1; with unit_scale = 0, s_t is 1.  A token with a non-zero byte in `starts` is the first of a document: a_t = 0
+ * and s_t = 1 there, h_t = i_t x_t whatever came before (a NaN too), and its a_decay is not used.
+ *   x, a_decay, a_in, h  [B,L,D] io_dtype    rate [D] fp32, >= 0    starts [B,L] bytes, or NULL    h_init, h_final [B,D] fp32
+ * e2ttt_scan_fwd runs whole sequences, e2ttt_scan_step a few tokens on a state (decoding), without a workspace; both move the same state and may follow each other.
+ * Arithmetic: fp32; a_t - 1 and 1 - a_t^2 are formed without the rounding of a_t next to 1, so that long memories keep their precision.  With bf16 I/O gates are good
+ * to some 2^-21, and logits below -43 count as -43.  A call repeats bit for bit; last bits of h (fp32), the states and the gradients depend on how many sequences share the call
+ * (a long sequence is cut into parts that run side by side), but not on what is in them.  A NaN or an infinity stays in its channel, and reaches what follows it up to the next
+ * start (in the reverse pass: what comes before it, too).
+ * D up to 2^20, L up to 2^30, B L D up to 2^40, B times the blocks of 64 channels up to 2^24; any width and length, elements' alignment; 16 bytes, and widths that are a
+ * multiple of 16 bytes, load faster.  h_init may be NULL (zeros), h_final may alias it; no other output may overlap an input.
+ * Calls that may run at the same time need workspaces of their own.  There is no device status in them. */
+typedef struct {
+    int32_t B, L, D;    /* sequences, tokens, channels */
+    int32_t io_dtype;   /* e2ttt_dtype of x, a_decay, a_in, h and their gradients */
+    int32_t gate;       /* E2TTT_GATE_NONE or E2TTT_GATE_SIGMOID: the input gate */
+    int32_t unit_scale; /* 1: s_t = sqrt(1 - a_t^2) (inputs of unit variance leave a state of unit variance); 0: s_t = 1 */
+} e2ttt_scan_params;
+
+/* What a forward leaves in its workspace for the reverse pass: nothing; the state before every 64th token (4 bytes a channel), beside which the reverse pass reads x, a_decay
+ * and a_in again; or those states and x, a_decay and a_in in the 8-bit form of e2ttt_pack8 (a little over a byte a value, widths and lengths rounded up to 64), so that the caller
+ * need not keep them.  The reverse pass is then the adjoint at the values that are read back; the states it multiplies are walked again from
+ * them, from the forward's own state before every 64th token. */
+typedef enum { E2TTT_SAVE_NONE = 0, E2TTT_SAVE_STATES = 1, E2TTT_SAVE_PACKED = 2 } e2ttt_save;
+
+/* Bytes of workspace of e2ttt_scan_fwd with this `save`, and of e2ttt_scan_bwd with this `saved` (for saved = E2TTT_SAVE_NONE: those of E2TTT_SAVE_STATES).
+ * With E2TTT_SAVE_NONE 0: the forward may be given a NULL workspace. */
+E2TTT_API int e2ttt_scan_workspace_bytes(const e2ttt_scan_params* p, int save, size_t* bytes);
+E2TTT_API int e2ttt_scan_fwd(const e2ttt_scan_params* p, const void* x, const void* a_decay, const void* a_in, const float* rate,
+                             const uint8_t* starts, const float* h_init, void* h, float* h_final, void* workspace, size_t workspace_bytes,
+                             int save, void* stream);
+
+/* Reverse pass: gradients of x, a_decay, a_in (io_dtype), rate (fp32, over all tokens in a fixed order) and h_init (fp32) from d_h and dh_final (NULL: zeros).
+ * saved: what the forward of the same inputs left in the workspace (with E2TTT_SAVE_PACKED x, a_decay and a_in are not read and may be NULL); E2TTT_SAVE_NONE: the states
+ * are computed again first.  dh_init may alias dh_final.  Where 1 - a_t^2 is 0 in 32 bits the derivative of s_t is taken as 0. */
+E2TTT_API int e2ttt_scan_bwd(const e2ttt_scan_params* p, const void* x, const void* a_decay, const void* a_in, const float* rate,
+                             const uint8_t* starts, const float* h_init, const void* d_h, const float* dh_final, void* d_x, void* da_decay,
+                             void* da_in, float* d_rate, float* dh_init, void* workspace, size_t workspace_bytes, int saved, void* stream);
+
+/* The L tokens of the call (meant for one or a few) on the state h_state [B,D]; h_out may alias it.  Not NULL. */
+E2TTT_API int e2ttt_scan_step(const e2ttt_scan_params* p, const void* x, const void* a_decay, const void* a_in, const float* rate,
+                              const uint8_t* starts, const float* h_state, void* h, float* h_out, void* stream);
+
+/* 8-bit checkpoints of activations: what a reverse pass will read is put away in a little over a byte a value.  A row is cut into blocks of 32 neighbouring values
+ * (the last may be shorter); a block has a scale 2^e, e the smallest integer with 127 2^e >= max |x| (in -126 .. 121: values below 2^-127 become 0, those above
+ * 127 2^121 become that), and codes rint(x 2^-e), ties to even: off by at most 1/127 of the block's largest value.  A block that holds a NaN or an infinity is read back as NaNs.  Every
+ * step is exact, so there is one answer.
+ *   x      [rows, cols] io_dtype       codes [rows, cols] signed bytes       scales [rows, ceil(cols / 32)] bytes: e + 127; 255 for NaNs
+ * e2ttt_unpack8 writes code 2^e, rounded once (bf16: exactly).  rows up to 2^40, cols up to 2^30, rows times cols (rounded up to 32) up to 2^40.  Alignment: elements';
+ * 16 bytes of x, 8 of codes and cols a multiple of 32 are fastest. */
+typedef struct {
+    int64_t rows;
+    int32_t cols;
+    int32_t io_dtype; /* e2ttt_dtype of x */
+} e2ttt_pack_params;
+E2TTT_API int e2ttt_pack8(const e2ttt_pack_params* p, const void* x, int8_t* codes, uint8_t* scales, void* stream);
+E2TTT_API int e2ttt_unpack8(const e2ttt_pack_params* p, const int8_t* codes, const uint8_t* scales, void* x, void* stream);
+
+/* The block join's training step with its inputs kept in that form: e2ttt_join_fwd that leaves o, a and x (as rows of H d columns, blocks of 32 of them, across heads)
+ * in `packed`, and e2ttt_join_bwd that reads them from there: the gradients of e2ttt_join_bwd at the values that are read back.  The forward's outputs are those of
+ * e2ttt_join_fwd, bit for bit; x_out may alias x and n_out a as there.  packed: e2ttt_join_packed_bytes, 256-byte aligned, the caller's until the reverse pass. */
+E2TTT_API int e2ttt_join_packed_bytes(const e2ttt_join_params* p, size_t* bytes);
+E2TTT_API int e2ttt_join_fwd_packed(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post,
+                                    const float* res_scale, const float* w_pre, void* x_out, void* n_out, void* packed,
+                                    size_t packed_bytes, void* stream);
+E2TTT_API int e2ttt_join_bwd_packed(const e2ttt_join_params* p, const void* packed, size_t packed_bytes, const float* w_post,
+                                    const float* res_scale, const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a,
+                                    void* d_x, float* d_w_post, float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
 /* Reads back the device status word of the last launch that used `workspace` (the first word of every
  * workspace).  workspace == NULL reads the word of the scratch array e2ttt_chunk_fwd_noalloc uses on the
  * current device (0 if that entry point has not run there yet).  This is the one entry point that

@@ -19,6 +19,7 @@ E2TTT_MLP_GELU, E2TTT_SWIGLU = 0, 1
 E2TTT_F32, E2TTT_BF16 = 0, 1
 E2TTT_IMPL_AUTO, E2TTT_IMPL_SIMT, E2TTT_IMPL_TCGEN05, E2TTT_IMPL_TILED = 0, 1, 2, 3
 E2TTT_GATE_NONE, E2TTT_GATE_SIGMOID, E2TTT_GATE_SILU = 0, 1, 2
+E2TTT_SAVE_NONE, E2TTT_SAVE_STATES, E2TTT_SAVE_PACKED = 0, 1, 2
 E2TTT_OK = 0
 
 
@@ -42,6 +43,15 @@ class e2ttt_delta_params(ctypes.Structure):
 class e2ttt_join_params(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("d", ctypes.c_int32),
                 ("io_dtype", ctypes.c_int32), ("gate", ctypes.c_int32), ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float)]
+
+
+class e2ttt_scan_params(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("unit_scale", ctypes.c_int32)]
+
+
+class e2ttt_pack_params(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("io_dtype", ctypes.c_int32)]
 
 
 class E2TTTError(RuntimeError):
@@ -102,6 +112,26 @@ def lib() -> ctypes.CDLL:
         L.e2ttt_join_fwd.restype = cp
         L.e2ttt_join_bwd.argtypes = [jp] + [vp] * 15 + [ctypes.c_size_t, vp]
         L.e2ttt_join_bwd.restype = cp
+        L.e2ttt_join_packed_bytes.argtypes = [jp, ctypes.POINTER(ctypes.c_size_t)]
+        L.e2ttt_join_packed_bytes.restype = cp
+        L.e2ttt_join_fwd_packed.argtypes = [jp] + [vp] * 9 + [ctypes.c_size_t, vp]
+        L.e2ttt_join_fwd_packed.restype = cp
+        L.e2ttt_join_bwd_packed.argtypes = [jp, vp, ctypes.c_size_t] + [vp] * 12 + [ctypes.c_size_t, vp]
+        L.e2ttt_join_bwd_packed.restype = cp
+        sp = ctypes.POINTER(e2ttt_scan_params)
+        L.e2ttt_scan_workspace_bytes.argtypes = [sp, cp, ctypes.POINTER(ctypes.c_size_t)]
+        L.e2ttt_scan_workspace_bytes.restype = cp
+        L.e2ttt_scan_fwd.argtypes = [sp] + [vp] * 9 + [ctypes.c_size_t, cp, vp]
+        L.e2ttt_scan_fwd.restype = cp
+        L.e2ttt_scan_bwd.argtypes = [sp] + [vp] * 14 + [ctypes.c_size_t, cp, vp]
+        L.e2ttt_scan_bwd.restype = cp
+        L.e2ttt_scan_step.argtypes = [sp] + [vp] * 9
+        L.e2ttt_scan_step.restype = cp
+        kp = ctypes.POINTER(e2ttt_pack_params)
+        L.e2ttt_pack8.argtypes = [kp] + [vp] * 4
+        L.e2ttt_pack8.restype = cp
+        L.e2ttt_unpack8.argtypes = [kp] + [vp] * 4
+        L.e2ttt_unpack8.restype = cp
         L.e2ttt_device_status.argtypes = [vp, vp, ctypes.POINTER(cp)]
         L.e2ttt_device_status.restype = cp
         L.e2ttt_selftest_wait_timeout.argtypes = [vp, ctypes.c_size_t, ctypes.c_longlong, vp]
@@ -459,6 +489,128 @@ def e2ttt_join_bwd(p, o, a, x, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a,
     st = (_lib or lib()).e2ttt_join_bwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, _stream_ptr(stream))
     if st != E2TTT_OK:
         raise E2TTTError(st, "e2ttt_join_bwd")
+    return st
+
+
+def e2ttt_join_packed_bytes(p: e2ttt_join_params) -> int:
+    n = ctypes.c_size_t()
+    st = (_lib or lib()).e2ttt_join_packed_bytes(ctypes.byref(p), ctypes.byref(n))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_packed_bytes")
+    return int(n.value)
+
+
+def e2ttt_join_fwd_packed(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out, packed, stream=None):
+    """int e2ttt_join_fwd_packed(...) of include/e2ttt.h: the join, its inputs kept in 8 bits in `packed` (a uint8 tensor).  Raises on error."""
+    io = _io_torch_dtype(p)
+    so, sx, sw = (p.B, p.H, p.L, p.d), (p.B, p.L, p.H * p.d), (p.H * p.d,)
+    args = (_ptr(o, io, so, "o"), _ptr(a, io, sx, "a"), _ptr(x, io, sx, "x"), _ptr(w_post, _F32, sw, "w_post"),
+            _ptr(res_scale, _F32, sw, "res_scale"), _ptr(w_pre, _F32, sw, "w_pre"), _ptr(x_out, io, sx, "x_out"),
+            _ptr(n_out, io, sx, "n_out"), _ptr(packed, torch.uint8, None, "packed"))
+    _here(o, a, x, w_post, res_scale, w_pre, x_out, n_out, packed)
+    st = (_lib or lib()).e2ttt_join_fwd_packed(ctypes.byref(p), *args, packed.numel() if packed is not None else 0, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_fwd_packed")
+    return st
+
+
+def e2ttt_join_bwd_packed(p, packed, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre, workspace,
+                          stream=None):
+    """int e2ttt_join_bwd_packed(...) of include/e2ttt.h: its reverse pass on what e2ttt_join_fwd_packed kept.  Raises on error."""
+    io = _io_torch_dtype(p)
+    so, sx, sw = (p.B, p.H, p.L, p.d), (p.B, p.L, p.H * p.d), (p.H * p.d,)
+    kept = _ptr(packed, torch.uint8, None, "packed")
+    args = (_ptr(w_post, _F32, sw, "w_post"), _ptr(res_scale, _F32, sw, "res_scale"), _ptr(w_pre, _F32, sw, "w_pre"),
+            _ptr(d_x_out, io, sx, "d_x_out"), _ptr(d_n, io, sx, "d_n"), _ptr(d_o, io, so, "d_o"), _ptr(d_a, io, sx, "d_a"),
+            _ptr(d_x, io, sx, "d_x"), _ptr(d_w_post, _F32, sw, "d_w_post"), _ptr(d_res_scale, _F32, sw, "d_res_scale"),
+            _ptr(d_w_pre, _F32, sw, "d_w_pre"), _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(packed, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre, workspace)
+    st = (_lib or lib()).e2ttt_join_bwd_packed(ctypes.byref(p), kept, packed.numel() if packed is not None else 0, *args,
+                                               workspace.numel() if workspace is not None else 0, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_join_bwd_packed")
+    return st
+
+
+def make_scan_params(B, L, D, io_dtype=E2TTT_F32, gate=E2TTT_GATE_SIGMOID, unit_scale=1):
+    return e2ttt_scan_params(B, L, D, io_dtype, gate, unit_scale)
+
+
+def e2ttt_scan_workspace_bytes(p: e2ttt_scan_params, save: int) -> int:
+    n = ctypes.c_size_t()
+    st = (_lib or lib()).e2ttt_scan_workspace_bytes(ctypes.byref(p), int(save), ctypes.byref(n))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_scan_workspace_bytes")
+    return int(n.value)
+
+
+def e2ttt_scan_fwd(p, x, a_decay, a_in, rate, starts, h_init, h, h_final, workspace=None, save=E2TTT_SAVE_NONE, stream=None):
+    """int e2ttt_scan_fwd(...) of include/e2ttt.h: the gated linear recurrence over whole sequences.  `starts` is a uint8 tensor.  Raises on error."""
+    io = _io_torch_dtype(p)
+    sx, s2, ss = (p.B, p.L, p.D), (p.B, p.L), (p.B, p.D)
+    args = (_ptr(x, io, sx, "x"), _ptr(a_decay, io, sx, "a_decay"), _ptr(a_in, io, sx, "a_in"), _ptr(rate, _F32, (p.D,), "rate"),
+            _ptr(starts, torch.uint8, s2, "starts"), _ptr(h_init, _F32, ss, "h_init"), _ptr(h, io, sx, "h"), _ptr(h_final, _F32, ss, "h_final"),
+            _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(x, a_decay, a_in, rate, starts, h_init, h, h_final, workspace)
+    st = (_lib or lib()).e2ttt_scan_fwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, int(save), _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_scan_fwd")
+    return st
+
+
+def e2ttt_scan_bwd(p, x, a_decay, a_in, rate, starts, h_init, d_h, dh_final, d_x, da_decay, da_in, d_rate, dh_init, workspace,
+                   saved=E2TTT_SAVE_NONE, stream=None):
+    """int e2ttt_scan_bwd(...) of include/e2ttt.h: its reverse pass.  Raises on error."""
+    io = _io_torch_dtype(p)
+    sx, s2, ss = (p.B, p.L, p.D), (p.B, p.L), (p.B, p.D)
+    args = (_ptr(x, io, sx, "x"), _ptr(a_decay, io, sx, "a_decay"), _ptr(a_in, io, sx, "a_in"), _ptr(rate, _F32, (p.D,), "rate"),
+            _ptr(starts, torch.uint8, s2, "starts"), _ptr(h_init, _F32, ss, "h_init"), _ptr(d_h, io, sx, "d_h"),
+            _ptr(dh_final, _F32, ss, "dh_final"), _ptr(d_x, io, sx, "d_x"), _ptr(da_decay, io, sx, "da_decay"), _ptr(da_in, io, sx, "da_in"),
+            _ptr(d_rate, _F32, (p.D,), "d_rate"), _ptr(dh_init, _F32, ss, "dh_init"), _ptr(workspace, torch.uint8, None, "workspace"))
+    _here(x, a_decay, a_in, rate, starts, h_init, d_h, dh_final, d_x, da_decay, da_in, d_rate, dh_init, workspace)
+    st = (_lib or lib()).e2ttt_scan_bwd(ctypes.byref(p), *args, workspace.numel() if workspace is not None else 0, int(saved), _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_scan_bwd")
+    return st
+
+
+def e2ttt_scan_step(p, x, a_decay, a_in, rate, starts, h_state, h, h_out, stream=None):
+    """int e2ttt_scan_step(...) of include/e2ttt.h: p.L tokens per sequence on a state.  Raises on error."""
+    io = _io_torch_dtype(p)
+    B, L, D = p.B, p.L, p.D
+    sx, ss = (B, L, D), (B, D)
+    args = (_ptr(x, io, sx, "x"), _ptr(a_decay, io, sx, "a_decay"), _ptr(a_in, io, sx, "a_in"), _ptr(rate, _F32, (D,), "rate"),
+            _ptr(starts, torch.uint8, (B, L), "starts"), _ptr(h_state, _F32, ss, "h_state"), _ptr(h, io, sx, "h"), _ptr(h_out, _F32, ss, "h_out"))
+    _here(x, a_decay, a_in, rate, starts, h_state, h, h_out)
+    st = (_lib or lib()).e2ttt_scan_step(ctypes.byref(p), *args, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_scan_step")
+    return st
+
+
+def make_pack_params(rows, cols, io_dtype=E2TTT_F32):
+    return e2ttt_pack_params(rows, cols, io_dtype)
+
+
+def e2ttt_pack8(p, x, codes, scales, stream=None):
+    """int e2ttt_pack8(...) of include/e2ttt.h: x [rows, cols] as int8 codes and uint8 scales of blocks of 32.  Raises on error."""
+    sx = (p.rows, p.cols)
+    args = (_ptr(x, _io_torch_dtype(p), sx, "x"), _ptr(codes, torch.int8, sx, "codes"), _ptr(scales, torch.uint8, (p.rows, -(-p.cols // 32)), "scales"))
+    _here(x, codes, scales)
+    st = (_lib or lib()).e2ttt_pack8(ctypes.byref(p), *args, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_pack8")
+    return st
+
+
+def e2ttt_unpack8(p, codes, scales, x, stream=None):
+    """int e2ttt_unpack8(...) of include/e2ttt.h: what codes and scales stand for.  Raises on error."""
+    sx = (p.rows, p.cols)
+    args = (_ptr(codes, torch.int8, sx, "codes"), _ptr(scales, torch.uint8, (p.rows, -(-p.cols // 32)), "scales"), _ptr(x, _io_torch_dtype(p), sx, "x"))
+    _here(codes, scales, x)
+    st = (_lib or lib()).e2ttt_unpack8(ctypes.byref(p), *args, _stream_ptr(stream))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_unpack8")
     return st
 
 

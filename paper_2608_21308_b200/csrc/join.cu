@@ -12,11 +12,14 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <string.h>
+
 #include <initializer_list>
 
 #include "../../include/e2ttt.h"
 #include "api_checks.h"
 #include "join.h"
+#include "pack8.cuh"
 
 namespace e2ttt {
 namespace {
@@ -153,8 +156,10 @@ template <int BYTES> __device__ __forceinline__ void copy_piece(void* dst, const
         const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
         if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
         else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
-    } else {
+    } else if constexpr (BYTES == 2) {
         *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(src);
+    } else {
+        *reinterpret_cast<uint8_t*>(dst) = *reinterpret_cast<const uint8_t*>(src);
     }
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -175,8 +180,20 @@ template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, i
 // of 2048 in bf16: 65 us with them, 72 without; fp32, whose threads take two pieces of four, 8000 tokens of 768: 41 and 35.
 template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256; }
 
-template <typename IO, int V, int NC, int TMAX>
-__global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_fwd_kernel(const JoinArgs a, const int depth) {
+// A piece of one of the packed tensors: its codes, and by its block's first lane the scale.  Every lane of a warp calls; c is the piece's place in the row.
+template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scales, const Piece<IO, V>& p, int c, bool in) {
+    float v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = in ? ldf(p.x[j]) : 0.0f;
+    const uint32_t byte = pack8::group_scale<V>(v);
+    if (!in) return;
+    *reinterpret_cast<pack8::Codes<V>*>(codes + c * V) = pack8::encode<V>(v, byte);
+    if (c % (pack8::kBlock / V) == 0) scales[c / (pack8::kBlock / V)] = (uint8_t)byte;
+}
+
+// PACK: o, x and a are also left in 8 bits, as they were read
+template <typename IO, int V, int NC, int TMAX, bool PACK>
+__global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_fwd_kernel(const JoinArgs a, const JoinPacked k, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
@@ -225,6 +242,16 @@ __global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_
         copy_wait(depth - 1);
         const P* r = ring + slot * 3 * NC * T;
         slot = slot + 1 == depth ? 0 : slot + 1;
+        if constexpr (PACK) {
+            uint8_t *codes = a.packed + tok * k.code_row, *scales = a.packed + k.scales + tok * k.scale_row;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                const int c = tid + i * T;
+                keep_piece<IO, V>(codes, scales, r[i * T], c, c < cols);
+                keep_piece<IO, V>(codes + k.code_step, scales + k.scale_step, r[(NC + i) * T], c, c < cols);
+                if (a.a) keep_piece<IO, V>(codes + 2 * k.code_step, scales + 2 * k.scale_step, r[(2 * NC + i) * T], c, c < cols);
+            }
+        }
         float y[NC][V], hs[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
@@ -279,15 +306,41 @@ __global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_
     }
 }
 
-template <typename IO, int V, int NC, int TMAX>
-__global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBwdArgs ba, const int depth) {
+// What a thread of the reverse pass has under way of one token: its pieces of o, x and a as they are, or their codes and the words that hold their blocks' scales.
+template <typename IO, int V, int NC, bool PACK> struct Inputs {
+    static constexpr int kBytes = 3 * NC * (int)sizeof(Piece<IO, V>);
+    const Piece<IO, V>* r;
+    __device__ __forceinline__ void get(int which, int i, int T, int, float (&v)[V]) const {
+        const Piece<IO, V> p = r[(which * NC + i) * T];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = ldf(p.x[j]);
+    }
+};
+template <typename IO, int V, int NC> struct Inputs<IO, V, NC, true> {
+    static constexpr int kBytes = 3 * NC * (V + 4);
+    const pack8::Codes<V>* codes;
+    const uint32_t* words;
+    __device__ __forceinline__ void get(int which, int i, int T, int c, float (&v)[V]) const {
+        const uint32_t word = words[(which * NC + i) * T];
+        pack8::decode<V>(codes[(which * NC + i) * T], word >> c / (pack8::kBlock / V) % 4 * 8 & 0xffu, v);
+    }
+};
+
+template <typename IO, int V, int NC, int TMAX, bool PACK>
+__global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBwdArgs ba, const JoinPacked k, const int depth) {
     extern __shared__ __align__(16) char smem[];
     using P = Piece<IO, V>;
+    using In = Inputs<IO, V, NC, PACK>;
     constexpr bool KEPT = TMAX == 256;
     const JoinArgs& a = ba.f;
+    const bool gated = a.gate != E2TTT_GATE_NONE;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
-    P* ring = reinterpret_cast<P*>(smem) + tid;  // [depth][5][NC][T]
-    Sums sums = make_sums(smem + (size_t)depth * 5 * NC * T * sizeof(P), cols, a.d / V, a.H);
+    // the pieces of a token: of d_x_out and d_n behind those of o, x and a; with packed inputs [depth][2][NC][T] pieces, then the words, then the codes
+    constexpr int OWN = PACK ? 2 : 5, DX = PACK ? 0 : 3;
+    P* ring = reinterpret_cast<P*>(smem) + tid;
+    uint32_t* words = reinterpret_cast<uint32_t*>(smem + (size_t)depth * 2 * NC * T * sizeof(P)) + tid;
+    pack8::Codes<V>* codes = reinterpret_cast<pack8::Codes<V>*>(smem + (size_t)depth * NC * T * (2 * sizeof(P) + 12)) + tid;
+    Sums sums = make_sums(smem + (size_t)depth * T * (2 * NC * sizeof(P) + In::kBytes), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
     int64_t own[NC];  // a piece of o within its token: head and place in the head
 #pragma unroll
@@ -301,16 +354,27 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
     const Stride stride(a, gridDim.x, sums.G);
     auto load = [&](int64_t tok, int slot) {
         if (tok < tokens) {
-            P* r = ring + slot * 5 * NC * T;
+            P* r = ring + slot * OWN * NC * T;
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
                 const int c = tid + i * T;
                 if (c >= cols) continue;
-                copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + ahead.base + own[i]);
-                copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
-                if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
-                copy_piece<sizeof(P)>(r + (3 * NC + i) * T, reinterpret_cast<const P*>(ba.d_x_out) + tok * cols + c);
-                if (a.w_pre) copy_piece<sizeof(P)>(r + (4 * NC + i) * T, reinterpret_cast<const P*>(ba.d_n) + tok * cols + c);
+                if constexpr (PACK) {
+                    const int at = slot * 3 * NC * T + i * T;
+                    const uint8_t *from = a.packed + tok * k.code_row + c * V, *scale = a.packed + k.scales + tok * k.scale_row + c / (pack8::kBlock / V) / 4 * 4;
+#pragma unroll
+                    for (int w = 0; w < 3; ++w) {
+                        if (w == 2 && !gated) continue;
+                        copy_piece<V>(codes + at + w * NC * T, from + w * k.code_step);
+                        copy_piece<4>(words + at + w * NC * T, scale + w * k.scale_step);
+                    }
+                } else {
+                    copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + ahead.base + own[i]);
+                    copy_piece<sizeof(P)>(r + (NC + i) * T, reinterpret_cast<const P*>(a.x) + tok * cols + c);
+                    if (a.a) copy_piece<sizeof(P)>(r + (2 * NC + i) * T, reinterpret_cast<const P*>(a.a) + tok * cols + c);
+                }
+                copy_piece<sizeof(P)>(r + (DX * NC + i) * T, reinterpret_cast<const P*>(ba.d_x_out) + tok * cols + c);
+                if (a.w_pre) copy_piece<sizeof(P)>(r + ((DX + 1) * NC + i) * T, reinterpret_cast<const P*>(ba.d_n) + tok * cols + c);
             }
         }
         stride.move(ahead);
@@ -337,19 +401,23 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
     for (; tok < tokens; tok += gridDim.x) {
         load(tok + (depth - 1) * (int64_t)gridDim.x, slot == 0 ? depth - 1 : slot - 1);
         copy_wait(depth - 1);
-        const P* r = ring + slot * 5 * NC * T;
+        const P* r = ring + slot * OWN * NC * T;
+        In in;
+        if constexpr (PACK) {
+            in.codes = codes + slot * 3 * NC * T;
+            in.words = words + slot * 3 * NC * T;
+        } else {
+            in.r = r;
+        }
         slot = slot + 1 == depth ? 0 : slot + 1;
         float y[NC][V], xo[NC][V], sg[NC][V], hs[NC], inv[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             hs[i] = 0.0f;
             if (tid + i * T >= cols) continue;
-            const P po = r[i * T];
+            in.get(0, i, T, tid + i * T, y[i]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                y[i][j] = ldf(po.x[j]);
-                hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
-            }
+            for (int j = 0; j < V; ++j) hs[i] = fmaf(y[i][j], y[i][j], hs[i]);
         }
         head_sums<NC>(sums, hs);
         float sum[2] = {0.0f, 0.0f};  // of x_out^2 and of dn w x_out
@@ -358,14 +426,17 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
             const int c = tid + i * T;
             if (c >= cols) continue;
             inv[i] = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
-            const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T], pn = r[(4 * NC + i) * T];
+            const P pn = r[((DX + 1) * NC + i) * T];
+            float vx[V], va[V];
+            in.get(1, i, T, c, vx);
             const Weights<V> wr = KEPT ? wrs[i] : weights<V>(a.res_scale, c), wp = KEPT ? wps[i] : weights<V>(a.w_post, c);
 #pragma unroll
             for (int j = 0; j < V; ++j) xo[i][j] = 1.0f;
-            if (a.a) {
+            if (gated) {
+                in.get(2, i, T, c, va);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float av = ldf(pa.x[j]), w = smaller_part<IO>(av), sig = av > 0.0f ? 1.0f - w : w;
+                    const float av = va[j], w = smaller_part<IO>(av), sig = av > 0.0f ? 1.0f - w : w;
                     if (KEPT) sg[i][j] = w;
                     xo[i][j] = silu ? av * sig : sig;
                 }
@@ -373,7 +444,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 y[i][j] *= inv[i];
-                xo[i][j] = fmaf(wr.x[j] * xo[i][j], y[i][j] * wp.x[j], ldf(px.x[j]));
+                xo[i][j] = fmaf(wr.x[j] * xo[i][j], y[i][j] * wp.x[j], vx[j]);
                 sum[0] = fmaf(xo[i][j], xo[i][j], sum[0]);
             }
             if (a.w_pre) {
@@ -393,7 +464,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
             const int c = tid + i * T;
             hs[i] = 0.0f;
             if (c >= cols) continue;
-            const P pa = r[(2 * NC + i) * T], pd = r[(3 * NC + i) * T], pn = r[(4 * NC + i) * T];
+            const P pd = r[(DX * NC + i) * T], pn = r[((DX + 1) * NC + i) * T];
             float dx[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) dx[j] = ldf(pd.x[j]);
@@ -411,11 +482,13 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
 #pragma unroll
             for (int j = 0; j < V; ++j) stf(dx_p.x[j], dx[j]);
             reinterpret_cast<P*>(ba.d_x)[tok * cols + c] = dx_p;
-            if (a.a) {
+            if (gated) {
                 P da_p;
+                float va[V];
+                in.get(2, i, T, c, va);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float av = ldf(pa.x[j]), w = KEPT ? sg[i][j] : smaller_part<IO>(av);
+                    const float av = va[j], w = KEPT ? sg[i][j] : smaller_part<IO>(av);
                     const float sig = av > 0.0f ? 1.0f - w : w, rest = av > 0.0f ? w : 1.0f - w, dev = silu ? fmaf(av, rest, 1.0f) : rest;
                     stf(da_p.x[j], dx[j] * wr.x[j] * wp.x[j] * y[i][j] * (sig * dev));
                     dx[j] *= silu ? av * sig : sig;
@@ -506,48 +579,56 @@ int piece_of(const JoinArgs& a, std::initializer_list<const void*> ptrs) {
 struct Shape {
     int threads, depth, smem;
 };
-// tensors: how many are read per token; room: shared memory that a CTA may take for its ring where more than one token is to be under way
-Shape shape_of(const JoinArgs& a, int V, int NC, int tensors, int room) {
+// own: bytes that a thread reads per token; room: shared memory that a CTA may take for its ring where more than one token is to be under way
+Shape shape_of(const JoinArgs& a, int V, int NC, int own, int room) {
     const int cols = a.H * a.d / V, t = ((cols + NC - 1) / NC + 31) / 32 * 32;
-    const int stage = tensors * NC * t * V * (a.f32 ? 4 : 2), G = a.d / V;
+    const int stage = own * t, G = a.d / V;
     const bool lanes = G <= 32 && (G & (G - 1)) == 0;
     int depth = room / stage;
     depth = depth > 4 ? 4 : (depth < 1 ? 1 : depth);
     return {t, depth, depth * stage + (64 + (lanes ? 0 : cols + a.H)) * 4};
 }
 
-template <typename IO, int V, int NC, int TMAX> int launch_fwd(const JoinArgs& a, const Shape& s, cudaStream_t st) {
-    auto kernel = join_fwd_kernel<IO, V, NC, TMAX>;
-    cudaError_t e = allow_shared_memory<join_fwd_kernel<IO, V, NC, TMAX>>();
+JoinPacked packed_of(const JoinArgs& a) { return join_packed((int64_t)a.B * a.L, a.H * a.d, a.gate == E2TTT_GATE_NONE ? 2 : 3); }
+
+template <typename IO, int V, int NC, int TMAX, bool PACK> int launch_fwd(const JoinArgs& a, const Shape& s, cudaStream_t st) {
+    auto kernel = join_fwd_kernel<IO, V, NC, TMAX, PACK>;
+    cudaError_t e = allow_shared_memory<join_fwd_kernel<IO, V, NC, TMAX, PACK>>();
     if (e != cudaSuccess) return (int)e;
     constexpr int threads = kept<V, TMAX>() ? 768 : 1024;  // on an SM
     const int64_t tokens = (int64_t)a.B * a.L, most = 148 * (threads / s.threads > 16 ? 16 : threads / s.threads);
-    kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a, s.depth);
+    kernel<<<(unsigned)(tokens < most ? tokens : most), s.threads, s.smem, st>>>(a, packed_of(a), s.depth);
     return (int)cudaGetLastError();
 }
-template <typename IO, int V, int NC, int TMAX> int launch_bwd(const JoinBwdArgs& b, const Shape& s, cudaStream_t st) {
-    auto kernel = join_bwd_kernel<IO, V, NC, TMAX>;
-    cudaError_t e = allow_shared_memory<join_bwd_kernel<IO, V, NC, TMAX>>();
+template <typename IO, int V, int NC, int TMAX, bool PACK> int launch_bwd(const JoinBwdArgs& b, const Shape& s, cudaStream_t st) {
+    auto kernel = join_bwd_kernel<IO, V, NC, TMAX, PACK>;
+    cudaError_t e = allow_shared_memory<join_bwd_kernel<IO, V, NC, TMAX, PACK>>();
     if (e != cudaSuccess) return (int)e;
     const int grid = join_bwd_grid((int64_t)b.f.B * b.f.L, b.f.H * b.f.d);
-    kernel<<<grid, s.threads, s.smem, st>>>(b, s.depth);
+    kernel<<<grid, s.threads, s.smem, st>>>(b, packed_of(b.f), s.depth);
     e = cudaGetLastError();
     if (e != cudaSuccess) return (int)e;
     join_sum_kernel<<<(b.f.H * b.f.d + kSumCols - 1) / kSumCols, 1024, 0, st>>>(b, grid);
     return (int)cudaGetLastError();
 }
 
-template <typename IO, int V, int NC> int sized(const JoinArgs& a, cudaStream_t st) {
-    const Shape s = shape_of(a, V, NC, 3, 56 * 1024);
+template <typename IO, int V, int NC, bool PACK> int sized(const JoinArgs& a, cudaStream_t st) {
+    const Shape s = shape_of(a, V, NC, 3 * NC * V * (int)sizeof(IO), 56 * 1024);
     if constexpr (V * NC == 8)
-        if (s.threads <= 256) return launch_fwd<IO, V, NC, 256>(a, s, st);
-    return launch_fwd<IO, V, NC, 512>(a, s, st);
+        if (s.threads <= 256) return launch_fwd<IO, V, NC, 256, PACK>(a, s, st);
+    return launch_fwd<IO, V, NC, 512, PACK>(a, s, st);
+}
+template <typename IO, int V, int NC, bool PACK> int sized(const JoinBwdArgs& b, cudaStream_t st) {
+    const Shape s = shape_of(b.f, V, NC, 2 * NC * V * (int)sizeof(IO) + Inputs<IO, V, NC, PACK>::kBytes, 110 * 1024);
+    if constexpr (V * NC == 8)
+        if (s.threads <= 256) return launch_bwd<IO, V, NC, 256, PACK>(b, s, st);
+    return launch_bwd<IO, V, NC, 512, PACK>(b, s, st);
+}
+template <typename IO, int V, int NC> int sized(const JoinArgs& a, cudaStream_t st) {
+    return a.packed ? sized<IO, V, NC, true>(a, st) : sized<IO, V, NC, false>(a, st);
 }
 template <typename IO, int V, int NC> int sized(const JoinBwdArgs& b, cudaStream_t st) {
-    const Shape s = shape_of(b.f, V, NC, 5, 110 * 1024);
-    if constexpr (V * NC == 8)
-        if (s.threads <= 256) return launch_bwd<IO, V, NC, 256>(b, s, st);
-    return launch_bwd<IO, V, NC, 512>(b, s, st);
+    return b.f.packed ? sized<IO, V, NC, true>(b, st) : sized<IO, V, NC, false>(b, st);
 }
 // 8 values a thread up to 4096 columns (512 threads), 16 above
 template <typename IO, typename Args> int dispatch(const Args& args, int v, bool wide, cudaStream_t st) {
@@ -604,11 +685,60 @@ bool f32_aligned(std::initializer_list<const void*> ptrs) {
 
 JoinArgs args_of(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
                  const float* w_pre, void* x_out, void* n_out) {
-    return {p->B, p->H, p->L, p->d, p->io_dtype == E2TTT_F32, p->gate, p->post_eps, p->pre_eps, o, a, x, w_post, res_scale, w_pre, x_out, n_out};
+    return {p->B, p->H, p->L, p->d, p->io_dtype == E2TTT_F32, p->gate, p->post_eps, p->pre_eps, o, a, x, w_post, res_scale, w_pre, x_out, n_out, nullptr};
 }
 
 size_t bytes_of(const e2ttt_join_params* p) {
     return kStatusBytes + (size_t)join_bwd_grid((int64_t)p->B * p->L, p->H * p->d) * 2 * p->H * p->d * 4;
+}
+
+size_t packed_bytes_of(const e2ttt_join_params* p) {
+    return (size_t)join_packed((int64_t)p->B * p->L, p->H * p->d, p->gate == E2TTT_GATE_NONE ? 2 : 3).total;
+}
+
+// keep: the inputs are left in, or read from, `packed`
+int check_packed(const e2ttt_join_params* p, bool keep, const void* packed, size_t bytes) {
+    if (!keep) return E2TTT_OK;
+    if (!packed || bytes < packed_bytes_of(p)) return E2TTT_ERR_WORKSPACE;
+    return aligned(packed, 256) ? E2TTT_OK : E2TTT_ERR_ALIGN;
+}
+
+int forward(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale, const float* w_pre,
+            void* x_out, void* n_out, bool keep, void* packed, size_t packed_bytes, void* stream) {
+    int rc = check(p);
+    if (rc) return rc;
+    if (!o || !x || !w_post || !res_scale || !x_out || !a != (p->gate == E2TTT_GATE_NONE) || !w_pre != !n_out) return E2TTT_ERR_NULL;
+    if (!io_aligned(p, {o, a, x, x_out, n_out}) || !f32_aligned({w_post, res_scale, w_pre})) return E2TTT_ERR_ALIGN;
+    rc = check_packed(p, keep, packed, packed_bytes);
+    if (rc) return rc;
+    rc = check_device();
+    if (rc) return rc;
+    JoinArgs args = args_of(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out);
+    if (keep) args.packed = static_cast<uint8_t*>(packed);
+    return join_fwd_launch(args, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+}
+
+int reverse(const e2ttt_join_params* p, const void* o, const void* a, const void* x, bool keep, const void* packed, size_t packed_bytes,
+            const float* w_post, const float* res_scale, const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a, void* d_x,
+            float* d_w_post, float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check(p);
+    if (rc) return rc;
+    const bool gated = p->gate != E2TTT_GATE_NONE;
+    if (!keep && (!o || !x || !a == gated)) return E2TTT_ERR_NULL;
+    if (!w_post || !res_scale || !d_x_out || !d_o || !d_x || !d_w_post || !d_res_scale) return E2TTT_ERR_NULL;
+    if (!d_a == gated || !w_pre != !d_n || !w_pre != !d_w_pre) return E2TTT_ERR_NULL;
+    if (!io_aligned(p, {o, a, x, d_x_out, d_n, d_o, d_a, d_x}) || !f32_aligned({w_post, res_scale, w_pre, d_w_post, d_res_scale, d_w_pre}))
+        return E2TTT_ERR_ALIGN;
+    rc = check_packed(p, keep, packed, packed_bytes);
+    if (rc) return rc;
+    if (!workspace || workspace_bytes < bytes_of(p)) return E2TTT_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return E2TTT_ERR_ALIGN;
+    rc = check_device();
+    if (rc) return rc;
+    JoinBwdArgs b{args_of(p, o, a, x, w_post, res_scale, w_pre, nullptr, nullptr), d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre,
+                  reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes)};
+    if (keep) b.f.packed = static_cast<uint8_t*>(const_cast<void*>(packed));
+    return join_bwd_launch(b, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
 }
 
 }  // namespace
@@ -625,32 +755,34 @@ int e2ttt_join_workspace_bytes(const e2ttt_join_params* p, size_t* bytes) {
 
 int e2ttt_join_fwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
                    const float* w_pre, void* x_out, void* n_out, void* stream) {
-    int rc = check(p);
-    if (rc) return rc;
-    if (!o || !x || !w_post || !res_scale || !x_out || !a != (p->gate == E2TTT_GATE_NONE) || !w_pre != !n_out) return E2TTT_ERR_NULL;
-    if (!io_aligned(p, {o, a, x, x_out, n_out}) || !f32_aligned({w_post, res_scale, w_pre})) return E2TTT_ERR_ALIGN;
-    rc = check_device();
-    if (rc) return rc;
-    return join_fwd_launch(args_of(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out), stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+    return forward(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out, false, nullptr, 0, stream);
 }
 
 int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
                    const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a, void* d_x, float* d_w_post,
                    float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream) {
-    int rc = check(p);
+    return reverse(p, o, a, x, false, nullptr, 0, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre, workspace,
+                   workspace_bytes, stream);
+}
+
+int e2ttt_join_packed_bytes(const e2ttt_join_params* p, size_t* bytes) {
+    if (!bytes) return E2TTT_ERR_NULL;
+    const int rc = check(p);
     if (rc) return rc;
-    if (!o || !x || !w_post || !res_scale || !d_x_out || !d_o || !d_x || !d_w_post || !d_res_scale) return E2TTT_ERR_NULL;
-    const bool gated = p->gate != E2TTT_GATE_NONE;
-    if (!a == gated || !d_a == gated || !w_pre != !d_n || !w_pre != !d_w_pre) return E2TTT_ERR_NULL;
-    if (!io_aligned(p, {o, a, x, d_x_out, d_n, d_o, d_a, d_x}) || !f32_aligned({w_post, res_scale, w_pre, d_w_post, d_res_scale, d_w_pre}))
-        return E2TTT_ERR_ALIGN;
-    if (!workspace || workspace_bytes < bytes_of(p)) return E2TTT_ERR_WORKSPACE;
-    if (!aligned(workspace, 256)) return E2TTT_ERR_ALIGN;
-    rc = check_device();
-    if (rc) return rc;
-    JoinBwdArgs b{args_of(p, o, a, x, w_post, res_scale, w_pre, nullptr, nullptr), d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale, d_w_pre,
-                  reinterpret_cast<float*>(static_cast<char*>(workspace) + kStatusBytes)};
-    return join_bwd_launch(b, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+    *bytes = packed_bytes_of(p);
+    return E2TTT_OK;
+}
+
+int e2ttt_join_fwd_packed(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post, const float* res_scale,
+                          const float* w_pre, void* x_out, void* n_out, void* packed, size_t packed_bytes, void* stream) {
+    return forward(p, o, a, x, w_post, res_scale, w_pre, x_out, n_out, true, packed, packed_bytes, stream);
+}
+
+int e2ttt_join_bwd_packed(const e2ttt_join_params* p, const void* packed, size_t packed_bytes, const float* w_post, const float* res_scale,
+                          const float* w_pre, const void* d_x_out, const void* d_n, void* d_o, void* d_a, void* d_x, float* d_w_post,
+                          float* d_res_scale, float* d_w_pre, void* workspace, size_t workspace_bytes, void* stream) {
+    return reverse(p, nullptr, nullptr, nullptr, true, packed, packed_bytes, w_post, res_scale, w_pre, d_x_out, d_n, d_o, d_a, d_x, d_w_post, d_res_scale,
+                   d_w_pre, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

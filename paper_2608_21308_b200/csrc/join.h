@@ -14,7 +14,25 @@ struct JoinArgs {
     const void *o, *a, *x;                        // a may be null (no gate)
     const float *w_post, *res_scale, *w_pre;      // w_pre may be null (no second norm)
     void *x_out, *n_out;                          // n_out: null with w_pre
+    uint8_t* packed;                              // o, x and a in 8 bits (JoinPacked); null: not kept, or (reverse pass) not read
 };
+
+// Where the packed inputs lie: codes of o, x and, with a gate, a as rows of H d columns filled up to blocks of 32, then their scales, rows filled up to words.
+struct JoinPacked {
+    int64_t code_row, scale_row;    // bytes of a row
+    int64_t code_step, scale_step;  // bytes of a tensor
+    int64_t scales, total;          // where the scales start; bytes in all
+};
+inline JoinPacked join_packed(int64_t tokens, int width, int tensors) {
+    JoinPacked l{};
+    l.code_row = (width + 31) / 32 * 32;
+    l.scale_row = (l.code_row / 32 + 3) / 4 * 4;
+    l.code_step = tokens * l.code_row;
+    l.scale_step = tokens * l.scale_row;
+    l.scales = tensors * l.code_step;
+    l.total = l.scales + tensors * l.scale_step;
+    return l;
+}
 
 struct JoinBwdArgs {
     JoinArgs f;

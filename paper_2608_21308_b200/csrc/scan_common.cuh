@@ -1,0 +1,178 @@
+// Gated linear recurrence: the gates of a token, two channels at a time, and the tokens of a thread.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "scan.h"
+
+namespace e2ttt {
+namespace scan {
+
+constexpr unsigned kAll = 0xffffffffu;
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+
+// two fp32 values at a time (one instruction on this architecture)
+__device__ __forceinline__ uint64_t u2(float2 a) { return *reinterpret_cast<const uint64_t*>(&a); }
+__device__ __forceinline__ float2 f2(uint64_t a) { return *reinterpret_cast<const float2*>(&a); }
+__device__ __forceinline__ float2 dup(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(u2(a)), "l"(u2(b)), "l"(u2(c)));
+    return f2(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(u2(a)), "l"(u2(b)));
+    return f2(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(u2(a)), "l"(u2(b)));
+    return f2(r);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rsqrt_fast(float x) {
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 1 / (1 + exp(-x)); with bf16 I/O the special function unit's exponential and reciprocal (2^-22 each) are enough
+template <typename IO> __device__ __forceinline__ float2 sigmoid2(float2 x) {
+    if constexpr (sizeof(IO) == 4) {
+        return make_float2(__frcp_rn(1.0f + expf(-x.x)), __frcp_rn(1.0f + expf(-x.y)));
+    } else {
+        const float2 t = mul2(x, dup(-kLog2e));
+        const float2 e = add2(make_float2(ex2(t.x), ex2(t.y)), dup(1.0f));
+        return make_float2(rcp(e.x), rcp(e.y));
+    }
+}
+
+// The smaller of sigmoid(x) and 1 - sigmoid(x), e / (1 + e) with e = exp(-|x|); its sign says which: positive where x > 0 and it is 1 - sigmoid(x).  The reverse pass needs
+// both, and what an open gate leaves of 1 would be lost in a difference.
+template <typename IO> __device__ __forceinline__ float smaller_part(float x) {
+    if constexpr (sizeof(IO) == 4) {
+        const float e = expf(-fabsf(x));
+        return copysignf(e * __frcp_rn(1.0f + e), x);
+    } else {
+        const float e = ex2(fabsf(x) * -kLog2e);
+        return copysignf(e * rcp(1.0f + e), x);
+    }
+}
+__device__ __forceinline__ float open_part(float w) { return signbit(w) ? -w : 1.0f - w; }    // sigmoid(x)
+__device__ __forceinline__ float closed_part(float w) { return signbit(w) ? 1.0f + w : w; }   // 1 - sigmoid(x)
+template <typename IO> __device__ __forceinline__ float2 smaller_part2(float2 x) { return make_float2(smaller_part<IO>(x.x), smaller_part<IO>(x.y)); }
+__device__ __forceinline__ float2 open2(float2 w) { return make_float2(open_part(w.x), open_part(w.y)); }
+__device__ __forceinline__ float2 closed2(float2 w) { return make_float2(closed_part(w.x), closed_part(w.y)); }
+
+// exp(y) - 1 for -1/4 <= y <= 0: the series to y^7 / 7! (2e-9 of the result)
+__device__ __forceinline__ float2 expm1_near(float2 y) {
+    float2 p = fma2(y, dup(1.0f / 5040.0f), dup(1.0f / 720.0f));
+    p = fma2(p, y, dup(1.0f / 120.0f));
+    p = fma2(p, y, dup(1.0f / 24.0f));
+    p = fma2(p, y, dup(1.0f / 6.0f));
+    p = fma2(p, y, dup(0.5f));
+    p = fma2(p, y, dup(1.0f));
+    return mul2(p, y);
+}
+
+// A token's decay for two channels.  Near 1, where a's own rounding is what a long memory adds up, it is kept as c = a - 1; far from it (log a below -1/4), where c's rounding
+// would be what a leaves of a state, as c = a.  one = 1 - a^2.
+struct Decay {
+    float2 c, one;
+    unsigned far;  // bit 0: the first channel's c is a, bit 1: the second's
+};
+// sg = sigmoid(a_decay).  NEAR: the rates are at most 1/4, so that no decay is far from 1.
+template <typename IO, bool UNIT, bool NEAR> __device__ __forceinline__ Decay decay(float2 sg, float2 neg_rate) {
+    const float2 y = mul2(neg_rate, sg);
+    Decay d;
+    d.c = expm1_near(y);
+    d.far = 0;
+    if (UNIT) d.one = mul2(make_float2(-d.c.x, -d.c.y), add2(d.c, dup(2.0f)));
+    if constexpr (!NEAR) {
+        float2 e;
+        if constexpr (sizeof(IO) == 4) e = make_float2(expf(y.x), expf(y.y));
+        else e = make_float2(ex2(y.x * kLog2e), ex2(y.y * kLog2e));
+        if (y.x < -0.25f) {
+            d.far = 1;
+            d.c.x = e.x;
+            if (UNIT) d.one.x = fmaf(-e.x, e.x, 1.0f);
+        }
+        if (y.y < -0.25f) {
+            d.far |= 2;
+            d.c.y = e.y;
+            if (UNIT) d.one.y = fmaf(-e.y, e.y, 1.0f);
+        }
+    }
+    return d;
+}
+// a h
+template <bool NEAR> __device__ __forceinline__ float2 fade(float2 h, float2 c, unsigned far) {
+    if constexpr (NEAR) return fma2(h, c, h);
+    return fma2(h, c, make_float2(far & 1 ? 0.0f : h.x, far & 2 ? 0.0f : h.y));
+}
+
+// 1 / sqrt(x), 0 for 0
+template <typename IO> __device__ __forceinline__ float inv_sqrt(float x) {
+    float y;
+    if constexpr (sizeof(IO) == 4) {
+        y = rsqrtf(x);
+        y = y * fmaf(-0.5f * x * y, y, 1.5f);  // Newton's step: 2^-23
+    } else {
+        y = rsqrt_fast(x);
+    }
+    return x > 1e-37f ? y : 0.0f;
+}
+template <typename IO> __device__ __forceinline__ float2 inv_sqrt2(float2 x) { return make_float2(inv_sqrt<IO>(x.x), inv_sqrt<IO>(x.y)); }
+
+template <typename IO> __device__ __forceinline__ float to_f32(IO x);
+template <> __device__ __forceinline__ float to_f32(float x) { return x; }
+template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// Two neighbouring channels of a row; `n` of them are there.  `pair`: the row's channels lie at a multiple of the pair's size.
+template <typename IO> __device__ __forceinline__ float2 load2(const void* base, int64_t at, int n, bool pair) {
+    const IO* p = static_cast<const IO*>(base) + at;
+    if (pair && n == 2) {
+        if constexpr (sizeof(IO) == 4) {
+            return *reinterpret_cast<const float2*>(p);
+        } else {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+            return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        }
+    }
+    return make_float2(n > 0 ? to_f32<IO>(p[0]) : 0.0f, n > 1 ? to_f32<IO>(p[1]) : 0.0f);
+}
+template <typename IO> __device__ __forceinline__ void store2(void* base, int64_t at, int n, bool pair, float2 v) {
+    IO* p = static_cast<IO*>(base) + at;
+    if (pair && n == 2) {
+        if constexpr (sizeof(IO) == 4) {
+            *reinterpret_cast<float2*>(p) = v;
+        } else {
+            const __nv_bfloat162 w = __floats2bfloat162_rn(v.x, v.y);
+            *reinterpret_cast<__nv_bfloat162*>(p) = w;
+        }
+        return;
+    }
+    if (n > 0) put(p, v.x);
+    if (n > 1) put(p + 1, v.y);
+}
+
+}  // namespace scan
+}  // namespace e2ttt
