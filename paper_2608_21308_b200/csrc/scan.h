@@ -15,8 +15,8 @@ struct ScanShape {
     constexpr int64_t spans() const { return ((int64_t)L + kScanSpan - 1) / kScanSpan; }
 };
 
-// CTAs of a block of channels, along the tokens
-int scan_parts(const ScanShape& s);
+// CTAs of the reverse pass that share a block of channels, along the tokens
+int scan_bwd_parts(const ScanShape& s);
 
 struct ScanLayout {  // byte offsets
     size_t states;   // [B][spans][D] fp32: the state before every 64th token

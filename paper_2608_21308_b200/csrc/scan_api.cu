@@ -13,7 +13,7 @@ ScanLayout scan_layout(const ScanShape& s, int save) {
     const size_t tensors = save == E2TTT_SAVE_PACKED ? (s.gate ? 3 : 2) : 0, rows = (size_t)s.B * s.blocks() * s.spans() * kScanSpan;
     l.states = kStatusBytes;
     l.rates = l.states + round((size_t)s.B * s.spans() * s.D * 4);
-    l.codes = l.rates + round((size_t)s.B * scan_parts(s) * s.D * 4);
+    l.codes = l.rates + round((size_t)s.B * scan_bwd_parts(s) * s.D * 4);
     l.code_step = rows * kScanCh;
     l.scales = l.codes + tensors * l.code_step;
     l.scale_step = rows * 2;

@@ -174,5 +174,86 @@ template <typename IO> __device__ __forceinline__ void store2(void* base, int64_
     if (n > 1) put(p + 1, v.y);
 }
 
+// ---- a warp's tokens of a tile, ahead in shared memory: rows of 64 channels, one tensor after the other.  Every warp reads back only what it copied itself.
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 or 4 bytes, zeros where `in` is false (nothing is read then)
+__device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_at(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(void* dst, const void* src, bool in) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_at(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
+// How rows are read: pieces of 16 bytes, of 4, or value by value (odd rows, and addresses, of bf16)
+enum { kBy16 = 0, kBy4 = 1, kByValue = 2 };
+inline int reads_by(int D, bool f32, uintptr_t all) {
+    const int size = f32 ? 4 : 2;
+    if (all % 16 == 0 && (int64_t)D * size % 16 == 0) return kBy16;
+    return all % 4 == 0 && (int64_t)D * size % 4 == 0 ? kBy4 : kByValue;
+}
+
+// ROWS tokens of `src` from row t on, channels c .. c + 63, as far as there are tokens (L) and channels (D); `at` is where token 0 of the sequence starts
+template <typename IO, int ROWS> __device__ __forceinline__ void copy_rows(IO* dst, const IO* src, int64_t at, int t, int L, int c, int D, int by, int lane) {
+    if (by == kBy16) {
+        constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;  // pieces of a row; rows a warp copies at once
+        const int row = lane / PER, ch = lane % PER * V;
+        const bool col = c + ch < D;
+        const IO* p = src + at + (int64_t)(t + row) * D + c + ch;
+#pragma unroll
+        for (int i = 0; i < ROWS; i += STEP) {
+            const bool in = col && t + row + i < L;
+            copy16(dst + (row + i) * kScanCh + ch, in ? p + (int64_t)i * D : src, in);
+        }
+        return;
+    }
+    constexpr int V = 4 / (int)sizeof(IO);
+    if (by == kBy4) {
+        for (int i = lane; i < ROWS * kScanCh / V; i += 32) {
+            const int row = i / (kScanCh / V), ch = i % (kScanCh / V) * V;
+            const bool in = c + ch < D && t + row < L;
+            copy4(dst + row * kScanCh + ch, in ? src + at + (int64_t)(t + row) * D + c + ch : src, in);
+        }
+        return;
+    }
+    for (int i = lane; i < ROWS * kScanCh; i += 32) {
+        const int row = i / kScanCh, ch = i % kScanCh;
+        IO v = IO(0.0f);
+        if (c + ch < D && t + row < L) v = src[at + (int64_t)(t + row) * D + c + ch];
+        dst[i] = v;
+    }
+}
+
+// a lane's two channels of a row in shared memory
+template <typename IO> __device__ __forceinline__ float2 row2(const IO* row, int lane) {
+    if constexpr (sizeof(IO) == 4) {
+        return reinterpret_cast<const float2*>(row)[lane];
+    } else {
+        const uint32_t w = reinterpret_cast<const uint32_t*>(row)[lane];
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+}
+
+// ---- runs of tokens: what goes in, P times, plus what a run makes of nothing.  A run with a start in it lets nothing through, an infinity or a NaN neither.
+__device__ __forceinline__ float through(float P, float in, float own) { return P == 0.0f ? own : fmaf(P, in, own); }
+__device__ __forceinline__ float2 through2(float2 P, float2 in, float2 own) { return make_float2(through(P.x, in.x, own.x), through(P.y, in.y, own.y)); }
+
+// ---- CTAs of a cluster: the parts of a sequence's channels along its tokens
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// writes v where CTA `rank` of the cluster has what lies at `here`
+__device__ __forceinline__ void put_remote(float4* here, uint32_t rank, float4 v) {
+    uint32_t there;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_at(here)), "r"(rank));
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
 }  // namespace scan
 }  // namespace e2ttt

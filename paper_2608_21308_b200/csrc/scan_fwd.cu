@@ -1,6 +1,10 @@
 // Gated linear recurrence, forward.  h_t = a_t h_{t-1} + b_t is linear in the state: over a run of tokens h_out = P h_in + h', P the product of the a_t and h' the run's
-// end from a zero state.  A CTA has 64 channels of a sequence and walks its tokens 64 at a time; a lane has two channels, a warp eight tokens of the tile, whose
-// P and h' meet in shared memory.
+// end from a zero state.  A CTA has 64 channels of a sequence; a lane has two of them, a warp kTok tokens of a tile, whose P and h' meet in shared memory.  Where there are
+// few channels and sequences, the tiles of a sequence are dealt out to the CTAs of a cluster, whose P and h' meet through distributed shared memory: no CTA waits for another
+// kernel's work, nothing lies in global memory between them, and every sum has one order.
+#include <type_traits>
+
+#include "api_checks.h"
 #include "pack8.cuh"
 #include "scan_common.cuh"
 
@@ -8,101 +12,196 @@ namespace e2ttt {
 namespace {
 using namespace scan;
 
-constexpr int kTok = 8;  // tokens of a thread in a tile
+constexpr int kStages = 2;
+template <typename IO> constexpr int kTokOf = sizeof(IO) == 2 ? 16 : 8;
+
+// what the runs of a tile and the parts of a cluster leave for one another, twice in turn
+struct Meet {
+    float4 runs[2][kWarps][32];  // P and h' of a warp's tokens
+    float4 parts[2][8][32];      // of a CTA's tile
+};
+
+// The 8-bit form of a warp's rows of one tensor: a lane takes 16 bytes, an aligned group of lanes a block.
+template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const IO* rows, uint8_t* codes, uint8_t* scales, int n, int lane) {
+    constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;
+    const int row = lane / PER, piece = lane % PER;
+#pragma unroll
+    for (int i = 0; i < ROWS; i += STEP) {
+        const uint4 raw = *reinterpret_cast<const uint4*>(rows + (row + i) * kScanCh + piece * V);
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (V == 8) {
+                v[2 * j] = __uint_as_float(w[j] << 16);
+                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            } else {
+                v[j] = __uint_as_float(w[j]);
+            }
+        }
+        const uint32_t byte = pack8::group_scale<V>(v);
+        if (row + i >= n) continue;
+        *reinterpret_cast<pack8::Codes<V>*>(codes + (row + i) * kScanCh + piece * V) = pack8::encode<V>(v, byte);
+        if (piece % (pack8::kBlock / V) == 0) scales[(row + i) * 2 + piece / (pack8::kBlock / V)] = (uint8_t)byte;
+    }
+}
 
 template <typename IO, bool GATE, bool UNIT, bool PACK>
-__global__ void __launch_bounds__(kThreads) scan_fwd_kernel(const ScanArgs a, const bool pair) {
-    __shared__ float4 runs[2][kWarps][32];
+__global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a, const int by, const bool pair, const int parts) {
+    constexpr int TOK = kTokOf<IO>, TILE = TOK * kWarps, NT = GATE ? 3 : 2;
+    extern __shared__ __align__(16) char smem[];
+    Meet& meet = *reinterpret_cast<Meet*>(smem);
     const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t blocks = a.s.blocks(), spans = a.s.spans();
-    const int64_t b = blockIdx.x / blocks, blk = blockIdx.x - b * blocks;
-    const int c0 = (int)blk * kScanCh + 2 * lane, n = max(0, min(2, D - c0));
+    const int64_t blocks = a.s.blocks(), spans = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
+    const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
+    const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
+    IO* ring = reinterpret_cast<IO*>(smem + sizeof(Meet)) + warp * (kStages * NT * TOK * kScanCh);
+    const int64_t seq = b * L * (int64_t)D;
     float2 rate = load2<float>(a.rate, c0, n, false);
+    const bool near = __syncthreads_and(rate.x <= 0.25f && rate.y <= 0.25f);
     rate = make_float2(-rate.x, -rate.y);
     float2 carry = a.h_init ? load2<float>(a.h_init, b * D + c0, n, false) : dup(0.0f);
-    int flip = 0;
-    for (int64_t tile = 0; tile < spans; ++tile, flip ^= 1) {
-        const int t0 = (int)(tile * kScanSpan) + warp * kTok;
-        if (a.states && warp == 0) store2<float>(a.states, (b * spans + tile) * D + c0, n, false, carry);
-        float2 h[kTok], P[kTok], hh = dup(0.0f), pp = dup(1.0f);
+    if (parts > 1) cluster_sync();  // the others' shared memory is there
+    const int64_t tiles = ((int64_t)L + TILE - 1) / TILE;
+    unsigned next_first = 0;
+    auto load = [&](int64_t tile, int slot) {
+        next_first = 0;
+        if (tile < tiles) {
+            const int t = (int)(tile * TILE) + warp * TOK;
+            IO* to = ring + slot * (NT * TOK * kScanCh);
+            copy_rows<IO, TOK>(to, static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
+            copy_rows<IO, TOK>(to + TOK * kScanCh, static_cast<const IO*>(a.r), seq, t, L, first, D, by, lane);
+            if (GATE) copy_rows<IO, TOK>(to + 2 * TOK * kScanCh, static_cast<const IO*>(a.g), seq, t, L, first, D, by, lane);
+            if (a.starts && lane < TOK && t + lane < L) next_first = a.starts[b * L + t + lane];
+        }
+        copy_commit();
+    };
+    load(part, 0);
+    unsigned byte0 = next_first;
+    load(part + parts, 1);
+    int slot = 0;
+    // every CTA of a cluster takes every turn: its part of the last one may be empty
+    for (int64_t turn = 0; turn * parts < tiles; ++turn, slot ^= 1) {
+        const int64_t tile = turn * parts + part;
+        const int t0 = (int)min(tile * TILE + warp * TOK, (int64_t)L), have = min(TOK, L - t0);
+        const unsigned starts = __ballot_sync(kAll, byte0 != 0);
+        byte0 = next_first;
+        const IO* rows = ring + slot * (NT * TOK * kScanCh);
+        copy_wait<kStages - 1>();
+        __syncwarp();
+        float2 h[TOK], P[TOK], hh = dup(0.0f), pp = dup(1.0f);
+        auto walk = [&](auto plain) {  // plain: all tokens are there, none is a start, no decay is far from 1
+            constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-            const int t = t0 + j;
-            const bool in = t < L;
-            const int64_t at = (b * L + t) * D + c0;
-            const float2 x = load2<IO>(a.x, at, in ? n : 0, pair), r = load2<IO>(a.r, at, in ? n : 0, pair);
-            const float2 g = GATE ? load2<IO>(a.g, at, in ? n : 0, pair) : dup(0.0f);
-            if (PACK) {
-                const float2 v[3] = {x, r, g};
-#pragma unroll
-                for (int k = 0; k < (GATE ? 3 : 2); ++k) {
-                    uint32_t m = max(pack8::magnitude(v[k].x), pack8::magnitude(v[k].y));
-#pragma unroll
-                    for (int s = 1; s < 16; s <<= 1) m = max(m, __shfl_xor_sync(kAll, m, s));
-                    const uint32_t byte = pack8::scale_byte(m);
-                    const float w[2] = {v[k].x, v[k].y};
-                    const int64_t row = (b * blocks + blk) * spans * kScanSpan + t;
-                    *reinterpret_cast<pack8::Codes<2>*>(a.codes + k * a.code_step + row * kScanCh + 2 * lane) = pack8::encode<2>(w, byte);
-                    if ((lane & 15) == 0) a.scales[k * a.scale_step + row * 2 + (lane >> 4)] = (uint8_t)byte;
+            for (int j = 0; j < TOK; ++j) {
+                if (PLAIN || j < have) {
+                    float2 u = row2(rows + j * kScanCh, lane);
+                    const Decay d = decay<IO, UNIT, PLAIN>(sigmoid2<IO>(row2(rows + (TOK + j) * kScanCh, lane)), rate);
+                    if (GATE) u = mul2(u, sigmoid2<IO>(row2(rows + (2 * TOK + j) * kScanCh, lane)));
+                    if (!PLAIN && (starts >> j & 1)) {
+                        hh = u;
+                        pp = dup(0.0f);
+                    } else {
+                        if (UNIT) u = mul2(u, mul2(d.one, inv_sqrt2<IO>(d.one)));
+                        hh = add2(fade<PLAIN>(hh, d.c, d.far), u);
+                        pp = fade<PLAIN>(pp, d.c, d.far);
+                    }
                 }
+                h[j] = hh;
+                P[j] = pp;
             }
-            float2 u = x;
-            if (GATE) u = mul2(u, sigmoid2<IO>(g));
-            const Decay d = decay<IO, UNIT, false>(sigmoid2<IO>(r), rate);
-            if (in && a.starts && a.starts[b * L + t]) {
-                hh = u;
-                pp = dup(0.0f);
-            } else if (in) {
-                if (UNIT) u = mul2(u, mul2(d.one, inv_sqrt2<IO>(d.one)));
-                hh = add2(fade<false>(hh, d.c, d.far), u);
-                pp = fade<false>(pp, d.c, d.far);
-            }
-            h[j] = hh;
-            P[j] = pp;
-        }
-        runs[flip][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
-        __syncthreads();
-        float2 in = carry;
-        for (int w = 0; w < kWarps; ++w) {
-            const float4 q = runs[flip][w][lane];
-            if (w == warp) in = carry;
-            carry.x = q.x == 0.0f ? q.z : fmaf(q.x, carry.x, q.z);
-            carry.y = q.y == 0.0f ? q.w : fmaf(q.y, carry.y, q.w);
-        }
-        if (a.h) {
+        };
+        if (near && have == TOK && !starts) walk(std::true_type{});
+        else walk(std::false_type{});
+        if (PACK && have > 0) {
+            const int64_t row = unit * spans * kScanSpan + t0;
 #pragma unroll
-            for (int j = 0; j < kTok; ++j) {
-                if (t0 + j >= L) continue;
-                float2 y;
-                y.x = P[j].x == 0.0f ? h[j].x : fmaf(P[j].x, in.x, h[j].x);
-                y.y = P[j].y == 0.0f ? h[j].y : fmaf(P[j].y, in.y, h[j].y);
-                store2<IO>(a.h, (b * L + t0 + j) * D + c0, n, pair, y);
+            for (int k = 0; k < NT; ++k)
+                pack_rows<IO, TOK>(rows + k * TOK * kScanCh, a.codes + k * a.code_step + row * kScanCh, a.scales + k * a.scale_step + row * 2, have, lane);
+        }
+        __syncwarp();
+        load((turn + 2) * parts + part, slot);
+        meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
+        __syncthreads();
+        float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps before this one
+        if (parts == 1) own = carry;
+        float2 P_all = P_in, all = own;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float4 q = meet.runs[slot][w][lane];
+            if (w == warp) {
+                P_in = P_all;
+                own = all;
             }
+            all = through2(make_float2(q.x, q.y), all, make_float2(q.z, q.w));
+            P_all = mul2(P_all, make_float2(q.x, q.y));
+        }
+        float2 in = own;
+        if (parts == 1) {
+            carry = all;
+        } else {
+            if (warp < parts) put_remote(&meet.parts[slot][part][lane], warp, make_float4(P_all.x, P_all.y, all.x, all.y));
+            cluster_sync();
+            for (int k = 0; k < parts; ++k) {
+                const float4 q = meet.parts[slot][k][lane];
+                if (k == part) in = through2(P_in, carry, own);
+                carry = through2(make_float2(q.x, q.y), carry, make_float2(q.z, q.w));
+            }
+        }
+        if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
+        if (a.h) {
+            const int64_t at = seq + (int64_t)t0 * D + c0;
+#pragma unroll
+            for (int j = 0; j < TOK; ++j)
+                if (j < have) store2<IO>(a.h, at + (int64_t)j * D, n, pair, through2(P[j], in, h[j]));
         }
     }
-    if (a.h_final && warp == 0) store2<float>(a.h_final, b * D + c0, n, false, carry);
+    if (a.h_final && part == 0 && warp == 0) store2<float>(a.h_final, b * D + c0, n, false, carry);
+    copy_wait<0>();
 }
 
-template <typename IO, bool GATE, bool UNIT> int launch(const ScanArgs& a, bool pair, cudaStream_t st) {
-    const unsigned grid = (unsigned)(a.s.B * a.s.blocks());
-    if (a.codes) scan_fwd_kernel<IO, GATE, UNIT, true><<<grid, kThreads, 0, st>>>(a, pair);
-    else scan_fwd_kernel<IO, GATE, UNIT, false><<<grid, kThreads, 0, st>>>(a, pair);
-    return (int)cudaGetLastError();
+// CTAs of a cluster
+int parts_of(const ScanShape& s) {
+    const int64_t units = s.B * s.blocks(), tiles = ((int64_t)s.L + 127) / 128;
+    int parts = 1;
+    while (parts < 8 && units * parts < 296 && parts < tiles) parts *= 2;
+    return parts;
 }
-template <typename IO> int dispatch(const ScanArgs& a, bool pair, cudaStream_t st) {
-    if (a.s.gate) return a.s.unit ? launch<IO, true, true>(a, pair, st) : launch<IO, true, false>(a, pair, st);
-    return a.s.unit ? launch<IO, false, true>(a, pair, st) : launch<IO, false, false>(a, pair, st);
+
+template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
+    auto kernel = scan_fwd_kernel<IO, GATE, UNIT, PACK>;
+    cudaError_t e = allow_shared_memory<scan_fwd_kernel<IO, GATE, UNIT, PACK>>();
+    if (e != cudaSuccess) return (int)e;
+    const int parts = parts_of(a.s);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(a.s.B * a.s.blocks() * parts));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Meet) + kStages * (GATE ? 3 : 2) * kTokOf<IO> * kWarps * kScanCh * sizeof(IO);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    return (int)cudaLaunchKernelEx(&cfg, kernel, a, by, pair, parts);
+}
+template <typename IO, bool GATE, bool UNIT> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
+    return a.codes ? launch<IO, GATE, UNIT, true>(a, by, pair, st) : launch<IO, GATE, UNIT, false>(a, by, pair, st);
+}
+template <typename IO> int dispatch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
+    if (a.s.gate) return a.s.unit ? launch<IO, true, true>(a, by, pair, st) : launch<IO, true, false>(a, by, pair, st);
+    return a.s.unit ? launch<IO, false, true>(a, by, pair, st) : launch<IO, false, false>(a, by, pair, st);
 }
 
 }  // namespace
 
-int scan_parts(const ScanShape&) { return 1; }
-
 int scan_fwd_launch(const ScanArgs& a, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const uintptr_t all = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.r) | reinterpret_cast<uintptr_t>(a.g) | reinterpret_cast<uintptr_t>(a.h);
-    const bool pair = a.s.D % 2 == 0 && all % (a.s.f32 ? 8 : 4) == 0;
-    return a.s.f32 ? dispatch<float>(a, pair, st) : dispatch<__nv_bfloat16>(a, pair, st);
+    const uintptr_t in = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.r) | reinterpret_cast<uintptr_t>(a.g);
+    const int by = reads_by(a.s.D, a.s.f32, in);
+    const bool pair = a.s.D % 2 == 0 && reinterpret_cast<uintptr_t>(a.h) % (a.s.f32 ? 8 : 4) == 0;
+    return a.s.f32 ? dispatch<float>(a, by, pair, st) : dispatch<__nv_bfloat16>(a, by, pair, st);
 }
 
 }  // namespace e2ttt

@@ -300,7 +300,8 @@ def test_a_sequence_does_not_depend_on_what_is_in_the_others():
 
 
 def test_more_than_two_to_the_31_elements():
-    """The last tokens lie 2^31 elements into every tensor; behind a start they have to come out as they do alone, forward and back."""
+    """The last tokens lie 2^31 elements into every tensor; behind a start they have to come out as they do alone, forward and back.  Going back, the long call has its
+    tiles in several parts, whose sums are rounded elsewhere: a value may be rounded to the next step of bf16, 2^-7 of it."""
     L, D, n = (1 << 20) + 64, 2048, 64
     g = torch.Generator(device="cuda").manual_seed(0)
     x, r = (torch.zeros(1, L, D, device="cuda", dtype=torch.bfloat16) for _ in range(2))
@@ -325,7 +326,9 @@ def test_more_than_two_to_the_31_elements():
     assert torch.equal(h2, h1) and torch.equal(last1, last)
     dx1, dr1 = torch.empty_like(x1), torch.empty_like(x1)
     E.e2ttt_scan_bwd(p1, None, None, None, rate, starts[:, -n:].contiguous(), None, h1, end, dx1, dr1, None, *out1, ws1, 2)
-    assert torch.equal(r[:, -n:], dx1) and torch.equal(dr[:, -n:], dr1)
+    for got, alone in ((r[:, -n:], dx1), (dr[:, -n:], dr1)):
+        got, alone = got.float(), alone.float()
+        assert bool(((got - alone).abs() <= 2.0 ** -7 * alone.abs() + 1e-5 * alone.abs().max()).all())
     assert not bool(r[:, :-n].any()) and not bool(h[:, :-n].any())  # nothing came before
 
 
