@@ -18,9 +18,11 @@ constexpr int kTok = 8, kTile = kTok * kWarps, kStages = 2;
 static_assert(kTile == kScanSpan, "a tile starts from a saved state");
 
 struct Meet {
-    float4 runs[2][kWarps][32];  // P and h' of a warp's tokens
-    float4 parts[2][8][32];      // P and v' of a CTA's tile
-    float2 ends[2][kWarps][32];  // v' of a warp's tokens
+    float4 runs[2][kWarps][32];        // P and h' of a warp's tokens
+    float2 ends[2][kWarps][32];        // v' of a warp's tokens
+    float2 carry[2][32];               // the adjoint that a turn's tokens hand on
+    Meeting meeting;
+    float2 stash[kWarps][kTok][32];    // a thread's own, for want of registers
 };
 
 // what a warp has under way of a tile
@@ -37,7 +39,8 @@ template <typename IO, int NT> struct Rows<IO, NT, true> {
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, false>& r, int j, int lane) { return row2<IO>(r.in[K][j], lane); }
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, true>& r, int j, int lane) {
     const uint32_t w = reinterpret_cast<const uint16_t*>(r.codes[K][j])[lane];
-    return mul2(make_float2(pack8::number<0>(w), pack8::number<1>(w)), dup(pack8::scale(r.scales[K][j][lane >> 4])));
+    // a block that is not finite has codes of 0 and an infinite scale: NaN
+    return mul2(make_float2(pack8::number<0>(w), pack8::number<1>(w)), dup(__uint_as_float((uint32_t)r.scales[K][j][lane >> 4] << 23)));
 }
 
 template <typename IO, bool GATE, bool UNIT, bool PACK>
@@ -47,17 +50,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     extern __shared__ __align__(16) char smem[];
     Meet& meet = *reinterpret_cast<Meet*>(smem);
     const ScanArgs& a = ba.f;
-    const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
     R* ring = reinterpret_cast<R*>(smem + sizeof(Meet)) + warp * kStages;
     const int64_t blocks = a.s.blocks(), tiles = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
+    const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
     const int64_t seq = b * L * (int64_t)D;
     float2 rate = load2<float>(a.rate, c0, n, false);
-    const bool near = __syncthreads_and(rate.x <= 0.25f && rate.y <= 0.25f);
+    const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
     rate = make_float2(-rate.x, -rate.y);
-    float2 carry = ba.dh_final ? load2<float>(ba.dh_final, b * D + c0, n, false) : dup(0.0f), sum = dup(0.0f);
-    if (parts > 1) cluster_sync();  // the others' shared memory is there
+    float2 end = ba.dh_final ? load2<float>(ba.dh_final, b * D + c0, n, false) : dup(0.0f), sum = dup(0.0f);  // end: what the last turn hands on, in one warp
+    const int ender = parts == 1 ? 0 : kWarps - 1;
+    if (warp == ender) meet.carry[1][lane] = end;
+    if (parts > 1) meeting_init(meet.meeting);
     unsigned next_first = 0;
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
@@ -86,7 +92,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     unsigned byte0 = next_first;
     load((turns - 2) * parts + part, 1);
     int slot = 0;
-    for (int64_t turn = turns - 1; turn >= 0; --turn, slot ^= 1) {
+    uint32_t parity = 0;
+    bool met = true;
+    for (int64_t turn = turns - 1; turn >= 0; --turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
         const int t0 = (int)min(tile * kTile + warp * kTok, (int64_t)L), have = min(kTok, L - t0);
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
@@ -95,42 +103,42 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         const R& rows = ring[slot];
         copy_wait<kStages - 1>();
         __syncwarp();
-        float2 c[kTok], wr[kTok], wi[kTok], rs[kTok];
+        // of token j: c as in the forward; to_x = s i, what lam is multiplied with in d_x; to_r, first sg a u / s, then sg (h_{t-1} - a u / s); sg; to_a = d_a_decay / (d_log_a sg).
+        // In the stash: s u (1 - i), what lam is multiplied with in d_a_in.
+        float2 c[kTok], to_x[kTok], to_r[kTok], sg[kTok], to_a[kTok];
         unsigned far = 0;  // two bits a token
         float2 hh = dup(0.0f), pp = dup(1.0f), v = dup(0.0f);
-        const bool plain = near && have == kTok && !starts;  // all tokens are there, none is a start, no decay is far from 1
-        auto scale = [&](auto is_plain, int j) {             // s of token j
-            constexpr bool PLAIN = decltype(is_plain)::value;
-            if (!UNIT || (!PLAIN && (starts >> j & 1))) return dup(1.0f);
-            float2 one = mul2(make_float2(-c[j].x, -c[j].y), add2(c[j], dup(2.0f)));
-            if (!PLAIN && (far >> 2 * j & 1)) one.x = fmaf(-c[j].x, c[j].x, 1.0f);
-            if (!PLAIN && (far >> 2 * j & 2)) one.y = fmaf(-c[j].y, c[j].y, 1.0f);
-            return mul2(one, rs[j]);
-        };
+        const bool plain = near && have == kTok && !starts;  // all tokens and channels are there, none is a start, no decay is far from 1
         auto gather = [&](auto is_plain) {
             constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
             for (int j = 0; j < kTok; ++j) {
-                c[j] = wr[j] = wi[j] = rs[j] = dup(0.0f);
+                if (!PLAIN) c[j] = to_x[j] = to_r[j] = sg[j] = to_a[j] = dup(0.0f);
                 if (!PLAIN && j >= have) continue;
-                float2 u = input<0>(rows, j, lane);
-                wr[j] = smaller_part2<IO>(input<1>(rows, j, lane));
+                const float2 x = input<0>(rows, j, lane), er = exp_neg<IO>(input<1>(rows, j, lane));
+                float2 ig = dup(1.0f), shut = dup(0.0f);
                 if constexpr (GATE) {
-                    wi[j] = smaller_part2<IO>(input<2>(rows, j, lane));
-                    u = mul2(u, open2(wi[j]));
+                    const float2 eg = exp_neg<IO>(input<2>(rows, j, lane));
+                    ig = reciprocal<IO>(add2(eg, dup(1.0f)));
+                    shut = mul2(eg, ig);
                 }
-                const Decay d = decay<IO, UNIT, PLAIN>(open2(wr[j]), rate);
+                sg[j] = reciprocal<IO>(add2(er, dup(1.0f)));
+                to_a[j] = mul2(rate, mul2(er, sg[j]));
+                const Decay d = decay<IO, UNIT, PLAIN>(sg[j], rate);
                 c[j] = d.c;
                 if (!PLAIN) far |= d.far << 2 * j;
-                if (UNIT) rs[j] = inv_sqrt2<IO>(d.one);
-                if (!PLAIN && (starts >> j & 1)) {
-                    hh = u;
-                    pp = dup(0.0f);
-                    continue;
+                const bool start = !PLAIN && (starts >> j & 1);
+                to_x[j] = ig;
+                to_r[j] = dup(0.0f);
+                if (UNIT && !start) {
+                    const float2 rs = inv_sqrt2<PLAIN>(d.one);
+                    to_r[j] = mul2(sg[j], fade<PLAIN>(mul2(mul2(x, ig), rs), d.c, d.far));
+                    to_x[j] = mul2(ig, mul2(d.one, rs));
                 }
-                if (UNIT) u = mul2(u, mul2(d.one, rs[j]));
-                hh = add2(fade<PLAIN>(hh, d.c, d.far), u);
-                pp = fade<PLAIN>(pp, d.c, d.far);
+                const float2 bj = mul2(to_x[j], x);
+                if (GATE) meet.stash[warp][j][lane] = mul2(bj, shut);
+                hh = start ? bj : add2(fade<PLAIN>(hh, d.c, d.far), bj);
+                pp = start ? dup(0.0f) : fade<PLAIN>(pp, d.c, d.far);
             }
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {
@@ -144,75 +152,66 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
         meet.ends[slot][warp][lane] = v;
         __syncthreads();
-        float2 P_in = dup(1.0f), own = parts == 1 ? carry : dup(0.0f), P_all = P_in, all = own;  // the warps after this one; all of them
-#pragma unroll
-        for (int w = kWarps - 1; w >= 0; --w) {
-            const float4 q = meet.runs[slot][w][lane];
-            if (w == warp) {
-                P_in = P_all;
-                own = all;
-            }
-            if (w < warp) continue;
-            all = through2(make_float2(q.x, q.y), all, meet.ends[slot][w][lane]);
-            P_all = mul2(P_all, make_float2(q.x, q.y));
-        }
-        for (int w = warp - 1; w >= 0; --w) {
-            const float4 q = meet.runs[slot][w][lane];
-            all = through2(make_float2(q.x, q.y), all, meet.ends[slot][w][lane]);
-            P_all = mul2(P_all, make_float2(q.x, q.y));
-        }
+        float2 in = meet.carry[slot ^ 1][lane];  // what the tokens after the turn's hand on
         for (int w = 0; w < warp; ++w) {
             const float4 q = meet.runs[slot][w][lane];
             state = through2(make_float2(q.x, q.y), state, make_float2(q.z, q.w));
         }
-        float2 in = own;
         if (parts == 1) {
-            carry = all;
-        } else {
-            if (warp < parts) put_remote(&meet.parts[slot][part][lane], warp, make_float4(P_all.x, P_all.y, all.x, all.y));
-            cluster_sync();
-            for (int k = parts - 1; k >= 0; --k) {
-                const float4 q = meet.parts[slot][k][lane];
-                if (k == part) in = through2(P_in, carry, own);
-                carry = through2(make_float2(q.x, q.y), carry, make_float2(q.z, q.w));
+            for (int w = kWarps - 1; w > warp; --w) {
+                const float4 q = meet.runs[slot][w][lane];
+                in = through2(make_float2(q.x, q.y), in, meet.ends[slot][w][lane]);
             }
+            if (warp == ender) meet.carry[slot][lane] = end = through2(pp, in, v);
+        } else {
+            float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps after this one
+            for (int w = kWarps - 1; w > warp; --w) {
+                const float4 q = meet.runs[slot][w][lane];
+                own = through2(make_float2(q.x, q.y), own, meet.ends[slot][w][lane]);
+                P_in = both(P_in, make_float2(q.x, q.y));
+            }
+            if (warp == 0) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, v));
+            if (met) met = await_parts(meet.meeting, slot, parity);
+            for (int k = parts - 1; k > part; --k) {
+                const float4 q = meet.meeting.parts[slot][k][lane];
+                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+            }
+            if (warp == ender) {
+                end = in;
+                for (int k = part; k >= 0; --k) {
+                    const float4 q = meet.meeting.parts[slot][k][lane];
+                    end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
+                }
+                if (!met) end = dup(__uint_as_float(0x7fc00000u));
+                meet.carry[slot][lane] = end;
+            }
+            in = through2(P_in, in, own);
         }
         auto spread = [&](auto is_plain) {
             constexpr bool PLAIN = decltype(is_plain)::value;
-            float2 hp[kTok];  // the state before a token
 #pragma unroll
             for (int j = 0; j < kTok; ++j) {
-                hp[j] = state;
                 if (!PLAIN && j >= have) continue;
-                float2 u = input<0>(rows, j, lane);
-                if (GATE) u = mul2(u, open2(wi[j]));
-                if (!PLAIN && (starts >> j & 1)) state = u;
-                else state = add2(fade<PLAIN>(state, c[j], far >> 2 * j), mul2(u, scale(is_plain, j)));
+                const bool start = !PLAIN && (starts >> j & 1);
+                const float2 bj = mul2(to_x[j], input<0>(rows, j, lane));
+                to_r[j] = start ? dup(0.0f) : UNIT ? fma2(to_r[j], dup(-1.0f), mul2(sg[j], state)) : mul2(sg[j], state);
+                state = start ? bj : add2(fade<PLAIN>(state, c[j], far >> 2 * j), bj);
             }
             const int64_t at = seq + (int64_t)t0 * D + c0;
+            const int m = PLAIN ? 2 : n;
+            const bool two = PLAIN || pair;
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {
                 if (!PLAIN && j >= have) continue;
                 const bool start = !PLAIN && (starts >> j & 1);
+                const int64_t to = at + j * (int64_t)D;
                 in = add2(in, row2<IO>(rows.d_h[j], lane));
-                const float2 ls = mul2(in, scale(is_plain, j)), oi = open2(wi[j]);
-                float2 u = input<0>(rows, j, lane);
-                if (GATE) u = mul2(u, oi);
-                store2<IO>(ba.d_x, at + (int64_t)j * D, n, pair, GATE ? mul2(ls, oi) : ls);
-                if (GATE) store2<IO>(ba.d_g, at + (int64_t)j * D, n, pair, mul2(mul2(ls, u), closed2(wi[j])));
+                store2<IO>(ba.d_x, to, m, two, mul2(in, to_x[j]));
+                if (GATE) store2<IO>(ba.d_g, to, m, two, mul2(in, meet.stash[warp][j][lane]));
                 in = start ? dup(0.0f) : fade<PLAIN>(in, c[j], far >> 2 * j);  // a lam
-                float2 dl = dup(0.0f);                                        // d_log_a sg
-                const float2 sg = open2(wr[j]);
-                if (!start) {
-                    float2 to = hp[j];
-                    if (UNIT) {
-                        const float2 ur = mul2(u, rs[j]), au = fade<PLAIN>(ur, c[j], far >> 2 * j);
-                        to = add2(to, make_float2(-au.x, -au.y));
-                    }
-                    dl = mul2(mul2(in, to), sg);
-                    sum = add2(sum, make_float2(-dl.x, -dl.y));
-                }
-                store2<IO>(ba.d_r, at + (int64_t)j * D, n, pair, mul2(mul2(dl, rate), closed2(wr[j])));
+                const float2 dl = start ? dup(0.0f) : mul2(in, to_r[j]);      // d_log_a sg
+                sum = fma2(dl, dup(-1.0f), sum);
+                store2<IO>(ba.d_r, to, m, two, mul2(dl, to_a[j]));
             }
         };
         if (plain) spread(std::true_type{});
@@ -220,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         __syncwarp();
         load((turn - 2) * parts + part, slot);
     }
-    if (part == 0 && warp == 0) store2<float>(ba.dh_init, b * D + c0, n, false, carry);
+    if (part == 0 && warp == ender) store2<float>(ba.dh_init, b * D + c0, n, false, end);
     __syncthreads();
     meet.ends[0][warp][lane] = sum;
     __syncthreads();

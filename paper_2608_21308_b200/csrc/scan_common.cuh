@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "scan.h"
+#include "sm100.cuh"
 
 namespace e2ttt {
 namespace scan {
@@ -51,43 +52,35 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// 1 / (1 + exp(-x)); with bf16 I/O the special function unit's exponential and reciprocal (2^-22 each) are enough
-template <typename IO> __device__ __forceinline__ float2 sigmoid2(float2 x) {
+// 1 + exp(-x), for the sigmoid 1 / (1 + exp(-x)) and what it leaves of 1, exp(-x) / (1 + exp(-x)): an open gate's rest is computed, not subtracted.  The exponential is capped at 2^62
+// (a logit of -43 or less): the product of two stays finite, and 1 - a^2 above 0 at any ordinary rate.  With bf16 I/O the special function unit's 2^-22 is enough.
+template <typename IO> __device__ __forceinline__ float2 exp_neg(float2 x) {
+    float2 e;
     if constexpr (sizeof(IO) == 4) {
-        return make_float2(__frcp_rn(1.0f + expf(-x.x)), __frcp_rn(1.0f + expf(-x.y)));
+        e = make_float2(expf(-x.x), expf(-x.y));
     } else {
         const float2 t = mul2(x, dup(-kLog2e));
-        const float2 e = add2(make_float2(ex2(t.x), ex2(t.y)), dup(1.0f));
-        return make_float2(rcp(e.x), rcp(e.y));
+        e = make_float2(ex2(t.x), ex2(t.y));
     }
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(0x1p62f));  // a NaN stays one
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(0x1p62f));
+    return e;
 }
-
-// The smaller of sigmoid(x) and 1 - sigmoid(x), e / (1 + e) with e = exp(-|x|); its sign says which: positive where x > 0 and it is 1 - sigmoid(x).  The reverse pass needs
-// both, and what an open gate leaves of 1 would be lost in a difference.
-template <typename IO> __device__ __forceinline__ float smaller_part(float x) {
+template <typename IO> __device__ __forceinline__ float2 reciprocal(float2 x) {
+    if constexpr (sizeof(IO) == 4) return make_float2(__frcp_rn(x.x), __frcp_rn(x.y));
+    return make_float2(rcp(x.x), rcp(x.y));
+}
+template <typename IO> __device__ __forceinline__ float2 sigmoid2(float2 x) { return reciprocal<IO>(add2(exp_neg<IO>(x), dup(1.0f))); }
+// the sigmoids of two pairs; with bf16 I/O one reciprocal of both denominators: the special function unit bounds the forward otherwise
+template <typename IO> __device__ __forceinline__ void sigmoids(float2 x, float2 y, float2& sx, float2& sy) {
     if constexpr (sizeof(IO) == 4) {
-        const float e = expf(-fabsf(x));
-        return copysignf(e * __frcp_rn(1.0f + e), x);
+        sx = sigmoid2<IO>(x);
+        sy = sigmoid2<IO>(y);
     } else {
-        const float e = ex2(fabsf(x) * -kLog2e);
-        return copysignf(e * rcp(1.0f + e), x);
+        const float2 p = add2(exp_neg<IO>(x), dup(1.0f)), q = add2(exp_neg<IO>(y), dup(1.0f)), r = reciprocal<IO>(mul2(p, q));
+        sx = mul2(q, r);
+        sy = mul2(p, r);
     }
-}
-__device__ __forceinline__ float open_part(float w) { return signbit(w) ? -w : 1.0f - w; }    // sigmoid(x)
-__device__ __forceinline__ float closed_part(float w) { return signbit(w) ? 1.0f + w : w; }   // 1 - sigmoid(x)
-template <typename IO> __device__ __forceinline__ float2 smaller_part2(float2 x) { return make_float2(smaller_part<IO>(x.x), smaller_part<IO>(x.y)); }
-__device__ __forceinline__ float2 open2(float2 w) { return make_float2(open_part(w.x), open_part(w.y)); }
-__device__ __forceinline__ float2 closed2(float2 w) { return make_float2(closed_part(w.x), closed_part(w.y)); }
-
-// exp(y) - 1 for -1/4 <= y <= 0: the series to y^7 / 7! (2e-9 of the result)
-__device__ __forceinline__ float2 expm1_near(float2 y) {
-    float2 p = fma2(y, dup(1.0f / 5040.0f), dup(1.0f / 720.0f));
-    p = fma2(p, y, dup(1.0f / 120.0f));
-    p = fma2(p, y, dup(1.0f / 24.0f));
-    p = fma2(p, y, dup(1.0f / 6.0f));
-    p = fma2(p, y, dup(0.5f));
-    p = fma2(p, y, dup(1.0f));
-    return mul2(p, y);
 }
 
 // A token's decay for two channels.  Near 1, where a's own rounding is what a long memory adds up, it is kept as c = a - 1; far from it (log a below -1/4), where c's rounding
@@ -96,13 +89,21 @@ struct Decay {
     float2 c, one;
     unsigned far;  // bit 0: the first channel's c is a, bit 1: the second's
 };
-// sg = sigmoid(a_decay).  NEAR: the rates are at most 1/4, so that no decay is far from 1.
+// Whether a rate's decays are all near 1, and none of them 1
+__device__ __forceinline__ bool near_rate(float rate) { return rate >= 1e-10f && rate <= 0.25f; }
+// sg = sigmoid(a_decay).  NEAR: near_rate of both channels.
 template <typename IO, bool UNIT, bool NEAR> __device__ __forceinline__ Decay decay(float2 sg, float2 neg_rate) {
     const float2 y = mul2(neg_rate, sg);
     Decay d;
-    d.c = expm1_near(y);
+    // exp(y) - 1 for -1/4 <= y <= 0: the series to y^6 / 6! (5e-8 of the result at the end of the range)
+    float2 p = fma2(y, dup(1.0f / 720.0f), dup(1.0f / 120.0f));
+    p = fma2(p, y, dup(1.0f / 24.0f));
+    p = fma2(p, y, dup(1.0f / 6.0f));
+    p = fma2(p, y, dup(0.5f));
+    p = fma2(p, y, dup(1.0f));
+    d.c = mul2(p, y);
     d.far = 0;
-    if (UNIT) d.one = mul2(make_float2(-d.c.x, -d.c.y), add2(d.c, dup(2.0f)));
+    if (UNIT) d.one = mul2(d.c, fma2(d.c, dup(-1.0f), dup(-2.0f)));
     if constexpr (!NEAR) {
         float2 e;
         if constexpr (sizeof(IO) == 4) e = make_float2(expf(y.x), expf(y.y));
@@ -125,19 +126,18 @@ template <bool NEAR> __device__ __forceinline__ float2 fade(float2 h, float2 c, 
     if constexpr (NEAR) return fma2(h, c, h);
     return fma2(h, c, make_float2(far & 1 ? 0.0f : h.x, far & 2 ? 0.0f : h.y));
 }
-
-// 1 / sqrt(x), 0 for 0
-template <typename IO> __device__ __forceinline__ float inv_sqrt(float x) {
-    float y;
-    if constexpr (sizeof(IO) == 4) {
-        y = rsqrtf(x);
-        y = y * fmaf(-0.5f * x * y, y, 1.5f);  // Newton's step: 2^-23
-    } else {
-        y = rsqrt_fast(x);
-    }
-    return x > 1e-37f ? y : 0.0f;
+// sqrt(x), and 1 / sqrt(x) with 0 for 0; both good to 2^-22.  NEAR: x is not 0.
+__device__ __forceinline__ float2 sqrt2(float2 x) {
+    float2 y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+    return y;
 }
-template <typename IO> __device__ __forceinline__ float2 inv_sqrt2(float2 x) { return make_float2(inv_sqrt<IO>(x.x), inv_sqrt<IO>(x.y)); }
+template <bool NEAR> __device__ __forceinline__ float2 inv_sqrt2(float2 x) {
+    const float2 y = make_float2(rsqrt_fast(x.x), rsqrt_fast(x.y));
+    if constexpr (NEAR) return y;
+    return make_float2(x.x > 1e-37f ? y.x : 0.0f, x.y > 1e-37f ? y.y : 0.0f);
+}
 
 template <typename IO> __device__ __forceinline__ float to_f32(IO x);
 template <> __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -196,6 +196,18 @@ inline int reads_by(int D, bool f32, uintptr_t all) {
 
 // ROWS tokens of `src` from row t on, channels c .. c + 63, as far as there are tokens (L) and channels (D); `at` is where token 0 of the sequence starts
 template <typename IO, int ROWS> __device__ __forceinline__ void copy_rows(IO* dst, const IO* src, int64_t at, int t, int L, int c, int D, int by, int lane) {
+    if (by == kBy16 && c + kScanCh <= D && t + ROWS <= L) {  // all there
+        constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;
+        const int row = lane / PER, ch = lane % PER * V;
+        const IO* p = src + (at + (int64_t)t * D + c) + (row * (int64_t)D + ch);
+        IO* q = dst + row * kScanCh + ch;
+#pragma unroll
+        for (int i = 0; i < ROWS; i += STEP) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(q + i * kScanCh)), "l"(p) : "memory");
+            p += STEP * (int64_t)D;
+        }
+        return;
+    }
     if (by == kBy16) {
         constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;  // pieces of a row; rows a warp copies at once
         const int row = lane / PER, ch = lane % PER * V;
@@ -239,20 +251,44 @@ template <typename IO> __device__ __forceinline__ float2 row2(const IO* row, int
 __device__ __forceinline__ float through(float P, float in, float own) { return P == 0.0f ? own : fmaf(P, in, own); }
 __device__ __forceinline__ float2 through2(float2 P, float2 in, float2 own) { return make_float2(through(P.x, in.x, own.x), through(P.y, in.y, own.y)); }
 
-// ---- CTAs of a cluster: the parts of a sequence's channels along its tokens
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
+// P of two runs, the second of which may have a start in it
+__device__ __forceinline__ float2 both(float2 P, float2 next) { return make_float2(next.x == 0.0f ? 0.0f : P.x * next.x, next.y == 0.0f ? 0.0f : P.y * next.y); }
+
+// ---- CTAs of a cluster: the parts of a sequence's channels along its tokens.  Every turn each leaves its tile's run with all of them by asynchronous stores, which count
+// themselves on the receiver's barrier (a release of the CTA's global stores, as a cluster's barrier takes, would wait for all of them).  A buffer is used again two turns later: a CTA
+// sends there only after all others have sent what follows it, which they do when their warps have read it.
+struct Meeting {
+    float4 parts[2][8][32];  // P and what a tile makes of nothing, of every CTA
+    uint64_t full[2];
+};
+__device__ __forceinline__ void meeting_init(Meeting& m) {
+    if (threadIdx.x == 0) {
+        sm100::mbar_init(&m.full[0], 1);
+        sm100::mbar_init(&m.full[1], 1);
+        sm100::fence_mbar_init();
+    }
+    sm100::cluster_sync();  // the others' shared memory is there
 }
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// writes v where CTA `rank` of the cluster has what lies at `here`
-__device__ __forceinline__ void put_remote(float4* here, uint32_t rank, float4 v) {
+__device__ __forceinline__ uint32_t in_cta(uint32_t at, uint32_t rank) {
     uint32_t there;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_at(here)), "r"(rank));
-    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    return there;
+}
+// one warp sends
+__device__ __forceinline__ void send_part(Meeting& m, int slot, int part, int parts, int lane, float2 P, float2 own) {
+    if (lane == 0) sm100::mbar_expect_tx(&m.full[slot], parts * 512);
+    __syncwarp();
+    const uint32_t data = smem_at(&m.parts[slot][part][lane]), bar = smem_at(&m.full[slot]);
+    for (int k = 0; k < parts; ++k)
+        sm100::st_async_v4(in_cta(data, k), __float_as_uint(P.x), __float_as_uint(P.y), __float_as_uint(own.x), __float_as_uint(own.y), in_cta(bar, k));
+}
+// Bounded: the stores cannot fail short of a device fault.  False once a wait gave up; what is computed from then on is made NaN.
+__device__ __forceinline__ bool await_parts(Meeting& m, int slot, uint32_t parity) {
+    if (sm100::mbar_try_wait<true>(&m.full[slot], parity)) return true;
+    const long long t0 = clock64();
+    while (!sm100::mbar_try_wait<true>(&m.full[slot], parity))
+        if (clock64() - t0 > sm100::kWaitCycles) return false;
+    return true;
 }
 
 }  // namespace scan

@@ -15,10 +15,11 @@ using namespace scan;
 constexpr int kStages = 2;
 template <typename IO> constexpr int kTokOf = sizeof(IO) == 2 ? 16 : 8;
 
-// what the runs of a tile and the parts of a cluster leave for one another, twice in turn
+// what the warps of a tile and the parts of a cluster leave for one another, twice in turn
 struct Meet {
     float4 runs[2][kWarps][32];  // P and h' of a warp's tokens
-    float4 parts[2][8][32];      // of a CTA's tile
+    float2 carry[2][32];         // the state after a turn's tokens
+    Meeting meeting;
 };
 
 // The 8-bit form of a warp's rows of one tensor: a lane takes 16 bytes, an aligned group of lanes a block.
@@ -51,17 +52,20 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     constexpr int TOK = kTokOf<IO>, TILE = TOK * kWarps, NT = GATE ? 3 : 2;
     extern __shared__ __align__(16) char smem[];
     Meet& meet = *reinterpret_cast<Meet*>(smem);
-    const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
     const int64_t blocks = a.s.blocks(), spans = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
+    const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
     IO* ring = reinterpret_cast<IO*>(smem + sizeof(Meet)) + warp * (kStages * NT * TOK * kScanCh);
     const int64_t seq = b * L * (int64_t)D;
     float2 rate = load2<float>(a.rate, c0, n, false);
-    const bool near = __syncthreads_and(rate.x <= 0.25f && rate.y <= 0.25f);
+    const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
     rate = make_float2(-rate.x, -rate.y);
-    float2 carry = a.h_init ? load2<float>(a.h_init, b * D + c0, n, false) : dup(0.0f);
-    if (parts > 1) cluster_sync();  // the others' shared memory is there
+    float2 end = a.h_init ? load2<float>(a.h_init, b * D + c0, n, false) : dup(0.0f);  // the state after the last turn, in one warp
+    const int ender = parts == 1 ? kWarps - 1 : 0;
+    if (warp == ender) meet.carry[1][lane] = end;
+    if (parts > 1) meeting_init(meet.meeting);
     const int64_t tiles = ((int64_t)L + TILE - 1) / TILE;
     unsigned next_first = 0;
     auto load = [&](int64_t tile, int slot) {
@@ -80,8 +84,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     unsigned byte0 = next_first;
     load(part + parts, 1);
     int slot = 0;
+    uint32_t parity = 0;
+    bool met = true;
     // every CTA of a cluster takes every turn: its part of the last one may be empty
-    for (int64_t turn = 0; turn * parts < tiles; ++turn, slot ^= 1) {
+    for (int64_t turn = 0; turn * parts < tiles; ++turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
         const int t0 = (int)min(tile * TILE + warp * TOK, (int64_t)L), have = min(TOK, L - t0);
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
@@ -90,19 +96,26 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         copy_wait<kStages - 1>();
         __syncwarp();
         float2 h[TOK], P[TOK], hh = dup(0.0f), pp = dup(1.0f);
-        auto walk = [&](auto plain) {  // plain: all tokens are there, none is a start, no decay is far from 1
-            constexpr bool PLAIN = decltype(plain)::value;
+        const bool plain = near && have == TOK && !starts;  // all tokens and channels are there, none is a start, no decay is far from 1
+        auto walk = [&](auto is_plain) {
+            constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
                 if (PLAIN || j < have) {
-                    float2 u = row2(rows + j * kScanCh, lane);
-                    const Decay d = decay<IO, UNIT, PLAIN>(sigmoid2<IO>(row2(rows + (TOK + j) * kScanCh, lane)), rate);
-                    if (GATE) u = mul2(u, sigmoid2<IO>(row2(rows + (2 * TOK + j) * kScanCh, lane)));
+                    float2 u = row2(rows + j * kScanCh, lane), sg;
+                    if constexpr (GATE) {
+                        float2 ig;
+                        sigmoids<IO>(row2(rows + (TOK + j) * kScanCh, lane), row2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
+                        u = mul2(u, ig);
+                    } else {
+                        sg = sigmoid2<IO>(row2(rows + (TOK + j) * kScanCh, lane));
+                    }
+                    const Decay d = decay<IO, UNIT, PLAIN>(sg, rate);
                     if (!PLAIN && (starts >> j & 1)) {
                         hh = u;
                         pp = dup(0.0f);
                     } else {
-                        if (UNIT) u = mul2(u, mul2(d.one, inv_sqrt2<IO>(d.one)));
+                        if (UNIT) u = mul2(u, sqrt2(d.one));
                         hh = add2(fade<PLAIN>(hh, d.c, d.far), u);
                         pp = fade<PLAIN>(pp, d.c, d.far);
                     }
@@ -111,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                 P[j] = pp;
             }
         };
-        if (near && have == TOK && !starts) walk(std::true_type{});
+        if (plain) walk(std::true_type{});
         else walk(std::false_type{});
         if (PACK && have > 0) {
             const int64_t row = unit * spans * kScanSpan + t0;
@@ -123,40 +136,51 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         load((turn + 2) * parts + part, slot);
         meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
         __syncthreads();
-        float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps before this one
-        if (parts == 1) own = carry;
-        float2 P_all = P_in, all = own;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float4 q = meet.runs[slot][w][lane];
-            if (w == warp) {
-                P_in = P_all;
-                own = all;
-            }
-            all = through2(make_float2(q.x, q.y), all, make_float2(q.z, q.w));
-            P_all = mul2(P_all, make_float2(q.x, q.y));
-        }
-        float2 in = own;
+        const float2 before = meet.carry[slot ^ 1][lane];  // the state before the turn's tokens
+        float2 in = before;
         if (parts == 1) {
-            carry = all;
-        } else {
-            if (warp < parts) put_remote(&meet.parts[slot][part][lane], warp, make_float4(P_all.x, P_all.y, all.x, all.y));
-            cluster_sync();
-            for (int k = 0; k < parts; ++k) {
-                const float4 q = meet.parts[slot][k][lane];
-                if (k == part) in = through2(P_in, carry, own);
-                carry = through2(make_float2(q.x, q.y), carry, make_float2(q.z, q.w));
+            for (int w = 0; w < warp; ++w) {
+                const float4 q = meet.runs[slot][w][lane];
+                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
             }
+            if (warp == ender) meet.carry[slot][lane] = end = through2(pp, in, hh);
+        } else {
+            float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps before this one
+            for (int w = 0; w < warp; ++w) {
+                const float4 q = meet.runs[slot][w][lane];
+                own = through2(make_float2(q.x, q.y), own, make_float2(q.z, q.w));
+                P_in = both(P_in, make_float2(q.x, q.y));
+            }
+            if (warp == kWarps - 1) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, hh));
+            if (met) met = await_parts(meet.meeting, slot, parity);
+            for (int k = 0; k < part; ++k) {
+                const float4 q = meet.meeting.parts[slot][k][lane];
+                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+            }
+            if (warp == ender) {
+                end = in;
+                for (int k = part; k < parts; ++k) {
+                    const float4 q = meet.meeting.parts[slot][k][lane];
+                    end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
+                }
+                if (!met) end = dup(__uint_as_float(0x7fc00000u));
+                meet.carry[slot][lane] = end;
+            }
+            in = through2(P_in, in, own);
         }
         if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
-        if (a.h) {
-            const int64_t at = seq + (int64_t)t0 * D + c0;
+        if (!a.h) continue;
+        const int64_t at = seq + (int64_t)t0 * D + c0;
+        if (plain) {
+#pragma unroll
+            for (int j = 0; j < TOK; ++j) store2<IO>(a.h, at + j * (int64_t)D, 2, true, fma2(P[j], in, h[j]));
+        } else {
 #pragma unroll
             for (int j = 0; j < TOK; ++j)
-                if (j < have) store2<IO>(a.h, at + (int64_t)j * D, n, pair, through2(P[j], in, h[j]));
+                if (j < have) store2<IO>(a.h, at + j * (int64_t)D, n, pair, through2(P[j], in, h[j]));
         }
     }
-    if (a.h_final && part == 0 && warp == 0) store2<float>(a.h_final, b * D + c0, n, false, carry);
+    if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
     copy_wait<0>();
 }
 

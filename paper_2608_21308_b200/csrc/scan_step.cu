@@ -25,7 +25,7 @@ template <typename IO, bool GATE, bool UNIT> __global__ void __launch_bounds__(k
         if (a.starts && a.starts[(int64_t)b * a.s.L + t]) {
             h = u;
         } else {
-            if (UNIT) u = mul2(u, mul2(d.one, inv_sqrt2<IO>(d.one)));
+            if (UNIT) u = mul2(u, sqrt2(d.one));
             h = add2(fade<false>(h, d.c, d.far), u);
         }
         store2<IO>(a.h, at, n, pair, h);
