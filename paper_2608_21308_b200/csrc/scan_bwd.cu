@@ -9,6 +9,7 @@
 #include "api_checks.h"
 #include "pack8.cuh"
 #include "scan_common.cuh"
+#include "scan_map.h"
 
 namespace e2ttt {
 namespace {
@@ -21,37 +22,45 @@ struct Meet {
     float4 runs[2][kWarps][32];        // P and h' of a warp's tokens
     float2 ends[2][kWarps][32];        // v' of a warp's tokens
     float2 carry[2][32];               // the adjoint that a turn's tokens hand on
+    uint64_t full[kWarps][kStages];
     Meeting meeting;
     float2 stash[kWarps][kTok][32];    // a thread's own, for want of registers
 };
 
+constexpr int kMeet = (sizeof(Meet) + 127) / 128 * 128;
+
 // what a warp has under way of a tile
-template <typename IO, int NT, bool PACK> struct Rows {
+template <typename IO, int NT, bool PACK> struct alignas(128) Rows {
     IO in[NT][kTok][kScanCh];
     IO d_h[kTok][kScanCh];
+    static constexpr int kBytes = (NT + 1) * kTok * kScanCh * (int)sizeof(IO);
 };
-template <typename IO, int NT> struct Rows<IO, NT, true> {
+template <typename IO, int NT> struct alignas(128) Rows<IO, NT, true> {
     uint8_t codes[NT][kTok][kScanCh];
     IO d_h[kTok][kScanCh];
-    uint8_t scales[NT][kTok][2];
+    alignas(16) uint8_t scales[NT][kTok][2];
+    static constexpr int kBytes = NT * kTok * (kScanCh + 2) + kTok * kScanCh * (int)sizeof(IO);
 };
 
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, false>& r, int j, int lane) { return row2<IO>(r.in[K][j], lane); }
+template <int K, typename IO, int NT> __device__ __forceinline__ float2 logit(const Rows<IO, NT, false>& r, int j, int lane) { return logit2<IO>(r.in[K][j], lane); }
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, true>& r, int j, int lane) {
     const uint32_t w = reinterpret_cast<const uint16_t*>(r.codes[K][j])[lane];
     // a block that is not finite has codes of 0 and an infinite scale: NaN
     return mul2(make_float2(pack8::number<0>(w), pack8::number<1>(w)), dup(__uint_as_float((uint32_t)r.scales[K][j][lane >> 4] << 23)));
 }
 
+template <int K, typename IO, int NT> __device__ __forceinline__ float2 logit(const Rows<IO, NT, true>& r, int j, int lane) { return capped(input<K>(r, j, lane)); }
+
 template <typename IO, bool GATE, bool UNIT, bool PACK>
-__global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_kernel(const ScanBwdArgs ba, const int by, const bool pair, const int parts) {
+__global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_kernel(const ScanBwdArgs ba, const __grid_constant__ ScanMaps maps, const int by, const bool pair, const int parts) {
     constexpr int NT = GATE ? 3 : 2;
     using R = Rows<IO, NT, PACK>;
-    extern __shared__ __align__(16) char smem[];
+    extern __shared__ __align__(128) char smem[];
     Meet& meet = *reinterpret_cast<Meet*>(smem);
     const ScanArgs& a = ba.f;
     const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
-    R* ring = reinterpret_cast<R*>(smem + sizeof(Meet)) + warp * kStages;
+    R* ring = reinterpret_cast<R*>(smem + kMeet) + warp * kStages;
     const int64_t blocks = a.s.blocks(), tiles = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
@@ -63,36 +72,58 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     float2 end = ba.dh_final ? load2<float>(ba.dh_final, b * D + c0, n, false) : dup(0.0f), sum = dup(0.0f);  // end: what the last turn hands on, in one warp
     const int ender = parts == 1 ? 0 : kWarps - 1;
     if (warp == ender) meet.carry[1][lane] = end;
+    uint64_t* full = meet.full[warp];
+    if (by == kByTile && lane == 0) {
+        for (int i = 0; i < kStages; ++i) sm100::mbar_init(&full[i], 1);
+        sm100::fence_mbar_init();
+    }
+    __syncwarp();
     if (parts > 1) meeting_init(meet.meeting);
     unsigned next_first = 0;
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
-        if (tile >= 0 && tile < tiles) {
+        if (tile >= 0 && tile * kTile + warp * kTok < L) {
             const int t = (int)(tile * kTile) + warp * kTok;
             R& to = ring[slot];
-            if constexpr (PACK) {
-                const int64_t row = unit * tiles * kScanSpan + t;
+            const int64_t row = unit * tiles * kScanSpan + t;
+            if (by == kByTile) {
+                if (lane == 0) {
+                    sm100::mbar_expect_tx(&full[slot], R::kBytes);
 #pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    copy16(&to.codes[k][0][0] + lane * 16, a.codes + k * a.code_step + row * kScanCh + lane * 16, true);
-                    if (lane == k) copy16(&to.scales[k][0][0], a.scales + k * a.scale_step + row * 2, true);
+                    for (int k = 0; k < NT; ++k) {
+                        if constexpr (PACK) {
+                            bulk_load(to.codes[k][0], a.codes + k * a.code_step + row * kScanCh, kTok * kScanCh, &full[slot]);
+                            bulk_load(to.scales[k][0], a.scales + k * a.scale_step + row * 2, kTok * 2, &full[slot]);
+                        } else {
+                            tile_load(to.in[k][0], &maps.m[k], first, t, (int)b, &full[slot]);
+                        }
+                    }
+                    tile_load(to.d_h[0], &maps.m[3], first, t, (int)b, &full[slot]);
                 }
             } else {
-                copy_rows<IO, kTok>(to.in[0][0], static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
-                copy_rows<IO, kTok>(to.in[1][0], static_cast<const IO*>(a.r), seq, t, L, first, D, by, lane);
-                if constexpr (GATE) copy_rows<IO, kTok>(to.in[2][0], static_cast<const IO*>(a.g), seq, t, L, first, D, by, lane);
+                if constexpr (PACK) {
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) {
+                        copy16(&to.codes[k][0][0] + lane * 16, a.codes + k * a.code_step + row * kScanCh + lane * 16);
+                        if (lane == k) copy16(&to.scales[k][0][0], a.scales + k * a.scale_step + row * 2);
+                    }
+                } else {
+                    copy_rows<IO, kTok>(to.in[0][0], static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
+                    copy_rows<IO, kTok>(to.in[1][0], static_cast<const IO*>(a.r), seq, t, L, first, D, by, lane);
+                    if constexpr (GATE) copy_rows<IO, kTok>(to.in[2][0], static_cast<const IO*>(a.g), seq, t, L, first, D, by, lane);
+                }
+                copy_rows<IO, kTok>(to.d_h[0], static_cast<const IO*>(ba.d_h), seq, t, L, first, D, by, lane);
             }
-            copy_rows<IO, kTok>(to.d_h[0], static_cast<const IO*>(ba.d_h), seq, t, L, first, D, by, lane);
             if (a.starts && lane < kTok && t + lane < L) next_first = a.starts[b * L + t + lane];
         }
-        copy_commit();
+        if (by != kByTile) copy_commit();
     };
     const int64_t turns = (tiles + parts - 1) / parts;
     load((turns - 1) * parts + part, 0);
     unsigned byte0 = next_first;
     load((turns - 2) * parts + part, 1);
     int slot = 0;
-    uint32_t parity = 0;
+    uint32_t parity = 0, taken = 0;  // taken: which phase a stage's barrier is in (a warp may have no tokens in the first turn)
     bool met = true;
     for (int64_t turn = turns - 1; turn >= 0; --turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
@@ -101,7 +132,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         byte0 = next_first;
         float2 state = tile < tiles ? load2<float>(a.states, (b * tiles + tile) * D + c0, n, false) : dup(0.0f);
         const R& rows = ring[slot];
-        copy_wait<kStages - 1>();
+        if (by != kByTile) {
+            copy_wait<kStages - 1>();
+        } else if (have > 0) {
+            if (met) met = await<false>(&full[slot], taken >> slot & 1);
+            taken ^= 1u << slot;
+        }
         __syncwarp();
         // of token j: c as in the forward; to_x = s i, what lam is multiplied with in d_x; to_r, first sg a u / s, then sg (h_{t-1} - a u / s); sg; to_a = d_a_decay / (d_log_a sg).
         // In the stash: s u (1 - i), what lam is multiplied with in d_a_in.
@@ -115,10 +151,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             for (int j = 0; j < kTok; ++j) {
                 if (!PLAIN) c[j] = to_x[j] = to_r[j] = sg[j] = to_a[j] = dup(0.0f);
                 if (!PLAIN && j >= have) continue;
-                const float2 x = input<0>(rows, j, lane), er = exp_neg<IO>(input<1>(rows, j, lane));
+                const float2 x = input<0>(rows, j, lane), er = exp_neg<IO>(logit<1>(rows, j, lane));
                 float2 ig = dup(1.0f), shut = dup(0.0f);
                 if constexpr (GATE) {
-                    const float2 eg = exp_neg<IO>(input<2>(rows, j, lane));
+                    const float2 eg = exp_neg<IO>(logit<2>(rows, j, lane));
                     ig = reciprocal<IO>(add2(eg, dup(1.0f)));
                     shut = mul2(eg, ig);
                 }
@@ -171,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 P_in = both(P_in, make_float2(q.x, q.y));
             }
             if (warp == 0) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, v));
-            if (met) met = await_parts(meet.meeting, slot, parity);
+            if (met) met = await<true>(&meet.meeting.full[slot], parity);
             for (int k = parts - 1; k > part; --k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
                 in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
@@ -182,11 +218,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                     const float4 q = meet.meeting.parts[slot][k][lane];
                     end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
                 }
-                if (!met) end = dup(__uint_as_float(0x7fc00000u));
                 meet.carry[slot][lane] = end;
             }
             in = through2(P_in, in, own);
         }
+        if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
         auto spread = [&](auto is_plain) {
             constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
@@ -223,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     __syncthreads();
     meet.ends[0][warp][lane] = sum;
     __syncthreads();
-    copy_wait<0>();
+    if (by != kByTile) copy_wait<0>();
     if (warp != 0) return;
     sum = meet.ends[0][0][lane];
     for (int w = 1; w < kWarps; ++w) sum = add2(sum, meet.ends[0][w][lane]);
@@ -253,7 +289,7 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwd
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.B * s.blocks() * parts));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(Meet) + kStages * kWarps * sizeof(Rows<IO, GATE ? 3 : 2, PACK>);
+    cfg.dynamicSmemBytes = kMeet + kStages * kWarps * sizeof(Rows<IO, GATE ? 3 : 2, PACK>);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -261,7 +297,11 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwd
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, kernel, b, by, pair, parts);
+    ScanMaps maps{};
+    const void* in[4] = {b.f.x, b.f.r, b.f.g, b.d_h};
+    for (int k = PACK ? 3 : 0; by == kByTile && k < 4; ++k)
+        if (in[k] && !scan_map(&maps.m[k], in[k], s, kTok)) by = kBy4;
+    e = cudaLaunchKernelEx(&cfg, kernel, b, maps, by, pair, parts);
     if (e != cudaSuccess) return (int)e;
     scan_rate_kernel<<<(s.D + 31) / 32, 256, 0, st>>>(b.part, b.d_rate, (int64_t)s.B * parts, s.D);
     return (int)cudaGetLastError();

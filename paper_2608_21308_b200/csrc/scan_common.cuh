@@ -52,19 +52,19 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// 1 + exp(-x), for the sigmoid 1 / (1 + exp(-x)) and what it leaves of 1, exp(-x) / (1 + exp(-x)): an open gate's rest is computed, not subtracted.  The exponential is capped at 2^62
-// (a logit of -43 or less): the product of two stays finite, and 1 - a^2 above 0 at any ordinary rate.  With bf16 I/O the special function unit's 2^-22 is enough.
+// Logits count from -43 on: the product of two exp(-x) stays finite, and 1 - a^2 above 0 at any ordinary rate.  A NaN stays one.
+constexpr float kLeast = -43.0f;
+__device__ __forceinline__ float2 capped(float2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(kLeast));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(kLeast));
+    return x;
+}
+// exp(-x) of capped logits, for the sigmoid 1 / (1 + exp(-x)) and what it leaves of 1, exp(-x) / (1 + exp(-x)): an open gate's rest is computed, not subtracted.  With bf16 I/O
+// the special function unit's 2^-22 is enough.
 template <typename IO> __device__ __forceinline__ float2 exp_neg(float2 x) {
-    float2 e;
-    if constexpr (sizeof(IO) == 4) {
-        e = make_float2(expf(-x.x), expf(-x.y));
-    } else {
-        const float2 t = mul2(x, dup(-kLog2e));
-        e = make_float2(ex2(t.x), ex2(t.y));
-    }
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.x) : "f"(0x1p62f));  // a NaN stays one
-    asm("min.NaN.f32 %0, %0, %1;" : "+f"(e.y) : "f"(0x1p62f));
-    return e;
+    if constexpr (sizeof(IO) == 4) return make_float2(expf(-x.x), expf(-x.y));
+    const float2 t = mul2(x, dup(-kLog2e));
+    return make_float2(ex2(t.x), ex2(t.y));
 }
 template <typename IO> __device__ __forceinline__ float2 reciprocal(float2 x) {
     if constexpr (sizeof(IO) == 4) return make_float2(__frcp_rn(x.x), __frcp_rn(x.y));
@@ -176,50 +176,36 @@ template <typename IO> __device__ __forceinline__ void store2(void* base, int64_
 
 // ---- a warp's tokens of a tile, ahead in shared memory: rows of 64 channels, one tensor after the other.  Every warp reads back only what it copied itself.
 __device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-// 16 or 4 bytes, zeros where `in` is false (nothing is read then)
-__device__ __forceinline__ void copy16(void* dst, const void* src, bool in) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_at(dst)), "l"(src), "r"(in ? 16 : 0) : "memory");
+__device__ __forceinline__ void copy16(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(dst)), "l"(src) : "memory");
 }
+// 4 bytes, zeros where `in` is false (nothing is read then)
 __device__ __forceinline__ void copy4(void* dst, const void* src, bool in) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_at(dst)), "l"(src), "r"(in ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+// tiles and contiguous pieces by the copy engine, counted on a barrier; what lies outside the tensor is filled with zeros
+__device__ __forceinline__ void tile_load(void* dst, const void* map, int c, int t, int b, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_at(dst)), "l"(map), "r"(c), "r"(t),
+                 "r"(b), "r"(smem_at(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(dst)), "l"(src), "r"(bytes), "r"(smem_at(bar)) : "memory");
+}
 
-// How rows are read: pieces of 16 bytes, of 4, or value by value (odd rows, and addresses, of bf16)
-enum { kBy16 = 0, kBy4 = 1, kByValue = 2 };
+// How rows are read: tiles by the copy engine (addresses and row lengths that are a multiple of 16 bytes; one lane starts them, and no other instruction waits for a place in the
+// load queue), pieces of 4 bytes, or value by value (odd rows, and addresses, of bf16)
+enum { kByTile = 0, kBy4 = 1, kByValue = 2 };
 inline int reads_by(int D, bool f32, uintptr_t all) {
     const int size = f32 ? 4 : 2;
-    if (all % 16 == 0 && (int64_t)D * size % 16 == 0) return kBy16;
+    if (all % 16 == 0 && (int64_t)D * size % 16 == 0) return kByTile;
     return all % 4 == 0 && (int64_t)D * size % 4 == 0 ? kBy4 : kByValue;
 }
 
 // ROWS tokens of `src` from row t on, channels c .. c + 63, as far as there are tokens (L) and channels (D); `at` is where token 0 of the sequence starts
 template <typename IO, int ROWS> __device__ __forceinline__ void copy_rows(IO* dst, const IO* src, int64_t at, int t, int L, int c, int D, int by, int lane) {
-    if (by == kBy16 && c + kScanCh <= D && t + ROWS <= L) {  // all there
-        constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;
-        const int row = lane / PER, ch = lane % PER * V;
-        const IO* p = src + (at + (int64_t)t * D + c) + (row * (int64_t)D + ch);
-        IO* q = dst + row * kScanCh + ch;
-#pragma unroll
-        for (int i = 0; i < ROWS; i += STEP) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_at(q + i * kScanCh)), "l"(p) : "memory");
-            p += STEP * (int64_t)D;
-        }
-        return;
-    }
-    if (by == kBy16) {
-        constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;  // pieces of a row; rows a warp copies at once
-        const int row = lane / PER, ch = lane % PER * V;
-        const bool col = c + ch < D;
-        const IO* p = src + at + (int64_t)(t + row) * D + c + ch;
-#pragma unroll
-        for (int i = 0; i < ROWS; i += STEP) {
-            const bool in = col && t + row + i < L;
-            copy16(dst + (row + i) * kScanCh + ch, in ? p + (int64_t)i * D : src, in);
-        }
-        return;
-    }
     constexpr int V = 4 / (int)sizeof(IO);
     if (by == kBy4) {
         for (int i = lane; i < ROWS * kScanCh / V; i += 32) {
@@ -244,6 +230,17 @@ template <typename IO> __device__ __forceinline__ float2 row2(const IO* row, int
     } else {
         const uint32_t w = reinterpret_cast<const uint32_t*>(row)[lane];
         return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+}
+
+// the same of a logit, capped
+template <typename IO> __device__ __forceinline__ float2 logit2(const IO* row, int lane) {
+    if constexpr (sizeof(IO) == 4) {
+        return capped(row2(row, lane));
+    } else {
+        const __nv_bfloat162 w = __hmax2_nan(reinterpret_cast<const __nv_bfloat162*>(row)[lane], __float2bfloat162_rn(kLeast));
+        const uint32_t u = *reinterpret_cast<const uint32_t*>(&w);
+        return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
     }
 }
 
@@ -282,11 +279,11 @@ __device__ __forceinline__ void send_part(Meeting& m, int slot, int part, int pa
     for (int k = 0; k < parts; ++k)
         sm100::st_async_v4(in_cta(data, k), __float_as_uint(P.x), __float_as_uint(P.y), __float_as_uint(own.x), __float_as_uint(own.y), in_cta(bar, k));
 }
-// Bounded: the stores cannot fail short of a device fault.  False once a wait gave up; what is computed from then on is made NaN.
-__device__ __forceinline__ bool await_parts(Meeting& m, int slot, uint32_t parity) {
-    if (sm100::mbar_try_wait<true>(&m.full[slot], parity)) return true;
+// Bounded: neither the copies nor the stores of a cluster can fail short of a device fault.  False once a wait gave up; what is computed from then on is made NaN.
+template <bool CLUSTER> __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
+    if (sm100::mbar_try_wait<CLUSTER>(bar, parity)) return true;
     const long long t0 = clock64();
-    while (!sm100::mbar_try_wait<true>(&m.full[slot], parity))
+    while (!sm100::mbar_try_wait<CLUSTER>(bar, parity))
         if (clock64() - t0 > sm100::kWaitCycles) return false;
     return true;
 }

@@ -7,6 +7,7 @@
 #include "api_checks.h"
 #include "pack8.cuh"
 #include "scan_common.cuh"
+#include "scan_map.h"
 
 namespace e2ttt {
 namespace {
@@ -19,8 +20,11 @@ template <typename IO> constexpr int kTokOf = sizeof(IO) == 2 ? 16 : 8;
 struct Meet {
     float4 runs[2][kWarps][32];  // P and h' of a warp's tokens
     float2 carry[2][32];         // the state after a turn's tokens
+    uint64_t full[kWarps][kStages];
     Meeting meeting;
 };
+
+constexpr int kMeet = (sizeof(Meet) + 127) / 128 * 128;
 
 // The 8-bit form of a warp's rows of one tensor: a lane takes 16 bytes, an aligned group of lanes a block.
 template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const IO* rows, uint8_t* codes, uint8_t* scales, int n, int lane) {
@@ -48,16 +52,16 @@ template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const
 }
 
 template <typename IO, bool GATE, bool UNIT, bool PACK>
-__global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a, const int by, const bool pair, const int parts) {
+__global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a, const __grid_constant__ ScanMaps maps, const int by, const bool pair, const int parts) {
     constexpr int TOK = kTokOf<IO>, TILE = TOK * kWarps, NT = GATE ? 3 : 2;
-    extern __shared__ __align__(16) char smem[];
+    extern __shared__ __align__(128) char smem[];
     Meet& meet = *reinterpret_cast<Meet*>(smem);
     const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
     const int64_t blocks = a.s.blocks(), spans = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
     const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
-    IO* ring = reinterpret_cast<IO*>(smem + sizeof(Meet)) + warp * (kStages * NT * TOK * kScanCh);
+    IO* ring = reinterpret_cast<IO*>(smem + kMeet) + warp * (kStages * NT * TOK * kScanCh);
     const int64_t seq = b * L * (int64_t)D;
     float2 rate = load2<float>(a.rate, c0, n, false);
     const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
@@ -65,20 +69,34 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     float2 end = a.h_init ? load2<float>(a.h_init, b * D + c0, n, false) : dup(0.0f);  // the state after the last turn, in one warp
     const int ender = parts == 1 ? kWarps - 1 : 0;
     if (warp == ender) meet.carry[1][lane] = end;
+    uint64_t* full = meet.full[warp];
+    if (by == kByTile && lane == 0) {
+        for (int i = 0; i < kStages; ++i) sm100::mbar_init(&full[i], 1);
+        sm100::fence_mbar_init();
+    }
+    __syncwarp();
     if (parts > 1) meeting_init(meet.meeting);
     const int64_t tiles = ((int64_t)L + TILE - 1) / TILE;
     unsigned next_first = 0;
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
-        if (tile < tiles) {
+        if (tile * TILE + warp * TOK < L) {
             const int t = (int)(tile * TILE) + warp * TOK;
             IO* to = ring + slot * (NT * TOK * kScanCh);
-            copy_rows<IO, TOK>(to, static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
-            copy_rows<IO, TOK>(to + TOK * kScanCh, static_cast<const IO*>(a.r), seq, t, L, first, D, by, lane);
-            if (GATE) copy_rows<IO, TOK>(to + 2 * TOK * kScanCh, static_cast<const IO*>(a.g), seq, t, L, first, D, by, lane);
+            if (by == kByTile) {
+                if (lane == 0) {
+                    sm100::mbar_expect_tx(&full[slot], NT * TOK * kScanCh * sizeof(IO));
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) tile_load(to + k * TOK * kScanCh, &maps.m[k], first, t, (int)b, &full[slot]);
+                }
+            } else {
+                copy_rows<IO, TOK>(to, static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
+                copy_rows<IO, TOK>(to + TOK * kScanCh, static_cast<const IO*>(a.r), seq, t, L, first, D, by, lane);
+                if (GATE) copy_rows<IO, TOK>(to + 2 * TOK * kScanCh, static_cast<const IO*>(a.g), seq, t, L, first, D, by, lane);
+            }
             if (a.starts && lane < TOK && t + lane < L) next_first = a.starts[b * L + t + lane];
         }
-        copy_commit();
+        if (by != kByTile) copy_commit();
     };
     load(part, 0);
     unsigned byte0 = next_first;
@@ -93,7 +111,8 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
         byte0 = next_first;
         const IO* rows = ring + slot * (NT * TOK * kScanCh);
-        copy_wait<kStages - 1>();
+        if (by != kByTile) copy_wait<kStages - 1>();
+        else if (met && have > 0) met = await<false>(&full[slot], parity);
         __syncwarp();
         float2 h[TOK], P[TOK], hh = dup(0.0f), pp = dup(1.0f);
         const bool plain = near && have == TOK && !starts;  // all tokens and channels are there, none is a start, no decay is far from 1
@@ -105,10 +124,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                     float2 u = row2(rows + j * kScanCh, lane), sg;
                     if constexpr (GATE) {
                         float2 ig;
-                        sigmoids<IO>(row2(rows + (TOK + j) * kScanCh, lane), row2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
+                        sigmoids<IO>(logit2(rows + (TOK + j) * kScanCh, lane), logit2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
                         u = mul2(u, ig);
                     } else {
-                        sg = sigmoid2<IO>(row2(rows + (TOK + j) * kScanCh, lane));
+                        sg = sigmoid2<IO>(logit2(rows + (TOK + j) * kScanCh, lane));
                     }
                     const Decay d = decay<IO, UNIT, PLAIN>(sg, rate);
                     if (!PLAIN && (starts >> j & 1)) {
@@ -152,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                 P_in = both(P_in, make_float2(q.x, q.y));
             }
             if (warp == kWarps - 1) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, hh));
-            if (met) met = await_parts(meet.meeting, slot, parity);
+            if (met) met = await<true>(&meet.meeting.full[slot], parity);
             for (int k = 0; k < part; ++k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
                 in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
@@ -163,11 +182,11 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                     const float4 q = meet.meeting.parts[slot][k][lane];
                     end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
                 }
-                if (!met) end = dup(__uint_as_float(0x7fc00000u));
                 meet.carry[slot][lane] = end;
             }
             in = through2(P_in, in, own);
         }
+        if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
         if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
         if (!a.h) continue;
         const int64_t at = seq + (int64_t)t0 * D + c0;
@@ -181,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         }
     }
     if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
-    copy_wait<0>();
+    if (by != kByTile) copy_wait<0>();
 }
 
 // CTAs of a cluster
@@ -200,7 +219,7 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArg
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(a.s.B * a.s.blocks() * parts));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(Meet) + kStages * (GATE ? 3 : 2) * kTokOf<IO> * kWarps * kScanCh * sizeof(IO);
+    cfg.dynamicSmemBytes = kMeet + kStages * (GATE ? 3 : 2) * kTokOf<IO> * kWarps * kScanCh * sizeof(IO);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -208,7 +227,11 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArg
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;
-    return (int)cudaLaunchKernelEx(&cfg, kernel, a, by, pair, parts);
+    ScanMaps maps{};
+    const void* in[3] = {a.x, a.r, a.g};
+    for (int k = 0; by == kByTile && k < (GATE ? 3 : 2); ++k)
+        if (!scan_map(&maps.m[k], in[k], a.s, kTokOf<IO>)) by = kBy4;
+    return (int)cudaLaunchKernelEx(&cfg, kernel, a, maps, by, pair, parts);
 }
 template <typename IO, bool GATE, bool UNIT> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
     return a.codes ? launch<IO, GATE, UNIT, true>(a, by, pair, st) : launch<IO, GATE, UNIT, false>(a, by, pair, st);

@@ -20,8 +20,8 @@ template <typename IO, bool GATE, bool UNIT> __global__ void __launch_bounds__(k
         const int64_t at = ((int64_t)b * a.s.L + t) * D + c0;
         float2 u = load2<IO>(a.x, at, n, pair);
         const float2 r = load2<IO>(a.r, at, n, pair);
-        if (GATE) u = mul2(u, sigmoid2<IO>(load2<IO>(a.g, at, n, pair)));
-        const Decay d = decay<IO, UNIT, false>(sigmoid2<IO>(r), rate);
+        if (GATE) u = mul2(u, sigmoid2<IO>(capped(load2<IO>(a.g, at, n, pair))));
+        const Decay d = decay<IO, UNIT, false>(sigmoid2<IO>(capped(r)), rate);
         if (a.starts && a.starts[(int64_t)b * a.s.L + t]) {
             h = u;
         } else {

@@ -243,14 +243,14 @@ def test_gates_wide_open_and_shut(io, save):
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_logits_without_bound_and_a_rate_of_zero(io):
-    """Nothing is NaN at infinite logits or where a_t is 1: there the derivative of s_t is taken as 0.  Logits count from -62 log 2 on."""
+    """Nothing is NaN at infinite logits or where a_t is 1: there the derivative of s_t is taken as 0.  Logits count from -43 on."""
     x, d = make(1, 100, 64, io, seed=9)
     x["r"][:, 5:9, :4], x["r"][:, 20, 4:8], x["g"][:, 30, :4], x["g"][:, 31, :4] = -np.inf, np.inf, -np.inf, np.inf
     x["r"][:, :, 60] = -np.inf
     x["rate"][63] = 0.0
     r = Run(x, io)
     out, got = r.fwd(), r.bwd(d)
-    x["r"], x["g"] = (np.maximum(x[n], -62 * np.log(2.0)) for n in ("r", "g"))
+    x["r"], x["g"] = (np.maximum(x[n], -43.0) for n in ("r", "g"))
     check_forward(out, x, io)
     check_backward(got, x, d, io, False)
 
