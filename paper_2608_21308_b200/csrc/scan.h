@@ -15,6 +15,13 @@ struct ScanShape {
     constexpr int64_t spans() const { return ((int64_t)L + kScanSpan - 1) / kScanSpan; }
 };
 
+// CTAs that share a block of channels of a sequence: as many as fill the GPU's 148 SMs once, `on_sm` on each, up to a cluster of eight and a tile each.  All of them run
+// at once then: a second, part-filled round of CTAs that walk a whole sequence would take as long as the first.
+inline int scan_parts(const ScanShape& s, int tile, int on_sm) {
+    const int64_t fit = 148 * on_sm / (s.B * s.blocks()), tiles = ((int64_t)s.L + tile - 1) / tile, parts = fit < tiles ? fit : tiles;
+    return (int)(parts < 1 ? 1 : parts > 8 ? 8 : parts);
+}
+
 // CTAs of the reverse pass that share a block of channels, along the tokens
 int scan_bwd_parts(const ScanShape& s);
 

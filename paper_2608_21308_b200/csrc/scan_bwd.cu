@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
     const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
     const int64_t seq = b * L * (int64_t)D;
+    const Pairs pairs = make_pairs();
     float2 rate = load2<float>(a.rate, c0, n, false);
     const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
     rate = make_float2(-rate.x, -rate.y);
@@ -139,8 +140,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             taken ^= 1u << slot;
         }
         __syncwarp();
-        // of token j: c as in the forward; to_x = s i, what lam is multiplied with in d_x; to_r, first sg a u / s, then sg (h_{t-1} - a u / s); sg; to_a = d_a_decay / (d_log_a sg).
-        // In the stash: s u (1 - i), what lam is multiplied with in d_a_in.
+        // of token j: c as in the forward; to_x = -s i, what -lam is multiplied with in d_x (with a^2 - 1 at hand -s takes no special function); to_r, first sg a u / s, then
+        // sg (h_{t-1} - a u / s); sg; to_a = d_a_decay / (d_log_a sg).  In the stash: -s u (1 - i), what -lam is multiplied with in d_a_in.
         float2 c[kTok], to_x[kTok], to_r[kTok], sg[kTok], to_a[kTok];
         unsigned far = 0;  // two bits a token
         float2 hh = dup(0.0f), pp = dup(1.0f), v = dup(0.0f);
@@ -151,29 +152,30 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             for (int j = 0; j < kTok; ++j) {
                 if (!PLAIN) c[j] = to_x[j] = to_r[j] = sg[j] = to_a[j] = dup(0.0f);
                 if (!PLAIN && j >= have) continue;
-                const float2 x = input<0>(rows, j, lane), er = exp_neg<IO>(logit<1>(rows, j, lane));
+                const float2 x = input<0>(rows, j, lane), er = exp_neg<IO>(pairs, logit<1>(rows, j, lane));
                 float2 ig = dup(1.0f), shut = dup(0.0f);
                 if constexpr (GATE) {
-                    const float2 eg = exp_neg<IO>(logit<2>(rows, j, lane));
-                    ig = reciprocal<IO>(add2(eg, dup(1.0f)));
+                    const float2 eg = exp_neg<IO>(pairs, logit<2>(rows, j, lane));
+                    ig = reciprocal<IO>(add2(eg, pairs.one));
                     shut = mul2(eg, ig);
                 }
-                sg[j] = reciprocal<IO>(add2(er, dup(1.0f)));
+                sg[j] = reciprocal<IO>(add2(er, pairs.one));
                 to_a[j] = mul2(rate, mul2(er, sg[j]));
-                const Decay d = decay<IO, UNIT, PLAIN>(sg[j], rate);
+                const Decay d = decay<IO, UNIT, PLAIN>(pairs, sg[j], rate);
                 c[j] = d.c;
                 if (!PLAIN) far |= d.far << 2 * j;
                 const bool start = !PLAIN && (starts >> j & 1);
-                to_x[j] = ig;
                 to_r[j] = dup(0.0f);
                 if (UNIT && !start) {
-                    const float2 rs = inv_sqrt2<PLAIN>(d.one);
+                    const float2 rs = inv_sqrt_minus<PLAIN>(d.minus);
                     to_r[j] = mul2(sg[j], fade<PLAIN>(mul2(mul2(x, ig), rs), d.c, d.far));
-                    to_x[j] = mul2(ig, mul2(d.one, rs));
+                    to_x[j] = mul2(ig, mul2(d.minus, rs));
+                } else {
+                    to_x[j] = mul2(ig, pairs.minus_one);
                 }
                 const float2 bj = mul2(to_x[j], x);
                 if (GATE) meet.stash[warp][j][lane] = mul2(bj, shut);
-                hh = start ? bj : add2(fade<PLAIN>(hh, d.c, d.far), bj);
+                hh = fma2(bj, pairs.minus_one, start ? dup(0.0f) : fade<PLAIN>(hh, d.c, d.far));
                 pp = start ? dup(0.0f) : fade<PLAIN>(pp, d.c, d.far);
             }
 #pragma unroll
@@ -189,39 +191,50 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         meet.ends[slot][warp][lane] = v;
         __syncthreads();
         float2 in = meet.carry[slot ^ 1][lane];  // what the tokens after the turn's hand on
-        for (int w = 0; w < warp; ++w) {
-            const float4 q = meet.runs[slot][w][lane];
-            state = through2(make_float2(q.x, q.y), state, make_float2(q.z, q.w));
-        }
-        if (parts == 1) {
-            for (int w = kWarps - 1; w > warp; --w) {
+        auto meet_others = [&](auto is_cut) {
+            constexpr bool CUT = decltype(is_cut)::value;
+#pragma unroll
+            for (int w = 0; w < kWarps - 1; ++w) {
+                if (w >= warp) break;
                 const float4 q = meet.runs[slot][w][lane];
-                in = through2(make_float2(q.x, q.y), in, meet.ends[slot][w][lane]);
+                state = through<CUT>(make_float2(q.x, q.y), state, make_float2(q.z, q.w));
             }
-            if (warp == ender) meet.carry[slot][lane] = end = through2(pp, in, v);
-        } else {
+            if (parts == 1) {
+#pragma unroll
+                for (int w = kWarps - 1; w > 0; --w) {
+                    if (w <= warp) break;
+                    const float4 q = meet.runs[slot][w][lane];
+                    in = through<CUT>(make_float2(q.x, q.y), in, meet.ends[slot][w][lane]);
+                }
+                if (warp == ender) meet.carry[slot][lane] = end = through<CUT>(pp, in, v);
+                return;
+            }
             float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps after this one
-            for (int w = kWarps - 1; w > warp; --w) {
+#pragma unroll
+            for (int w = kWarps - 1; w > 0; --w) {
+                if (w <= warp) break;
                 const float4 q = meet.runs[slot][w][lane];
-                own = through2(make_float2(q.x, q.y), own, meet.ends[slot][w][lane]);
-                P_in = both(P_in, make_float2(q.x, q.y));
+                own = through<CUT>(make_float2(q.x, q.y), own, meet.ends[slot][w][lane]);
+                P_in = both<CUT>(P_in, make_float2(q.x, q.y));
             }
-            if (warp == 0) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, v));
+            if (warp == 0) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, v));
             if (met) met = await<true>(&meet.meeting.full[slot], parity);
             for (int k = parts - 1; k > part; --k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
-                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+                in = through<CUT>(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
             }
             if (warp == ender) {
                 end = in;
                 for (int k = part; k >= 0; --k) {
                     const float4 q = meet.meeting.parts[slot][k][lane];
-                    end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
+                    end = through<CUT>(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
                 }
                 meet.carry[slot][lane] = end;
             }
-            in = through2(P_in, in, own);
-        }
+            in = through<CUT>(P_in, in, own);
+        };
+        if (a.starts) meet_others(std::true_type{});
+        else meet_others(std::false_type{});
         if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
         auto spread = [&](auto is_plain) {
             constexpr bool PLAIN = decltype(is_plain)::value;
@@ -230,8 +243,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 if (!PLAIN && j >= have) continue;
                 const bool start = !PLAIN && (starts >> j & 1);
                 const float2 bj = mul2(to_x[j], input<0>(rows, j, lane));
-                to_r[j] = start ? dup(0.0f) : UNIT ? fma2(to_r[j], dup(-1.0f), mul2(sg[j], state)) : mul2(sg[j], state);
-                state = start ? bj : add2(fade<PLAIN>(state, c[j], far >> 2 * j), bj);
+                to_r[j] = start ? dup(0.0f) : UNIT ? fma2(to_r[j], pairs.minus_one, mul2(sg[j], state)) : mul2(sg[j], state);
+                state = fma2(bj, pairs.minus_one, start ? dup(0.0f) : fade<PLAIN>(state, c[j], far >> 2 * j));
             }
             const int64_t at = seq + (int64_t)t0 * D + c0;
             const int m = PLAIN ? 2 : n;
@@ -242,11 +255,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 const bool start = !PLAIN && (starts >> j & 1);
                 const int64_t to = at + j * (int64_t)D;
                 in = add2(in, row2<IO>(rows.d_h[j], lane));
-                store2<IO>(ba.d_x, to, m, two, mul2(in, to_x[j]));
-                if (GATE) store2<IO>(ba.d_g, to, m, two, mul2(in, meet.stash[warp][j][lane]));
+                const float2 minus = mul2(in, pairs.minus_one);
+                store2<IO>(ba.d_x, to, m, two, mul2(minus, to_x[j]));
+                if (GATE) store2<IO>(ba.d_g, to, m, two, mul2(minus, meet.stash[warp][j][lane]));
                 in = start ? dup(0.0f) : fade<PLAIN>(in, c[j], far >> 2 * j);  // a lam
                 const float2 dl = start ? dup(0.0f) : mul2(in, to_r[j]);      // d_log_a sg
-                sum = fma2(dl, dup(-1.0f), sum);
+                sum = add2(sum, dl);
                 store2<IO>(ba.d_r, to, m, two, mul2(dl, to_a[j]));
             }
         };
@@ -257,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     }
     if (part == 0 && warp == ender) store2<float>(ba.dh_init, b * D + c0, n, false, end);
     __syncthreads();
-    meet.ends[0][warp][lane] = sum;
+    meet.ends[0][warp][lane] = make_float2(-sum.x, -sum.y);
     __syncthreads();
     if (by != kByTile) copy_wait<0>();
     if (warp != 0) return;
@@ -316,12 +330,7 @@ template <typename IO> int dispatch(const ScanBwdArgs& b, int by, bool pair, cud
 
 }  // namespace
 
-int scan_bwd_parts(const ScanShape& s) {
-    const int64_t units = s.B * s.blocks();
-    int parts = 1;
-    while (parts < 8 && units * parts < 296 && parts < s.spans()) parts *= 2;
-    return parts;
-}
+int scan_bwd_parts(const ScanShape& s) { return scan_parts(s, kTile, s.f32 ? 1 : 2); }
 
 int scan_bwd_launch(const ScanBwdArgs& b, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -52,6 +52,20 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Constants of the gates as pairs.  They are kept in registers by hand: the compiler would rather load them again at every use, two moves for one instruction.
+struct Pairs {
+    float2 neg_log2e, one, two, minus_one, e1, e2, e3, e4;
+};
+__device__ __forceinline__ float2 kept(float x) {
+    float y;
+    asm volatile("mov.b32 %0, %1;" : "=f"(y) : "f"(x));
+    return dup(y);
+}
+// (exp(y) - 1) / y = 1 + e1 y + .. + e4 y^4 on [-1/4, 0], fitted to the least largest relative error: 2.9e-9
+__device__ __forceinline__ Pairs make_pairs() {
+    return Pairs{kept(-kLog2e), kept(1.0f), kept(2.0f), kept(-1.0f), kept(0.49999964f), kept(0.16665289f), kept(0.04150013f), kept(0.00753017f)};
+}
+
 // Logits count from -43 on: the product of two exp(-x) stays finite, and 1 - a^2 above 0 at any ordinary rate.  A NaN stays one.
 constexpr float kLeast = -43.0f;
 __device__ __forceinline__ float2 capped(float2 x) {
@@ -61,49 +75,47 @@ __device__ __forceinline__ float2 capped(float2 x) {
 }
 // exp(-x) of capped logits, for the sigmoid 1 / (1 + exp(-x)) and what it leaves of 1, exp(-x) / (1 + exp(-x)): an open gate's rest is computed, not subtracted.  With bf16 I/O
 // the special function unit's 2^-22 is enough.
-template <typename IO> __device__ __forceinline__ float2 exp_neg(float2 x) {
+template <typename IO> __device__ __forceinline__ float2 exp_neg(const Pairs& k, float2 x) {
     if constexpr (sizeof(IO) == 4) return make_float2(expf(-x.x), expf(-x.y));
-    const float2 t = mul2(x, dup(-kLog2e));
+    const float2 t = mul2(x, k.neg_log2e);
     return make_float2(ex2(t.x), ex2(t.y));
 }
 template <typename IO> __device__ __forceinline__ float2 reciprocal(float2 x) {
     if constexpr (sizeof(IO) == 4) return make_float2(__frcp_rn(x.x), __frcp_rn(x.y));
     return make_float2(rcp(x.x), rcp(x.y));
 }
-template <typename IO> __device__ __forceinline__ float2 sigmoid2(float2 x) { return reciprocal<IO>(add2(exp_neg<IO>(x), dup(1.0f))); }
+template <typename IO> __device__ __forceinline__ float2 sigmoid2(const Pairs& k, float2 x) { return reciprocal<IO>(add2(exp_neg<IO>(k, x), k.one)); }
 // the sigmoids of two pairs; with bf16 I/O one reciprocal of both denominators: the special function unit bounds the forward otherwise
-template <typename IO> __device__ __forceinline__ void sigmoids(float2 x, float2 y, float2& sx, float2& sy) {
+template <typename IO> __device__ __forceinline__ void sigmoids(const Pairs& k, float2 x, float2 y, float2& sx, float2& sy) {
     if constexpr (sizeof(IO) == 4) {
-        sx = sigmoid2<IO>(x);
-        sy = sigmoid2<IO>(y);
+        sx = sigmoid2<IO>(k, x);
+        sy = sigmoid2<IO>(k, y);
     } else {
-        const float2 p = add2(exp_neg<IO>(x), dup(1.0f)), q = add2(exp_neg<IO>(y), dup(1.0f)), r = reciprocal<IO>(mul2(p, q));
+        const float2 p = add2(exp_neg<IO>(k, x), k.one), q = add2(exp_neg<IO>(k, y), k.one), r = reciprocal<IO>(mul2(p, q));
         sx = mul2(q, r);
         sy = mul2(p, r);
     }
 }
 
 // A token's decay for two channels.  Near 1, where a's own rounding is what a long memory adds up, it is kept as c = a - 1; far from it (log a below -1/4), where c's rounding
-// would be what a leaves of a state, as c = a.  one = 1 - a^2.
+// would be what a leaves of a state, as c = a.  minus = a^2 - 1.
 struct Decay {
-    float2 c, one;
+    float2 c, minus;
     unsigned far;  // bit 0: the first channel's c is a, bit 1: the second's
 };
 // Whether a rate's decays are all near 1, and none of them 1
 __device__ __forceinline__ bool near_rate(float rate) { return rate >= 1e-10f && rate <= 0.25f; }
 // sg = sigmoid(a_decay).  NEAR: near_rate of both channels.
-template <typename IO, bool UNIT, bool NEAR> __device__ __forceinline__ Decay decay(float2 sg, float2 neg_rate) {
+template <typename IO, bool UNIT, bool NEAR> __device__ __forceinline__ Decay decay(const Pairs& k, float2 sg, float2 neg_rate) {
     const float2 y = mul2(neg_rate, sg);
     Decay d;
-    // exp(y) - 1 for -1/4 <= y <= 0: the series to y^6 / 6! (5e-8 of the result at the end of the range)
-    float2 p = fma2(y, dup(1.0f / 720.0f), dup(1.0f / 120.0f));
-    p = fma2(p, y, dup(1.0f / 24.0f));
-    p = fma2(p, y, dup(1.0f / 6.0f));
-    p = fma2(p, y, dup(0.5f));
-    p = fma2(p, y, dup(1.0f));
+    float2 p = fma2(y, k.e4, k.e3);
+    p = fma2(p, y, k.e2);
+    p = fma2(p, y, k.e1);
+    p = fma2(p, y, k.one);
     d.c = mul2(p, y);
     d.far = 0;
-    if (UNIT) d.one = mul2(d.c, fma2(d.c, dup(-1.0f), dup(-2.0f)));
+    if (UNIT) d.minus = mul2(d.c, add2(d.c, k.two));
     if constexpr (!NEAR) {
         float2 e;
         if constexpr (sizeof(IO) == 4) e = make_float2(expf(y.x), expf(y.y));
@@ -111,12 +123,12 @@ template <typename IO, bool UNIT, bool NEAR> __device__ __forceinline__ Decay de
         if (y.x < -0.25f) {
             d.far = 1;
             d.c.x = e.x;
-            if (UNIT) d.one.x = fmaf(-e.x, e.x, 1.0f);
+            if (UNIT) d.minus.x = fmaf(e.x, e.x, -1.0f);
         }
         if (y.y < -0.25f) {
             d.far |= 2;
             d.c.y = e.y;
-            if (UNIT) d.one.y = fmaf(-e.y, e.y, 1.0f);
+            if (UNIT) d.minus.y = fmaf(e.y, e.y, -1.0f);
         }
     }
     return d;
@@ -126,17 +138,17 @@ template <bool NEAR> __device__ __forceinline__ float2 fade(float2 h, float2 c, 
     if constexpr (NEAR) return fma2(h, c, h);
     return fma2(h, c, make_float2(far & 1 ? 0.0f : h.x, far & 2 ? 0.0f : h.y));
 }
-// sqrt(x), and 1 / sqrt(x) with 0 for 0; both good to 2^-22.  NEAR: x is not 0.
-__device__ __forceinline__ float2 sqrt2(float2 x) {
+// sqrt(-x), and 1 / sqrt(-x) with 0 for 0; both good to 2^-22.  NEAR: x is not 0.
+__device__ __forceinline__ float2 sqrt_minus(float2 x) {
     float2 y;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(-x.x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(-x.y));
     return y;
 }
-template <bool NEAR> __device__ __forceinline__ float2 inv_sqrt2(float2 x) {
-    const float2 y = make_float2(rsqrt_fast(x.x), rsqrt_fast(x.y));
+template <bool NEAR> __device__ __forceinline__ float2 inv_sqrt_minus(float2 x) {
+    const float2 y = make_float2(rsqrt_fast(-x.x), rsqrt_fast(-x.y));
     if constexpr (NEAR) return y;
-    return make_float2(x.x > 1e-37f ? y.x : 0.0f, x.y > 1e-37f ? y.y : 0.0f);
+    return make_float2(x.x < -1e-37f ? y.x : 0.0f, x.y < -1e-37f ? y.y : 0.0f);
 }
 
 template <typename IO> __device__ __forceinline__ float to_f32(IO x);
@@ -244,12 +256,17 @@ template <typename IO> __device__ __forceinline__ float2 logit2(const IO* row, i
     }
 }
 
-// ---- runs of tokens: what goes in, P times, plus what a run makes of nothing.  A run with a start in it lets nothing through, an infinity or a NaN neither.
-__device__ __forceinline__ float through(float P, float in, float own) { return P == 0.0f ? own : fmaf(P, in, own); }
-__device__ __forceinline__ float2 through2(float2 P, float2 in, float2 own) { return make_float2(through(P.x, in.x, own.x), through(P.y, in.y, own.y)); }
-
-// P of two runs, the second of which may have a start in it
-__device__ __forceinline__ float2 both(float2 P, float2 next) { return make_float2(next.x == 0.0f ? 0.0f : P.x * next.x, next.y == 0.0f ? 0.0f : P.y * next.y); }
+// ---- runs of tokens: what goes in, P times, plus what a run makes of nothing.  CUT: there are starts, and a run with one in it lets nothing through, an infinity or a NaN
+// neither.
+template <bool CUT> __device__ __forceinline__ float2 through(float2 P, float2 in, float2 own) {
+    if constexpr (!CUT) return fma2(P, in, own);
+    return make_float2(P.x == 0.0f ? own.x : fmaf(P.x, in.x, own.x), P.y == 0.0f ? own.y : fmaf(P.y, in.y, own.y));
+}
+// P of two runs
+template <bool CUT> __device__ __forceinline__ float2 both(float2 P, float2 next) {
+    if constexpr (!CUT) return mul2(P, next);
+    return make_float2(next.x == 0.0f ? 0.0f : P.x * next.x, next.y == 0.0f ? 0.0f : P.y * next.y);
+}
 
 // ---- CTAs of a cluster: the parts of a sequence's channels along its tokens.  Every turn each leaves its tile's run with all of them by asynchronous stores, which count
 // themselves on the receiver's barrier (a release of the CTA's global stores, as a cluster's barrier takes, would wait for all of them).  A buffer is used again two turns later: a CTA

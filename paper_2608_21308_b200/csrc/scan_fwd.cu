@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
     IO* ring = reinterpret_cast<IO*>(smem + kMeet) + warp * (kStages * NT * TOK * kScanCh);
     const int64_t seq = b * L * (int64_t)D;
+    const Pairs pairs = make_pairs();
     float2 rate = load2<float>(a.rate, c0, n, false);
     const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
     rate = make_float2(-rate.x, -rate.y);
@@ -124,17 +125,17 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                     float2 u = row2(rows + j * kScanCh, lane), sg;
                     if constexpr (GATE) {
                         float2 ig;
-                        sigmoids<IO>(logit2(rows + (TOK + j) * kScanCh, lane), logit2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
+                        sigmoids<IO>(pairs, logit2(rows + (TOK + j) * kScanCh, lane), logit2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
                         u = mul2(u, ig);
                     } else {
-                        sg = sigmoid2<IO>(logit2(rows + (TOK + j) * kScanCh, lane));
+                        sg = sigmoid2<IO>(pairs, logit2(rows + (TOK + j) * kScanCh, lane));
                     }
-                    const Decay d = decay<IO, UNIT, PLAIN>(sg, rate);
+                    const Decay d = decay<IO, UNIT, PLAIN>(pairs, sg, rate);
                     if (!PLAIN && (starts >> j & 1)) {
                         hh = u;
                         pp = dup(0.0f);
                     } else {
-                        if (UNIT) u = mul2(u, sqrt2(d.one));
+                        if (UNIT) u = mul2(u, sqrt_minus(d.minus));
                         hh = add2(fade<PLAIN>(hh, d.c, d.far), u);
                         pp = fade<PLAIN>(pp, d.c, d.far);
                     }
@@ -157,35 +158,44 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         __syncthreads();
         const float2 before = meet.carry[slot ^ 1][lane];  // the state before the turn's tokens
         float2 in = before;
-        if (parts == 1) {
-            for (int w = 0; w < warp; ++w) {
-                const float4 q = meet.runs[slot][w][lane];
-                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+        auto meet_others = [&](auto is_cut) {
+            constexpr bool CUT = decltype(is_cut)::value;
+            if (parts == 1) {
+#pragma unroll
+                for (int w = 0; w < kWarps - 1; ++w) {
+                    if (w >= warp) break;
+                    const float4 q = meet.runs[slot][w][lane];
+                    in = through<CUT>(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+                }
+                if (warp == ender) meet.carry[slot][lane] = end = through<CUT>(pp, in, hh);
+                return;
             }
-            if (warp == ender) meet.carry[slot][lane] = end = through2(pp, in, hh);
-        } else {
             float2 P_in = dup(1.0f), own = dup(0.0f);  // the warps before this one
-            for (int w = 0; w < warp; ++w) {
+#pragma unroll
+            for (int w = 0; w < kWarps - 1; ++w) {
+                if (w >= warp) break;
                 const float4 q = meet.runs[slot][w][lane];
-                own = through2(make_float2(q.x, q.y), own, make_float2(q.z, q.w));
-                P_in = both(P_in, make_float2(q.x, q.y));
+                own = through<CUT>(make_float2(q.x, q.y), own, make_float2(q.z, q.w));
+                P_in = both<CUT>(P_in, make_float2(q.x, q.y));
             }
-            if (warp == kWarps - 1) send_part(meet.meeting, slot, part, parts, lane, both(P_in, pp), through2(pp, own, hh));
+            if (warp == kWarps - 1) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, hh));
             if (met) met = await<true>(&meet.meeting.full[slot], parity);
             for (int k = 0; k < part; ++k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
-                in = through2(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
+                in = through<CUT>(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
             }
             if (warp == ender) {
                 end = in;
                 for (int k = part; k < parts; ++k) {
                     const float4 q = meet.meeting.parts[slot][k][lane];
-                    end = through2(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
+                    end = through<CUT>(make_float2(q.x, q.y), end, make_float2(q.z, q.w));
                 }
                 meet.carry[slot][lane] = end;
             }
-            in = through2(P_in, in, own);
-        }
+            in = through<CUT>(P_in, in, own);
+        };
+        if (a.starts) meet_others(std::true_type{});
+        else meet_others(std::false_type{});
         if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
         if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
         if (!a.h) continue;
@@ -196,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         } else {
 #pragma unroll
             for (int j = 0; j < TOK; ++j)
-                if (j < have) store2<IO>(a.h, at + j * (int64_t)D, n, pair, through2(P[j], in, h[j]));
+                if (j < have) store2<IO>(a.h, at + j * (int64_t)D, n, pair, through<true>(P[j], in, h[j]));
         }
     }
     if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
@@ -204,12 +214,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
 }
 
 // CTAs of a cluster
-int parts_of(const ScanShape& s) {
-    const int64_t units = s.B * s.blocks(), tiles = ((int64_t)s.L + 127) / 128;
-    int parts = 1;
-    while (parts < 8 && units * parts < 296 && parts < tiles) parts *= 2;
-    return parts;
-}
+int parts_of(const ScanShape& s) { return scan_parts(s, kTokOf<__nv_bfloat16> * kWarps, 2); }
 
 template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
     auto kernel = scan_fwd_kernel<IO, GATE, UNIT, PACK>;

@@ -13,6 +13,7 @@ template <typename IO, bool GATE, bool UNIT> __global__ void __launch_bounds__(k
     const int n = min(2, D - c0);
     if (n <= 0) return;
     const bool even = (D & 1) == 0 && ((reinterpret_cast<uintptr_t>(a.rate) | reinterpret_cast<uintptr_t>(a.h_init) | reinterpret_cast<uintptr_t>(a.h_final)) & 7) == 0;
+    const Pairs pairs = make_pairs();
     float2 rate = load2<float>(a.rate, c0, n, even);
     rate = make_float2(-rate.x, -rate.y);
     float2 h = load2<float>(a.h_init, (int64_t)b * D + c0, n, even);
@@ -20,12 +21,12 @@ template <typename IO, bool GATE, bool UNIT> __global__ void __launch_bounds__(k
         const int64_t at = ((int64_t)b * a.s.L + t) * D + c0;
         float2 u = load2<IO>(a.x, at, n, pair);
         const float2 r = load2<IO>(a.r, at, n, pair);
-        if (GATE) u = mul2(u, sigmoid2<IO>(capped(load2<IO>(a.g, at, n, pair))));
-        const Decay d = decay<IO, UNIT, false>(sigmoid2<IO>(capped(r)), rate);
+        if (GATE) u = mul2(u, sigmoid2<IO>(pairs, capped(load2<IO>(a.g, at, n, pair))));
+        const Decay d = decay<IO, UNIT, false>(pairs, sigmoid2<IO>(pairs, capped(r)), rate);
         if (a.starts && a.starts[(int64_t)b * a.s.L + t]) {
             h = u;
         } else {
-            if (UNIT) u = mul2(u, sqrt2(d.one));
+            if (UNIT) u = mul2(u, sqrt_minus(d.minus));
             h = add2(fade<false>(h, d.c, d.far), u);
         }
         store2<IO>(a.h, at, n, pair, h);
