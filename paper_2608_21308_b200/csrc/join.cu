@@ -181,13 +181,13 @@ template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, i
 template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256; }
 
 // A piece of one of the packed tensors: its codes, and by its block's first lane the scale.  Every lane of a warp calls; c is the piece's place in the row.
-template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scales, const Piece<IO, V>& p, int c, bool in) {
-    float v[V];
+template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scales, Piece<IO, V> p, int c, bool in) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = in ? ldf(p.x[j]) : 0.0f;
-    const uint32_t byte = pack8::group_scale<V>(v);
+    for (int j = 0; j < V; ++j)
+        if (!in) p.x[j] = IO(0.0f);
+    const uint32_t byte = pack8::group_scale<IO, V>(p.x);
     if (!in) return;
-    *reinterpret_cast<pack8::Codes<V>*>(codes + c * V) = pack8::encode<V>(v, byte);
+    *reinterpret_cast<pack8::Codes<V>*>(codes + c * V) = pack8::encode<IO, V>(p.x, byte);
     if (c % (pack8::kBlock / V) == 0) scales[c / (pack8::kBlock / V)] = (uint8_t)byte;
 }
 

@@ -1,5 +1,6 @@
 // 8-bit checkpoints of activations: rows cut into blocks of 32 values, signed bytes and a power of two per block.  One pass, every byte read once and written once:
-// HBM bounds it.
+// HBM bounds it.  A lane takes 16 bytes of x at a time (less where rows or addresses do not allow it) and an aligned group of lanes a block, whose largest magnitude takes two or three
+// shuffles; four such pieces are under way per lane.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <string.h>
@@ -12,8 +13,6 @@ namespace e2ttt {
 namespace {
 using namespace pack8;
 
-__device__ __forceinline__ float ldf(float x) { return x; }
-__device__ __forceinline__ float ldf(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void stf(float& y, float x) { y = x; }
 __device__ __forceinline__ void stf(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }
 
@@ -22,73 +21,103 @@ template <typename IO, int V> struct alignas(sizeof(IO) * V) Values {
 };
 
 struct PackArgs {
-    int64_t rows, pieces;  // pieces: groups of V values, blocks filled up to 32
-    int cols, blocks;      // blocks of a row
+    int64_t pieces;  // groups of V values, every row's last block filled up to 32
+    int cols, blocks;  // blocks of a row
     const void* x;
     void* y;
     int8_t* codes;
     uint8_t* scales;
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kDeep = 4;
 
-// A thread takes V neighbouring values, an aligned group of 32 / V lanes a block.
-template <typename IO, int V> __global__ void __launch_bounds__(kThreads) pack8_kernel(const PackArgs a) {
-    const int64_t step = (int64_t)gridDim.x * kThreads;
-    for (int64_t first = (int64_t)blockIdx.x * kThreads; first < a.pieces; first += step) {
-        const int64_t i = first + threadIdx.x, block = i / (kBlock / V), row = block / a.blocks;
-        const int c = (int)(block - row * a.blocks) * kBlock + (int)(i % (kBlock / V)) * V;
-        const bool in = i < a.pieces && c < a.cols;
-        float x[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = 0.0f;
-        if (in) {
-            const Values<IO, V> v = *reinterpret_cast<const Values<IO, V>*>(static_cast<const IO*>(a.x) + row * a.cols + c);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = ldf(v.x[j]);
+// Where a piece lies.  FLAT: rows are whole blocks, so that they follow one another without a gap.
+template <int V, bool FLAT> struct Place {
+    int64_t block, at;
+    bool in;
+    __device__ __forceinline__ Place(const PackArgs& a, int64_t i) {
+        block = i / (kBlock / V);
+        in = i < a.pieces;
+        if (FLAT) {
+            at = i * V;
+        } else {
+            const int64_t row = a.pieces >> 31 ? block / a.blocks : (int64_t)((uint32_t)block / (uint32_t)a.blocks);
+            const int c = (int)(block - row * a.blocks) * kBlock + (int)(i % (kBlock / V)) * V;
+            at = row * a.cols + c;
+            in = in && c < a.cols;
         }
-        const uint32_t byte = group_scale<V>(x);
-        if (!in) continue;
-        *reinterpret_cast<Codes<V>*>(a.codes + row * a.cols + c) = encode<V>(x, byte);
-        if (i % (kBlock / V) == 0) a.scales[block] = (uint8_t)byte;
+    }
+};
+
+template <typename IO, int V, bool FLAT> __global__ void __launch_bounds__(kThreads) pack8_kernel(const PackArgs a) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kDeep) + threadIdx.x;
+    Values<IO, V> v[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+        const Place<V, FLAT> p(a, first + k * kThreads);
+        if (p.in) {
+            v[k] = *reinterpret_cast<const Values<IO, V>*>(static_cast<const IO*>(a.x) + p.at);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[k].x[j] = IO(0.0f);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+        const Place<V, FLAT> p(a, first + k * kThreads);
+        const uint32_t byte = group_scale<IO, V>(v[k].x);
+        if (!p.in) continue;
+        *reinterpret_cast<Codes<V>*>(a.codes + p.at) = encode<IO, V>(v[k].x, byte);
+        if (threadIdx.x % (kBlock / V) == 0) a.scales[p.block] = (uint8_t)byte;
     }
 }
 
-template <typename IO, int V> __global__ void __launch_bounds__(kThreads) unpack8_kernel(const PackArgs a) {
-    const int64_t step = (int64_t)gridDim.x * kThreads;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < a.pieces; i += step) {
-        const int64_t block = i / (kBlock / V), row = block / a.blocks;
-        const int c = (int)(block - row * a.blocks) * kBlock + (int)(i % (kBlock / V)) * V;
-        if (c >= a.cols) continue;
+template <typename IO, int V, bool FLAT> __global__ void __launch_bounds__(kThreads) unpack8_kernel(const PackArgs a) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kDeep) + threadIdx.x;
+    Codes<V> c[kDeep];
+    uint32_t byte[kDeep];
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+        const Place<V, FLAT> p(a, first + k * kThreads);
+        if (!p.in) continue;
+        c[k] = *reinterpret_cast<const Codes<V>*>(a.codes + p.at);
+        byte[k] = a.scales[p.block];
+    }
+#pragma unroll
+    for (int k = 0; k < kDeep; ++k) {
+        const Place<V, FLAT> p(a, first + k * kThreads);
+        if (!p.in) continue;
         float x[V];
-        decode<V>(*reinterpret_cast<const Codes<V>*>(a.codes + row * a.cols + c), a.scales[block], x);
+        decode<V>(c[k], byte[k], x);
         Values<IO, V> v;
 #pragma unroll
         for (int j = 0; j < V; ++j) stf(v.x[j], x[j]);
-        *reinterpret_cast<Values<IO, V>*>(static_cast<IO*>(a.y) + row * a.cols + c) = v;
+        *reinterpret_cast<Values<IO, V>*>(static_cast<IO*>(a.y) + p.at) = v;
     }
 }
 
-template <typename IO, int V, bool PACK> int launch(PackArgs a, cudaStream_t st) {
-    a.pieces = a.rows * a.blocks * (kBlock / V);
-    const int64_t need = (a.pieces + kThreads - 1) / kThreads, most = 148 * 8;
-    const unsigned grid = (unsigned)(need < most ? need : most);
-    if (PACK) pack8_kernel<IO, V><<<grid, kThreads, 0, st>>>(a);
-    else unpack8_kernel<IO, V><<<grid, kThreads, 0, st>>>(a);
+template <typename IO, int V, bool PACK, bool FLAT> int launch(const PackArgs& a, cudaStream_t st) {
+    const unsigned grid = (unsigned)((a.pieces + kThreads * kDeep - 1) / (kThreads * kDeep));
+    if (PACK) pack8_kernel<IO, V, FLAT><<<grid, kThreads, 0, st>>>(a);
+    else unpack8_kernel<IO, V, FLAT><<<grid, kThreads, 0, st>>>(a);
     return (int)cudaGetLastError();
+}
+template <typename IO, int V, bool PACK> int launch(PackArgs a, int64_t rows, cudaStream_t st) {
+    a.pieces = rows * a.blocks * (kBlock / V);
+    return a.cols % kBlock == 0 ? launch<IO, V, PACK, true>(a, st) : launch<IO, V, PACK, false>(a, st);
 }
 
 // values a thread takes: the most that the row length and the addresses allow
-template <bool PACK> int dispatch(const PackArgs& a, bool f32, cudaStream_t st) {
+template <bool PACK> int dispatch(const PackArgs& a, int64_t rows, bool f32, cudaStream_t st) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(PACK ? a.x : a.y), c = reinterpret_cast<uintptr_t>(a.codes);
     const int size = f32 ? 4 : 2;
     int v = 16 / size;
     while (v > 1 && (a.cols % v || x % (size * v) || c % v)) v >>= 1;
-    if (f32) return v == 4 ? launch<float, 4, PACK>(a, st) : v == 2 ? launch<float, 2, PACK>(a, st) : launch<float, 1, PACK>(a, st);
-    return v == 8   ? launch<__nv_bfloat16, 8, PACK>(a, st)
-           : v == 4 ? launch<__nv_bfloat16, 4, PACK>(a, st)
-           : v == 2 ? launch<__nv_bfloat16, 2, PACK>(a, st)
-                    : launch<__nv_bfloat16, 1, PACK>(a, st);
+    if (f32) return v == 4 ? launch<float, 4, PACK>(a, rows, st) : v == 2 ? launch<float, 2, PACK>(a, rows, st) : launch<float, 1, PACK>(a, rows, st);
+    return v == 8   ? launch<__nv_bfloat16, 8, PACK>(a, rows, st)
+           : v == 4 ? launch<__nv_bfloat16, 4, PACK>(a, rows, st)
+           : v == 2 ? launch<__nv_bfloat16, 2, PACK>(a, rows, st)
+                    : launch<__nv_bfloat16, 1, PACK>(a, rows, st);
 }
 
 int run(const e2ttt_pack_params* p, const void* x, void* y, int8_t* codes, uint8_t* scales, void* stream) {
@@ -102,10 +131,10 @@ int run(const e2ttt_pack_params* p, const void* x, void* y, int8_t* codes, uint8
     if (!aligned(data, p->io_dtype == E2TTT_F32 ? 4 : 2)) return E2TTT_ERR_ALIGN;
     const int rc = check_device();
     if (rc) return rc;
-    const PackArgs a{p->rows, 0, p->cols, (int)blocks, x, y, codes, scales};
+    const PackArgs a{0, p->cols, (int)blocks, x, y, codes, scales};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const bool f32 = p->io_dtype == E2TTT_F32;
-    return (x ? dispatch<true>(a, f32, st) : dispatch<false>(a, f32, st)) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+    return (x ? dispatch<true>(a, p->rows, f32, st) : dispatch<false>(a, p->rows, f32, st)) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
 }
 
 }  // namespace

@@ -26,28 +26,20 @@ struct Meet {
 
 constexpr int kMeet = (sizeof(Meet) + 127) / 128 * 128;
 
-// The 8-bit form of a warp's rows of one tensor: a lane takes 16 bytes, an aligned group of lanes a block.
+// The 8-bit form of a warp's rows of one tensor: a lane takes 32 bytes, half a block in bf16 and a quarter of one in fp32, and writes their codes at once.
 template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const IO* rows, uint8_t* codes, uint8_t* scales, int n, int lane) {
-    constexpr int V = 16 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;
-    const int row = lane / PER, piece = lane % PER;
+    constexpr int V = 32 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;  // lanes of a row; rows a warp takes at once
+    const int row = lane / PER, chunk = lane % PER;
 #pragma unroll
     for (int i = 0; i < ROWS; i += STEP) {
-        const uint4 raw = *reinterpret_cast<const uint4*>(rows + (row + i) * kScanCh + piece * V);
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        float v[V];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (V == 8) {
-                v[2 * j] = __uint_as_float(w[j] << 16);
-                v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            } else {
-                v[j] = __uint_as_float(w[j]);
-            }
-        }
-        const uint32_t byte = pack8::group_scale<V>(v);
+        struct alignas(16) Piece {
+            IO x[V];
+        };
+        const Piece p = *reinterpret_cast<const Piece*>(rows + (row + i) * kScanCh + chunk * V);
+        const uint32_t byte = pack8::group_scale<IO, V>(p.x);
         if (row + i >= n) continue;
-        *reinterpret_cast<pack8::Codes<V>*>(codes + (row + i) * kScanCh + piece * V) = pack8::encode<V>(v, byte);
-        if (piece % (pack8::kBlock / V) == 0) scales[(row + i) * 2 + piece / (pack8::kBlock / V)] = (uint8_t)byte;
+        *reinterpret_cast<pack8::Codes<V>*>(codes + (row + i) * kScanCh + chunk * V) = pack8::encode<IO, V>(p.x, byte);
+        if (chunk % (pack8::kBlock / V) == 0) scales[(row + i) * 2 + chunk / (pack8::kBlock / V)] = (uint8_t)byte;
     }
 }
 
@@ -115,6 +107,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         if (by != kByTile) copy_wait<kStages - 1>();
         else if (met && have > 0) met = await<false>(&full[slot], parity);
         __syncwarp();
+        if (PACK && have > 0) {
+            const int64_t row = unit * spans * kScanSpan + t0;
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+                pack_rows<IO, TOK>(rows + k * TOK * kScanCh, a.codes + k * a.code_step + row * kScanCh, a.scales + k * a.scale_step + row * 2, have, lane);
+        }
         float2 h[TOK], P[TOK], hh = dup(0.0f), pp = dup(1.0f);
         const bool plain = near && have == TOK && !starts;  // all tokens and channels are there, none is a start, no decay is far from 1
         auto walk = [&](auto is_plain) {
@@ -146,12 +144,6 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         };
         if (plain) walk(std::true_type{});
         else walk(std::false_type{});
-        if (PACK && have > 0) {
-            const int64_t row = unit * spans * kScanSpan + t0;
-#pragma unroll
-            for (int k = 0; k < NT; ++k)
-                pack_rows<IO, TOK>(rows + k * TOK * kScanCh, a.codes + k * a.code_step + row * kScanCh, a.scales + k * a.scale_step + row * 2, have, lane);
-        }
         __syncwarp();
         load((turn + 2) * parts + part, slot);
         meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
