@@ -180,15 +180,13 @@ template <int V> __device__ __forceinline__ Weights<V> weights(const float* w, i
 // of 2048 in bf16: 65 us with them, 72 without; fp32, whose threads take two pieces of four, 8000 tokens of 768: 41 and 35.
 template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256; }
 
-// A piece of one of the packed tensors: its codes, and by its block's first lane the scale.  Every lane of a warp calls; c is the piece's place in the row.
-template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scales, Piece<IO, V> p, int c, bool in) {
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (!in) p.x[j] = IO(0.0f);
-    const uint32_t byte = pack8::group_scale<IO, V>(p.x);
+// A piece of one of the packed tensors: its codes, and by its block's first lane the scale.  Every lane of a warp calls.
+template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scale, const Piece<IO, V>& p, bool in) {
+    const uint32_t byte = pack8::group_scale<IO, V>(p.x, in);
+    const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, byte, pack8::rare_scale(byte));
     if (!in) return;
-    *reinterpret_cast<pack8::Codes<V>*>(codes + c * V) = pack8::encode<IO, V>(p.x, byte);
-    if (c % (pack8::kBlock / V) == 0) scales[c / (pack8::kBlock / V)] = (uint8_t)byte;
+    *reinterpret_cast<pack8::Codes<V>*>(codes) = code;
+    if (threadIdx.x % (pack8::kBlock / V) == 0) *scale = (uint8_t)byte;
 }
 
 // PACK: o, x and a are also left in 8 bits, as they were read
@@ -237,27 +235,34 @@ __global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_
     int64_t tok = blockIdx.x;
     for (int i = 0; i + 1 < depth; ++i) load(tok + i * (int64_t)gridDim.x, i);
     int slot = 0;
+    uint8_t *code_at = a.packed + tok * k.code_row + tid * V, *scale_at = a.packed + k.scales + tok * k.scale_row + tid / (pack8::kBlock / V);
     for (; tok < tokens; tok += gridDim.x) {
         load(tok + (depth - 1) * (int64_t)gridDim.x, slot == 0 ? depth - 1 : slot - 1);
         copy_wait(depth - 1);
         const P* r = ring + slot * 3 * NC * T;
         slot = slot + 1 == depth ? 0 : slot + 1;
+        P held[PACK ? 3 * NC : 1];  // read once where they are also packed
         if constexpr (PACK) {
-            uint8_t *codes = a.packed + tok * k.code_row, *scales = a.packed + k.scales + tok * k.scale_row;
+#pragma unroll
+            for (int i = 0; i < 3 * NC; ++i) held[i] = r[i * T];
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const int c = tid + i * T;
-                keep_piece<IO, V>(codes, scales, r[i * T], c, c < cols);
-                keep_piece<IO, V>(codes + k.code_step, scales + k.scale_step, r[(NC + i) * T], c, c < cols);
-                if (a.a) keep_piece<IO, V>(codes + 2 * k.code_step, scales + 2 * k.scale_step, r[(2 * NC + i) * T], c, c < cols);
+                const bool in = tid + i * T < cols;
+                uint8_t *codes = code_at + i * T * V, *scales = scale_at + i * T / (pack8::kBlock / V);
+                keep_piece<IO, V>(codes, scales, held[i], in);
+                keep_piece<IO, V>(codes + k.code_step, scales + k.scale_step, held[NC + i], in);
+                if (a.a) keep_piece<IO, V>(codes + 2 * k.code_step, scales + 2 * k.scale_step, held[2 * NC + i], in);
             }
+            code_at += gridDim.x * k.code_row;
+            scale_at += gridDim.x * k.scale_row;
         }
+        auto piece = [&](int which, int i) { return PACK ? held[PACK ? which * NC + i : 0] : r[(which * NC + i) * T]; };
         float y[NC][V], hs[NC];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             hs[i] = 0.0f;
             if (tid + i * T >= cols) continue;
-            const P po = r[i * T];
+            const P po = piece(0, i);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 y[i][j] = ldf(po.x[j]);
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_
             const int c = tid + i * T;
             if (c >= cols) continue;
             const float inv = rsqrtf(fmaf(hs[i], per_d, a.post_eps));
-            const P px = r[(NC + i) * T], pa = r[(2 * NC + i) * T];
+            const P px = piece(1, i), pa = piece(2, i);
             const Weights<V> wr = kept<V, TMAX>() ? wrs[i] : weights<V>(a.res_scale, c), wp = kept<V, TMAX>() ? wps[i] : weights<V>(a.w_post, c);
             if (a.a) {
 #pragma unroll
@@ -352,6 +357,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
     const bool silu = a.gate == E2TTT_GATE_SILU;
     Place ahead(a, blockIdx.x, sums.G);
     const Stride stride(a, gridDim.x, sums.G);
+    const uint8_t *code_at = a.packed + blockIdx.x * k.code_row + tid * V, *scale_at = a.packed + k.scales + blockIdx.x * k.scale_row;
     auto load = [&](int64_t tok, int slot) {
         if (tok < tokens) {
             P* r = ring + slot * OWN * NC * T;
@@ -361,7 +367,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
                 if (c >= cols) continue;
                 if constexpr (PACK) {
                     const int at = slot * 3 * NC * T + i * T;
-                    const uint8_t *from = a.packed + tok * k.code_row + c * V, *scale = a.packed + k.scales + tok * k.scale_row + c / (pack8::kBlock / V) / 4 * 4;
+                    const uint8_t *from = code_at + i * T * V, *scale = scale_at + c / (pack8::kBlock / V * 4) * 4;
 #pragma unroll
                     for (int w = 0; w < 3; ++w) {
                         if (w == 2 && !gated) continue;
@@ -378,6 +384,10 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
             }
         }
         stride.move(ahead);
+        if constexpr (PACK) {
+            code_at += gridDim.x * k.code_row;
+            scale_at += gridDim.x * k.scale_row;
+        }
         copy_commit();
     };
     Place here = ahead;

@@ -55,19 +55,15 @@ template <typename IO, int V, bool FLAT> __global__ void __launch_bounds__(kThre
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {
         const Place<V, FLAT> p(a, first + k * kThreads);
-        if (p.in) {
-            v[k] = *reinterpret_cast<const Values<IO, V>*>(static_cast<const IO*>(a.x) + p.at);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[k].x[j] = IO(0.0f);
-        }
+        if (p.in) v[k] = *reinterpret_cast<const Values<IO, V>*>(static_cast<const IO*>(a.x) + p.at);
     }
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {
         const Place<V, FLAT> p(a, first + k * kThreads);
-        const uint32_t byte = group_scale<IO, V>(v[k].x);
+        const uint32_t byte = group_scale<IO, V>(v[k].x, p.in);
+        const Codes<V> code = encode<IO, V>(v[k].x, byte, rare_scale(byte));
         if (!p.in) continue;
-        *reinterpret_cast<Codes<V>*>(a.codes + p.at) = encode<IO, V>(v[k].x, byte);
+        *reinterpret_cast<Codes<V>*>(a.codes + p.at) = code;
         if (threadIdx.x % (kBlock / V) == 0) a.scales[p.block] = (uint8_t)byte;
     }
 }

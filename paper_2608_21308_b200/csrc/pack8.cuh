@@ -21,18 +21,36 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
 __device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float(byte == kNan ? 0u : (254u - byte) << 23); }
 __device__ __forceinline__ float scale(uint32_t byte) { return __uint_as_float(byte == kNan ? 0x7fc00000u : byte << 23); }
 
+// two fp32 values at a time (one instruction on this architecture)
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(r)
+        : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)), "l"(*reinterpret_cast<const uint64_t*>(&c)));
+    return *reinterpret_cast<const float2*>(&r);
+}
 // rint(x / scale) in the low byte: 1.5 2^23 has a step of 1
 __device__ __forceinline__ uint32_t code(float x, float inverse) { return __float_as_uint(fmaf(x, inverse, 12582912.0f)); }
+__device__ __forceinline__ void codes2(float x, float y, float inverse, uint32_t& cx, uint32_t& cy) {
+    const float2 r = fma2(make_float2(x, y), make_float2(inverse, inverse), make_float2(12582912.0f, 12582912.0f));
+    cx = __float_as_uint(r.x);
+    cy = __float_as_uint(r.y);
+}
 constexpr uint32_t kLargest = 248;  // scale byte of 2^121: the only one with values above 127 of its units
 __device__ __forceinline__ float limited(float x) { return fminf(fmaxf(x, -0x1.fcp127f), 0x1.fcp127f); }
 // low bytes of four words
 __device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// the J-th code of a word, as a number: 2^23 + (code + 128), less 2^23 + 128
-template <int J> __device__ __forceinline__ float number(uint32_t codes) {
-    return __uint_as_float(__byte_perm(codes ^ 0x80808080u, 0x4b000000u, 0x7440 + J)) - 8388736.0f;
+// the J-th code of a word, biased, as a number: 2^23 + 128 + code
+template <int J> __device__ __forceinline__ float biased(uint32_t codes) { return __uint_as_float(__byte_perm(codes ^ 0x80808080u, 0x4b000000u, 0x7440 + J)); }
+// two codes' values: (biased - (2^23 + 128)) scale, exact in one step; for scales from 2^104 on, where the product alone would be infinite (and for blocks of NaNs), in two
+__device__ __forceinline__ float2 values2(float2 b, float s, bool two_steps) {
+    if (two_steps) return make_float2((b.x - 8388736.0f) * s, (b.y - 8388736.0f) * s);
+    const float off = -8388736.0f * s;
+    return fma2(b, make_float2(s, s), make_float2(off, off));
 }
+__device__ __forceinline__ bool wants_two_steps(uint32_t byte) { return byte >= 231; }
 
 // bits of the largest magnitude among neighbouring values, as they lie in memory (bits of magnitudes are in the order of their values, NaNs on top)
 template <typename IO, int V> __device__ __forceinline__ uint32_t magnitude(const IO (&x)[V]) {
@@ -41,7 +59,7 @@ template <typename IO, int V> __device__ __forceinline__ uint32_t magnitude(cons
         uint32_t w[V / 2];
         memcpy(w, x, 2 * V);
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) m = __vmaxu2(m, w[j] & 0x7fff7fffu);
+        for (int j = 0; j < V / 2; ++j) asm("max.u16x2 %0, %0, %1;" : "+r"(m) : "r"(w[j] & 0x7fff7fffu));
         return max(m & 0xffff0000u, m << 16);
     } else {
 #pragma unroll
@@ -49,9 +67,9 @@ template <typename IO, int V> __device__ __forceinline__ uint32_t magnitude(cons
         return m;
     }
 }
-// the scale byte of V values whose block's other pieces lie in the other lanes of an aligned group of 32 / V lanes; every lane of the warp calls
-template <typename IO, int V> __device__ __forceinline__ uint32_t group_scale(const IO (&x)[V]) {
-    uint32_t m = magnitude<IO, V>(x);
+// the scale byte of V values whose block's other pieces lie in the other lanes of an aligned group of 32 / V lanes; every lane of the warp calls, with in = false if it has none
+template <typename IO, int V> __device__ __forceinline__ uint32_t group_scale(const IO (&x)[V], bool in = true) {
+    uint32_t m = in ? magnitude<IO, V>(x) : 0u;
 #pragma unroll
     for (int s = 1; s < kBlock / V; s <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
     return scale_byte(m);
@@ -60,12 +78,28 @@ template <typename IO, int V> __device__ __forceinline__ uint32_t group_scale(co
 template <int V> struct alignas(V) Codes {
     int8_t x[V];
 };
-template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t byte) {
+// V neighbouring values as fp32
+template <typename IO, int V> __device__ __forceinline__ void widen(const IO (&in)[V], float (&x)[V]) {
+    if constexpr (sizeof(IO) == 2 && V % 2 == 0) {
+        uint32_t w[V / 2];
+        memcpy(w, in, 2 * V);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            x[2 * j] = __uint_as_float(w[j] << 16);
+            x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = (float)in[j];
+    }
+}
+// `rare`: some lane's block has the largest scale or is not finite (a vote of the warp, so that the branch is one)
+__device__ __forceinline__ bool rare_scale(uint32_t byte) { return __any_sync(0xffffffffu, byte >= kLargest); }
+template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t byte, bool rare) {
     const float inv = inverse_scale(byte);
     float x[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = (float)in[j];
-    if (byte >= kLargest) {
+    widen<IO, V>(in, x);
+    if (rare) {
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] = byte == kNan ? 0.0f : limited(x[j]);
     }
@@ -73,7 +107,12 @@ template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const I
     if constexpr (V >= 4) {
         uint32_t w[V / 4];
 #pragma unroll
-        for (int k = 0; k < V / 4; ++k) w[k] = bytes4(code(x[4 * k], inv), code(x[4 * k + 1], inv), code(x[4 * k + 2], inv), code(x[4 * k + 3], inv));
+        for (int k = 0; k < V / 4; ++k) {
+            uint32_t c[4];
+            codes2(x[4 * k], x[4 * k + 1], inv, c[0], c[1]);
+            codes2(x[4 * k + 2], x[4 * k + 3], inv, c[2], c[3]);
+            w[k] = bytes4(c[0], c[1], c[2], c[3]);
+        }
         memcpy(&out, w, V);
     } else {
 #pragma unroll
@@ -86,12 +125,23 @@ template <int V> __device__ __forceinline__ void decode(const Codes<V>& c, uint3
     if constexpr (V >= 4) {
         uint32_t w[V / 4];
         memcpy(w, &c, V);
+        float2 v[V / 2];
 #pragma unroll
         for (int k = 0; k < V / 4; ++k) {
-            x[4 * k] = number<0>(w[k]) * s;
-            x[4 * k + 1] = number<1>(w[k]) * s;
-            x[4 * k + 2] = number<2>(w[k]) * s;
-            x[4 * k + 3] = number<3>(w[k]) * s;
+            v[2 * k] = make_float2(biased<0>(w[k]), biased<1>(w[k]));
+            v[2 * k + 1] = make_float2(biased<2>(w[k]), biased<3>(w[k]));
+        }
+        if (__builtin_expect(wants_two_steps(byte), 0)) {
+#pragma unroll
+            for (int k = 0; k < V / 2; ++k) v[k] = values2(v[k], s, true);
+        } else {
+#pragma unroll
+            for (int k = 0; k < V / 2; ++k) v[k] = values2(v[k], s, false);
+        }
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) {
+            x[2 * k] = v[k].x;
+            x[2 * k + 1] = v[k].y;
         }
     } else {
 #pragma unroll

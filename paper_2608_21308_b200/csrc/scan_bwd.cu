@@ -47,9 +47,9 @@ template <int K, typename IO, int NT> __device__ __forceinline__ float2 logit(co
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, true>& r, int j, int lane) {
     const uint32_t w = reinterpret_cast<const uint16_t*>(r.codes[K][j])[lane];
     // a block that is not finite has codes of 0 and an infinite scale: NaN
-    return mul2(make_float2(pack8::number<0>(w), pack8::number<1>(w)), dup(__uint_as_float((uint32_t)r.scales[K][j][lane >> 4] << 23)));
+    const float s = __uint_as_float((uint32_t)r.scales[K][j][lane >> 4] << 23);
+    return mul2(add2(make_float2(pack8::biased<0>(w), pack8::biased<1>(w)), dup(-8388736.0f)), dup(s));
 }
-
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 logit(const Rows<IO, NT, true>& r, int j, int lane) { return capped(input<K>(r, j, lane)); }
 
 template <typename IO, bool GATE, bool UNIT, bool PACK>
