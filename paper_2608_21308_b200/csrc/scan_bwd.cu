@@ -38,8 +38,13 @@ template <typename IO, int NT, bool PACK> struct alignas(128) Rows {
 template <typename IO, int NT> struct alignas(128) Rows<IO, NT, true> {
     uint8_t codes[NT][kTok][kScanCh];
     IO d_h[kTok][kScanCh];
-    alignas(16) uint8_t scales[NT][kTok][2];
+    alignas(128) uint8_t scales[NT][kTok][2];
     static constexpr int kBytes = NT * kTok * (kScanCh + 2) + kTok * kScanCh * (int)sizeof(IO);
+};
+
+// where a warp's gradients wait to be stored by the copy engine: in the place of what they are the gradients of, or, with packed inputs, in a place of their own
+template <typename IO, int NT, bool PACK> struct Outs {
+    IO g[PACK ? NT : 1][kTok][kScanCh];
 };
 
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(const Rows<IO, NT, false>& r, int j, int lane) { return row2<IO>(r.in[K][j], lane); }
@@ -52,7 +57,8 @@ template <int K, typename IO, int NT> __device__ __forceinline__ float2 input(co
 }
 template <int K, typename IO, int NT> __device__ __forceinline__ float2 logit(const Rows<IO, NT, true>& r, int j, int lane) { return capped(input<K>(r, j, lane)); }
 
-template <typename IO, bool GATE, bool UNIT, bool PACK>
+// TILE: rows are read by kByTile
+template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE>
 __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_kernel(const ScanBwdArgs ba, const __grid_constant__ ScanMaps maps, const int by, const bool pair, const int parts) {
     constexpr int NT = GATE ? 3 : 2;
     using R = Rows<IO, NT, PACK>;
@@ -60,12 +66,15 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     Meet& meet = *reinterpret_cast<Meet*>(smem);
     const ScanArgs& a = ba.f;
     const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
+    using O = Outs<IO, NT, PACK>;
     R* ring = reinterpret_cast<R*>(smem + kMeet) + warp * kStages;
+    O* outs = reinterpret_cast<O*>(smem + kMeet + kWarps * kStages * sizeof(R)) + warp;
     const int64_t blocks = a.s.blocks(), tiles = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
     const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
     const int64_t seq = b * L * (int64_t)D;
+    const bool even = (D & 1) == 0;  // rows of states (in the workspace) are pairs
     const Pairs pairs = make_pairs();
     float2 rate = load2<float>(a.rate, c0, n, false);
     const bool near = __syncthreads_and(whole && near_rate(rate.x) && near_rate(rate.y));
@@ -74,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     const int ender = parts == 1 ? 0 : kWarps - 1;
     if (warp == ender) meet.carry[1][lane] = end;
     uint64_t* full = meet.full[warp];
-    if (by == kByTile && lane == 0) {
+    if (TILE && lane == 0) {
         for (int i = 0; i < kStages; ++i) sm100::mbar_init(&full[i], 1);
         sm100::fence_mbar_init();
     }
@@ -87,7 +96,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             const int t = (int)(tile * kTile) + warp * kTok;
             R& to = ring[slot];
             const int64_t row = unit * tiles * kScanSpan + t;
-            if (by == kByTile) {
+            if constexpr (TILE) {
                 if (lane == 0) {
                     sm100::mbar_expect_tx(&full[slot], R::kBytes);
 #pragma unroll
@@ -96,10 +105,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                             bulk_load(to.codes[k][0], a.codes + k * a.code_step + row * kScanCh, kTok * kScanCh, &full[slot]);
                             bulk_load(to.scales[k][0], a.scales + k * a.scale_step + row * 2, kTok * 2, &full[slot]);
                         } else {
-                            tile_load(to.in[k][0], &maps.m[k], first, t, (int)b, &full[slot]);
+                            tile_load(to.in[k][0], &maps.in[k], first, t, (int)b, &full[slot]);
                         }
                     }
-                    tile_load(to.d_h[0], &maps.m[3], first, t, (int)b, &full[slot]);
+                    tile_load(to.d_h[0], &maps.in[3], first, t, (int)b, &full[slot]);
                 }
             } else {
                 if constexpr (PACK) {
@@ -117,12 +126,14 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             }
             if (a.starts && lane < kTok && t + lane < L) next_first = a.starts[b * L + t + lane];
         }
-        if (by != kByTile) copy_commit();
+        if (!TILE) copy_commit();
     };
     const int64_t turns = (tiles + parts - 1) / parts;
     load((turns - 1) * parts + part, 0);
     unsigned byte0 = next_first;
     load((turns - 2) * parts + part, 1);
+    auto state_of = [&](int64_t tile) { return tile >= 0 && tile < tiles ? load2<float>(a.states, (b * tiles + tile) * D + c0, n, even) : dup(0.0f); };
+    float2 next_state = state_of((turns - 1) * parts + part);  // a turn ahead
     int slot = 0;
     uint32_t parity = 0, taken = 0;  // taken: which phase a stage's barrier is in (a warp may have no tokens in the first turn)
     bool met = true;
@@ -131,9 +142,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         const int t0 = (int)min(tile * kTile + warp * kTok, (int64_t)L), have = min(kTok, L - t0);
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
         byte0 = next_first;
-        float2 state = tile < tiles ? load2<float>(a.states, (b * tiles + tile) * D + c0, n, false) : dup(0.0f);
-        const R& rows = ring[slot];
-        if (by != kByTile) {
+        float2 state = next_state;
+        next_state = state_of(tile - parts);
+        R& rows = ring[slot];
+        if constexpr (!TILE) {
             copy_wait<kStages - 1>();
         } else if (have > 0) {
             if (met) met = await<false>(&full[slot], taken >> slot & 1);
@@ -187,6 +199,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         };
         if (plain) gather(std::true_type{});
         else gather(std::false_type{});
+        if (TILE && turn != turns - 1) {  // the last turn's gradients have left its stage by now
+            if (lane == 0) bulk_read_done();
+            __syncwarp();
+            load((turn - 1) * parts + part, slot ^ 1);
+            byte0 = next_first;
+        }
         meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
         meet.ends[slot][warp][lane] = v;
         __syncthreads();
@@ -247,33 +265,51 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 state = fma2(bj, pairs.minus_one, start ? dup(0.0f) : fade<PLAIN>(state, c[j], far >> 2 * j));
             }
             const int64_t at = seq + (int64_t)t0 * D + c0;
-            const int m = PLAIN ? 2 : n;
-            const bool two = PLAIN || pair;
+            auto put = [&](int k, void* out, int j, float2 v) {
+                if constexpr (TILE && PACK) put_row2<IO>(outs->g[k][j], lane, v);
+                else if constexpr (TILE) put_row2<IO>(rows.in[k][j], lane, v);
+                else store2<IO>(out, at + j * (int64_t)D, PLAIN ? 2 : n, PLAIN || pair, v);
+            };
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {
                 if (!PLAIN && j >= have) continue;
                 const bool start = !PLAIN && (starts >> j & 1);
-                const int64_t to = at + j * (int64_t)D;
                 in = add2(in, row2<IO>(rows.d_h[j], lane));
                 const float2 minus = mul2(in, pairs.minus_one);
-                store2<IO>(ba.d_x, to, m, two, mul2(minus, to_x[j]));
-                if (GATE) store2<IO>(ba.d_g, to, m, two, mul2(minus, meet.stash[warp][j][lane]));
+                put(0, ba.d_x, j, mul2(minus, to_x[j]));
+                if (GATE) put(2, ba.d_g, j, mul2(minus, meet.stash[warp][j][lane]));
                 in = start ? dup(0.0f) : fade<PLAIN>(in, c[j], far >> 2 * j);  // a lam
                 const float2 dl = start ? dup(0.0f) : mul2(in, to_r[j]);      // d_log_a sg
                 sum = add2(sum, dl);
-                store2<IO>(ba.d_r, to, m, two, mul2(dl, to_a[j]));
+                put(1, ba.d_r, j, mul2(dl, to_a[j]));
             }
         };
         if (plain) spread(std::true_type{});
         else spread(std::false_type{});
-        __syncwarp();
-        load((turn - 2) * parts + part, slot);
+        if constexpr (TILE) {
+            sm100::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && have > 0) {
+#pragma unroll
+                for (int k = 0; k < NT; ++k) {
+                    const IO* from = nullptr;
+                    if constexpr (PACK) from = outs->g[k][0];
+                    else from = rows.in[k][0];
+                    tile_store(&maps.out[k], first, t0, (int)b, from);
+                }
+                bulk_commit();
+            }
+        } else {
+            __syncwarp();
+            load((turn - 2) * parts + part, slot);
+        }
     }
     if (part == 0 && warp == ender) store2<float>(ba.dh_init, b * D + c0, n, false, end);
     __syncthreads();
     meet.ends[0][warp][lane] = make_float2(-sum.x, -sum.y);
     __syncthreads();
-    if (by != kByTile) copy_wait<0>();
+    if (TILE) bulk_done();
+    else copy_wait<0>();
     if (warp != 0) return;
     sum = meet.ends[0][0][lane];
     for (int w = 1; w < kWarps; ++w) sum = add2(sum, meet.ends[0][w][lane]);
@@ -294,16 +330,16 @@ __global__ void __launch_bounds__(256) scan_rate_kernel(const float* part, float
     d_rate[c] = y;
 }
 
-template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwdArgs& b, int by, bool pair, cudaStream_t st) {
-    auto kernel = scan_bwd_kernel<IO, GATE, UNIT, PACK>;
-    cudaError_t e = allow_shared_memory<scan_bwd_kernel<IO, GATE, UNIT, PACK>>();
+template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE> int launch(const ScanBwdArgs& b, const ScanMaps& maps, int by, bool pair, cudaStream_t st) {
+    auto kernel = scan_bwd_kernel<IO, GATE, UNIT, PACK, TILE>;
+    cudaError_t e = allow_shared_memory<scan_bwd_kernel<IO, GATE, UNIT, PACK, TILE>>();
     if (e != cudaSuccess) return (int)e;
     const ScanShape& s = b.f.s;
     const int parts = scan_bwd_parts(s);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(s.B * s.blocks() * parts));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kMeet + kStages * kWarps * sizeof(Rows<IO, GATE ? 3 : 2, PACK>);
+    cfg.dynamicSmemBytes = kMeet + kStages * kWarps * sizeof(Rows<IO, GATE ? 3 : 2, PACK>) + (PACK ? kWarps * sizeof(Outs<IO, GATE ? 3 : 2, true>) : 0);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -311,14 +347,20 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwd
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;
-    ScanMaps maps{};
-    const void* in[4] = {b.f.x, b.f.r, b.f.g, b.d_h};
-    for (int k = PACK ? 3 : 0; by == kByTile && k < 4; ++k)
-        if (in[k] && !scan_map(&maps.m[k], in[k], s, kTok)) by = kBy4;
     e = cudaLaunchKernelEx(&cfg, kernel, b, maps, by, pair, parts);
     if (e != cudaSuccess) return (int)e;
     scan_rate_kernel<<<(s.D + 31) / 32, 256, 0, st>>>(b.part, b.d_rate, (int64_t)s.B * parts, s.D);
     return (int)cudaGetLastError();
+}
+template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwdArgs& b, int by, bool pair, cudaStream_t st) {
+    ScanMaps maps{};
+    const void* in[4] = {b.f.x, b.f.r, b.f.g, b.d_h};
+    for (int k = PACK ? 3 : 0; by == kByTile && k < 4; ++k)
+        if (in[k] && !scan_map(&maps.in[k], in[k], b.f.s, kTok)) by = kBy4;
+    const void* out[3] = {b.d_x, b.d_r, b.d_g};
+    for (int k = 0; by == kByTile && k < (GATE ? 3 : 2); ++k)
+        if (!scan_map(&maps.out[k], out[k], b.f.s, kTok)) by = kBy4;
+    return by == kByTile ? launch<IO, GATE, UNIT, PACK, true>(b, maps, by, pair, st) : launch<IO, GATE, UNIT, PACK, false>(b, maps, by, pair, st);
 }
 template <typename IO, bool GATE, bool UNIT> int launch(const ScanBwdArgs& b, int by, bool pair, cudaStream_t st) {
     return b.f.codes ? launch<IO, GATE, UNIT, true>(b, by, pair, st) : launch<IO, GATE, UNIT, false>(b, by, pair, st);
@@ -337,7 +379,8 @@ int scan_bwd_launch(const ScanBwdArgs& b, void* stream) {
     uintptr_t in = reinterpret_cast<uintptr_t>(b.d_h), out = 0;
     if (!b.f.codes) in |= reinterpret_cast<uintptr_t>(b.f.x) | reinterpret_cast<uintptr_t>(b.f.r) | reinterpret_cast<uintptr_t>(b.f.g);
     for (const void* p : {b.d_x, b.d_r, b.d_g}) out |= reinterpret_cast<uintptr_t>(p);
-    const int by = reads_by(b.f.s.D, b.f.s.f32, in);
+    int by = reads_by(b.f.s.D, b.f.s.f32, in);
+    if (by == kByTile && out % 16 != 0) by = kBy4;
     const bool pair = b.f.s.D % 2 == 0 && out % (b.f.s.f32 ? 8 : 4) == 0;
     return b.f.s.f32 ? dispatch<float>(b, by, pair, st) : dispatch<__nv_bfloat16>(b, by, pair, st);
 }

@@ -203,11 +203,18 @@ __device__ __forceinline__ void tile_load(void* dst, const void* map, int c, int
                  "r"(b), "r"(smem_at(bar))
                  : "memory");
 }
+// a tile from shared memory; what lies outside the tensor is not written
+__device__ __forceinline__ void tile_store(const void* map, int c, int t, int b, const void* src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(c), "r"(t), "r"(b), "r"(smem_at(src)) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_read_done() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }  // shared memory may be written again
+__device__ __forceinline__ void bulk_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_at(dst)), "l"(src), "r"(bytes), "r"(smem_at(bar)) : "memory");
 }
 
-// How rows are read: tiles by the copy engine (addresses and row lengths that are a multiple of 16 bytes; one lane starts them, and no other instruction waits for a place in the
+// How rows are read (fp32 always by one of the first two): tiles by the copy engine (addresses and row lengths that are a multiple of 16 bytes; one lane starts them, and no other instruction waits for a place in the
 // load queue), pieces of 4 bytes, or value by value (odd rows, and addresses, of bf16)
 enum { kByTile = 0, kBy4 = 1, kByValue = 2 };
 inline int reads_by(int D, bool f32, uintptr_t all) {
@@ -218,24 +225,42 @@ inline int reads_by(int D, bool f32, uintptr_t all) {
 
 // ROWS tokens of `src` from row t on, channels c .. c + 63, as far as there are tokens (L) and channels (D); `at` is where token 0 of the sequence starts
 template <typename IO, int ROWS> __device__ __forceinline__ void copy_rows(IO* dst, const IO* src, int64_t at, int t, int L, int c, int D, int by, int lane) {
-    constexpr int V = 4 / (int)sizeof(IO);
+    const IO* from = src + (at + (int64_t)t * D + c);
     if (by == kBy4) {
-        for (int i = lane; i < ROWS * kScanCh / V; i += 32) {
-            const int row = i / (kScanCh / V), ch = i % (kScanCh / V) * V;
-            const bool in = c + ch < D && t + row < L;
-            copy4(dst + row * kScanCh + ch, in ? src + at + (int64_t)(t + row) * D + c + ch : src, in);
+        constexpr int V = 4 / (int)sizeof(IO), WORDS = kScanCh / V / 32;  // words of a row that a lane copies
+#pragma unroll
+        for (int h = 0; h < WORDS; ++h) {
+            const int ch = (lane + 32 * h) * V;
+            const IO* p = from + ch;
+#pragma unroll
+            for (int row = 0; row < ROWS; ++row, p += D) {
+                const bool in = c + ch < D && t + row < L;
+                copy4(dst + row * kScanCh + ch, in ? p : src, in);
+            }
         }
         return;
     }
-    for (int i = lane; i < ROWS * kScanCh; i += 32) {
-        const int row = i / kScanCh, ch = i % kScanCh;
-        IO v = IO(0.0f);
-        if (c + ch < D && t + row < L) v = src[at + (int64_t)(t + row) * D + c + ch];
-        dst[i] = v;
+    if constexpr (sizeof(IO) == 2) {
+        const IO* p = from + 2 * lane;
+        const int n = D - c - 2 * lane;
+        uint32_t w[ROWS];
+#pragma unroll
+        for (int row = 0; row < ROWS; ++row, p += D) {
+            uint32_t x = 0, y = 0;
+            if (t + row < L && n > 0) x = *reinterpret_cast<const uint16_t*>(p);
+            if (t + row < L && n > 1) y = *reinterpret_cast<const uint16_t*>(p + 1);
+            w[row] = x | y << 16;
+        }
+#pragma unroll
+        for (int row = 0; row < ROWS; ++row) reinterpret_cast<uint32_t*>(dst + row * kScanCh)[lane] = w[row];
     }
 }
 
 // a lane's two channels of a row in shared memory
+template <typename IO> __device__ __forceinline__ void put_row2(IO* row, int lane, float2 v) {
+    if constexpr (sizeof(IO) == 4) reinterpret_cast<float2*>(row)[lane] = v;
+    else reinterpret_cast<__nv_bfloat162*>(row)[lane] = __floats2bfloat162_rn(v.x, v.y);
+}
 template <typename IO> __device__ __forceinline__ float2 row2(const IO* row, int lane) {
     if constexpr (sizeof(IO) == 4) {
         return reinterpret_cast<const float2*>(row)[lane];

@@ -44,9 +44,10 @@ template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const
     }
 }
 
-template <typename IO, bool GATE, bool UNIT, bool PACK>
+// TILE: rows are read by kByTile
+template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE>
 __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a, const __grid_constant__ ScanMaps maps, const int by, const bool pair, const int parts) {
-    constexpr int TOK = kTokOf<IO>, TILE = TOK * kWarps, NT = GATE ? 3 : 2;
+    constexpr int TOK = kTokOf<IO>, kTile = TOK * kWarps, NT = GATE ? 3 : 2;
     extern __shared__ __align__(128) char smem[];
     Meet& meet = *reinterpret_cast<Meet*>(smem);
     const int D = a.s.D, L = a.s.L, lane = threadIdx.x & 31, warp = __shfl_sync(kAll, threadIdx.x >> 5, 0);
@@ -64,24 +65,24 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     const int ender = parts == 1 ? kWarps - 1 : 0;
     if (warp == ender) meet.carry[1][lane] = end;
     uint64_t* full = meet.full[warp];
-    if (by == kByTile && lane == 0) {
+    if (TILE && lane == 0) {
         for (int i = 0; i < kStages; ++i) sm100::mbar_init(&full[i], 1);
         sm100::fence_mbar_init();
     }
     __syncwarp();
     if (parts > 1) meeting_init(meet.meeting);
-    const int64_t tiles = ((int64_t)L + TILE - 1) / TILE;
+    const int64_t tiles = ((int64_t)L + kTile - 1) / kTile;
     unsigned next_first = 0;
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
-        if (tile * TILE + warp * TOK < L) {
-            const int t = (int)(tile * TILE) + warp * TOK;
+        if (tile * kTile + warp * TOK < L) {
+            const int t = (int)(tile * kTile) + warp * TOK;
             IO* to = ring + slot * (NT * TOK * kScanCh);
-            if (by == kByTile) {
+            if constexpr (TILE) {
                 if (lane == 0) {
                     sm100::mbar_expect_tx(&full[slot], NT * TOK * kScanCh * sizeof(IO));
 #pragma unroll
-                    for (int k = 0; k < NT; ++k) tile_load(to + k * TOK * kScanCh, &maps.m[k], first, t, (int)b, &full[slot]);
+                    for (int k = 0; k < NT; ++k) tile_load(to + k * TOK * kScanCh, &maps.in[k], first, t, (int)b, &full[slot]);
                 }
             } else {
                 copy_rows<IO, TOK>(to, static_cast<const IO*>(a.x), seq, t, L, first, D, by, lane);
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
             }
             if (a.starts && lane < TOK && t + lane < L) next_first = a.starts[b * L + t + lane];
         }
-        if (by != kByTile) copy_commit();
+        if (!TILE) copy_commit();
     };
     load(part, 0);
     unsigned byte0 = next_first;
@@ -101,11 +102,11 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     // every CTA of a cluster takes every turn: its part of the last one may be empty
     for (int64_t turn = 0; turn * parts < tiles; ++turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
-        const int t0 = (int)min(tile * TILE + warp * TOK, (int64_t)L), have = min(TOK, L - t0);
+        const int t0 = (int)min(tile * kTile + warp * TOK, (int64_t)L), have = min(TOK, L - t0);
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
         byte0 = next_first;
         const IO* rows = ring + slot * (NT * TOK * kScanCh);
-        if (by != kByTile) copy_wait<kStages - 1>();
+        if (!TILE) copy_wait<kStages - 1>();
         else if (met && have > 0) met = await<false>(&full[slot], parity);
         __syncwarp();
         if (PACK && have > 0) {
@@ -203,15 +204,15 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         }
     }
     if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
-    if (by != kByTile) copy_wait<0>();
+    if (!TILE) copy_wait<0>();
 }
 
 // CTAs of a cluster
 int parts_of(const ScanShape& s) { return scan_parts(s, kTokOf<__nv_bfloat16> * kWarps, 2); }
 
-template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
-    auto kernel = scan_fwd_kernel<IO, GATE, UNIT, PACK>;
-    cudaError_t e = allow_shared_memory<scan_fwd_kernel<IO, GATE, UNIT, PACK>>();
+template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE> int launch(const ScanArgs& a, const ScanMaps& maps, int by, bool pair, cudaStream_t st) {
+    auto kernel = scan_fwd_kernel<IO, GATE, UNIT, PACK, TILE>;
+    cudaError_t e = allow_shared_memory<scan_fwd_kernel<IO, GATE, UNIT, PACK, TILE>>();
     if (e != cudaSuccess) return (int)e;
     const int parts = parts_of(a.s);
     cudaLaunchConfig_t cfg{};
@@ -225,11 +226,14 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArg
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;
+    return (int)cudaLaunchKernelEx(&cfg, kernel, a, maps, by, pair, parts);
+}
+template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
     ScanMaps maps{};
     const void* in[3] = {a.x, a.r, a.g};
     for (int k = 0; by == kByTile && k < (GATE ? 3 : 2); ++k)
-        if (!scan_map(&maps.m[k], in[k], a.s, kTokOf<IO>)) by = kBy4;
-    return (int)cudaLaunchKernelEx(&cfg, kernel, a, maps, by, pair, parts);
+        if (!scan_map(&maps.in[k], in[k], a.s, kTokOf<IO>)) by = kBy4;
+    return by == kByTile ? launch<IO, GATE, UNIT, PACK, true>(a, maps, by, pair, st) : launch<IO, GATE, UNIT, PACK, false>(a, maps, by, pair, st);
 }
 template <typename IO, bool GATE, bool UNIT> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
     return a.codes ? launch<IO, GATE, UNIT, true>(a, by, pair, st) : launch<IO, GATE, UNIT, false>(a, by, pair, st);

@@ -9,7 +9,7 @@
 namespace e2ttt {
 
 struct ScanMaps {
-    CUtensorMap m[4];
+    CUtensorMap in[4], out[3];
 };
 
 inline bool scan_map(CUtensorMap* map, const void* base, const ScanShape& s, int tokens) {
