@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     const int64_t blocks = a.s.blocks(), spans = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
-    const bool whole = pair && first + kScanCh <= D;  // all channels are there, and stored in pairs
+    const bool whole = (TILE || pair) && first + kScanCh <= D;  // all channels are there, and stored in pairs
     IO* ring = reinterpret_cast<IO*>(smem + kMeet) + warp * (kStages * NT * TOK * kScanCh);
     const int64_t seq = b * L * (int64_t)D;
     const Pairs pairs = make_pairs();
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         const int t0 = (int)min(tile * kTile + warp * TOK, (int64_t)L), have = min(TOK, L - t0);
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
         byte0 = next_first;
-        const IO* rows = ring + slot * (NT * TOK * kScanCh);
+        IO* rows = ring + slot * (NT * TOK * kScanCh);
         if (!TILE) copy_wait<kStages - 1>();
         else if (met && have > 0) met = await<false>(&full[slot], parity);
         __syncwarp();
@@ -147,7 +147,14 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         if (plain) walk(std::true_type{});
         else walk(std::false_type{});
         __syncwarp();
-        load((turn + 2) * parts + part, slot);
+        if constexpr (!TILE) {
+            load((turn + 2) * parts + part, slot);
+        } else if (turn != 0) {  // the last turn's states have left its stage by now
+            if (lane == 0) bulk_read_done();
+            __syncwarp();
+            load((turn + 1) * parts + part, slot ^ 1);
+            byte0 = next_first;
+        }
         meet.runs[slot][warp][lane] = make_float4(pp.x, pp.y, hh.x, hh.y);
         __syncthreads();
         const float2 before = meet.carry[slot ^ 1][lane];  // the state before the turn's tokens
@@ -193,18 +200,31 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
         if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
         if (!a.h) continue;
-        const int64_t at = seq + (int64_t)t0 * D + c0;
-        if (plain) {
+        if constexpr (TILE) {  // in the place of x
+            if (plain) {
 #pragma unroll
-            for (int j = 0; j < TOK; ++j) store2<IO>(a.h, at + j * (int64_t)D, 2, true, fma2(P[j], in, h[j]));
+                for (int j = 0; j < TOK; ++j) put_row2<IO>(rows + j * kScanCh, lane, fma2(P[j], in, h[j]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < TOK; ++j)
+                    if (j < have) put_row2<IO>(rows + j * kScanCh, lane, through<true>(P[j], in, h[j]));
+            }
+            sm100::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && have > 0) {
+                tile_store(&maps.out[0], first, t0, (int)b, rows);
+                bulk_commit();
+            }
         } else {
+            const int64_t at = seq + (int64_t)t0 * D + c0;
 #pragma unroll
             for (int j = 0; j < TOK; ++j)
                 if (j < have) store2<IO>(a.h, at + j * (int64_t)D, n, pair, through<true>(P[j], in, h[j]));
         }
     }
     if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
-    if (!TILE) copy_wait<0>();
+    if (TILE) bulk_done();
+    else copy_wait<0>();
 }
 
 // CTAs of a cluster
@@ -233,6 +253,7 @@ template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanArg
     const void* in[3] = {a.x, a.r, a.g};
     for (int k = 0; by == kByTile && k < (GATE ? 3 : 2); ++k)
         if (!scan_map(&maps.in[k], in[k], a.s, kTokOf<IO>)) by = kBy4;
+    if (by == kByTile && a.h && !scan_map(&maps.out[0], a.h, a.s, kTokOf<IO>)) by = kBy4;
     return by == kByTile ? launch<IO, GATE, UNIT, PACK, true>(a, maps, by, pair, st) : launch<IO, GATE, UNIT, PACK, false>(a, maps, by, pair, st);
 }
 template <typename IO, bool GATE, bool UNIT> int launch(const ScanArgs& a, int by, bool pair, cudaStream_t st) {
@@ -248,7 +269,8 @@ template <typename IO> int dispatch(const ScanArgs& a, int by, bool pair, cudaSt
 int scan_fwd_launch(const ScanArgs& a, void* stream) {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const uintptr_t in = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.r) | reinterpret_cast<uintptr_t>(a.g);
-    const int by = reads_by(a.s.D, a.s.f32, in);
+    int by = reads_by(a.s.D, a.s.f32, in);
+    if (by == kByTile && reinterpret_cast<uintptr_t>(a.h) % 16 != 0) by = kBy4;
     const bool pair = a.s.D % 2 == 0 && reinterpret_cast<uintptr_t>(a.h) % (a.s.f32 ? 8 : 4) == 0;
     return a.s.f32 ? dispatch<float>(a, by, pair, st) : dispatch<__nv_bfloat16>(a, by, pair, st);
 }
