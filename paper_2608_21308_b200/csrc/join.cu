@@ -182,8 +182,8 @@ template <int V, int TMAX> constexpr bool kept() { return V == 8 && TMAX == 256;
 
 // A piece of one of the packed tensors: its codes, and by its block's first lane the scale.  Every lane of a warp calls.
 template <typename IO, int V> __device__ __forceinline__ void keep_piece(uint8_t* codes, uint8_t* scale, const Piece<IO, V>& p, bool in) {
-    const uint32_t byte = pack8::group_scale<IO, V>(p.x, in);
-    const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, byte, pack8::rare_scale(byte));
+    uint32_t byte;
+    const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, pack8::group_magnitude<IO, V>(p.x, in), byte);
     if (!in) return;
     *reinterpret_cast<pack8::Codes<V>*>(codes) = code;
     if (threadIdx.x % (pack8::kBlock / V) == 0) *scale = (uint8_t)byte;

@@ -60,8 +60,8 @@ template <typename IO, int V, bool FLAT> __global__ void __launch_bounds__(kThre
 #pragma unroll
     for (int k = 0; k < kDeep; ++k) {
         const Place<V, FLAT> p(a, first + k * kThreads);
-        const uint32_t byte = group_scale<IO, V>(v[k].x, p.in);
-        const Codes<V> code = encode<IO, V>(v[k].x, byte, rare_scale(byte));
+        uint32_t byte;
+        const Codes<V> code = encode<IO, V>(v[k].x, group_magnitude<IO, V>(v[k].x, p.in), byte);
         if (!p.in) continue;
         *reinterpret_cast<Codes<V>*>(a.codes + p.at) = code;
         if (threadIdx.x % (kBlock / V) == 0) a.scales[p.block] = (uint8_t)byte;

@@ -11,14 +11,10 @@ namespace pack8 {
 constexpr int kBlock = 32;
 constexpr uint32_t kNan = 255;  // scale byte of a block that holds a NaN or an infinity
 
-// Scale byte e + 127 of a block whose largest magnitude has these bits: the smallest e with 127 2^e >= m 2^k, that is k - 6 up to m = 127 / 64 and k - 5 above it.
-// An infinity or a NaN has bits from 0x7f800000 on (a NaN must arrive as its bits: compare as integers, not by fmaxf).
-__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
-    const int e = (int)((bits + 0x1ffffu) >> 23) - 6;
-    return bits >= 0x7f800000u ? kNan : (uint32_t)max(1, min(248, e));
-}
-// 2^-e; 0 for a block that is not finite
-__device__ __forceinline__ float inverse_scale(uint32_t byte) { return __uint_as_float(byte == kNan ? 0u : (254u - byte) << 23); }
+// Scale byte e + 127 of a block whose largest magnitude has these bits: the smallest e with 127 2^e >= m 2^k, that is k - 6 up to m = 127 / 64 and k - 5 above it.  Up to
+// kOrdinary, 127 2^121; what is above (and infinities and NaNs, from 0x7f800000 on) encode() sees to.
+constexpr uint32_t kOrdinary = 0x7f7e0000u, kLargest = 248;
+__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) { return (uint32_t)max(1, (int)((bits + 0x1ffffu) >> 23) - 6); }
 __device__ __forceinline__ float scale(uint32_t byte) { return __uint_as_float(byte == kNan ? 0x7fc00000u : byte << 23); }
 
 // two fp32 values at a time (one instruction on this architecture)
@@ -36,7 +32,6 @@ __device__ __forceinline__ void codes2(float x, float y, float inverse, uint32_t
     cx = __float_as_uint(r.x);
     cy = __float_as_uint(r.y);
 }
-constexpr uint32_t kLargest = 248;  // scale byte of 2^121: the only one with values above 127 of its units
 __device__ __forceinline__ float limited(float x) { return fminf(fmaxf(x, -0x1.fcp127f), 0x1.fcp127f); }
 // low bytes of four words
 __device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -67,12 +62,12 @@ template <typename IO, int V> __device__ __forceinline__ uint32_t magnitude(cons
         return m;
     }
 }
-// the scale byte of V values whose block's other pieces lie in the other lanes of an aligned group of 32 / V lanes; every lane of the warp calls, with in = false if it has none
-template <typename IO, int V> __device__ __forceinline__ uint32_t group_scale(const IO (&x)[V], bool in = true) {
+// the same of the block of V values whose other pieces lie in the other lanes of an aligned group of 32 / V lanes; every lane of the warp calls, with in = false if it has none
+template <typename IO, int V> __device__ __forceinline__ uint32_t group_magnitude(const IO (&x)[V], bool in = true) {
     uint32_t m = in ? magnitude<IO, V>(x) : 0u;
 #pragma unroll
     for (int s = 1; s < kBlock / V; s <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, s));
-    return scale_byte(m);
+    return m;
 }
 
 template <int V> struct alignas(V) Codes {
@@ -93,16 +88,18 @@ template <typename IO, int V> __device__ __forceinline__ void widen(const IO (&i
         for (int j = 0; j < V; ++j) x[j] = (float)in[j];
     }
 }
-// `rare`: some lane's block has the largest scale or is not finite (a vote of the warp, so that the branch is one)
-__device__ __forceinline__ bool rare_scale(uint32_t byte) { return __any_sync(0xffffffffu, byte >= kLargest); }
-template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t byte, bool rare) {
-    const float inv = inverse_scale(byte);
+// Codes of V values of a block and its scale byte, from the bits of its largest magnitude.  Every lane of the warp calls: what is out of the ordinary is one branch, by a vote.
+template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t bits, uint32_t& byte) {
+    byte = scale_byte(bits);
     float x[V];
     widen<IO, V>(in, x);
-    if (rare) {
+    if (__any_sync(0xffffffffu, bits > kOrdinary)) {
+        byte = min(byte, kLargest);
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = byte == kNan ? 0.0f : limited(x[j]);
+        for (int j = 0; j < V; ++j) x[j] = bits >= 0x7f800000u ? 0.0f : limited(x[j]);
     }
+    const float inv = __uint_as_float((254u - byte) << 23);  // 2^-e
+    if (bits >= 0x7f800000u) byte = kNan;
     Codes<V> out;
     if constexpr (V >= 4) {
         uint32_t w[V / 4];
@@ -121,8 +118,8 @@ template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const I
     return out;
 }
 template <int V> __device__ __forceinline__ void decode(const Codes<V>& c, uint32_t byte, float (&x)[V]) {
-    const float s = scale(byte);
     if constexpr (V >= 4) {
+        const float s = __uint_as_float(byte << 23);  // infinite for a block of NaNs, which takes the other branch
         uint32_t w[V / 4];
         memcpy(w, &c, V);
         float2 v[V / 2];
@@ -133,7 +130,7 @@ template <int V> __device__ __forceinline__ void decode(const Codes<V>& c, uint3
         }
         if (__builtin_expect(wants_two_steps(byte), 0)) {
 #pragma unroll
-            for (int k = 0; k < V / 2; ++k) v[k] = values2(v[k], s, true);
+            for (int k = 0; k < V / 2; ++k) v[k] = values2(v[k], scale(byte), true);
         } else {
 #pragma unroll
             for (int k = 0; k < V / 2; ++k) v[k] = values2(v[k], s, false);
@@ -145,7 +142,7 @@ template <int V> __device__ __forceinline__ void decode(const Codes<V>& c, uint3
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = (float)c.x[j] * s;
+        for (int j = 0; j < V; ++j) x[j] = (float)c.x[j] * scale(byte);
     }
 }
 

@@ -264,11 +264,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 to_r[j] = start ? dup(0.0f) : UNIT ? fma2(to_r[j], pairs.minus_one, mul2(sg[j], state)) : mul2(sg[j], state);
                 state = fma2(bj, pairs.minus_one, start ? dup(0.0f) : fade<PLAIN>(state, c[j], far >> 2 * j));
             }
-            const int64_t at = seq + (int64_t)t0 * D + c0;
             auto put = [&](int k, void* out, int j, float2 v) {
                 if constexpr (TILE && PACK) put_row2<IO>(outs->g[k][j], lane, v);
                 else if constexpr (TILE) put_row2<IO>(rows.in[k][j], lane, v);
-                else store2<IO>(out, at + j * (int64_t)D, PLAIN ? 2 : n, PLAIN || pair, v);
+                else store2<IO>(out, seq + (t0 + j) * (int64_t)D + c0, PLAIN ? 2 : n, PLAIN || pair, v);
             };
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {

@@ -36,8 +36,8 @@ template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const
             IO x[V];
         };
         const Piece p = *reinterpret_cast<const Piece*>(rows + (row + i) * kScanCh + chunk * V);
-        const uint32_t byte = pack8::group_scale<IO, V>(p.x);
-        const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, byte, pack8::rare_scale(byte));
+        uint32_t byte;
+        const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, pack8::group_magnitude<IO, V>(p.x), byte);
         if (row + i >= n) continue;
         *reinterpret_cast<pack8::Codes<V>*>(codes + (row + i) * kScanCh + chunk * V) = code;
         if (chunk % (pack8::kBlock / V) == 0) scales[(row + i) * 2 + chunk / (pack8::kBlock / V)] = (uint8_t)byte;
