@@ -258,9 +258,10 @@ def test_logits_without_bound_and_a_rate_of_zero(io):
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("save", ["states", "packed"])
 @pytest.mark.parametrize("where,bad", [("x", np.nan), ("x", np.inf), ("r", np.nan), ("g", np.nan)])
-def test_what_a_nan_reaches(io, save, where, bad):
+@pytest.mark.parametrize("D", [70, 72])
+def test_what_a_nan_reaches(io, save, where, bad, D):
     """A channel's NaN stays in it, between two starts; in 8 bits its block of 32 channels is NaN at that token."""
-    B, L, D = 2, 300, 70
+    B, L = 2, 300
     x, d = make(B, L, D, io, seed=10)
     x["starts"] = np.zeros((B, L), np.uint8)
     x["starts"][0, [100, 229]] = 1
@@ -330,6 +331,40 @@ def test_more_than_two_to_the_31_elements():
         got, alone = got.float(), alone.float()
         assert bool(((got - alone).abs() <= 2.0 ** -7 * alone.abs() + 1e-5 * alone.abs().max()).all())
     assert not bool(r[:, :-n].any()) and not bool(h[:, :-n].any())  # nothing came before
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_unaligned_outputs_only(io):
+    """Inputs that the copy engine could read, gradients and states that it could not write."""
+    x, d = make(1, 140, 64, io, docs=True, seed=15)
+    shift = lambda s, t: torch.zeros(int(np.prod(s)) + 1, device="cuda", dtype=t)[1:].view(s)  # noqa: E731
+    for save in ("states", "packed"):
+        r = Run(x, io, save)
+        h, last = shift(r.x.shape, r.x.dtype), shift(r.h0.shape, torch.float32)
+        E.e2ttt_scan_fwd(r.p, r.x, r.r, r.g, r.rate, r.starts, r.h0, h, last, r.ws, r.save)
+        check_forward({"h": h, "h_final": last}, x, io)
+        out = [shift(r.x.shape, r.x.dtype) for _ in range(3)] + [torch.empty_like(r.rate), torch.empty_like(r.h0)]
+        E.e2ttt_scan_bwd(r.p, r.x, r.r, r.g, r.rate, r.starts, r.h0, dev(d["d_h"], io), dev(d["dh_final"]), *out, r.ws, r.save)
+        check_backward(dict(zip(("d_x", "da_decay", "da_in", "d_rate", "dh_init"), out)), x, d, io, save == "packed")
+
+
+@pytest.mark.parametrize("B,L,D", [(1, 20000, 128), (9, 1500, 1024), (150, 129, 64), (300, 200, 64)])
+def test_every_way_of_sharing_a_sequence(B, L, D):
+    """Few channels and many tokens (clusters of eight), several rounds of smaller clusters, one CTA a sequence; the second half of a long sequence, from the state of the first,
+    is what it is in one piece."""
+    x, _ = make(B, L, D, "bf16", docs=False, seed=16)
+    r = Run(x, "bf16", "none")
+    whole = r.fwd()
+    cut = L // 2
+    part = lambda lo, hi, h0: {**{n: t[:, lo:hi] if n in ("x", "r", "g") else t for n, t in x.items()}, "h0": h0}  # noqa: E731
+    one = Run(part(0, cut, x["h0"]), "bf16", "none").fwd()
+    two = Run(part(cut, L, one["h_final"].cpu().numpy()), "bf16", "none").fwd()
+    h = torch.cat([one["h"], two["h"]], 1).float()
+    big = float(whole["h_final"].abs().max())
+    # states in fp32 agree to both calls' shares; h is rounded to bf16 in both: one step of it, 2^-7, apart at most
+    tol = 2 * share("bf16", L) * 40
+    assert bool(((two["h_final"] - whole["h_final"]).abs() <= tol * big).all())
+    assert bool(((h - whole["h"].float()).abs() <= 2.0 ** -7 * h.abs() + tol * big).all())
 
 
 def test_graphs_of_two_streams_and_replays():
