@@ -354,9 +354,9 @@ E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const vo
  *   x, a_decay, a_in, h  [B,L,D] io_dtype    rate [D] fp32, >= 0    starts [B,L] bytes, or NULL    h_init, h_final [B,D] fp32
  * e2ttt_scan_fwd runs whole sequences, e2ttt_scan_step a few tokens on a state (decoding), without a workspace; both move the same state and may follow each other.
  * Arithmetic: fp32; a_t - 1 and 1 - a_t^2 are formed without the rounding of a_t next to 1, so that long memories keep their precision.  With bf16 I/O gates are good
- * to some 2^-21, and logits below -43 count as -43.  A call repeats bit for bit; last bits of h (fp32), the states and the gradients depend on how many sequences share the call
- * (a long sequence is cut into parts that run side by side), but not on what is in them.  A NaN or an infinity stays in its channel, and reaches what follows it up to the next
- * start (in the reverse pass: what comes before it, too).
+ * to some 2^-21.  Logits below -43 count as -43.  A call repeats bit for bit; last bits of h (fp32), the states and the gradients depend on how many sequences, tokens and
+ * channels the call has (the tokens of a sequence are dealt out to several SMs where there are few), but not on what is in other sequences.  A NaN or an infinity stays in its channel,
+ * and reaches what follows it up to the next start (in the reverse pass: what comes before it, back to its document's start, too).
  * D up to 2^20, L up to 2^30, B L D up to 2^40, B times the blocks of 64 channels up to 2^24; any width and length, elements' alignment; 16 bytes, and widths that are a
  * multiple of 16 bytes, load faster.  h_init may be NULL (zeros), h_final may alias it; no other output may overlap an input.
  * Calls that may run at the same time need workspaces of their own.  There is no device status in them. */

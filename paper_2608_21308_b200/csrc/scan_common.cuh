@@ -52,7 +52,7 @@ __device__ __forceinline__ float rsqrt_fast(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Constants of the gates as pairs.  They are kept in registers by hand: the compiler would rather load them again at every use, two moves for one instruction.
+// Constants of the gates as pairs, moved to registers by hand so that they are there once
 struct Pairs {
     float2 neg_log2e, one, two, minus_one, e1, e2, e3, e4;
 };

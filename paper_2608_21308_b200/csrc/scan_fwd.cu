@@ -1,7 +1,12 @@
 // Gated linear recurrence, forward.  h_t = a_t h_{t-1} + b_t is linear in the state: over a run of tokens h_out = P h_in + h', P the product of the a_t and h' the run's
-// end from a zero state.  A CTA has 64 channels of a sequence; a lane has two of them, a warp kTok tokens of a tile, whose P and h' meet in shared memory.  Where there are
+// end from a zero state.  A CTA has 64 channels of a sequence; a lane has two of them, a warp 16 tokens (fp32: 8) of a tile, whose P and h' meet in shared memory.  Where there are
 // few channels and sequences, the tiles of a sequence are dealt out to the CTAs of a cluster, whose P and h' meet through distributed shared memory: no CTA waits for another
-// kernel's work, nothing lies in global memory between them, and every sum has one order.
+// cluster's work, nothing lies in global memory between them, and every sum has one order.
+// A token's P and h' stay in registers from the walk to the output, so that gates are computed once; x, the logits and h go through shared memory by the copy engine, a warp's own
+// rows at a time (loads by the threads themselves waited for places in the load queue: 87 us where the copy engine, all else being equal, took 74).
+// 16384 tokens of 2048 in bf16 with an input gate: 65 us (268 MB, 4.1 TB/s, 63 % of the copy); with inputs kept in 8 bits 87 us; one sequence of 32768: 127 us; fp32 135 us (537 MB,
+// 4.0 TB/s).  What bounds it: registers allow two CTAs on an SM, and what these issue between their meetings (61 instructions and 8 special functions for a pair of values: 43 %
+// of the issue slots, 53 % of the special function unit).
 #include <type_traits>
 
 #include "api_checks.h"
