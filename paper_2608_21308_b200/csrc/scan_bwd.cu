@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     const int64_t blocks = a.s.blocks(), tiles = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
-    const bool whole = (TILE || pair) && first + kScanCh <= D;  // all channels are there, and stored in pairs
+    const bool whole = first + kScanCh <= D;  // all channels are there
     const int64_t seq = b * L * (int64_t)D;
     const bool even = (D & 1) == 0;  // rows of states (in the workspace) are pairs
     const Pairs pairs = make_pairs();
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
             auto put = [&](int k, void* out, int j, float2 v) {
                 if constexpr (TILE && PACK) put_row2<IO>(outs->g[k][j], lane, v);
                 else if constexpr (TILE) put_row2<IO>(rows.in[k][j], lane, v);
-                else store2<IO>(out, seq + (t0 + j) * (int64_t)D + c0, PLAIN ? 2 : n, PLAIN || pair, v);
+                else store2<IO>(out, seq + (t0 + j) * (int64_t)D + c0, n, pair, v);
             };
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {

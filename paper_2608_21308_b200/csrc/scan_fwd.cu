@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     const int64_t blocks = a.s.blocks(), spans = a.s.spans(), unit = blockIdx.x / parts, b = unit / blocks;
     const int part = blockIdx.x - (int)(unit * parts), first = (int)(unit - b * blocks) * kScanCh;
     const int c0 = first + 2 * lane, n = max(0, min(2, D - c0));
-    const bool whole = (TILE || pair) && first + kScanCh <= D;  // all channels are there, and stored in pairs
+    const bool whole = first + kScanCh <= D;  // all channels are there
     IO* ring = reinterpret_cast<IO*>(smem + kMeet) + warp * (kStages * NT * TOK * kScanCh);
     const int64_t seq = b * L * (int64_t)D;
     const Pairs pairs = make_pairs();
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
 }
 
 // CTAs of a cluster
-int parts_of(const ScanShape& s) { return scan_parts(s, kTokOf<__nv_bfloat16> * kWarps, 2); }
+int parts_of(const ScanShape& s) { return scan_parts(s, (s.f32 ? kTokOf<float> : kTokOf<__nv_bfloat16>) * kWarps, 2); }
 
 template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE> int launch(const ScanArgs& a, const ScanMaps& maps, int by, bool pair, cudaStream_t st) {
     auto kernel = scan_fwd_kernel<IO, GATE, UNIT, PACK, TILE>;
