@@ -323,6 +323,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
 __global__ void __launch_bounds__(256) scan_rate_kernel(const float* part, float* d_rate, const int64_t rows, const int D) {
     __shared__ float sums[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // it is launched beside the end of the reverse pass, and reads only when that is done
     float y = 0.0f;
     if (c < D)
         for (int64_t i = warp; i < rows; i += 8) y += part[i * D + c];
@@ -352,8 +353,16 @@ template <typename IO, bool GATE, bool UNIT, bool PACK, bool TILE> int launch(co
     cfg.numAttrs = parts > 1 ? 1 : 0;
     e = cudaLaunchKernelEx(&cfg, kernel, b, maps, by, pair, parts);
     if (e != cudaSuccess) return (int)e;
-    scan_rate_kernel<<<(s.D + 31) / 32, 256, 0, st>>>(b.part, b.d_rate, (int64_t)s.B * parts, s.D);
-    return (int)cudaGetLastError();
+    cudaLaunchConfig_t sum{};
+    sum.gridDim = dim3((unsigned)((s.D + 31) / 32));
+    sum.blockDim = dim3(256);
+    sum.stream = st;
+    at[0] = {};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    sum.attrs = at;
+    sum.numAttrs = 1;
+    return (int)cudaLaunchKernelEx(&sum, scan_rate_kernel, (const float*)b.part, b.d_rate, (int64_t)s.B * parts, s.D);
 }
 template <typename IO, bool GATE, bool UNIT, bool PACK> int launch(const ScanBwdArgs& b, int by, bool pair, cudaStream_t st) {
     ScanMaps maps{};
