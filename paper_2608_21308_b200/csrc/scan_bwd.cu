@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 const float2 bj = mul2(to_x[j], x);
                 if (GATE) meet.stash[warp][j][lane] = mul2(bj, shut);
                 hh = fma2(bj, pairs.minus_one, start ? dup(0.0f) : fade<PLAIN>(hh, d.c, d.far));
-                pp = start ? dup(0.0f) : fade<PLAIN>(pp, d.c, d.far);
+                pp = !PLAIN && cut_by(starts, j) ? dup(kCut) : fade<PLAIN>(pp, d.c, d.far);
             }
 #pragma unroll
             for (int j = kTok - 1; j >= 0; --j) {

@@ -282,16 +282,19 @@ template <typename IO> __device__ __forceinline__ float2 logit2(const IO* row, i
 }
 
 // ---- runs of tokens: what goes in, P times, plus what a run makes of nothing.  CUT: there are starts, and a run with one in it lets nothing through, an infinity or a NaN
-// neither.
+// neither.  Such a run has kCut for its P: a product of decays is never negative, but 0 where it underflows, and a NaN behind the start where a logit is one.
+constexpr float kCut = -1.0f;
 template <bool CUT> __device__ __forceinline__ float2 through(float2 P, float2 in, float2 own) {
     if constexpr (!CUT) return fma2(P, in, own);
-    return make_float2(P.x == 0.0f ? own.x : fmaf(P.x, in.x, own.x), P.y == 0.0f ? own.y : fmaf(P.y, in.y, own.y));
+    return make_float2(P.x < 0.0f ? own.x : fmaf(P.x, in.x, own.x), P.y < 0.0f ? own.y : fmaf(P.y, in.y, own.y));
 }
 // P of two runs
 template <bool CUT> __device__ __forceinline__ float2 both(float2 P, float2 next) {
     if constexpr (!CUT) return mul2(P, next);
-    return make_float2(next.x == 0.0f ? 0.0f : P.x * next.x, next.y == 0.0f ? 0.0f : P.y * next.y);
+    return make_float2(P.x < 0.0f || next.x < 0.0f ? kCut : P.x * next.x, P.y < 0.0f || next.y < 0.0f ? kCut : P.y * next.y);
 }
+// whether one of a run's tokens up to the j-th is a start
+__device__ __forceinline__ bool cut_by(unsigned starts, int j) { return (starts & ((2u << j) - 1)) != 0; }
 
 // ---- CTAs of a cluster: the parts of a sequence's channels along its tokens.  Every turn each leaves its tile's run with all of them by asynchronous stores, which count
 // themselves on the receiver's barrier (a release of the CTA's global stores, as a cluster's barrier takes, would wait for all of them).  A buffer is used again two turns later: a CTA

@@ -138,7 +138,6 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                     const Decay d = decay<IO, UNIT, PLAIN>(pairs, sg, rate);
                     if (!PLAIN && (starts >> j & 1)) {
                         hh = u;
-                        pp = dup(0.0f);
                     } else {
                         if (UNIT) u = mul2(u, sqrt_minus(d.minus));
                         hh = add2(fade<PLAIN>(hh, d.c, d.far), u);
@@ -146,8 +145,9 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                     }
                 }
                 h[j] = hh;
-                P[j] = pp;
+                P[j] = !PLAIN && cut_by(starts, j) ? dup(kCut) : pp;
             }
+            pp = P[TOK - 1];
         };
         if (plain) walk(std::true_type{});
         else walk(std::false_type{});
