@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 in = start ? dup(0.0f) : fade<PLAIN>(in, c[j], far >> 2 * j);  // a lam
                 const float2 dl = start ? dup(0.0f) : mul2(in, to_r[j]);      // d_log_a sg
                 sum = add2(sum, dl);
-                put(1, ba.d_r, j, mul2(dl, to_a[j]));
+                put(1, ba.d_r, j, start ? dl : mul2(dl, to_a[j]));  // a start's logit is not used, and may be a NaN
             }
         };
         if (plain) spread(std::true_type{});

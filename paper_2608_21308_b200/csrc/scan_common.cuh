@@ -281,6 +281,9 @@ template <typename IO> __device__ __forceinline__ float2 logit2(const IO* row, i
     }
 }
 
+// A start's decay logit: it is not used, but its sigmoid may share a reciprocal with the input gate's, which a NaN would reach
+__device__ __forceinline__ float2 no_nan(float2 logit) { return make_float2(fmaxf(logit.x, kLeast), fmaxf(logit.y, kLeast)); }
+
 // ---- runs of tokens: what goes in, P times, plus what a run makes of nothing.  CUT: there are starts, and a run with one in it lets nothing through, an infinity or a NaN
 // neither.  Such a run has kCut for its P: a product of decays is never negative, but 0 where it underflows, and a NaN behind the start where a logit is one.
 constexpr float kCut = -1.0f;

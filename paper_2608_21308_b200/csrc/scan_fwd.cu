@@ -129,8 +129,9 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                 if (PLAIN || j < have) {
                     float2 u = row2(rows + j * kScanCh, lane), sg;
                     if constexpr (GATE) {
-                        float2 ig;
-                        sigmoids<IO>(pairs, logit2(rows + (TOK + j) * kScanCh, lane), logit2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
+                        float2 ig, r = logit2(rows + (TOK + j) * kScanCh, lane);
+                        if (!PLAIN && (starts >> j & 1)) r = no_nan(r);
+                        sigmoids<IO>(pairs, r, logit2(rows + (2 * TOK + j) * kScanCh, lane), sg, ig);
                         u = mul2(u, ig);
                     } else {
                         sg = sigmoid2<IO>(pairs, logit2(rows + (TOK + j) * kScanCh, lane));

@@ -58,3 +58,27 @@ def test_without_an_input_gate_and_unit_scale(io, docs):
     run = S.Run(x, io)
     same(run.fwd(), {"h": h, "h_final": last})
     same(run.bwd(d), ref)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("gate,unit", [(True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("D", [64, 66, 65])
+@pytest.mark.parametrize("L", [333, 2100])
+def test_the_decay_logit_of_a_start_is_not_used(io, gate, unit, D, L):
+    """A NaN there changes nothing, bit for bit, and its gradient is zero."""
+    x, d = S.make(1, L, D, io, gate, unit, seed=21)
+    x["starts"] = np.zeros((1, L), np.uint8)
+    first = np.array([0, *STARTS, 230, 255, L - 1])
+    x["starts"][0, first] = 1
+    outs = []
+    for logit in (-43.0, np.nan):
+        x["r"][0, first] = logit
+        outs.append({})
+        for save in ("none", "states", "packed"):
+            run = S.Run(x, io, save)
+            outs[-1].update({(save, n): t for n, t in {**run.fwd(), **run.bwd(d)}.items()})
+        outs[-1].update({("step", n): t for n, t in S.Run(x, io).step().items()})
+    for n, t in outs[0].items():
+        assert torch.equal(t, outs[1][n]), n
+        if n[1] == "da_decay":
+            assert not bool(t[0, first].any())
