@@ -16,6 +16,7 @@
 #include <string.h>
 
 #include <initializer_list>
+#include <type_traits>
 
 #include "../../include/e2ttt.h"
 #include "api_checks.h"
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(TMAX, kept<V, TMAX>() ? 3 : 1024 / TMAX) join_
     }
 }
 
-// What a thread of the reverse pass has under way of one token: its pieces of o, x and a as they are, or their codes and the words that hold their blocks' scales.
+// What a thread of the reverse pass has under way of one token: its pieces of o, x and a as they are, or their codes and their blocks' scales, as the words that hold them.
 template <typename IO, int V, int NC, bool PACK> struct Inputs {
     static constexpr int kBytes = 3 * NC * (int)sizeof(Piece<IO, V>);
     const Piece<IO, V>* r;
@@ -323,13 +324,19 @@ template <typename IO, int V, int NC, bool PACK> struct Inputs {
     }
 };
 template <typename IO, int V, int NC> struct Inputs<IO, V, NC, true> {
-    static constexpr int kBytes = 3 * NC * (V + 4);
+    // Pieces of one value, of which a thread has up to sixteen, take the scale's byte alone: with words, 8192 columns of heads of three in fp32 asked for 232352 bytes of shared
+    // memory, more than there are.  2000 tokens of 4999 in fp32: 563 us, with words 674.
+    static constexpr bool kByte = V == 1;
+    using Scale = std::conditional_t<kByte, uint8_t, uint32_t>;
+    static constexpr int kBytes = 3 * NC * (V + (int)sizeof(Scale));
     const pack8::Codes<V>* codes;
-    const uint32_t* words;
+    const Scale* scales;
     __device__ __forceinline__ void get(int which, int i, int T, int c, float (&v)[V]) const {
-        const uint32_t word = words[(which * NC + i) * T];
-        pack8::decode<V>(codes[(which * NC + i) * T], word >> c / (pack8::kBlock / V) % 4 * 8 & 0xffu, v);
+        const uint32_t scale = scales[(which * NC + i) * T];
+        pack8::decode<V>(codes[(which * NC + i) * T], kByte ? scale : scale >> c / (pack8::kBlock / V) % 4 * 8 & 0xffu, v);
     }
+    // where the scale of piece c lies in its row
+    static __device__ __forceinline__ int at(int c) { return kByte ? c / pack8::kBlock : c / (pack8::kBlock / V * 4) * 4; }
 };
 
 template <typename IO, int V, int NC, int TMAX, bool PACK>
@@ -341,11 +348,13 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
     const JoinArgs& a = ba.f;
     const bool gated = a.gate != E2TTT_GATE_NONE;
     const int D = a.H * a.d, cols = D / V, T = blockDim.x, tid = threadIdx.x;
-    // the pieces of a token: of d_x_out and d_n behind those of o, x and a; with packed inputs [depth][2][NC][T] pieces, then the words, then the codes
+    // the pieces of a token: of d_x_out and d_n behind those of o, x and a; with packed inputs [depth][2][NC][T] pieces, then the scales, then the codes
     constexpr int OWN = PACK ? 2 : 5, DX = PACK ? 0 : 3;
     P* ring = reinterpret_cast<P*>(smem) + tid;
-    uint32_t* words = reinterpret_cast<uint32_t*>(smem + (size_t)depth * 2 * NC * T * sizeof(P)) + tid;
-    pack8::Codes<V>* codes = reinterpret_cast<pack8::Codes<V>*>(smem + (size_t)depth * NC * T * (2 * sizeof(P) + 12)) + tid;
+    using Kept = Inputs<IO, V, NC, true>;
+    using Scale = typename Kept::Scale;
+    Scale* scales = reinterpret_cast<Scale*>(smem + (size_t)depth * 2 * NC * T * sizeof(P)) + tid;
+    pack8::Codes<V>* codes = reinterpret_cast<pack8::Codes<V>*>(smem + (size_t)depth * NC * T * (2 * sizeof(P) + 3 * sizeof(Scale))) + tid;
     Sums sums = make_sums(smem + (size_t)depth * T * (2 * NC * sizeof(P) + In::kBytes), cols, a.d / V, a.H);
     const int64_t tokens = (int64_t)a.B * a.L;
     int64_t own[NC];  // a piece of o within its token: head and place in the head
@@ -368,12 +377,12 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
                 if (c >= cols) continue;
                 if constexpr (PACK) {
                     const int at = slot * 3 * NC * T + i * T;
-                    const uint8_t *from = code_at + i * T * V, *scale = scale_at + c / (pack8::kBlock / V * 4) * 4;
+                    const uint8_t *from = code_at + i * T * V, *scale = scale_at + Kept::at(c);
 #pragma unroll
                     for (int w = 0; w < 3; ++w) {
                         if (w == 2 && !gated) continue;
                         copy_piece<V>(codes + at + w * NC * T, from + w * k.code_step);
-                        copy_piece<4>(words + at + w * NC * T, scale + w * k.scale_step);
+                        copy_piece<sizeof(Scale)>(scales + at + w * NC * T, scale + w * k.scale_step);
                     }
                 } else {
                     copy_piece<sizeof(P)>(r + i * T, reinterpret_cast<const P*>(a.o) + ahead.base + own[i]);
@@ -416,7 +425,7 @@ __global__ void __launch_bounds__(TMAX, 512 / TMAX) join_bwd_kernel(const JoinBw
         In in;
         if constexpr (PACK) {
             in.codes = codes + slot * 3 * NC * T;
-            in.words = words + slot * 3 * NC * T;
+            in.scales = scales + slot * 3 * NC * T;
         } else {
             in.r = r;
         }
