@@ -359,7 +359,8 @@ E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const vo
  * and reaches what follows it up to the next start (in the reverse pass: what comes before it, back to its document's start, too).
  * D up to 2^20, L up to 2^30, B L D up to 2^40, B times the blocks of 64 channels up to 2^24; any width and length, elements' alignment; 16 bytes, and widths that are a
  * multiple of 16 bytes, load faster.  h_init may be NULL (zeros), h_final may alias it; no other output may overlap an input.
- * Calls that may run at the same time need workspaces of their own.  There is no device status in them. */
+ * Calls that may run at the same time need workspaces of their own.  There is no device status in them: a bounded wait that gave up, which none does short of a device fault,
+ * leaves NaN in the outputs, states and packed inputs that depend on what was not waited for, and in all that the waiting warp makes from then on. */
 typedef struct {
     int32_t B, L, D;    /* sequences, tokens, channels */
     int32_t io_dtype;   /* e2ttt_dtype of x, a_decay, a_in, h and their gradients */
@@ -419,7 +420,7 @@ E2TTT_API int e2ttt_join_bwd_packed(const e2ttt_join_params* p, const void* pack
                                     void* stream);
 
 /* Reads back the device status word of the last launch that used `workspace` (the first word of every
- * workspace).  workspace == NULL reads the word of the scratch array e2ttt_chunk_fwd_noalloc uses on the
+ * workspace but the block join's and the gated linear recurrence's, which have none).  workspace == NULL reads the word of the scratch array e2ttt_chunk_fwd_noalloc uses on the
  * current device (0 if that entry point has not run there yet).  This is the one entry point that
  * synchronises: it waits for `stream`.
  *   status  out (host)  0 after a clean run; otherwise the code of the first bounded device-side wait
@@ -473,6 +474,12 @@ E2TTT_API int e2ttt_chunk_fwd_noalloc(const e2ttt_params* p,
  * (No counterpart in the paper: an operational guard of this implementation.)
  * Returns E2TTT_OK (the kernel was enqueued) or E2TTT_ERR_NULL / _WORKSPACE / _ALIGN / _SHAPE / _ARCH / _CUDA. */
 E2TTT_API int e2ttt_selftest_wait_timeout(void* workspace, size_t workspace_bytes, long long limit_cycles, void* stream);
+
+/* The same for the gated linear recurrence, whose calls have no status word: from this call on, the device-side waits of e2ttt_scan_fwd and e2ttt_scan_bwd calls that this
+ * host thread makes give up after `limit_cycles` SM cycles (0: at once, without a look; negative: the library's own limit, some 1 s, again).  A call whose waits gave up
+ * returns E2TTT_OK and leaves NaN, as the recurrence's documentation has it; it waits for its own copies before it ends, and the context stays usable.
+ * Returns E2TTT_OK, or E2TTT_ERR_SHAPE above 2e9. */
+E2TTT_API int e2ttt_selftest_scan_wait_limit(long long limit_cycles);
 
 /* Static description of a status code (never NULL). */
 E2TTT_API const char* e2ttt_status_string(int status);

@@ -127,6 +127,8 @@ def lib() -> ctypes.CDLL:
         L.e2ttt_scan_bwd.restype = cp
         L.e2ttt_scan_step.argtypes = [sp] + [vp] * 9
         L.e2ttt_scan_step.restype = cp
+        L.e2ttt_selftest_scan_wait_limit.argtypes = [ctypes.c_longlong]
+        L.e2ttt_selftest_scan_wait_limit.restype = cp
         kp = ctypes.POINTER(e2ttt_pack_params)
         L.e2ttt_pack8.argtypes = [kp] + [vp] * 4
         L.e2ttt_pack8.restype = cp
@@ -585,6 +587,14 @@ def e2ttt_scan_step(p, x, a_decay, a_in, rate, starts, h_state, h, h_out, stream
     st = (_lib or lib()).e2ttt_scan_step(ctypes.byref(p), *args, _stream_ptr(stream))
     if st != E2TTT_OK:
         raise E2TTTError(st, "e2ttt_scan_step")
+    return st
+
+
+def e2ttt_selftest_scan_wait_limit(limit_cycles: int):
+    """int e2ttt_selftest_scan_wait_limit(...) of include/e2ttt.h: waits of this host thread's recurrence calls give up after so many cycles (-1: the library's limit)."""
+    st = (_lib or lib()).e2ttt_selftest_scan_wait_limit(int(limit_cycles))
+    if st != E2TTT_OK:
+        raise E2TTTError(st, "e2ttt_selftest_scan_wait_limit")
     return st
 
 

@@ -60,6 +60,7 @@ struct ScanArgs {
     float* states;          // null: not saved
     uint8_t *codes, *scales;  // null: inputs not kept in 8 bits
     size_t code_step, scale_step;
+    long long wait_cycles;  // after which a device-side wait gives up; 0: at once
 };
 
 struct ScanBwdArgs {

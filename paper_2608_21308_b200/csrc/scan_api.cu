@@ -3,6 +3,7 @@
 
 #include "api_checks.h"
 #include "scan.h"
+#include "sm100.cuh"
 
 namespace e2ttt {
 
@@ -55,6 +56,8 @@ int check_workspace(const void* ws, size_t bytes, size_t need) {
     return aligned(ws, 256) ? E2TTT_OK : E2TTT_ERR_ALIGN;
 }
 
+thread_local long long wait_cycles = sm100::kWaitCycles;  // of this host thread's calls
+
 void place(ScanArgs* a, const ScanLayout& l, void* workspace, int save) {
     char* ws = static_cast<char*>(workspace);
     if (save != E2TTT_SAVE_NONE) a->states = reinterpret_cast<float*>(ws + l.states);
@@ -94,6 +97,7 @@ int e2ttt_scan_fwd(const e2ttt_scan_params* p, const void* x, const void* a_deca
     rc = check_device();
     if (rc) return rc;
     a.x = x; a.r = a_decay; a.g = a_in; a.rate = rate; a.starts = starts; a.h_init = h_init; a.h = h; a.h_final = h_final;
+    a.wait_cycles = wait_cycles;
     place(&a, l, workspace, save);
     return scan_fwd_launch(a, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
 }
@@ -116,6 +120,7 @@ int e2ttt_scan_bwd(const e2ttt_scan_params* p, const void* x, const void* a_deca
     rc = check_device();
     if (rc) return rc;
     b.f.x = x; b.f.r = a_decay; b.f.g = a_in; b.f.rate = rate; b.f.starts = starts; b.f.h_init = h_init;
+    b.f.wait_cycles = wait_cycles;
     place(&b.f, l, workspace, save);
     if (saved == E2TTT_SAVE_NONE && scan_fwd_launch(b.f, stream) != 0) return E2TTT_ERR_CUDA;
     b.d_h = d_h; b.dh_final = dh_final; b.d_x = d_x; b.d_r = da_decay; b.d_g = da_in; b.d_rate = d_rate; b.dh_init = dh_init;
@@ -134,6 +139,12 @@ int e2ttt_scan_step(const e2ttt_scan_params* p, const void* x, const void* a_dec
     if (rc) return rc;
     a.x = x; a.r = a_decay; a.g = a_in; a.rate = rate; a.starts = starts; a.h_init = h_state; a.h = h; a.h_final = h_out;
     return scan_step_launch(a, stream) == 0 ? E2TTT_OK : E2TTT_ERR_CUDA;
+}
+
+int e2ttt_selftest_scan_wait_limit(long long limit_cycles) {
+    if (limit_cycles > sm100::kWaitCycles) return E2TTT_ERR_SHAPE;
+    wait_cycles = limit_cycles < 0 ? sm100::kWaitCycles : limit_cycles;
+    return E2TTT_OK;
 }
 
 }  // extern "C"

@@ -93,10 +93,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     }
     __syncwarp();
     if (parts > 1) meeting_init(meet.meeting);
+    auto has_rows = [&](int64_t tile) { return tile >= 0 && tile * kTile + warp * kTok < L; };
     unsigned next_first = 0;
+    bool met = true;  // no wait of this warp has given up
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
-        if (tile >= 0 && tile * kTile + warp * kTok < L) {
+        if ((!TILE || met) && has_rows(tile)) {
             const int t = (int)(tile * kTile) + warp * kTok;
             R& to = ring[slot];
             const int64_t row = unit * tiles * kScanSpan + t;
@@ -140,7 +142,17 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     float2 next_state = state_of((turns - 1) * parts + part);  // a turn ahead
     int slot = 0;
     uint32_t parity = 0, taken = 0;  // taken: which phase a stage's barrier is in (a warp may have no tokens in the first turn)
-    bool met = true;
+    auto give_up = [&](bool next) {  // next: the next turn's rows are under way
+        met = false;
+        if constexpr (TILE) {
+            if (next) (void)await_on<false>(&full[slot ^ 1], taken >> (slot ^ 1) & 1, sm100::kWaitCycles);
+            if (lane == 0) bulk_read_done();
+            __syncwarp();
+            fill(ring, kNans, kStages * sizeof(R));
+            if constexpr (PACK)
+                for (int i = 0; i < kStages; ++i) fill(ring[i].codes, 0, sizeof(ring[i].codes));
+        }
+    };
     for (int64_t turn = turns - 1; turn >= 0; --turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
         const int t0 = (int)min(tile * kTile + warp * kTok, (int64_t)L), have = min(kTok, L - t0);
@@ -152,7 +164,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         if constexpr (!TILE) {
             copy_wait<kStages - 1>();
         } else if (have > 0) {
-            if (met) met = await<false>(&full[slot], taken >> slot & 1);
+            if (met && !await<false>(&full[slot], taken >> slot & 1, a.wait_cycles)) {
+                (void)await_on<false>(&full[slot], taken >> slot & 1, sm100::kWaitCycles);
+                give_up(turn == turns - 1 && has_rows(tile - parts));
+            }
             taken ^= 1u << slot;
         }
         __syncwarp();
@@ -239,8 +254,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
                 own = through<CUT>(make_float2(q.x, q.y), own, meet.ends[slot][w][lane]);
                 P_in = both<CUT>(P_in, make_float2(q.x, q.y));
             }
-            if (warp == 0) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, v));
-            if (met) met = await<true>(&meet.meeting.full[slot], parity);
+            if (warp == 0 && met) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, v));
+            if (met && !await<true>(&meet.meeting.full[slot], parity, a.wait_cycles)) {
+                (void)await_on<true>(&meet.meeting.full[slot], parity, kSendCycles);
+                give_up(has_rows(tile - parts));
+            }
             for (int k = parts - 1; k > part; --k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
                 in = through<CUT>(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
@@ -257,7 +275,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
         };
         if (a.starts) meet_others(std::true_type{});
         else meet_others(std::false_type{});
-        if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
+        if (!met) {
+            in = end = no_value();
+            if (warp == ender) meet.carry[slot][lane] = end;
+        }
         auto spread = [&](auto is_plain) {
             constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
@@ -313,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(IO) == 2 ? 2 : 1) scan_bwd_ke
     __syncthreads();
     if (TILE) bulk_done();
     else copy_wait<0>();
+    if (parts > 1 && !met) sm100::cluster_sync();  // the others may not be done sending; whoever is has left, or comes here too
     if (warp != 0) return;
     sum = meet.ends[0][0][lane];
     for (int w = 1; w < kWarps; ++w) sum = add2(sum, meet.ends[0][w][lane]);

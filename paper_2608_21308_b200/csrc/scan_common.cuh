@@ -18,6 +18,7 @@ constexpr int kThreads = 32 * kWarps;
 __device__ __forceinline__ uint64_t u2(float2 a) { return *reinterpret_cast<const uint64_t*>(&a); }
 __device__ __forceinline__ float2 f2(uint64_t a) { return *reinterpret_cast<const float2*>(&a); }
 __device__ __forceinline__ float2 dup(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 no_value() { return dup(__uint_as_float(0x7fc00000u)); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(u2(a)), "l"(u2(b)), "l"(u2(c)));
@@ -327,14 +328,27 @@ __device__ __forceinline__ void send_part(Meeting& m, int slot, int part, int pa
     for (int k = 0; k < parts; ++k)
         sm100::st_async_v4(in_cta(data, k), __float_as_uint(P.x), __float_as_uint(P.y), __float_as_uint(own.x), __float_as_uint(own.y), in_cta(bar, k));
 }
-// Bounded: neither the copies nor the stores of a cluster can fail short of a device fault.  False once a wait gave up; what is computed from then on is made NaN.
-template <bool CLUSTER> __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity) {
-    if (sm100::mbar_try_wait<CLUSTER>(bar, parity)) return true;
+// ---- waits that give up.  Every wait is bounded, by `limit` cycles (0: it gives up without a look), though neither the copies nor the stores of a cluster can fail short of a
+// device fault.  A warp that gives up waits once more for what is under way to its shared memory, has NaNs for rows from then on, and neither loads, waits nor sends any more: what it
+// computes and hands on is NaN, and the waits of CTAs that it does not send to give up too.
+template <bool CLUSTER> __device__ __noinline__ bool await_on(uint64_t* bar, uint32_t parity, long long limit) {
     const long long t0 = clock64();
-    while (!sm100::mbar_try_wait<CLUSTER>(bar, parity))
-        if (clock64() - t0 > sm100::kWaitCycles) return false;
-    return true;
+    while (!__any_sync(kAll, clock64() - t0 >= limit))
+        if (__all_sync(kAll, sm100::mbar_try_wait<CLUSTER>(bar, parity))) return true;
+    return false;
 }
+// the whole warp calls, and gets one answer
+template <bool CLUSTER> __device__ __forceinline__ bool await(uint64_t* bar, uint32_t parity, long long limit) {
+    return __all_sync(kAll, limit != 0 && sm100::mbar_try_wait<CLUSTER>(bar, parity)) || await_on<CLUSTER>(bar, parity, limit);
+}
+constexpr long long kSendCycles = 100000;  // a store to another CTA takes some thousand
+// a warp's bytes in shared memory, 16 at a time
+static __device__ __noinline__ void fill(void* at, uint32_t word, int bytes) {
+    const int lane = threadIdx.x & 31;
+    for (int i = lane; i < bytes / 16; i += 32) static_cast<uint4*>(at)[i] = make_uint4(word, word, word, word);
+    __syncwarp();
+}
+constexpr uint32_t kNans = 0xffffffffu;  // in either type, and for the scales of packed rows
 
 }  // namespace scan
 }  // namespace e2ttt

@@ -77,10 +77,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     __syncwarp();
     if (parts > 1) meeting_init(meet.meeting);
     const int64_t tiles = ((int64_t)L + kTile - 1) / kTile;
+    auto has_rows = [&](int64_t tile) { return tile * kTile + warp * TOK < L; };
     unsigned next_first = 0;
+    bool met = true;  // no wait of this warp has given up
     auto load = [&](int64_t tile, int slot) {
         next_first = 0;
-        if (tile * kTile + warp * TOK < L) {
+        if ((!TILE || met) && has_rows(tile)) {
             const int t = (int)(tile * kTile) + warp * TOK;
             IO* to = ring + slot * (NT * TOK * kScanCh);
             if constexpr (TILE) {
@@ -103,7 +105,15 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     load(part + parts, 1);
     int slot = 0;
     uint32_t parity = 0;
-    bool met = true;
+    auto give_up = [&](bool next) {  // next: the next turn's rows are under way
+        met = false;
+        if constexpr (TILE) {
+            if (next) (void)await_on<false>(&full[slot ^ 1], parity ^ (uint32_t)slot, sm100::kWaitCycles);
+            if (lane == 0) bulk_read_done();
+            __syncwarp();
+            fill(ring, kNans, kStages * NT * TOK * kScanCh * (int)sizeof(IO));
+        }
+    };
     // every CTA of a cluster takes every turn: its part of the last one may be empty
     for (int64_t turn = 0; turn * parts < tiles; ++turn, slot ^= 1, parity ^= slot == 0) {
         const int64_t tile = turn * parts + part;
@@ -111,8 +121,12 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         const unsigned starts = __ballot_sync(kAll, byte0 != 0);
         byte0 = next_first;
         IO* rows = ring + slot * (NT * TOK * kScanCh);
-        if (!TILE) copy_wait<kStages - 1>();
-        else if (met && have > 0) met = await<false>(&full[slot], parity);
+        if (!TILE) {
+            copy_wait<kStages - 1>();
+        } else if (met && have > 0 && !await<false>(&full[slot], parity, a.wait_cycles)) {
+            (void)await_on<false>(&full[slot], parity, sm100::kWaitCycles);
+            give_up(turn == 0 && has_rows(tile + parts));
+        }
         __syncwarp();
         if (PACK && have > 0) {
             const int64_t row = unit * spans * kScanSpan + t0;
@@ -185,8 +199,11 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
                 own = through<CUT>(make_float2(q.x, q.y), own, make_float2(q.z, q.w));
                 P_in = both<CUT>(P_in, make_float2(q.x, q.y));
             }
-            if (warp == kWarps - 1) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, hh));
-            if (met) met = await<true>(&meet.meeting.full[slot], parity);
+            if (warp == kWarps - 1 && met) send_part(meet.meeting, slot, part, parts, lane, both<CUT>(P_in, pp), through<CUT>(pp, own, hh));
+            if (met && !await<true>(&meet.meeting.full[slot], parity, a.wait_cycles)) {
+                (void)await_on<true>(&meet.meeting.full[slot], parity, kSendCycles);
+                give_up(has_rows(tile + parts));
+            }
             for (int k = 0; k < part; ++k) {
                 const float4 q = meet.meeting.parts[slot][k][lane];
                 in = through<CUT>(make_float2(q.x, q.y), in, make_float2(q.z, q.w));
@@ -203,7 +220,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         };
         if (a.starts) meet_others(std::true_type{});
         else meet_others(std::false_type{});
-        if (!met) in = end = dup(__uint_as_float(0x7fc00000u));
+        if (!met) {
+            in = end = no_value();
+            if (warp == ender) meet.carry[slot][lane] = end;
+        }
         if (a.states && have > 0 && t0 % kScanSpan == 0) store2<float>(a.states, (b * spans + t0 / kScanSpan) * D + c0, n, false, in);
         if (!a.h) continue;
         if constexpr (TILE) {  // in the place of x
@@ -231,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
     if (a.h_final && part == 0 && warp == ender) store2<float>(a.h_final, b * D + c0, n, false, end);
     if (TILE) bulk_done();
     else copy_wait<0>();
+    if (parts > 1 && !met) sm100::cluster_sync();  // the others may not be done sending; whoever is has left, or comes here too
 }
 
 // CTAs of a cluster
