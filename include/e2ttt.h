@@ -354,9 +354,12 @@ E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const vo
  *   x, a_decay, a_in, h  [B,L,D] io_dtype    rate [D] fp32, >= 0    starts [B,L] bytes, or NULL    h_init, h_final [B,D] fp32
  * e2ttt_scan_fwd runs whole sequences, e2ttt_scan_step a few tokens on a state (decoding), without a workspace; both move the same state and may follow each other.
  * Arithmetic: fp32; a_t - 1 and 1 - a_t^2 are formed without the rounding of a_t next to 1, so that long memories keep their precision.  With bf16 I/O gates are good
- * to some 2^-21.  Logits below -43 count as -43.  A call repeats bit for bit; last bits of h (fp32), the states and the gradients depend on how many sequences, tokens and
+ * to some 2^-21.  Logits below -43 count as -43.  A call repeats bit for bit; last bits of h, the states and the gradients depend on how many sequences, tokens and
  * channels the call has (the tokens of a sequence are dealt out to several SMs where there are few), but not on what is in other sequences.  A NaN or an infinity stays in its channel,
- * and reaches what follows it up to the next start (in the reverse pass: what comes before it, back to its document's start, too).
+ * and reaches what follows it up to the next start, whatever the decays (in the reverse pass: what comes before it, back to its document's start, too).  With E2TTT_SAVE_PACKED
+ * the reverse pass reads NaNs for its token's block of 32 channels, an infinite logit's block as well.
+ * Blocks of 64 channels whose rates all lie between 1e-10 and 1/4 are fastest: one rate outside costs its block a third to 45 % more time, with fp32 I/O
+ * 17 to 30 %.
  * D up to 2^20, L up to 2^30, B L D up to 2^40, B times the blocks of 64 channels up to 2^24; any width and length, elements' alignment; 16 bytes, and widths that are a
  * multiple of 16 bytes, load faster.  h_init may be NULL (zeros), h_final may alias it; no other output may overlap an input.
  * Calls that may run at the same time need workspaces of their own.  There is no device status in them: a bounded wait that gave up, which none does short of a device fault,
@@ -369,8 +372,8 @@ typedef struct {
 } e2ttt_scan_params;
 
 /* What a forward leaves in its workspace for the reverse pass: nothing; the state before every 64th token (4 bytes a channel), beside which the reverse pass reads x, a_decay
- * and a_in again; or those states and x, a_decay and a_in in the 8-bit form of e2ttt_pack8 (a little over a byte a value, widths and lengths rounded up to 64), so that the caller
- * need not keep them.  The reverse pass is then the adjoint at the values that are read back; the states it multiplies are walked again from
+ * and a_in again; or those states and x, a_decay and a_in in the 8-bit form of e2ttt_pack8 (a little over a byte a value, widths and lengths rounded up to 64: calls of a few tokens
+ * or channels save nothing), so that the caller need not keep them.  The latter saves memory, not time: a forward takes a third more, a reverse pass a tenth.  The reverse pass is then the adjoint at the values that are read back; the states it multiplies are walked again from
  * them, from the forward's own state before every 64th token. */
 typedef enum { E2TTT_SAVE_NONE = 0, E2TTT_SAVE_STATES = 1, E2TTT_SAVE_PACKED = 2 } e2ttt_save;
 
@@ -408,7 +411,8 @@ E2TTT_API int e2ttt_pack8(const e2ttt_pack_params* p, const void* x, int8_t* cod
 E2TTT_API int e2ttt_unpack8(const e2ttt_pack_params* p, const int8_t* codes, const uint8_t* scales, void* x, void* stream);
 
 /* The block join's training step with its inputs kept in that form: e2ttt_join_fwd that leaves o, a and x (as rows of H d columns, blocks of 32 of them, across heads)
- * in `packed`, and e2ttt_join_bwd that reads them from there: the gradients of e2ttt_join_bwd at the values that are read back.  The forward's outputs are those of
+ * in `packed`, and e2ttt_join_bwd that reads them from there: the gradients of e2ttt_join_bwd at the values that are read back.  Memory is what it saves: the forward takes half as long
+ * again, the reverse pass with bf16 I/O up to a fifth more, with fp32 about as long.  The forward's outputs are those of
  * e2ttt_join_fwd, bit for bit; x_out may alias x and n_out a as there.  packed: e2ttt_join_packed_bytes, 256-byte aligned, the caller's until the reverse pass. */
 E2TTT_API int e2ttt_join_packed_bytes(const e2ttt_join_params* p, size_t* bytes);
 E2TTT_API int e2ttt_join_fwd_packed(const e2ttt_join_params* p, const void* o, const void* a, const void* x, const float* w_post,

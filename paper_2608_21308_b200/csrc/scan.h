@@ -17,7 +17,8 @@ struct ScanShape {
 
 // CTAs that share a block of channels of a sequence, the CTAs of a cluster: the number with the shortest way through, in turns of a tile per CTA.  kFit clusters of 1 to 8 CTAs
 // are on the GPU at a time with two CTAs on an SM (as the driver counts them; half of that with one).  Measured, in the forward with bf16 I/O: a turn takes 3.7 to 4.1 us
-// where an SM has two CTAs, 2.1 (one CTA) to 2.8 us (a cluster of eight) where it has one, and a round of clusters some 0.8 turns more to start and to end.
+// where an SM has two CTAs, 2.1 (one CTA) to 2.8 us (a cluster of eight) where it has one, and a round of clusters some 0.8 turns more to start and to end.  The reverse pass and
+// fp32 I/O go by the same figures, and the choice is the best of 1 to 8 or, with fp32 I/O, up to 12 % behind it.
 inline int scan_parts(const ScanShape& s, int tile, int on_sm) {
     constexpr int kFit[8] = {296, 148, 93, 71, 56, 45, 37, 33};
     constexpr float kAlone[8] = {0.53f, 0.64f, 0.65f, 0.66f, 0.67f, 0.68f, 0.69f, 0.69f}, kPair[8] = {0.95f, 1.0f, 1.0f, 1.0f, 1.01f, 1.02f, 1.03f, 1.03f};

@@ -6,7 +6,8 @@
 //   d_x = lam s i,   d_a_in = lam s u (1 - i),   d_log_a = a lam (h_{t-1} - a u / s),   d_a_decay = d_log_a log_a (1 - sg),   d_rate = -sum d_log_a sg.
 // What does not depend on lam is computed before the meeting and kept: c, -s i, sg a u / s, sg and a_decay's factor in registers, s u (1 - i) in shared memory.
 // Gradients go out through the place of what they are the gradients of, by the copy engine: stores from the threads between the steps held up the loads (162 to 217 us, as
-// the compiler laid them).  16384 tokens of 2048 in bf16: 133 us (470 MB, 3.5 TB/s); with inputs in 8 bits 151 us (373 MB: decoding costs more than the bytes save); fp32 267 us.
+// the compiler laid them).  16384 tokens of 2048 in bf16: 133 us (470 MB, 3.5 TB/s), 193 with rates of up to 4;
+// with inputs in 8 bits 150 us (373 MB: decoding costs more than the bytes save); fp32 267 us.  Rows that the copy engine cannot read: 347 us for 2046 channels, 412 for 2047.
 // Registers allow two CTAs on an SM (fp32: one); issue takes 47 % of its slots, the dependent steps of eight tokens back and forth the rest.
 #include <type_traits>
 

@@ -4,9 +4,10 @@
 // cluster's work, nothing lies in global memory between them, and every sum has one order.
 // A token's P and h' stay in registers from the walk to the output, so that gates are computed once; x, the logits and h go through shared memory by the copy engine, a warp's own
 // rows at a time (loads by the threads themselves waited for places in the load queue: 87 us where the copy engine, all else being equal, took 74).
-// 16384 tokens of 2048 in bf16 with an input gate: 65 us (268 MB, 4.1 TB/s, 63 % of the copy); with inputs kept in 8 bits 87 us; one sequence of 32768: 127 us; fp32 135 us (537 MB,
-// 4.0 TB/s).  What bounds it: registers allow two CTAs on an SM, and what these issue between their meetings (61 instructions and 8 special functions for a pair of values: 43 %
-// of the issue slots, 53 % of the special function unit).
+// 16384 tokens of 2048 in bf16 with an input gate: 64 us (268 MB, 4.2 TB/s, 64 % of the copy), 91 with rates of up to 4, whose decays take the exponential beside the series; with
+// inputs kept in 8 bits 86 us; one sequence of 32768: 127 us; fp32 137 us (537 MB, 3.9 TB/s).  Rows that the copy engine cannot read: 160 us for 2046 channels, 295 for 2047.
+// What bounds it: registers and shared memory allow two CTAs on an SM, and what these issue between their meetings (60 instructions and 8 special functions for a pair of values:
+// 43 % of the issue slots, 53 % of the special function unit).
 #include <type_traits>
 
 #include "api_checks.h"
