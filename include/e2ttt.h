@@ -357,7 +357,7 @@ E2TTT_API int e2ttt_join_bwd(const e2ttt_join_params* p, const void* o, const vo
  * to some 2^-21.  Logits below -43 count as -43.  A call repeats bit for bit; last bits of h, the states and the gradients depend on how many sequences, tokens and
  * channels the call has (the tokens of a sequence are dealt out to several SMs where there are few), but not on what is in other sequences.  A NaN or an infinity stays in its channel,
  * and reaches what follows it up to the next start, whatever the decays (in the reverse pass: what comes before it, back to its document's start, too).  With E2TTT_SAVE_PACKED
- * the reverse pass reads NaNs for its token's block of 32 channels, an infinite logit's block as well.
+ * the reverse pass reads NaNs for its token's block of 32 channels.
  * Blocks of 64 channels whose rates all lie between 1e-10 and 1/4 are fastest: one rate outside costs its block a third to 45 % more time, with fp32 I/O
  * 17 to 30 %.
  * D up to 2^20, L up to 2^30, B L D up to 2^40, B times the blocks of 64 channels up to 2^24; any width and length, elements' alignment; 16 bytes, and widths that are a
@@ -372,8 +372,9 @@ typedef struct {
 } e2ttt_scan_params;
 
 /* What a forward leaves in its workspace for the reverse pass: nothing; the state before every 64th token (4 bytes a channel), beside which the reverse pass reads x, a_decay
- * and a_in again; or those states and x, a_decay and a_in in the 8-bit form of e2ttt_pack8 (a little over a byte a value, widths and lengths rounded up to 64: calls of a few tokens
- * or channels save nothing), so that the caller need not keep them.  The latter saves memory, not time: a forward takes a third more, a reverse pass a tenth.  The reverse pass is then the adjoint at the values that are read back; the states it multiplies are walked again from
+ * and a_in again; or those states and x, a_decay and a_in in the 8-bit form of e2ttt_pack8 (logits as -43 to 43, infinite ones too: masked channels cost their
+ * neighbours no precision; a little over a byte a value, widths and lengths rounded up to 64: calls of a few tokens or channels save nothing), so that the caller need not keep them.
+ * The latter saves memory, not time: a forward takes a third more, a reverse pass a tenth.  The reverse pass is then the adjoint at the values that are read back; the states it multiplies are walked again from
  * them, from the forward's own state before every 64th token. */
 typedef enum { E2TTT_SAVE_NONE = 0, E2TTT_SAVE_STATES = 1, E2TTT_SAVE_PACKED = 2 } e2ttt_save;
 

@@ -14,6 +14,10 @@ constexpr uint32_t kNan = 255;  // scale byte of a block that holds a NaN or an 
 // Scale byte e + 127 of a block whose largest magnitude has these bits: the smallest e with 127 2^e >= m 2^k, that is k - 6 up to m = 127 / 64 and k - 5 above it.  Up to
 // kOrdinary, 127 2^121; what is above (and infinities and NaNs, from 0x7f800000 on) encode() sees to.
 constexpr uint32_t kOrdinary = 0x7f7e0000u, kLargest = 248;
+constexpr uint32_t kInfinite = 0x7f800000u;
+// Logits of the recurrence count from -43 to 43 (a sigmoid is 1 there): a masked one, however far out, does not cost its block the scale, nor an infinite one its values
+constexpr float kFarLogit = 43.0f;
+constexpr uint32_t kFarLogitBits = 0x422c0000u;
 __device__ __forceinline__ uint32_t scale_byte(uint32_t bits) { return (uint32_t)max(1, (int)((bits + 0x1ffffu) >> 23) - 6); }
 __device__ __forceinline__ float scale(uint32_t byte) { return __uint_as_float(byte == kNan ? 0x7fc00000u : byte << 23); }
 
@@ -89,17 +93,24 @@ template <typename IO, int V> __device__ __forceinline__ void widen(const IO (&i
     }
 }
 // Codes of V values of a block and its scale byte, from the bits of its largest magnitude.  Every lane of the warp calls: what is out of the ordinary is one branch, by a vote.
-template <typename IO, int V> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t bits, uint32_t& byte) {
+// LOGIT: the values are logits of the recurrence.
+template <typename IO, int V, bool LOGIT = false> __device__ __forceinline__ Codes<V> encode(const IO (&in)[V], uint32_t bits, uint32_t& byte) {
     byte = scale_byte(bits);
     float x[V];
     widen<IO, V>(in, x);
-    if (__any_sync(0xffffffffu, bits > kOrdinary)) {
+    if (__any_sync(0xffffffffu, bits > (LOGIT ? kFarLogitBits : kOrdinary))) {
+        if (LOGIT && bits <= kInfinite) {
+            bits = min(bits, kFarLogitBits);
+            byte = scale_byte(bits);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = fminf(fmaxf(x[j], -kFarLogit), kFarLogit);
+        }
         byte = min(byte, kLargest);
 #pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = bits >= 0x7f800000u ? 0.0f : limited(x[j]);
+        for (int j = 0; j < V; ++j) x[j] = bits >= kInfinite ? 0.0f : LOGIT ? x[j] : limited(x[j]);
     }
     const float inv = __uint_as_float((254u - byte) << 23);  // 2^-e
-    if (bits >= 0x7f800000u) byte = kNan;
+    if (bits >= kInfinite) byte = kNan;
     Codes<V> out;
     if constexpr (V >= 4) {
         uint32_t w[V / 4];

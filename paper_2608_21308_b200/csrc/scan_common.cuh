@@ -68,7 +68,7 @@ __device__ __forceinline__ Pairs make_pairs() {
 }
 
 // Logits count from -43 on: the product of two exp(-x) stays finite, and 1 - a^2 above 0 at any ordinary rate.  A NaN stays one.
-constexpr float kLeast = -43.0f;
+constexpr float kLeast = -43.0f;  // also what 8-bit inputs hold
 __device__ __forceinline__ float2 capped(float2 x) {
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(kLeast));
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(kLeast));

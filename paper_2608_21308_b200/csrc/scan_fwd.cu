@@ -33,7 +33,7 @@ struct Meet {
 constexpr int kMeet = (sizeof(Meet) + 127) / 128 * 128;
 
 // The 8-bit form of a warp's rows of one tensor: a lane takes 32 bytes, half a block in bf16 and a quarter of one in fp32, and writes their codes at once.
-template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const IO* rows, uint8_t* codes, uint8_t* scales, int n, int lane) {
+template <typename IO, int ROWS, bool LOGIT> __device__ __forceinline__ void pack_rows(const IO* rows, uint8_t* codes, uint8_t* scales, int n, int lane) {
     constexpr int V = 32 / (int)sizeof(IO), PER = kScanCh / V, STEP = 32 / PER;  // lanes of a row; rows a warp takes at once
     const int row = lane / PER, chunk = lane % PER;
 #pragma unroll
@@ -43,7 +43,7 @@ template <typename IO, int ROWS> __device__ __forceinline__ void pack_rows(const
         };
         const Piece p = *reinterpret_cast<const Piece*>(rows + (row + i) * kScanCh + chunk * V);
         uint32_t byte;
-        const pack8::Codes<V> code = pack8::encode<IO, V>(p.x, pack8::group_magnitude<IO, V>(p.x), byte);
+        const pack8::Codes<V> code = pack8::encode<IO, V, LOGIT>(p.x, pack8::group_magnitude<IO, V>(p.x), byte);
         if (row + i >= n) continue;
         *reinterpret_cast<pack8::Codes<V>*>(codes + (row + i) * kScanCh + chunk * V) = code;
         if (chunk % (pack8::kBlock / V) == 0) scales[(row + i) * 2 + chunk / (pack8::kBlock / V)] = (uint8_t)byte;
@@ -131,9 +131,10 @@ __global__ void __launch_bounds__(kThreads, 2) scan_fwd_kernel(const ScanArgs a,
         __syncwarp();
         if (PACK && have > 0) {
             const int64_t row = unit * spans * kScanSpan + t0;
+            uint8_t *codes = a.codes + row * kScanCh, *scales = a.scales + row * 2;
+            pack_rows<IO, TOK, false>(rows, codes, scales, have, lane);
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-                pack_rows<IO, TOK>(rows + k * TOK * kScanCh, a.codes + k * a.code_step + row * kScanCh, a.scales + k * a.scale_step + row * 2, have, lane);
+            for (int k = 1; k < NT; ++k) pack_rows<IO, TOK, true>(rows + k * TOK * kScanCh, codes + k * a.code_step, scales + k * a.scale_step, have, lane);
         }
         float2 h[TOK], P[TOK], hh = dup(0.0f), pp = dup(1.0f);
         const bool plain = near && have == TOK && !starts;  // all tokens and channels are there, none is a start, no decay is far from 1
