@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("far", [np.inf, 3e38, 1000.0, 44.0])
 def test_unbounded_logits(io, gate, L, D, far):
     x, d = S.make(1, L, D, io, gate, True, True, seed=30)
-    far = float(S.inputs.round_bf16(np.float32(far))) if io == "bf16" and np.isfinite(far) else np.float32(far)
+    far = S.inputs.round_bf16(np.array([far], np.float32)).item() if io == "bf16" and np.isfinite(far) else np.float32(far)
     x["r"][:, ::7, 3], x["r"][:, 1::5, 40], x["r"][:, 20:30, 61] = -far, far, -far
     if gate:
         x["g"][:, ::6, 5], x["g"][:, 2::9, 41], x["g"][:, 40:50, 62] = -far, far, -far
